@@ -32,7 +32,7 @@ extern "C" {
 
 #define IOLB_OK            0
 #define IOLB_EINVAL       -1   /* null pointer, non-positive extent, stride < 1, pad < 0, empty output */
-#define IOLB_EUNSUPPORTED -2   /* Winograd m outside {2,3,4,6}; algo or layout outside its enum */
+#define IOLB_EUNSUPPORTED -2   /* Winograd m outside {2,3,4,6}; algo, layout, type or activation outside its enum; dense layer too large */
 #define IOLB_ENOTILE      -3   /* no tile fits the LDS / register budgets */
 #define IOLB_EWORKSPACE   -4   /* workspace missing or too small */
 #define IOLB_EHIP         -5   /* a HIP runtime call or launch failed; see iolb_last_hip_error */
@@ -225,6 +225,68 @@ int iolb_bounds(const iolb_shape* shape, int64_t S_f_elems, iolb_bounds_out* out
  * transform B d B^T, kernel transform L g L^T, output transform A M A^T), row-major into host
  * arrays A[m][m+2], L[m+2][3], B[m+2][m+2].  Host only.  IOLB_EUNSUPPORTED for other m. */
 int iolb_winograd_matrices(int m, float* A, float* L, float* B);
+
+/* ---- Dense layers and 8-bit activation checkpoints -----------------------------------------------------
+ * What follows a network's convolutions: y = act(x W^T + b) with a residual, its gradients, and the activations that the
+ * backward pass needs held in 8 bits.  Tensors are fp32, fp16 or bf16, all of a call of one type, and hold rows of
+ * contiguous values whose starts are ld... values apart (at least the row's length; any alignment of the type's own size).  Sums are
+ * held in fp32 and rounded once to the tensor's type.  fp32 operands go to the matrix cores as the sum of three bf16 parts, which
+ * hold them to the last bit from 2^-110 up; below that the absolute error stays under 2^-133.  Infinities and NaN give
+ * what fp32 arithmetic gives.  Extents may be zero: no output then, or (a sum over nothing) bias and residual alone.
+ * These calls allocate nothing: scratch is the caller's, 256-byte aligned, at least as large as the ..._workspace_bytes
+ * call of the same arguments says (it may be 0: NULL then).  It depends on addresses too: tensors whose rows
+ * do not start on 16 bytes are copied.  They enqueue kernels only, on the stream of iolb_set_stream, and can be captured. */
+enum { IOLB_F32 = 0, IOLB_F16 = 1, IOLB_BF16 = 2 };
+/* silu: z / (1 + e^-z);  gelu: z Phi(z);  gelu_tanh: z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.  All three are 0 at
+ * -infinity; a NaN stays one. */
+enum { IOLB_ACT_NONE = 0, IOLB_ACT_RELU = 1, IOLB_ACT_SILU = 2, IOLB_ACT_GELU = 3, IOLB_ACT_GELU_TANH = 4 };
+
+/* z = x w^T + bias (+ residual if residual_first);  y = act(z) (+ residual otherwise).
+ * x [M][K], w [N][K], bias [N] or NULL, residual [M][N] or NULL, y [M][N]; y may be the residual itself, and overlaps nothing
+ * else.  zq, ze (both or neither): the checkpoint of z, from the fp32 sums, as iolb_checkpoint_pack lays it out.
+ * M, N up to 2^30, K up to 2^22 (IOLB_EUNSUPPORTED beyond). */
+typedef struct iolb_linear_args {
+    int64_t M, N, K;
+    int32_t dtype, act, residual_first;
+    const void *x, *w, *bias, *residual;
+    void* y;
+    int64_t ldx, ldw, ldr, ldy;
+    int8_t* zq;
+    uint8_t* ze;
+} iolb_linear_args;
+int iolb_linear_workspace_bytes(const iolb_linear_args* args, size_t* bytes);
+int iolb_linear(const iolb_linear_args* args, void* workspace, size_t workspace_bytes);
+
+/* The 8-bit checkpoint of x [rows][cols]: q [rows][cols] and one byte for each 32 values of a row, e [rows][ceil(cols / 32)].
+ * A value is q 2^(e - 127), q from -127 to 127, with the least exponent that brings the block's finite values within
+ * that (at least 2^-126, for fp16 2^-24; at most 2^122, for fp16 2^10, where q stops at 63), rounded to nearest even: an error of at
+ * most 1/127 of the block's largest value, 1/254 at best.  Values that are not finite become q = -128 and read back as NaN.
+ * Every value is one of the tensor's type, and of bf16. */
+int iolb_checkpoint_pack(const void* x, int64_t ldx, int64_t rows, int64_t cols, int dtype, int8_t* q, uint8_t* e);
+/* y [rows][cols] = act(values of the checkpoint). */
+int iolb_checkpoint_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, int act, int dtype, void* y, int64_t ldy);
+
+/* Gradients of iolb_linear from dy [M][N], w [N][K] and checkpoints: xq, xe of the layer's input, [M][K] (x = act_x of its values:
+ * an input that is another layer's activation is recomputed from that layer's checkpoint); zq, ze of what the activation
+ * was applied to, [M][N] (NULL with IOLB_ACT_NONE).
+ *   dz = dy act'(z);  dx [M][K] = dz w;  dw [N][K] = dz^T x;  db [N] = sum of dz over its rows
+ * dz [M][N] is the residual's gradient where that came before the activation.  Outputs are dense; each may be NULL, and w, xq
+ * with it.  The slope of relu at 0 is 0, and a dy that it stops is not looked at.  16-bit types: dz is rounded to the type
+ * once, before the products; db is summed before that.  Sums are added in a fixed order: equal calls give equal bits.
+ * M, N up to 2^22, K up to 2^30 (IOLB_EUNSUPPORTED beyond). */
+typedef struct iolb_linear_backward_args {
+    int64_t M, N, K;
+    int32_t dtype, act, x_act;
+    const void *dy, *w;
+    int64_t ldy, ldw;
+    const int8_t* xq;
+    const uint8_t* xe;
+    const int8_t* zq;
+    const uint8_t* ze;
+    void *dx, *dw, *db, *dz;
+} iolb_linear_backward_args;
+int iolb_linear_backward_workspace_bytes(const iolb_linear_backward_args* args, size_t* bytes);
+int iolb_linear_backward(const iolb_linear_backward_args* args, void* workspace, size_t workspace_bytes);
 
 /* Stream (a hipStream_t) later calls enqueue on; NULL selects the null stream. */
 int iolb_set_stream(void* hip_stream);

@@ -5,6 +5,7 @@ memory and the current stream.  There is no CPU fallback: a missing library rais
 """
 import ctypes
 import os
+from collections import namedtuple
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libiolbconv.so")
@@ -20,7 +21,34 @@ EXPORTS = ["conv_direct", "conv_direct_noalloc", "conv_direct_noalloc_max_weight
            "iolb_probe_hbm_copy", "iolb_probe_mfma_sink_bytes", "iolb_probe_mfma_f32",
            "iolb_probe_share_scratch_bytes", "iolb_probe_pipeline_share",
            "iolb_timing_enable", "iolb_timing_read", "iolb_release_workspace", "iolb_strerror",
-           "iolb_last_hip_error"]
+           "iolb_last_hip_error",
+           "iolb_linear", "iolb_linear_workspace_bytes", "iolb_checkpoint_pack", "iolb_checkpoint_unpack",
+           "iolb_linear_backward", "iolb_linear_backward_workspace_bytes"]
+
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+CHECKPOINT_BLOCK = 32                       # values of a row that share a scale
+
+
+class LinearArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("M", "N", "K")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "act", "residual_first")] + \
+               [(n, ctypes.c_void_p) for n in ("x", "w", "bias", "residual", "y")] + \
+               [(n, ctypes.c_int64) for n in ("ldx", "ldw", "ldr", "ldy")] + \
+               [(n, ctypes.c_void_p) for n in ("zq", "ze")]
+
+
+class LinearBackwardArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("M", "N", "K")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "act", "x_act")] + \
+               [(n, ctypes.c_void_p) for n in ("dy", "w")] + \
+               [(n, ctypes.c_int64) for n in ("ldy", "ldw")] + \
+               [(n, ctypes.c_void_p) for n in ("xq", "xe", "zq", "ze", "dx", "dw", "db", "dz")]
+
+
+#: The 8-bit checkpoint of a tensor of rows: q int8 [rows][cols], e uint8 [rows][ceil(cols / 32)].
+Checkpoint = namedtuple("Checkpoint", "q e")
+#: What linear_backward returns; None for what was not wanted.
+LinearGrads = namedtuple("LinearGrads", "dx dw db dz")
 
 
 class Shape(ctypes.Structure):
@@ -125,6 +153,15 @@ def lib():
                                                 ctypes.POINTER(ctypes.c_double)]
         L.iolb_release_workspace.restype = i
         L.iolb_release_workspace.argtypes = []
+        for name, args in (("iolb_linear", LinearArgs), ("iolb_linear_backward", LinearBackwardArgs)):
+            getattr(L, name).restype = i
+            getattr(L, name).argtypes = [ctypes.POINTER(args), vp, sz]
+            getattr(L, name + "_workspace_bytes").restype = i
+            getattr(L, name + "_workspace_bytes").argtypes = [ctypes.POINTER(args), ctypes.POINTER(sz)]
+        L.iolb_checkpoint_pack.restype = i
+        L.iolb_checkpoint_pack.argtypes = [vp] + [ctypes.c_int64] * 3 + [i, vp, vp]
+        L.iolb_checkpoint_unpack.restype = i
+        L.iolb_checkpoint_unpack.argtypes = [vp, vp] + [ctypes.c_int64] * 2 + [i, i, vp, ctypes.c_int64]
         L.iolb_strerror.restype = ctypes.c_char_p
         L.iolb_strerror.argtypes = [i]
         L.iolb_last_hip_error.restype = ctypes.c_char_p
@@ -458,3 +495,175 @@ def probe_pipeline_share(roles, iters=2000):
 
 def release_workspace():
     _check(lib().iolb_release_workspace())
+
+
+# ---- dense layers and 8-bit activation checkpoints -------------------------------------------------------
+
+def _dtype_code(dtype):
+    torch = _torch or _load_torch()
+    code = 0 if dtype == torch.float32 else 1 if dtype == torch.float16 else 2 if dtype == torch.bfloat16 else None
+    if code is None:
+        raise TypeError("dense layers take float32, float16 and bfloat16 tensors")
+    return code
+
+
+def _act_code(act):
+    try:
+        return ACTS[act]
+    except (KeyError, TypeError):
+        raise ValueError("act must be one of " + ", ".join(ACTS)) from None
+
+
+def _rows(t, name, dtype, device, shape=None):
+    """(address, values between rows) of a matrix on the GPU whose rows are contiguous."""
+    torch = _torch or _load_torch()
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2):
+        raise TypeError("%s must be a matrix of %s on the GPU" % (name, dtype))
+    if t.device != device:
+        raise ValueError(name + " is on another GPU")
+    rows, cols = t.shape
+    if shape is not None and (rows, cols) != shape:
+        raise ValueError("%s has the wrong shape" % name)
+    if rows == 0 or cols == 0:
+        return t.data_ptr(), cols
+    along, step = t.stride()[1], t.stride()[0]
+    if (cols > 1 and along != 1) or (rows > 1 and step < cols):
+        raise TypeError(name + " must have contiguous rows that do not overlap")
+    return t.data_ptr(), step if rows > 1 else cols
+
+
+def _dense(t, name, dtype, device, shape):
+    torch = _torch or _load_torch()
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise TypeError("%s must be a contiguous tensor of %s on the GPU" % (name, dtype))
+    if t.device != device:
+        raise ValueError(name + " is on another GPU")
+    if tuple(t.shape) != shape:
+        raise ValueError(name + " has the wrong shape")
+    return t.data_ptr()
+
+
+def _checkpoint_of(c, name, device, rows, cols):
+    torch = _torch or _load_torch()
+    if not (isinstance(c, tuple) and len(c) == 2):
+        raise TypeError(name + " must be a Checkpoint")
+    return (_dense(c[0], name + ".q", torch.int8, device, (rows, cols)),
+            _dense(c[1], name + ".e", torch.uint8, device, (rows, -(-cols // CHECKPOINT_BLOCK))))
+
+
+def _new_checkpoint(rows, cols, device):
+    torch = _torch or _load_torch()
+    return Checkpoint(torch.empty((rows, cols), dtype=torch.int8, device=device),
+                      torch.empty((rows, -(-cols // CHECKPOINT_BLOCK)), dtype=torch.uint8, device=device))
+
+
+def _use_stream_on(device):
+    if device.index != (_torch or _load_torch()).cuda.current_device():
+        raise ValueError("the tensors are not on the current GPU")
+    _use_current_stream()
+
+
+def _call_with_workspace(call, query, args, device):
+    # (the workspace comes from torch's allocator, which hands memory out again in the order of the stream)
+    torch = _torch or _load_torch()
+    need = ctypes.c_size_t(0)
+    _check(query(ctypes.byref(args), ctypes.byref(need)))
+    ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+    _check(call(ctypes.byref(args), ws.data_ptr() if ws is not None else None, need.value))
+
+
+def linear(x, w, bias=None, act="none", residual=None, residual_first=False, checkpoint=False, y=None):
+    """y = act(x w^T + bias) + residual, or act(x w^T + bias + residual) with residual_first, for x [M][K], w [N][K],
+    bias [N], residual [M][N]; all float32, all float16 or all bfloat16, rows contiguous.  checkpoint=True returns (y,
+    Checkpoint of what the activation was applied to).  y may be given, and may be the residual."""
+    torch = _torch or _load_torch()
+    if not isinstance(x, torch.Tensor) or not isinstance(w, torch.Tensor):
+        raise TypeError("x and w must be tensors")
+    dtype, device = x.dtype, x.device
+    code = _dtype_code(dtype)
+    px, ldx = _rows(x, "x", dtype, device)
+    pw, ldw = _rows(w, "w", dtype, device)
+    M, K = x.shape
+    N = w.shape[0]
+    if w.shape[1] != K:
+        raise ValueError("x and w have different numbers of columns")
+    pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else None
+    pr, ldr = _rows(residual, "residual", dtype, device, (M, N)) if residual is not None else (None, 0)
+    if y is None:
+        y = torch.empty((M, N), dtype=dtype, device=device)
+    py, ldy = _rows(y, "y", dtype, device, (M, N))
+    z = _new_checkpoint(M, N, device) if checkpoint else None
+    args = LinearArgs(M, N, K, code, _act_code(act), int(bool(residual_first)), px, pw, pb, pr, py, ldx, ldw, ldr, ldy,
+                      z.q.data_ptr() if checkpoint else None, z.e.data_ptr() if checkpoint else None)
+    L = lib()
+    _use_stream_on(device)
+    _call_with_workspace(L.iolb_linear, L.iolb_linear_workspace_bytes, args, device)
+    return (y, z) if checkpoint else y
+
+
+def checkpoint_pack(x):
+    """The 8-bit checkpoint of x [rows][cols]: 33/32 bytes a value, to be read by checkpoint_unpack and linear_backward."""
+    torch = _torch or _load_torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a tensor")
+    code = _dtype_code(x.dtype)
+    px, ldx = _rows(x, "x", x.dtype, x.device)
+    rows, cols = x.shape
+    c = _new_checkpoint(rows, cols, x.device)
+    _use_stream_on(x.device)
+    _check(lib().iolb_checkpoint_pack(px, ldx, rows, cols, code, c.q.data_ptr(), c.e.data_ptr()))
+    return c
+
+
+def checkpoint_unpack(c, dtype=None, act="none", y=None):
+    """act(the checkpoint's values) as a matrix of `dtype` (float32 unless y is given)."""
+    torch = _torch or _load_torch()
+    if not (isinstance(c, tuple) and len(c) == 2 and isinstance(c[0], torch.Tensor) and c[0].dim() == 2):
+        raise TypeError("c must be a Checkpoint")
+    rows, cols = c[0].shape
+    device = c[0].device
+    if dtype is None:
+        dtype = y.dtype if y is not None else torch.float32
+    code = _dtype_code(dtype)
+    pq, pe = _checkpoint_of(c, "c", device, rows, cols)
+    if y is None:
+        y = torch.empty((rows, cols), dtype=dtype, device=device)
+    py, ldy = _rows(y, "y", dtype, device, (rows, cols))
+    _use_stream_on(device)
+    _check(lib().iolb_checkpoint_unpack(pq, pe, rows, cols, _act_code(act), code, py, ldy))
+    return y
+
+
+def linear_backward(dy, w, x=None, z=None, act="none", x_act="none", want_dx=True, want_dw=True, want_db=True, want_dz=False):
+    """Gradients of linear(): LinearGrads(dx, dw, db, dz) from dy [M][N], w [N][K] and the checkpoints x of the layer's input
+    [M][K] (the input is x_act of it) and z of what the activation was applied to [M][N] (None for act="none").
+    dz = dy act'(z) is the gradient of a residual that was added first.  x is needed for dw, w for the sizes and dx."""
+    torch = _torch or _load_torch()
+    if not isinstance(dy, torch.Tensor) or not isinstance(w, torch.Tensor):
+        raise TypeError("dy and w must be tensors")
+    dtype, device = dy.dtype, dy.device
+    code = _dtype_code(dtype)
+    pdy, ldy = _rows(dy, "dy", dtype, device)
+    pw, ldw = _rows(w, "w", dtype, device)
+    M, N = dy.shape
+    K = w.shape[1]
+    if w.shape[0] != N:
+        raise ValueError("dy and w have different numbers of outputs")
+    a = _act_code(act)
+    if a and z is None:
+        raise ValueError("the activation's slope needs z")
+    if want_dw and x is None:
+        raise ValueError("dw needs x")
+    xq, xe = _checkpoint_of(x, "x", device, M, K) if x is not None else (None, None)
+    zq, ze = _checkpoint_of(z, "z", device, M, N) if z is not None else (None, None)
+
+    def out(want, *shape):
+        return torch.empty(shape, dtype=dtype, device=device) if want else None
+
+    g = LinearGrads(out(want_dx, M, K), out(want_dw, N, K), out(want_db, N), out(want_dz, M, N))
+    args = LinearBackwardArgs(M, N, K, code, a, _act_code(x_act), pdy, pw, ldy, ldw, xq, xe, zq, ze,
+                              *(t.data_ptr() if t is not None else None for t in g))
+    L = lib()
+    _use_stream_on(device)
+    _call_with_workspace(L.iolb_linear_backward, L.iolb_linear_backward_workspace_bytes, args, device)
+    return g

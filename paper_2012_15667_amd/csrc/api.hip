@@ -10,6 +10,7 @@
 #include <tuple>
 #include <vector>
 
+#include "dense.h"
 #include "iolbconv.h"
 #include "kernels.h"
 #include "split_plan.h"
@@ -677,6 +678,13 @@ int time_probe(int reps, float* ms_per_launch, Launch launch)
 
 }  // namespace
 
+namespace iolb {
+
+hipStream_t call_stream() { return t_stream; }
+int note_hip_error(hipError_t e) { return hip_fail(e); }
+
+}  // namespace iolb
+
 extern "C" {
 
 int conv_direct_cfg(const float* x, const float* w, float* y, int N, int C, int H, int W, int K, int R, int S,
@@ -1040,7 +1048,7 @@ const char* iolb_strerror(int code)
     switch (code) {
     case IOLB_OK: return "success";
     case IOLB_EINVAL: return "invalid argument";
-    case IOLB_EUNSUPPORTED: return "unsupported algorithm or Winograd tile size";
+    case IOLB_EUNSUPPORTED: return "unsupported algorithm, type, activation, size or Winograd tile size";
     case IOLB_ENOTILE: return "no tile fits the LDS / register budgets";
     case IOLB_EWORKSPACE: return "workspace missing, misaligned or too small";
     case IOLB_EHIP: return "HIP runtime error (see iolb_last_hip_error)";

@@ -1,0 +1,95 @@
+// Dense layers (y = act(x W^T + b) + r), 8-bit activation checkpoints and the layers' gradients: what the kernels share.
+//
+// Products run on the 16-bit matrix cores with sums in fp32.  bf16 and fp16 tensors go there as they are; an fp32 tensor as
+// the sum of three bf16 parts, x = h + m + l, eight significant bits each, of whose nine products the six that reach fp32
+// precision are taken (the other three are below 2^-24 of the product), smallest first.  A part is a "plane" of its own
+// in memory, and a product of two planes a "segment" of the sum.
+//
+// Not finite: h of an infinity or NaN is that value, m and l are zero.  h h then gives what fp32 arithmetic gives, while
+// the other products may turn 0 x inf into NaN or add infinities of the wrong sign; so h h comes last, and sums that are not
+// finite before it are cleared.  Likewise a value whose h would round up to infinity is cut off instead of rounded.
+#ifndef IOLB_DENSE_H
+#define IOLB_DENSE_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "iolbconv.h"
+
+namespace iolb {
+
+constexpr int CKPT_BLOCK = 32;              // values of a row that share a scale
+constexpr int MAX_SEGMENTS = 6;
+
+// ---- what is done to a sum before it is written --------------------------------------------------
+struct DenseFinish {
+    const void* bias;                       // may be null
+    const void* residual;                   // may be null
+    void* y;
+    int8_t* zq;                             // checkpoint of what the activation is applied to; may be null
+    uint8_t* ze;
+    long long ldr, ldy;
+    int M, N;
+    int act, first;                         // first: the residual is added before the activation
+    int vec_bias, vec_res, vec_y, vec_q;    // four neighbouring columns may be read / written at once
+};
+
+// C[m][n] = sum over segments and k of A[m][k] B[n][k]; both operands contiguous along k, 16-byte aligned rows.
+struct DenseProduct {
+    const void* a;
+    const void* b;
+    long long lda, ldb;                     // elements
+    int M, N, K;                            // K: a multiple of 8
+    int segments;
+    long long a_plane[MAX_SEGMENTS], b_plane[MAX_SEGMENTS];   // where the segment's planes start, in elements
+    int splits;                             // workgroups that share a tile's K; their sums go to `partial` if > 1
+    float* partial;                         // [splits][M][N rounded up to 4]
+    DenseFinish f;
+};
+
+// Blocks of the tile kernel.
+enum { DENSE_TILE_256, DENSE_TILE_128, DENSE_TILE_64, DENSE_TILES };
+struct DenseTilePlan { int tile, splits; };
+DenseTilePlan dense_tile_plan(int M, int N, int K, int segments);
+inline size_t dense_partial_bytes(int splits, long long M, long long N)
+{
+    return splits > 1 ? (size_t)splits * M * ((N + 3) / 4 * 4) * 4 : 0;
+}
+// dtype: of y, bias and residual; f16: the operands are fp16 (else bf16).
+hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st);
+
+// ---- operands laid out for the product --------------------------------------------------------------
+// Values v[r][c], rows x cols, from one of three sources:
+enum { DENSE_FROM_TENSOR, DENSE_FROM_CHECKPOINT, DENSE_FROM_GRADIENT };
+struct DenseLayout {
+    int rows, cols;
+    const void* src;                        // tensor: v = src;  gradient: v = src * act'(checkpoint), or src where q is null
+    long long ld;
+    int vec_src;                            // eight neighbouring columns may be read at once
+    const int8_t* q;                        // checkpoint: v = act(value)
+    const uint8_t* e;
+    int vec_q;
+    int act;
+    void* rowmajor;                         // [planes][rows][ld_rm], or null; columns up to the next multiple of 8 are zero
+    long long ld_rm;
+    void* transposed;                       // [planes][cols][ld_tr], or null; likewise
+    long long ld_tr;
+    void* copy;                             // v in the tensor's own type, [rows][cols], or null
+    float* colsum;                          // [ceil(rows / 64)][cols]: sums over 64 rows each, or null
+};
+// dtype: of src, copy and (16-bit types) the planes; planes: 1 or 3 (fp32: bf16 parts; 1 where the values are exact in bf16).
+hipError_t launch_dense_layout(int source, int dtype, int planes, const DenseLayout& l, hipStream_t st);
+// out[c] = sum of colsum over its `blocks` rows, in `dtype`.
+hipError_t launch_dense_colsum(const float* colsum, int blocks, int cols, void* out, int dtype, hipStream_t st);
+
+hipError_t launch_checkpoint_pack(const void* x, long long ldx, int rows, int cols, int dtype, int8_t* q, uint8_t* e, hipStream_t st);
+hipError_t launch_checkpoint_unpack(const int8_t* q, const uint8_t* e, int rows, int cols, int act, int dtype, void* y, long long ldy,
+                                    hipStream_t st);
+
+// The calling thread's stream, and its record of the last HIP error (IOLB_EHIP is returned).
+hipStream_t call_stream();
+int note_hip_error(hipError_t e);
+
+}  // namespace iolb
+
+#endif

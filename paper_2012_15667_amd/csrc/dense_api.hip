@@ -1,0 +1,316 @@
+// C entry points of dense layers, 8-bit checkpoints and gradients: argument checks, operand layouts, workspace, launches.
+#include <algorithm>
+
+#include "dense.h"
+
+namespace {
+
+using namespace iolb;
+
+constexpr int64_t MOST = (int64_t)1 << 30;             // rows and columns
+constexpr int64_t MOST_K = (int64_t)1 << 22;           // summed axis: a tile's rows are addressed with 32-bit offsets
+
+bool known_type(int dtype) { return dtype == IOLB_F32 || dtype == IOLB_F16 || dtype == IOLB_BF16; }
+bool known_act(int act) { return act >= IOLB_ACT_NONE && act <= IOLB_ACT_GELU_TANH; }
+int64_t size_of(int dtype) { return dtype == IOLB_F32 ? 4 : 2; }
+bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+
+// Hands out pieces of the caller's workspace; with no memory behind it, counts them.
+struct Pieces {
+    char* base;
+    size_t used = 0;
+    void* take(size_t bytes)
+    {
+        void* const p = base ? base + used : nullptr;
+        used += (bytes + 255) & ~(size_t)255;
+        return p;
+    }
+};
+
+// A 16-bit operand that the product kernel can read in place.
+bool direct(const void* p, int64_t ld, int64_t k, int dtype)
+{
+    return dtype != IOLB_F32 && k % 8 == 0 && ld % 8 == 0 && ld <= MOST_K && aligned_to(p, 16);
+}
+
+// The six products of three parts, smallest first; the three with a second operand that is one part exactly.
+void segments(DenseProduct* p, int planes_a, int planes_b, int64_t a_elems, int64_t b_elems)
+{
+    static const int six[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+    p->segments = 0;
+    for (const auto& s : six)
+        if (s[0] < planes_a && s[1] < planes_b) {
+            p->a_plane[p->segments] = s[0] * a_elems;
+            p->b_plane[p->segments] = s[1] * b_elems;
+            ++p->segments;
+        }
+}
+
+#define DENSE_HIP(call)                                          \
+    do {                                                         \
+        const hipError_t e__ = (call);                           \
+        if (e__ != hipSuccess) return note_hip_error(e__);       \
+    } while (0)
+
+int check_linear(const iolb_linear_args& a)
+{
+    if (a.M < 0 || a.N < 0 || a.K < 0) return IOLB_EINVAL;
+    if (!known_type(a.dtype) || !known_act(a.act)) return IOLB_EUNSUPPORTED;
+    if (a.M > MOST || a.N > MOST || a.K > MOST_K) return IOLB_EUNSUPPORTED;
+    if (a.M == 0 || a.N == 0) return IOLB_OK;
+    if (!a.y || (a.K > 0 && (!a.x || !a.w)) || !a.zq != !a.ze) return IOLB_EINVAL;
+    if ((a.M > 1 && (a.ldx < a.K || a.ldy < a.N || (a.residual && a.ldr < a.N))) || (a.N > 1 && a.ldw < a.K)) return IOLB_EINVAL;
+    const size_t size = (size_t)size_of(a.dtype);
+    for (const void* p : {a.x, a.w, a.bias, a.residual, (const void*)a.y})
+        if (!aligned_to(p, size)) return IOLB_EINVAL;
+    return IOLB_OK;
+}
+
+// Plans the call; with `launch`, makes it.  *need: bytes of workspace.
+int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
+{
+    *need = 0;
+    if (a.M == 0 || a.N == 0) return IOLB_OK;
+    Pieces pieces{static_cast<char*>(ws)};
+    const int64_t Kp = up8(a.K);
+    const int planes = a.dtype == IOLB_F32 ? 3 : 1;
+    DenseProduct p{};
+    p.M = (int)a.M; p.N = (int)a.N; p.K = (int)Kp;
+    segments(&p, planes, planes, a.M * Kp, a.N * Kp);
+    const bool x_direct = direct(a.x, a.ldx, a.K, a.dtype) || a.K == 0, w_direct = direct(a.w, a.ldw, a.K, a.dtype) || a.K == 0;
+    p.a = a.x; p.lda = a.ldx;
+    p.b = a.w; p.ldb = a.ldw;
+    void *xp = nullptr, *wp = nullptr;
+    if (!x_direct) { p.a = xp = pieces.take((size_t)planes * a.M * Kp * 2); p.lda = Kp; }
+    if (!w_direct) { p.b = wp = pieces.take((size_t)planes * a.N * Kp * 2); p.ldb = Kp; }
+    const DenseTilePlan plan = dense_tile_plan(p.M, p.N, p.K, p.segments);
+    p.splits = plan.splits;
+    p.partial = static_cast<float*>(pieces.take(dense_partial_bytes(plan.splits, a.M, a.N)));
+    *need = pieces.used;
+    if (!launch) return IOLB_OK;
+
+    const int64_t four = 4 * size_of(a.dtype);
+    p.f = DenseFinish{a.bias, a.residual, a.y, a.zq, a.ze, a.ldr, a.ldy, p.M, p.N, a.act, a.residual_first != 0,
+                      a.N % 4 == 0 && aligned_to(a.bias, four),
+                      a.N % 4 == 0 && a.ldr % 4 == 0 && aligned_to(a.residual, four),
+                      a.N % 4 == 0 && a.ldy % 4 == 0 && aligned_to(a.y, four),
+                      a.N % 4 == 0 && aligned_to(a.zq, 4)};
+    const hipStream_t st = call_stream();
+    const auto lay = [&](const void* src, int64_t ld, int64_t rows, void* to) {
+        DenseLayout l{};
+        l.rows = (int)rows; l.cols = (int)a.K;
+        l.src = src; l.ld = ld;
+        l.vec_src = ld * size_of(a.dtype) % 16 == 0 && aligned_to(src, 16);
+        l.rowmajor = to; l.ld_rm = Kp;
+        return launch_dense_layout(DENSE_FROM_TENSOR, a.dtype, planes, l, st);
+    };
+    if (!x_direct) DENSE_HIP(lay(a.x, a.ldx, a.M, xp));
+    if (!w_direct) DENSE_HIP(lay(a.w, a.ldw, a.N, wp));
+    DENSE_HIP(launch_dense_product(p, plan.tile, a.dtype, st));
+    return IOLB_OK;
+}
+
+int check_backward(const iolb_linear_backward_args& a)
+{
+    if (a.M < 0 || a.N < 0 || a.K < 0) return IOLB_EINVAL;
+    if (!known_type(a.dtype) || !known_act(a.act) || !known_act(a.x_act)) return IOLB_EUNSUPPORTED;
+    // each of the three is the summed axis of a product, or a dimension of one
+    if (a.M > MOST_K || a.N > MOST_K || a.K > MOST) return IOLB_EUNSUPPORTED;
+    if ((!a.xq) != (!a.xe) || (!a.zq) != (!a.ze)) return IOLB_EINVAL;
+    if (a.M > 0 && a.N > 0) {
+        if (!a.dy || (a.M > 1 && a.ldy < a.N)) return IOLB_EINVAL;
+        if (a.act != IOLB_ACT_NONE && !a.zq) return IOLB_EINVAL;
+        if (a.dx && a.K > 0 && (!a.w || (a.N > 1 && a.ldw < a.K))) return IOLB_EINVAL;
+        if (a.dw && a.K > 0 && !a.xq) return IOLB_EINVAL;
+    }
+    const size_t size = (size_t)size_of(a.dtype);
+    for (const void* p : {a.dy, a.w, (const void*)a.dx, (const void*)a.dw, (const void*)a.db, (const void*)a.dz})
+        if (!aligned_to(p, size)) return IOLB_EINVAL;
+    return IOLB_OK;
+}
+
+int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, bool launch)
+{
+    Pieces pieces{static_cast<char*>(ws)};
+    const int planes = a.dtype == IOLB_F32 ? 3 : 1;
+    // the input's checkpoint is exact in one bf16 part, unless a smooth activation has to be taken of it
+    const int planes_x = planes == 3 && a.x_act != IOLB_ACT_NONE && a.x_act != IOLB_ACT_RELU ? 3 : 1;
+    const int64_t Mp = up8(a.M), Np = up8(a.N);
+    const bool want_dx = a.dx && a.M > 0 && a.K > 0, want_dw = a.dw && a.N > 0 && a.K > 0;
+    const bool has_z = a.act != IOLB_ACT_NONE;
+
+    // dz = dy act'(z) along the rows for dx (dy itself where that is it), transposed for dW
+    const bool dy_is_dz = !has_z && direct(a.dy, a.ldy, a.N, a.dtype);
+    const bool dz_is_plane = a.dz && direct(a.dz, a.N, a.N, a.dtype);
+    const void* dz = a.dy;
+    int64_t ld_dz = a.ldy;
+    void *dz_to = nullptr, *dzt = nullptr, *wt = nullptr, *xt = nullptr;
+    if (want_dx && !dy_is_dz) {
+        ld_dz = Np;
+        dz = dz_to = dz_is_plane ? a.dz : pieces.take((size_t)planes * a.M * Np * 2);
+    }
+    if (want_dw) {
+        dzt = pieces.take((size_t)planes * a.N * Mp * 2);
+        xt = pieces.take((size_t)planes_x * a.K * Mp * 2);
+    }
+    if (want_dx) wt = pieces.take((size_t)planes * a.K * Np * 2);
+    const int row_blocks = (int)((a.M + 63) / 64);
+    float* const sums = static_cast<float*>(a.db ? pieces.take((size_t)row_blocks * a.N * 4) : nullptr);
+
+    DenseProduct px{}, pw{};
+    DenseTilePlan plan_x{}, plan_w{};
+    if (want_dx) {
+        px.M = (int)a.M; px.N = (int)a.K; px.K = (int)Np;
+        px.a = dz; px.lda = ld_dz; px.b = wt; px.ldb = Np;
+        segments(&px, planes, planes, a.M * Np, a.K * Np);
+        plan_x = dense_tile_plan(px.M, px.N, px.K, px.segments);
+        px.splits = plan_x.splits;
+    }
+    if (want_dw) {
+        pw.M = (int)a.N; pw.N = (int)a.K; pw.K = (int)Mp;
+        pw.a = dzt; pw.lda = Mp; pw.b = xt; pw.ldb = Mp;
+        segments(&pw, planes, planes_x, a.N * Mp, a.K * Mp);
+        plan_w = dense_tile_plan(pw.M, pw.N, pw.K, pw.segments);
+        pw.splits = plan_w.splits;
+    }
+    // one after the other on the stream: they share the room for partial sums
+    px.partial = pw.partial = static_cast<float*>(pieces.take(std::max(dense_partial_bytes(plan_x.splits, px.M, px.N),
+                                                                       dense_partial_bytes(plan_w.splits, pw.M, pw.N))));
+    *need = pieces.used;
+    if (!launch) return IOLB_OK;
+
+    const hipStream_t st = call_stream();
+    if (a.M > 0 && a.N > 0 && (dz_to || dzt || a.dz || sums)) {
+        DenseLayout l{};
+        l.rows = (int)a.M; l.cols = (int)a.N;
+        l.src = a.dy; l.ld = a.ldy;
+        l.vec_src = a.ldy * size_of(a.dtype) % 16 == 0 && aligned_to(a.dy, 16);
+        l.q = has_z ? a.zq : nullptr; l.e = a.ze; l.act = a.act;
+        l.vec_q = a.N % 8 == 0 && aligned_to(a.zq, 8);
+        l.rowmajor = dz_to; l.ld_rm = Np;
+        l.transposed = dzt; l.ld_tr = Mp;
+        l.copy = dz_to && dz_is_plane ? nullptr : a.dz;
+        l.colsum = sums;
+        DENSE_HIP(launch_dense_layout(DENSE_FROM_GRADIENT, a.dtype, planes, l, st));
+    }
+    if (a.db && a.N > 0) DENSE_HIP(launch_dense_colsum(sums, row_blocks, (int)a.N, a.db, a.dtype, st));
+    const auto finish = [&](void* out, int64_t m, int64_t n) {
+        DenseFinish f{};
+        f.y = out; f.ldy = n; f.M = (int)m; f.N = (int)n;
+        f.act = IOLB_ACT_NONE;
+        f.vec_y = n % 4 == 0 && aligned_to(out, 4 * size_of(a.dtype));
+        return f;
+    };
+    if (want_dx) {
+        DenseLayout l{};
+        l.rows = (int)a.N; l.cols = (int)a.K;
+        l.src = a.w; l.ld = a.ldw;
+        l.vec_src = a.ldw * size_of(a.dtype) % 16 == 0 && aligned_to(a.w, 16);
+        l.transposed = wt; l.ld_tr = Np;
+        DENSE_HIP(launch_dense_layout(DENSE_FROM_TENSOR, a.dtype, planes, l, st));
+        px.f = finish(a.dx, a.M, a.K);
+        DENSE_HIP(launch_dense_product(px, plan_x.tile, a.dtype, st));
+    }
+    if (want_dw) {
+        DenseLayout l{};
+        l.rows = (int)a.M; l.cols = (int)a.K;
+        l.q = a.xq; l.e = a.xe; l.act = a.x_act;
+        l.vec_q = a.K % 8 == 0 && aligned_to(a.xq, 8);
+        l.transposed = xt; l.ld_tr = Mp;
+        DENSE_HIP(launch_dense_layout(DENSE_FROM_CHECKPOINT, a.dtype, planes_x, l, st));
+        pw.f = finish(a.dw, a.N, a.K);
+        DENSE_HIP(launch_dense_product(pw, plan_w.tile, a.dtype, st));
+    }
+    return IOLB_OK;
+}
+
+// Nothing the C++ runtime throws crosses the C boundary.
+template <class F>
+int guarded(F f) noexcept
+{
+    try {
+        return f();
+    } catch (...) {
+        return note_hip_error(hipErrorOutOfMemory);
+    }
+}
+
+template <class Args>
+int checked_call(const Args* a, void* ws, size_t ws_bytes, int (*check)(const Args&), int (*run)(const Args&, void*, size_t*, bool))
+{
+    return guarded([&] {
+        if (!a) return IOLB_EINVAL;
+        const int rc = check(*a);
+        if (rc != IOLB_OK) return rc;
+        size_t need = 0;
+        run(*a, nullptr, &need, false);
+        if (need && (!ws || ws_bytes < need || !aligned_to(ws, 256))) return IOLB_EWORKSPACE;
+        return run(*a, ws, &need, true);
+    });
+}
+
+template <class Args>
+int needed_bytes(const Args* a, size_t* bytes, int (*check)(const Args&), int (*run)(const Args&, void*, size_t*, bool))
+{
+    return guarded([&] {
+        if (!a || !bytes) return IOLB_EINVAL;
+        const int rc = check(*a);
+        if (rc != IOLB_OK) return rc;
+        return run(*a, nullptr, bytes, false);
+    });
+}
+
+int check_checkpoint(int64_t rows, int64_t cols, int64_t ld, int dtype, const void* values, const void* q, const void* e)
+{
+    if (rows < 0 || cols < 0) return IOLB_EINVAL;
+    if (!known_type(dtype) || rows > MOST || cols > MOST) return IOLB_EUNSUPPORTED;
+    if (rows == 0 || cols == 0) return IOLB_OK;
+    if (!values || !q || !e || (rows > 1 && ld < cols) || !aligned_to(values, (size_t)size_of(dtype))) return IOLB_EINVAL;
+    return IOLB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int iolb_linear_workspace_bytes(const iolb_linear_args* args, size_t* bytes) { return needed_bytes(args, bytes, check_linear, run_linear); }
+
+int iolb_linear(const iolb_linear_args* args, void* workspace, size_t workspace_bytes)
+{
+    return checked_call(args, workspace, workspace_bytes, check_linear, run_linear);
+}
+
+int iolb_linear_backward_workspace_bytes(const iolb_linear_backward_args* args, size_t* bytes)
+{
+    return needed_bytes(args, bytes, check_backward, run_backward);
+}
+
+int iolb_linear_backward(const iolb_linear_backward_args* args, void* workspace, size_t workspace_bytes)
+{
+    return checked_call(args, workspace, workspace_bytes, check_backward, run_backward);
+}
+
+int iolb_checkpoint_pack(const void* x, int64_t ldx, int64_t rows, int64_t cols, int dtype, int8_t* q, uint8_t* e)
+{
+    return guarded([&] {
+        const int rc = check_checkpoint(rows, cols, ldx, dtype, x, q, e);
+        if (rc != IOLB_OK || rows == 0 || cols == 0) return rc;
+        DENSE_HIP(launch_checkpoint_pack(x, ldx, (int)rows, (int)cols, dtype, q, e, call_stream()));
+        return IOLB_OK;
+    });
+}
+
+int iolb_checkpoint_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, int act, int dtype, void* y, int64_t ldy)
+{
+    return guarded([&] {
+        const int rc = check_checkpoint(rows, cols, ldy, dtype, y, q, e);
+        if (rc != IOLB_OK) return rc;
+        if (!known_act(act)) return IOLB_EUNSUPPORTED;
+        if (rows == 0 || cols == 0) return IOLB_OK;
+        DENSE_HIP(launch_checkpoint_unpack(q, e, (int)rows, (int)cols, act, dtype, y, ldy, call_stream()));
+        return IOLB_OK;
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,287 @@
+// Operands of dense layers laid out for the product kernel, and 8-bit checkpoints.  Streaming kernels: bound by memory.
+#include "dense_math.h"
+#include "kernels.h"
+
+namespace iolb {
+
+namespace {
+
+// ---- layout -----------------------------------------------------------------------------------------
+// A workgroup takes 64 x 64 values: a thread reads eight neighbouring columns of two rows, forms the values (a tensor's, a
+// checkpoint's through an activation, or a gradient's through the activation's slope), and writes them as planes along the
+// rows; the transposed planes go through LDS, and the column sums (the bias gradient's first stage) too.
+constexpr int PITCH = 72;                          // 16-bit values of a transposed row in LDS: 144 bytes
+
+template <class T>
+__device__ __forceinline__ void load_eight(const T* p, int have, bool vec, float (&v)[8])
+{
+    if (vec && have >= 8) {
+        typedef T T8 __attribute__((ext_vector_type(8), aligned(16)));
+        const T8 t = *reinterpret_cast<const T8*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < have ? (float)p[i] : 0.f;
+    }
+}
+
+__device__ __forceinline__ void load_checkpoint(const int8_t* p, float unit, int have, bool vec, float (&v)[8])
+{
+    if (vec && have >= 8) {
+        const u32x2 t = *reinterpret_cast<const u32x2*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = ckpt_value((int)(t[i / 4] << (24 - 8 * (i % 4))) >> 24, unit);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < have ? ckpt_value(p[i], unit) : 0.f;
+    }
+}
+
+template <int DT, int PLANES>
+__device__ __forceinline__ void plane_bits(float v, unsigned short (&bits)[PLANES])
+{
+    if constexpr (PLANES == 3) dense_parts(v, bits[0], bits[1], bits[2]);
+    else if constexpr (DT == IOLB_F16) bits[0] = __builtin_bit_cast(unsigned short, (_Float16)v);
+    else bits[0] = __builtin_bit_cast(unsigned short, (__bf16)v);
+}
+
+template <int SOURCE, int DT, int PLANES>
+__global__ void __launch_bounds__(256)
+dense_layout_kernel(DenseLayout g, int blocks_c)
+{
+    typedef typename DenseType<DT>::type T;
+    __shared__ __align__(16) unsigned short turned[PLANES][64][PITCH];
+    __shared__ float sums[32][64 + 1];
+    const int tid = threadIdx.x, c8 = (tid & 7) * 8, r_in = tid >> 3;
+    const int c0 = (int)(blockIdx.x % blocks_c) * 64, r0 = (int)(blockIdx.x / blocks_c) * 64;
+    const int c = c0 + c8, have = g.cols - c;                      // may be negative
+    const long long blocks_q = (g.cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
+    float column[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int in = r_in + 32 * half, r = r0 + in;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const bool live = r < g.rows && have > 0;
+        if (live) {
+            if constexpr (SOURCE != DENSE_FROM_CHECKPOINT)
+                load_eight(static_cast<const T*>(g.src) + r * g.ld + c, have, g.vec_src, v);
+            if (SOURCE == DENSE_FROM_CHECKPOINT || (SOURCE == DENSE_FROM_GRADIENT && g.q)) {
+                float z[8];
+                const float unit = two_to((int)g.e[r * blocks_q + c / CKPT_BLOCK] - 127);
+                load_checkpoint(g.q + (long long)r * g.cols + c, unit, have, g.vec_q, z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if constexpr (SOURCE == DENSE_FROM_CHECKPOINT) v[i] = activate(z[i], g.act);
+                    else v[i] = i < have ? through_activation(v[i], z[i], g.act) : 0.f;
+                }
+            }
+        }
+        unsigned short bits[8][PLANES];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) plane_bits<DT, PLANES>(v[i], bits[i]);
+        if (live && g.rowmajor) {
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+                u32x4 w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = bits[2 * i][p] | (unsigned)bits[2 * i + 1][p] << 16;
+                *reinterpret_cast<u32x4*>(static_cast<unsigned short*>(g.rowmajor) + (p * (long long)g.rows + r) * g.ld_rm + c) = w;
+            }
+        }
+        if (live && g.copy) {
+            T* const to = static_cast<T*>(g.copy) + (long long)r * g.cols + c;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) to[i] = (T)v[i];
+        }
+        if (g.transposed) {
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) turned[p][c8 + i][in] = bits[i][p];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) column[i] += v[i];
+    }
+    if (g.colsum) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[r_in][c8 + i] = column[i];
+    }
+    __syncthreads();
+    if (g.transposed) {
+        // 64 rows of 64 values: eight threads a row, two rows a thread
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int tc = r_in + 32 * half;
+            if (c0 + tc < g.cols && r0 + c8 < g.rows) {
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p)
+                    *reinterpret_cast<u32x4*>(static_cast<unsigned short*>(g.transposed) + (p * (long long)g.cols + c0 + tc) * g.ld_tr + r0 + c8) =
+                        *reinterpret_cast<const u32x4*>(&turned[p][tc][c8]);
+            }
+        }
+    }
+    if (g.colsum && tid < 64 && c0 + tid < g.cols) {
+        float s = 0.f;
+        for (int i = 0; i < 32; ++i) s += sums[i][tid];
+        g.colsum[(long long)(r0 / 64) * g.cols + c0 + tid] = s;
+    }
+}
+
+// Sixteen threads a group of 16 columns, in a fixed order.
+template <int DT>
+__global__ void __launch_bounds__(256)
+dense_colsum_kernel(const float* colsum, int blocks, int cols, void* out)
+{
+    __shared__ float part[16][17];
+    const int cx = threadIdx.x & 15, by = threadIdx.x >> 4, c = blockIdx.x * 16 + cx;
+    float s = 0.f;
+    if (c < cols)
+        for (long long b = by; b < blocks; b += 16) s += colsum[b * cols + c];
+    part[by][cx] = s;
+    __syncthreads();
+    if (by == 0 && c < cols) {
+        s = 0.f;
+        for (int i = 0; i < 16; ++i) s += part[i][cx];
+        static_cast<typename DenseType<DT>::type*>(out)[c] = (typename DenseType<DT>::type)s;
+    }
+}
+
+// ---- checkpoints -------------------------------------------------------------------------------------
+// Four lanes share a block of 32, eight values each.  A workgroup covers `wide` threads of a row and 256 / wide rows.
+template <int DT>
+__global__ void __launch_bounds__(256)
+checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t* q, uint8_t* e, int wide_log, int vec_x, int vec_q)
+{
+    typedef typename DenseType<DT>::type T;
+    const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), ty = threadIdx.x >> wide_log;
+    const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 8);
+    const long long blocks = (cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
+    for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r - ty < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
+        const int have = r < rows ? cols - c : 0;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (have > 0) load_eight(static_cast<const T*>(x) + r * ldx + c, have, vec_x, v);
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_magnitude(v[i]));
+        most = fmaxf(most, __shfl_xor(most, 1));
+        most = fmaxf(most, __shfl_xor(most, 2));
+        if (have <= 0) continue;
+        const int ex = ckpt_exponent<DT>(most);
+        u32x2 code = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) code[i / 4] |= ckpt_code<DT>(v[i], ex) << 8 * (i % 4);
+        int8_t* const to = q + r * cols + c;
+        if (vec_q && have >= 8) {
+            *reinterpret_cast<u32x2*>(to) = code;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) to[i] = (int8_t)(code[i / 4] >> 8 * (i % 4));
+        }
+        if ((tx & 3) == 0) e[r * blocks + c / CKPT_BLOCK] = (uint8_t)(ex + 127);
+    }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(256)
+checkpoint_unpack_kernel(const int8_t* q, const uint8_t* e, int rows, int cols, int act, void* y, long long ldy, int wide_log, int vec_q, int vec_y)
+{
+    typedef typename DenseType<DT>::type T;
+    typedef T T8 __attribute__((ext_vector_type(8), aligned(16)));
+    const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), ty = threadIdx.x >> wide_log;
+    const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 8), have = cols - c;
+    const long long blocks = (cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
+    if (have <= 0) return;
+    for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
+        float v[8];
+        load_checkpoint(q + r * cols + c, two_to((int)e[r * blocks + c / CKPT_BLOCK] - 127), have, vec_q, v);
+        T* const to = static_cast<T*>(y) + r * ldy + c;
+        T8 t;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = (T)activate(v[i], act);
+        if (vec_y && have >= 8) {
+            *reinterpret_cast<T8*>(to) = t;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) to[i] = t[i];
+        }
+    }
+}
+
+struct RowGrid { dim3 grid; int wide_log; };
+RowGrid row_grid(int rows, int cols)
+{
+    int wide_log = 2;                               // whole blocks of 32
+    while (wide_log < 8 && (8LL << wide_log) < cols) ++wide_log;
+    const long long gx = (cols + (8LL << wide_log) - 1) / (8LL << wide_log), per = 256 >> wide_log;
+    const long long gy = (rows + per - 1) / per;
+    return {dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), wide_log};
+}
+
+bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+int size_of(int dtype) { return dtype == IOLB_F32 ? 4 : 2; }
+
+template <int SOURCE, int DT>
+hipError_t layout(int planes, const DenseLayout& l, hipStream_t st)
+{
+    const long long bc = (l.cols + 63) / 64, n = bc * ((l.rows + 63) / 64);
+    if (n > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (n == 0) return hipSuccess;
+    if constexpr (DT == IOLB_F32) {
+        if (planes == 3) dense_layout_kernel<SOURCE, DT, 3><<<(unsigned)n, 256, 0, st>>>(l, (int)bc);
+        else dense_layout_kernel<SOURCE, DT, 1><<<(unsigned)n, 256, 0, st>>>(l, (int)bc);
+    } else {
+        dense_layout_kernel<SOURCE, DT, 1><<<(unsigned)n, 256, 0, st>>>(l, (int)bc);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_dense_layout(int source, int dtype, int planes, const DenseLayout& l, hipStream_t st)
+{
+#define BY_TYPE(S)                                                                \
+    (dtype == IOLB_F32 ? layout<S, IOLB_F32>(planes, l, st) : dtype == IOLB_F16 ? layout<S, IOLB_F16>(planes, l, st) \
+                                                                              : layout<S, IOLB_BF16>(planes, l, st))
+    switch (source) {
+    case DENSE_FROM_TENSOR: return BY_TYPE(DENSE_FROM_TENSOR);
+    case DENSE_FROM_CHECKPOINT: return BY_TYPE(DENSE_FROM_CHECKPOINT);
+    default: return BY_TYPE(DENSE_FROM_GRADIENT);
+    }
+#undef BY_TYPE
+}
+
+hipError_t launch_dense_colsum(const float* colsum, int blocks, int cols, void* out, int dtype, hipStream_t st)
+{
+    const unsigned n = (unsigned)((cols + 15) / 16);
+    if (dtype == IOLB_F32) dense_colsum_kernel<IOLB_F32><<<n, 256, 0, st>>>(colsum, blocks, cols, out);
+    else if (dtype == IOLB_F16) dense_colsum_kernel<IOLB_F16><<<n, 256, 0, st>>>(colsum, blocks, cols, out);
+    else dense_colsum_kernel<IOLB_BF16><<<n, 256, 0, st>>>(colsum, blocks, cols, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_checkpoint_pack(const void* x, long long ldx, int rows, int cols, int dtype, int8_t* q, uint8_t* e, hipStream_t st)
+{
+    const RowGrid g = row_grid(rows, cols);
+    const int vec_x = aligned_to(x, 16) && ldx * size_of(dtype) % 16 == 0, vec_q = aligned_to(q, 8) && cols % 8 == 0;
+    if (dtype == IOLB_F32) checkpoint_pack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log, vec_x, vec_q);
+    else if (dtype == IOLB_F16) checkpoint_pack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log, vec_x, vec_q);
+    else checkpoint_pack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log, vec_x, vec_q);
+    return hipGetLastError();
+}
+
+hipError_t launch_checkpoint_unpack(const int8_t* q, const uint8_t* e, int rows, int cols, int act, int dtype, void* y, long long ldy,
+                                    hipStream_t st)
+{
+    const RowGrid g = row_grid(rows, cols);
+    const int vec_q = aligned_to(q, 8) && cols % 8 == 0, vec_y = aligned_to(y, 16) && ldy * size_of(dtype) % 16 == 0;
+    if (dtype == IOLB_F32) checkpoint_unpack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log, vec_q, vec_y);
+    else if (dtype == IOLB_F16) checkpoint_unpack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log, vec_q, vec_y);
+    else checkpoint_unpack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log, vec_q, vec_y);
+    return hipGetLastError();
+}
+
+}  // namespace iolb

@@ -1,0 +1,207 @@
+// Device arithmetic of dense layers and checkpoints: types, activations and their slopes, the 8-bit code.
+#ifndef IOLB_DENSE_MATH_H
+#define IOLB_DENSE_MATH_H
+
+#include "dense.h"
+#include "split_mfma.h"
+
+namespace iolb {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <int DT> struct DenseType;
+template <> struct DenseType<IOLB_F32> { typedef float type; };
+template <> struct DenseType<IOLB_F16> { typedef _Float16 type; };
+template <> struct DenseType<IOLB_BF16> { typedef __bf16 type; };
+
+// ---- activations, in 32 bits ----------------------------------------------------------------------
+// Phi(z) = P(normal <= z) by formula 7.1.26 of Abramowitz and Stegun (error of erf at most 1.5e-7), evaluated for -|z| so that
+// nothing cancels in the lower tail.
+__device__ __forceinline__ float normal_below(float z, float gauss /* e^(-z^2 / 2) */)
+{
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678f * fabsf(z));
+    const float p = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float tail = 0.5f * p * gauss;
+    return z > 0.f ? 1.f - tail : tail;
+}
+
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+
+constexpr float GELU_TANH_K = 1.5957691216f;      // 2 sqrt(2 / pi): (1 + tanh u) / 2 is the sigmoid of 2 u
+
+// Smooth activations tend to zero at -inf, where their formula is 0 x inf.
+__device__ __forceinline__ float activate(float z, int act)
+{
+    float y = z;
+    if (act == IOLB_ACT_RELU) return z <= 0.f ? 0.f : z;
+    if (act == IOLB_ACT_SILU) y = z * sigmoid(z);
+    if (act == IOLB_ACT_GELU) y = z * normal_below(z, __expf(-0.5f * z * z));
+    if (act == IOLB_ACT_GELU_TANH) y = z * sigmoid(GELU_TANH_K * (z + 0.044715f * z * z * z));
+    return act != IOLB_ACT_NONE && z == -__builtin_inff() ? 0.f : y;
+}
+
+// dy act'(z).  Beyond |z| = 60 the slopes are 0 or 1 to every bit; cutting z there keeps its powers finite.
+// (Comparisons, not fmin: a NaN stays one.)
+__device__ __forceinline__ float through_activation(float dy, float z, int act)
+{
+    if (act == IOLB_ACT_RELU) return z <= 0.f ? 0.f : z > 0.f ? dy : z;
+    z = z > 60.f ? 60.f : z < -60.f ? -60.f : z;
+    float slope = 1.f;
+    if (act == IOLB_ACT_SILU) {
+        const float s = sigmoid(z);
+        slope = s * (1.f + z * (1.f - s));
+    }
+    if (act == IOLB_ACT_GELU) {
+        const float g = __expf(-0.5f * z * z);
+        slope = normal_below(z, g) + z * g * 0.3989422804f;
+    }
+    if (act == IOLB_ACT_GELU_TANH) {
+        const float s = sigmoid(GELU_TANH_K * (z + 0.044715f * z * z * z));
+        slope = s + z * s * (1.f - s) * GELU_TANH_K * (1.f + 0.134145f * z * z);
+    }
+    return dy * slope;
+}
+
+// ---- the 8-bit code ---------------------------------------------------------------------------------
+// A block's values are q 2^e, q from -127 to 127, e the least exponent with |x| <= 127 2^e for its finite values, kept so that
+// every value is one of the tensor's type (fp16: multiples of 2^-24 up to 65504; else of 2^-126).  A power of two as the scale makes
+// the values exact in bf16: the backward pass hands them to the matrix cores without a second rounding, and an fp32 layer's
+// weight gradient needs three products of parts instead of six.  It costs up to one bit against a scale of max / 127.
+// q = -128 is a value that is not finite; it reads back as NaN.
+struct CkptRange { int lo, hi; };
+template <int DT> __device__ __forceinline__ CkptRange ckpt_range() { return DT == IOLB_F16 ? CkptRange{-24, 10} : CkptRange{-126, 122}; }
+
+__device__ __forceinline__ float finite_magnitude(float x)
+{
+    const float a = fabsf(x);
+    return a < __builtin_inff() ? a : 0.f;              // (false for NaN too)
+}
+
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }   // -126 <= e <= 127
+
+template <int DT>
+__device__ __forceinline__ int ckpt_exponent(float most)
+{
+    const unsigned u = __float_as_uint(most);
+    const int e = (int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x7e0000u ? 6 : 5);    // 127 = 1.984375 * 2^6
+    const CkptRange r = ckpt_range<DT>();
+    return e < r.lo ? r.lo : e > r.hi ? r.hi : e;
+}
+
+// x 2^-e rounded to nearest even, as the low byte.  At the largest exponent 64 2^e is beyond the type: 63 there.
+template <int DT>
+__device__ __forceinline__ unsigned ckpt_code(float x, int e)
+{
+    const float top = e == ckpt_range<DT>().hi ? 63.f : 127.f;
+    float q = __builtin_rintf(x * two_to(-e));
+    q = q > top ? top : q < -top ? -top : q;
+    const int code = fabsf(x) < __builtin_inff() ? (int)q : -128;
+    return (unsigned)code & 0xffu;
+}
+
+__device__ __forceinline__ float ckpt_value(int code, float unit) { return code == -128 ? __builtin_nanf("") : (float)code * unit; }
+
+// ---- three bf16 parts of an fp32 value ----------------------------------------------------------------
+__device__ __forceinline__ void dense_parts(float a, unsigned short& h, unsigned short& m, unsigned short& l)
+{
+    const unsigned u = __float_as_uint(a);
+    unsigned short hh = __builtin_bit_cast(unsigned short, (__bf16)a);
+    const bool finite = (u & 0x7f800000u) != 0x7f800000u;
+    if (finite && (hh & 0x7f80u) == 0x7f80u) hh = (unsigned short)(u >> 16);
+    const float r = finite ? a - __uint_as_float((unsigned)hh << 16) : 0.f;
+    const unsigned short mm = __builtin_bit_cast(unsigned short, (__bf16)r);
+    h = hh;
+    m = mm;
+    l = __builtin_bit_cast(unsigned short, (__bf16)(r - __uint_as_float((unsigned)mm << 16)));
+}
+
+// ---- the end of a product: four neighbouring columns n .. n + 3 of row m ---------------------------------
+template <class T>
+__device__ __forceinline__ void load_four(const T* p, int have, bool vec, float (&v)[4])
+{
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    if (vec && have > 0) {
+        const T4 t = *reinterpret_cast<const T4*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < have ? (float)p[i] : 0.f;
+    }
+}
+
+// z = sum + bias (+ residual, if it comes first)
+template <int DT>
+__device__ __forceinline__ void finish_sum(const DenseFinish& f, int m, int n, float (&z)[4])
+{
+    typedef typename DenseType<DT>::type T;
+    const int have = f.N - n;
+    float v[4];
+    if (f.bias) {
+        load_four(static_cast<const T*>(f.bias) + n, have, f.vec_bias, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += v[i];
+    }
+    if (f.residual && f.first) {
+        load_four(static_cast<const T*>(f.residual) + m * f.ldr + n, have, f.vec_res, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += v[i];
+    }
+}
+
+__device__ __forceinline__ void store_codes(int8_t* p, unsigned four, int have, bool vec)
+{
+    if (vec && have > 0) {
+        *reinterpret_cast<unsigned*>(p) = four;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) p[i] = (int8_t)(four >> 8 * i);
+    }
+}
+
+// The block's largest finite magnitude is `most`; `first_lane`: this lane writes the block's exponent.
+template <int DT>
+__device__ __forceinline__ void finish_checkpoint(const DenseFinish& f, int m, int n, const float (&z)[4], float most, bool first_lane)
+{
+    const int e = ckpt_exponent<DT>(most);
+    unsigned four = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) four |= ckpt_code<DT>(z[i], e) << 8 * i;
+    store_codes(f.zq + (long long)m * f.N + n, four, f.N - n, f.vec_q);
+    if (first_lane && n < f.N) f.ze[(long long)m * ((f.N + CKPT_BLOCK - 1) / CKPT_BLOCK) + n / CKPT_BLOCK] = (uint8_t)(e + 127);
+}
+
+// y = act(z) (+ residual, if it comes after); the one rounding to y's type
+template <int DT>
+__device__ __forceinline__ void finish_store(const DenseFinish& f, int m, int n, float (&z)[4])
+{
+    typedef typename DenseType<DT>::type T;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const int have = f.N - n;
+    if (f.act != IOLB_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = activate(z[i], f.act);
+    }
+    if (f.residual && !f.first) {
+        float v[4];
+        load_four(static_cast<const T*>(f.residual) + m * f.ldr + n, have, f.vec_res, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += v[i];
+    }
+    T* y = static_cast<T*>(f.y) + m * f.ldy + n;
+    if (f.vec_y && have > 0) {
+        T4 t;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] = (T)z[i];
+        *reinterpret_cast<T4*>(y) = t;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) y[i] = (T)z[i];
+    }
+}
+
+}  // namespace iolb
+
+#endif
