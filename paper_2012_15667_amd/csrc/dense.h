@@ -44,6 +44,7 @@ struct DenseProduct {
     long long a_plane[MAX_SEGMENTS], b_plane[MAX_SEGMENTS];   // where the segment's planes start, in elements
     int splits;                             // workgroups that share a tile's K; their sums go to `partial` if > 1
     float* partial;                         // [splits][M][N rounded up to 4]
+    int vec_a, vec_b;                       // kernels for few rows: whole 16-byte pieces of the operand may be read
     DenseFinish f;
 };
 
@@ -51,12 +52,18 @@ struct DenseProduct {
 enum { DENSE_TILE_256, DENSE_TILE_128, DENSE_TILE_64, DENSE_TILES };
 struct DenseTilePlan { int tile, splits; };
 DenseTilePlan dense_tile_plan(int M, int N, int K, int segments);
-inline size_t dense_partial_bytes(int splits, long long M, long long N)
-{
-    return splits > 1 ? (size_t)splits * M * ((N + 3) / 4 * 4) * 4 : 0;
-}
+inline size_t dense_partial_bytes(int splits, long long M, long long N) { return (size_t)splits * M * ((N + 3) / 4 * 4) * 4; }
 // dtype: of y, bias and residual; f16: the operands are fp16 (else bf16).
 hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st);
+
+// The same for few rows of A: both operands as the caller holds them (fp32 too: taken apart in the kernels), any K, bound by reading
+// B.  across: B is [K][N], summed along its rows.  K is shared by `splits` workgroups.  Sums go to `partial` if join is set
+// (always with splits > 1 or a checkpoint).
+constexpr int DENSE_ROWS_MOST = 64;
+struct DenseRowsPlan { int splits; bool join; };
+DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint);
+hipError_t launch_dense_rows(const DenseProduct& p, bool across, bool join, int dtype, hipStream_t st);
+hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st);
 
 // ---- operands laid out for the product --------------------------------------------------------------
 // Values v[r][c], rows x cols, from one of three sources:

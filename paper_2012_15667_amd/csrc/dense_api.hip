@@ -76,7 +76,26 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     const int64_t Kp = up8(a.K);
     const int planes = a.dtype == IOLB_F32 ? 3 : 1;
     DenseProduct p{};
-    p.M = (int)a.M; p.N = (int)a.N; p.K = (int)Kp;
+    const int64_t four = 4 * size_of(a.dtype);
+    p.f = DenseFinish{a.bias, a.residual, a.y, a.zq, a.ze, a.ldr, a.ldy, (int)a.M, (int)a.N, a.act, a.residual_first != 0,
+                      a.N % 4 == 0 && aligned_to(a.bias, four),
+                      a.N % 4 == 0 && a.ldr % 4 == 0 && aligned_to(a.residual, four),
+                      a.N % 4 == 0 && a.ldy % 4 == 0 && aligned_to(a.y, four),
+                      a.N % 4 == 0 && aligned_to(a.zq, 4)};
+    const auto pieces_of_16 = [&](const void* t, int64_t ld) { return aligned_to(t, 16) && ld * size_of(a.dtype) % 16 == 0; };
+    p.M = (int)a.M; p.N = (int)a.N;
+    if (a.M <= DENSE_ROWS_MOST) {
+        p.a = a.x; p.lda = a.ldx; p.vec_a = a.M == 1 ? aligned_to(a.x, 16) : pieces_of_16(a.x, a.ldx);
+        p.b = a.w; p.ldb = a.ldw; p.vec_b = a.N == 1 ? aligned_to(a.w, 16) : pieces_of_16(a.w, a.ldw);
+        p.K = (int)a.K;
+        const DenseRowsPlan plan = dense_rows_plan(p.M, p.N, p.K, a.dtype, false, a.zq != nullptr);
+        p.splits = plan.splits;
+        if (plan.join) p.partial = static_cast<float*>(pieces.take(dense_partial_bytes(plan.splits, a.M, a.N)));
+        *need = pieces.used;
+        if (launch) DENSE_HIP(launch_dense_rows(p, false, plan.join, a.dtype, call_stream()));
+        return IOLB_OK;
+    }
+    p.K = (int)Kp;
     segments(&p, planes, planes, a.M * Kp, a.N * Kp);
     const bool x_direct = direct(a.x, a.ldx, a.K, a.dtype) || a.K == 0, w_direct = direct(a.w, a.ldw, a.K, a.dtype) || a.K == 0;
     p.a = a.x; p.lda = a.ldx;
@@ -86,16 +105,10 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     if (!w_direct) { p.b = wp = pieces.take((size_t)planes * a.N * Kp * 2); p.ldb = Kp; }
     const DenseTilePlan plan = dense_tile_plan(p.M, p.N, p.K, p.segments);
     p.splits = plan.splits;
-    p.partial = static_cast<float*>(pieces.take(dense_partial_bytes(plan.splits, a.M, a.N)));
+    if (plan.splits > 1) p.partial = static_cast<float*>(pieces.take(dense_partial_bytes(plan.splits, a.M, a.N)));
     *need = pieces.used;
     if (!launch) return IOLB_OK;
 
-    const int64_t four = 4 * size_of(a.dtype);
-    p.f = DenseFinish{a.bias, a.residual, a.y, a.zq, a.ze, a.ldr, a.ldy, p.M, p.N, a.act, a.residual_first != 0,
-                      a.N % 4 == 0 && aligned_to(a.bias, four),
-                      a.N % 4 == 0 && a.ldr % 4 == 0 && aligned_to(a.residual, four),
-                      a.N % 4 == 0 && a.ldy % 4 == 0 && aligned_to(a.y, four),
-                      a.N % 4 == 0 && aligned_to(a.zq, 4)};
     const hipStream_t st = call_stream();
     const auto lay = [&](const void* src, int64_t ld, int64_t rows, void* to) {
         DenseLayout l{};
@@ -137,35 +150,51 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     // the input's checkpoint is exact in one bf16 part, unless a smooth activation has to be taken of it
     const int planes_x = planes == 3 && a.x_act != IOLB_ACT_NONE && a.x_act != IOLB_ACT_RELU ? 3 : 1;
     const int64_t Mp = up8(a.M), Np = up8(a.N);
-    const bool want_dx = a.dx && a.M > 0 && a.K > 0, want_dw = a.dw && a.N > 0 && a.K > 0;
+    const bool want_dx = a.dx && a.M > 0 && a.K > 0, few = a.M <= DENSE_ROWS_MOST, want_dw = a.dw && a.N > 0 && a.K > 0;
     const bool has_z = a.act != IOLB_ACT_NONE;
 
     // dz = dy act'(z) along the rows for dx (dy itself where that is it), transposed for dW
-    const bool dy_is_dz = !has_z && direct(a.dy, a.ldy, a.N, a.dtype);
-    const bool dz_is_plane = a.dz && direct(a.dz, a.N, a.N, a.dtype);
+    // (few rows: dx is taken from dz in the tensor's own type, dense, and from w as it is)
+    const bool dy_is_dz = !has_z && (few || direct(a.dy, a.ldy, a.N, a.dtype));
+    const bool dz_is_plane = a.dz && !few && direct(a.dz, a.N, a.N, a.dtype);
     const void* dz = a.dy;
     int64_t ld_dz = a.ldy;
-    void *dz_to = nullptr, *dzt = nullptr, *wt = nullptr, *xt = nullptr;
-    if (want_dx && !dy_is_dz) {
+    void *dz_to = nullptr, *dz_copy = a.dz, *dzt = nullptr, *wt = nullptr, *xt = nullptr;
+    if (want_dx && !dy_is_dz && few) {
+        if (!dz_copy) dz_copy = pieces.take((size_t)(a.M * a.N * size_of(a.dtype)));
+        ld_dz = a.N;
+        dz = dz_copy;
+    } else if (want_dx && !dy_is_dz) {
         ld_dz = Np;
         dz = dz_to = dz_is_plane ? a.dz : pieces.take((size_t)planes * a.M * Np * 2);
+        if (dz_is_plane) dz_copy = nullptr;
     }
     if (want_dw) {
         dzt = pieces.take((size_t)planes * a.N * Mp * 2);
         xt = pieces.take((size_t)planes_x * a.K * Mp * 2);
     }
-    if (want_dx) wt = pieces.take((size_t)planes * a.K * Np * 2);
+    if (want_dx && !few) wt = pieces.take((size_t)planes * a.K * Np * 2);
     const int row_blocks = (int)((a.M + 63) / 64);
     float* const sums = static_cast<float*>(a.db ? pieces.take((size_t)row_blocks * a.N * 4) : nullptr);
 
     DenseProduct px{}, pw{};
     DenseTilePlan plan_x{}, plan_w{};
-    if (want_dx) {
+    DenseRowsPlan rows_x{};
+    size_t partial_x = 0, partial_w = 0;
+    if (want_dx && few) {
+        px.M = (int)a.M; px.N = (int)a.K; px.K = (int)a.N;
+        px.a = dz; px.lda = ld_dz; px.vec_a = aligned_to(dz, 16) && (a.M == 1 || ld_dz * size_of(a.dtype) % 16 == 0);
+        px.b = a.w; px.ldb = a.ldw; px.vec_b = aligned_to(a.w, 4 * size_of(a.dtype)) && (a.N == 1 || a.ldw % 4 == 0);
+        rows_x = dense_rows_plan(px.M, px.N, px.K, a.dtype, true, false);
+        px.splits = rows_x.splits;
+        if (rows_x.join) partial_x = dense_partial_bytes(px.splits, px.M, px.N);
+    } else if (want_dx) {
         px.M = (int)a.M; px.N = (int)a.K; px.K = (int)Np;
         px.a = dz; px.lda = ld_dz; px.b = wt; px.ldb = Np;
         segments(&px, planes, planes, a.M * Np, a.K * Np);
         plan_x = dense_tile_plan(px.M, px.N, px.K, px.segments);
         px.splits = plan_x.splits;
+        if (px.splits > 1) partial_x = dense_partial_bytes(px.splits, px.M, px.N);
     }
     if (want_dw) {
         pw.M = (int)a.N; pw.N = (int)a.K; pw.K = (int)Mp;
@@ -173,15 +202,15 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         segments(&pw, planes, planes_x, a.N * Mp, a.K * Mp);
         plan_w = dense_tile_plan(pw.M, pw.N, pw.K, pw.segments);
         pw.splits = plan_w.splits;
+        if (pw.splits > 1) partial_w = dense_partial_bytes(pw.splits, pw.M, pw.N);
     }
     // one after the other on the stream: they share the room for partial sums
-    px.partial = pw.partial = static_cast<float*>(pieces.take(std::max(dense_partial_bytes(plan_x.splits, px.M, px.N),
-                                                                       dense_partial_bytes(plan_w.splits, pw.M, pw.N))));
+    px.partial = pw.partial = static_cast<float*>(pieces.take(std::max(partial_x, partial_w)));
     *need = pieces.used;
     if (!launch) return IOLB_OK;
 
     const hipStream_t st = call_stream();
-    if (a.M > 0 && a.N > 0 && (dz_to || dzt || a.dz || sums)) {
+    if (a.M > 0 && a.N > 0 && (dz_to || dzt || dz_copy || sums)) {
         DenseLayout l{};
         l.rows = (int)a.M; l.cols = (int)a.N;
         l.src = a.dy; l.ld = a.ldy;
@@ -190,7 +219,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         l.vec_q = a.N % 8 == 0 && aligned_to(a.zq, 8);
         l.rowmajor = dz_to; l.ld_rm = Np;
         l.transposed = dzt; l.ld_tr = Mp;
-        l.copy = dz_to && dz_is_plane ? nullptr : a.dz;
+        l.copy = dz_copy;
         l.colsum = sums;
         DENSE_HIP(launch_dense_layout(DENSE_FROM_GRADIENT, a.dtype, planes, l, st));
     }
@@ -202,7 +231,10 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         f.vec_y = n % 4 == 0 && aligned_to(out, 4 * size_of(a.dtype));
         return f;
     };
-    if (want_dx) {
+    if (want_dx && few) {
+        px.f = finish(a.dx, a.M, a.K);
+        DENSE_HIP(launch_dense_rows(px, true, rows_x.join, a.dtype, st));
+    } else if (want_dx) {
         DenseLayout l{};
         l.rows = (int)a.N; l.cols = (int)a.K;
         l.src = a.w; l.ld = a.ldw;

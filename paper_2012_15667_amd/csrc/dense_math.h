@@ -115,6 +115,19 @@ __device__ __forceinline__ void dense_parts(float a, unsigned short& h, unsigned
     l = __builtin_bit_cast(unsigned short, (__bf16)(r - __uint_as_float((unsigned)mm << 16)));
 }
 
+// ---- products -----------------------------------------------------------------------------------------
+template <bool F16>
+__device__ __forceinline__ f32x4 multiply(const u32x4& a, const u32x4& b, const f32x4& c)
+{
+    if constexpr (F16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Where 16-byte piece c of a 128-byte row lies in LDS: sixteen rows' pieces of the same c fall on different banks.
+__device__ __forceinline__ int place(int row, int piece) { return piece ^ (row & 7); }
+
 // ---- the end of a product: four neighbouring columns n .. n + 3 of row m ---------------------------------
 template <class T>
 __device__ __forceinline__ void load_four(const T* p, int have, bool vec, float (&v)[4])

@@ -17,20 +17,9 @@ namespace {
 constexpr int STEP = 64;                               // k of a stage
 constexpr int ROW_BYTES = 2 * STEP;
 
-__device__ __forceinline__ int place(int row, int piece) { return piece ^ (row & 7); }
-
 __device__ __forceinline__ void dma16(const char* base, unsigned offset, unsigned lds)
 {
     lds_dma_load_16(reinterpret_cast<const float*>(base), offset, lds);
-}
-
-template <bool F16>
-__device__ __forceinline__ f32x4 multiply(const u32x4& a, const u32x4& b, const f32x4& c)
-{
-    if constexpr (F16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 template <bool F16, int DT, int BM, int BN, int WM, int WN>
@@ -275,7 +264,11 @@ hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipS
 {
     hipError_t e = dtype == IOLB_F32 ? launch_tile<false, IOLB_F32>(p, tile, st)
                  : dtype == IOLB_F16 ? launch_tile<true, IOLB_F16>(p, tile, st) : launch_tile<false, IOLB_BF16>(p, tile, st);
-    if (e != hipSuccess || p.splits == 1) return e;
+    return e != hipSuccess || p.splits == 1 ? e : launch_dense_join(p, dtype, st);
+}
+
+hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st)
+{
     const dim3 grid((unsigned)((p.N + 1023) / 1024), (unsigned)(p.M < 65535 ? p.M : 65535));
     if (dtype == IOLB_F32) dense_join_kernel<IOLB_F32><<<grid, 256, 0, st>>>(p);
     else if (dtype == IOLB_F16) dense_join_kernel<IOLB_F16><<<grid, 256, 0, st>>>(p);
