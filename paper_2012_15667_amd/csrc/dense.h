@@ -31,7 +31,7 @@ struct DenseFinish {
     long long ldr, ldy;
     int M, N;
     int act, first;                         // first: the residual is added before the activation
-    int vec_bias, vec_res, vec_y, vec_q;    // four neighbouring columns may be read / written at once
+    int vec_bias, vec_res, vec_y, vec_q;    // eight neighbouring columns may be read / written as whole 16- or 8-byte pieces
 };
 
 // C[m][n] = sum over segments and k of A[m][k] B[n][k]; both operands contiguous along k, 16-byte aligned rows.

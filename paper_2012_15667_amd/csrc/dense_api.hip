@@ -76,13 +76,11 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     const int64_t Kp = up8(a.K);
     const int planes = a.dtype == IOLB_F32 ? 3 : 1;
     DenseProduct p{};
-    const int64_t four = 4 * size_of(a.dtype);
-    p.f = DenseFinish{a.bias, a.residual, a.y, a.zq, a.ze, a.ldr, a.ldy, (int)a.M, (int)a.N, a.act, a.residual_first != 0,
-                      a.N % 4 == 0 && aligned_to(a.bias, four),
-                      a.N % 4 == 0 && a.ldr % 4 == 0 && aligned_to(a.residual, four),
-                      a.N % 4 == 0 && a.ldy % 4 == 0 && aligned_to(a.y, four),
-                      a.N % 4 == 0 && aligned_to(a.zq, 4)};
     const auto pieces_of_16 = [&](const void* t, int64_t ld) { return aligned_to(t, 16) && ld * size_of(a.dtype) % 16 == 0; };
+    const bool eights = a.N % 8 == 0;
+    p.f = DenseFinish{a.bias, a.residual, a.y, a.zq, a.ze, a.ldr, a.ldy, (int)a.M, (int)a.N, a.act, a.residual_first != 0,
+                      eights && aligned_to(a.bias, 16), eights && pieces_of_16(a.residual, a.M == 1 ? 8 : a.ldr),
+                      eights && pieces_of_16(a.y, a.M == 1 ? 8 : a.ldy), eights && aligned_to(a.zq, 8)};
     p.M = (int)a.M; p.N = (int)a.N;
     if (a.M <= DENSE_ROWS_MOST) {
         p.a = a.x; p.lda = a.ldx; p.vec_a = a.M == 1 ? aligned_to(a.x, 16) : pieces_of_16(a.x, a.ldx);
@@ -228,7 +226,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         DenseFinish f{};
         f.y = out; f.ldy = n; f.M = (int)m; f.N = (int)n;
         f.act = IOLB_ACT_NONE;
-        f.vec_y = n % 4 == 0 && aligned_to(out, 4 * size_of(a.dtype));
+        f.vec_y = n % 8 == 0 && aligned_to(out, 16);
         return f;
     };
     if (want_dx && few) {

@@ -70,11 +70,13 @@ dense_layout_kernel(DenseLayout g, int blocks_c)
                 float z[8];
                 const float unit = two_to((int)g.e[r * blocks_q + c / CKPT_BLOCK] - 127);
                 load_checkpoint(g.q + (long long)r * g.cols + c, unit, have, g.vec_q, z);
+                by_activation(g.act, [&](auto act) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if constexpr (SOURCE == DENSE_FROM_CHECKPOINT) v[i] = activate(z[i], g.act);
-                    else v[i] = i < have ? through_activation(v[i], z[i], g.act) : 0.f;
-                }
+                    for (int i = 0; i < 8; ++i) {
+                        if constexpr (SOURCE == DENSE_FROM_CHECKPOINT) v[i] = activate<decltype(act)::value>(z[i]);
+                        else v[i] = i < have ? through_activation<decltype(act)::value>(v[i], z[i]) : 0.f;
+                    }
+                });
             }
         }
         unsigned short bits[8][PLANES];
@@ -199,8 +201,10 @@ checkpoint_unpack_kernel(const int8_t* q, const uint8_t* e, int rows, int cols, 
         load_checkpoint(q + r * cols + c, two_to((int)e[r * blocks + c / CKPT_BLOCK] - 127), have, vec_q, v);
         T* const to = static_cast<T*>(y) + r * ldy + c;
         T8 t;
+        by_activation(act, [&](auto a) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = (T)activate(v[i], act);
+            for (int i = 0; i < 8; ++i) t[i] = (T)activate<decltype(a)::value>(v[i]);
+        });
         if (vec_y && have >= 8) {
             *reinterpret_cast<T8*>(to) = t;
         } else {

@@ -5,6 +5,8 @@
 #include "dense.h"
 #include "split_mfma.h"
 
+#include <type_traits>
+
 namespace iolb {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -30,36 +32,53 @@ __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf
 constexpr float GELU_TANH_K = 1.5957691216f;      // 2 sqrt(2 / pi): (1 + tanh u) / 2 is the sigmoid of 2 u
 
 // Smooth activations tend to zero at -inf, where their formula is 0 x inf.
-__device__ __forceinline__ float activate(float z, int act)
+template <int ACT>
+__device__ __forceinline__ float activate(float z)
 {
-    float y = z;
-    if (act == IOLB_ACT_RELU) return z <= 0.f ? 0.f : z;
-    if (act == IOLB_ACT_SILU) y = z * sigmoid(z);
-    if (act == IOLB_ACT_GELU) y = z * normal_below(z, __expf(-0.5f * z * z));
-    if (act == IOLB_ACT_GELU_TANH) y = z * sigmoid(GELU_TANH_K * (z + 0.044715f * z * z * z));
-    return act != IOLB_ACT_NONE && z == -__builtin_inff() ? 0.f : y;
+    if constexpr (ACT == IOLB_ACT_NONE) return z;
+    if constexpr (ACT == IOLB_ACT_RELU) return z <= 0.f ? 0.f : z;
+    float y;
+    if constexpr (ACT == IOLB_ACT_SILU) y = z * sigmoid(z);
+    if constexpr (ACT == IOLB_ACT_GELU) y = z * normal_below(z, __expf(-0.5f * z * z));
+    if constexpr (ACT == IOLB_ACT_GELU_TANH) y = z * sigmoid(GELU_TANH_K * (z + 0.044715f * z * z * z));
+    return z == -__builtin_inff() ? 0.f : y;
 }
 
 // dy act'(z).  Beyond |z| = 60 the slopes are 0 or 1 to every bit; cutting z there keeps its powers finite.
 // (Comparisons, not fmin: a NaN stays one.)
-__device__ __forceinline__ float through_activation(float dy, float z, int act)
+template <int ACT>
+__device__ __forceinline__ float through_activation(float dy, float z)
 {
-    if (act == IOLB_ACT_RELU) return z <= 0.f ? 0.f : z > 0.f ? dy : z;
+    if constexpr (ACT == IOLB_ACT_NONE) return dy;
+    if constexpr (ACT == IOLB_ACT_RELU) return z <= 0.f ? 0.f : z > 0.f ? dy : z;
     z = z > 60.f ? 60.f : z < -60.f ? -60.f : z;
-    float slope = 1.f;
-    if (act == IOLB_ACT_SILU) {
+    float slope;
+    if constexpr (ACT == IOLB_ACT_SILU) {
         const float s = sigmoid(z);
         slope = s * (1.f + z * (1.f - s));
     }
-    if (act == IOLB_ACT_GELU) {
+    if constexpr (ACT == IOLB_ACT_GELU) {
         const float g = __expf(-0.5f * z * z);
         slope = normal_below(z, g) + z * g * 0.3989422804f;
     }
-    if (act == IOLB_ACT_GELU_TANH) {
+    if constexpr (ACT == IOLB_ACT_GELU_TANH) {
         const float s = sigmoid(GELU_TANH_K * (z + 0.044715f * z * z * z));
         slope = s + z * s * (1.f - s) * GELU_TANH_K * (1.f + 0.134145f * z * z);
     }
     return dy * slope;
+}
+
+// f called with the activation as an integral constant.
+template <class F>
+__device__ __forceinline__ void by_activation(int act, F f)
+{
+    switch (act) {
+    case IOLB_ACT_RELU: f(std::integral_constant<int, IOLB_ACT_RELU>{}); break;
+    case IOLB_ACT_SILU: f(std::integral_constant<int, IOLB_ACT_SILU>{}); break;
+    case IOLB_ACT_GELU: f(std::integral_constant<int, IOLB_ACT_GELU>{}); break;
+    case IOLB_ACT_GELU_TANH: f(std::integral_constant<int, IOLB_ACT_GELU_TANH>{}); break;
+    default: f(std::integral_constant<int, IOLB_ACT_NONE>{}); break;
+    }
 }
 
 // ---- the 8-bit code ---------------------------------------------------------------------------------
@@ -128,91 +147,123 @@ __device__ __forceinline__ f32x4 multiply(const u32x4& a, const u32x4& b, const 
 // Where 16-byte piece c of a 128-byte row lies in LDS: sixteen rows' pieces of the same c fall on different banks.
 __device__ __forceinline__ int place(int row, int piece) { return piece ^ (row & 7); }
 
-// ---- the end of a product: four neighbouring columns n .. n + 3 of row m ---------------------------------
-template <class T>
-__device__ __forceinline__ void load_four(const T* p, int have, bool vec, float (&v)[4])
+// ---- the end of a product: W (4 or 8) neighbouring columns n ... of row m --------------------------------
+// `vec` flags of DenseFinish hold for eight columns, and so for four.
+template <int W, class T>
+__device__ __forceinline__ void load_columns(const T* p, int have, bool vec, float (&v)[W])
 {
-    typedef T T4 __attribute__((ext_vector_type(4)));
+    typedef T TW __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
     if (vec && have > 0) {
-        const T4 t = *reinterpret_cast<const T4*>(p);
+        const TW t = *reinterpret_cast<const TW*>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
+        for (int i = 0; i < W; ++i) v[i] = (float)t[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < have ? (float)p[i] : 0.f;
+        for (int i = 0; i < W; ++i) v[i] = i < have ? (float)p[i] : 0.f;
     }
 }
 
-// z = sum + bias (+ residual, if it comes first)
-template <int DT>
-__device__ __forceinline__ void finish_sum(const DenseFinish& f, int m, int n, float (&z)[4])
+template <int DT, int W>
+__device__ __forceinline__ void load_bias(const DenseFinish& f, int n, float (&b)[W])
 {
     typedef typename DenseType<DT>::type T;
-    const int have = f.N - n;
-    float v[4];
     if (f.bias) {
-        load_four(static_cast<const T*>(f.bias) + n, have, f.vec_bias, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] += v[i];
-    }
-    if (f.residual && f.first) {
-        load_four(static_cast<const T*>(f.residual) + m * f.ldr + n, have, f.vec_res, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] += v[i];
-    }
-}
-
-__device__ __forceinline__ void store_codes(int8_t* p, unsigned four, int have, bool vec)
-{
-    if (vec && have > 0) {
-        *reinterpret_cast<unsigned*>(p) = four;
+        load_columns(static_cast<const T*>(f.bias) + n, f.N - n, f.vec_bias, b);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < have) p[i] = (int8_t)(four >> 8 * i);
+        for (int i = 0; i < W; ++i) b[i] = 0.f;
     }
 }
 
-// The block's largest finite magnitude is `most`; `first_lane`: this lane writes the block's exponent.
-template <int DT>
-__device__ __forceinline__ void finish_checkpoint(const DenseFinish& f, int m, int n, const float (&z)[4], float most, bool first_lane)
+template <int DT, int W>
+__device__ __forceinline__ void add_residual(const DenseFinish& f, int m, int n, float (&z)[W])
 {
-    const int e = ckpt_exponent<DT>(most);
-    unsigned four = 0;
+    typedef typename DenseType<DT>::type T;
+    float v[W];
+    load_columns(static_cast<const T*>(f.residual) + m * f.ldr + n, f.N - n, f.vec_res, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) four |= ckpt_code<DT>(z[i], e) << 8 * i;
-    store_codes(f.zq + (long long)m * f.N + n, four, f.N - n, f.vec_q);
-    if (first_lane && n < f.N) f.ze[(long long)m * ((f.N + CKPT_BLOCK - 1) / CKPT_BLOCK) + n / CKPT_BLOCK] = (uint8_t)(e + 127);
+    for (int i = 0; i < W; ++i) z[i] += v[i];
+}
+
+template <int W>
+__device__ __forceinline__ float largest_of(const float (&z)[W], int have)
+{
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) most = i < have ? fmaxf(most, finite_magnitude(z[i])) : most;
+    return most;
+}
+
+// Eight columns; the block's largest finite magnitude is `most`, and its first lane writes the exponent.
+template <int DT>
+__device__ __forceinline__ void store_codes(const DenseFinish& f, int m, int n, const float (&z)[8], float most)
+{
+    const int e = ckpt_exponent<DT>(most), have = f.N - n;
+    u32x2 code = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) code[i / 4] |= ckpt_code<DT>(z[i], e) << 8 * (i % 4);
+    int8_t* const to = f.zq + (long long)m * f.N + n;
+    if (f.vec_q) {
+        *reinterpret_cast<u32x2*>(to) = code;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < have) to[i] = (int8_t)(code[i / 4] >> 8 * (i % 4));
+    }
+    if (n % CKPT_BLOCK == 0) f.ze[(long long)m * ((f.N + CKPT_BLOCK - 1) / CKPT_BLOCK) + n / CKPT_BLOCK] = (uint8_t)(e + 127);
 }
 
 // y = act(z) (+ residual, if it comes after); the one rounding to y's type
-template <int DT>
-__device__ __forceinline__ void finish_store(const DenseFinish& f, int m, int n, float (&z)[4])
+template <int DT, int ACT, int W>
+__device__ __forceinline__ void store_columns(const DenseFinish& f, int m, int n, float (&z)[W])
 {
     typedef typename DenseType<DT>::type T;
-    typedef T T4 __attribute__((ext_vector_type(4)));
+    typedef T TW __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
     const int have = f.N - n;
-    if (f.act != IOLB_ACT_NONE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = activate(z[i], f.act);
-    }
-    if (f.residual && !f.first) {
-        float v[4];
-        load_four(static_cast<const T*>(f.residual) + m * f.ldr + n, have, f.vec_res, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] += v[i];
-    }
+    for (int i = 0; i < W; ++i) z[i] = activate<ACT>(z[i]);
+    if (f.residual && !f.first) add_residual<DT>(f, m, n, z);
     T* y = static_cast<T*>(f.y) + m * f.ldy + n;
-    if (f.vec_y && have > 0) {
-        T4 t;
+    if (f.vec_y) {
+        TW t;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = (T)z[i];
-        *reinterpret_cast<T4*>(y) = t;
+        for (int i = 0; i < W; ++i) t[i] = (T)z[i];
+        *reinterpret_cast<TW*>(y) = t;
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < W; ++i)
             if (i < have) y[i] = (T)z[i];
     }
+}
+
+// Four columns without a checkpoint, for a wave that holds them in one lane.
+template <int DT>
+__device__ __forceinline__ void finish_four(const DenseFinish& f, int m, int n, const f32x4& sum)
+{
+    if (m >= f.M || n >= f.N) return;
+    float z[4], b[4];
+    load_bias<DT>(f, n, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = sum[i] + b[i];
+    if (f.residual && f.first) add_residual<DT>(f, m, n, z);
+    by_activation(f.act, [&](auto act) { store_columns<DT, decltype(act)::value>(f, m, n, z); });
+}
+
+// Eight columns of row m, which four neighbouring lanes continue to a checkpoint's block.  Every lane of the wave calls.
+template <int DT, int ACT>
+__device__ __forceinline__ void finish_eight(const DenseFinish& f, int m, int n, const float (&bias)[8], float (&z)[8])
+{
+    const bool live = m < f.M && n < f.N;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] += bias[i];
+    if (live && f.residual && f.first) add_residual<DT>(f, m, n, z);
+    if (f.zq) {
+        float most = largest_of(z, f.N - n);
+        most = fmaxf(most, __shfl_xor(most, 1));
+        most = fmaxf(most, __shfl_xor(most, 2));
+        if (live) store_codes<DT>(f, m, n, z, most);
+    }
+    if (live) store_columns<DT, ACT>(f, m, n, z);
 }
 
 }  // namespace iolb

@@ -195,10 +195,8 @@ dense_few_kernel(DenseProduct p, int join)
     const int m = l16, n = n0 + 4 * grp;
     if (join) {
         keep_partial(p, blockIdx.y, m, n, c);
-    } else if (m < p.M && n < p.N) {
-        float z[4] = {c[0], c[1], c[2], c[3]};
-        finish_sum<DT>(p.f, m, n, z);
-        finish_store<DT>(p.f, m, n, z);
+    } else {
+        finish_four<DT>(p.f, m, n, c);
     }
 }
 
@@ -390,10 +388,8 @@ dense_rows_kernel(DenseProduct p, int join)
             if constexpr (ACROSS) c = f32x4{acc[t][0][i], acc[t][1][i], acc[t][2][i], acc[t][3][i]};
             if (join) {
                 keep_partial(p, blockIdx.y, m, n, c);
-            } else if (m < p.M && n < p.N) {
-                float z[4] = {c[0], c[1], c[2], c[3]};
-                finish_sum<DT>(p.f, m, n, z);
-                finish_store<DT>(p.f, m, n, z);
+            } else {
+                finish_four<DT>(p.f, m, n, c);
             }
         }
     }

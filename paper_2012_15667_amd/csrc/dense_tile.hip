@@ -54,20 +54,20 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
 
     // Rows beyond the operand are read from its last row: their sums are never stored.
     unsigned a_off[LA], b_off[LB];
-    const int piece = lane & 7;
+    const int from_piece = place(lane >> 3, lane & 7);           // (a load's rows start at a multiple of 8)
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
         const int r = (i * WAVES + wave) * 8 + (lane >> 3), have = p.M - 1 - m0;
-        a_off[i] = (unsigned)(2 * (r < have ? r : have)) * (unsigned)p.lda + 16u * place(r, piece);
+        a_off[i] = (unsigned)(2 * (r < have ? r : have)) * (unsigned)p.lda + 16u * from_piece;
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
         const int r = (i * WAVES + wave) * 8 + (lane >> 3), have = p.N - 1 - n0;
-        b_off[i] = (unsigned)(2 * (r < have ? r : have)) * (unsigned)p.ldb + 16u * place(r, piece);
+        b_off[i] = (unsigned)(2 * (r < have ? r : have)) * (unsigned)p.ldb + 16u * from_piece;
     }
     const char* const a0 = static_cast<const char*>(p.a) + 2 * (m0 * p.lda);
     const char* const b0 = static_cast<const char*>(p.b) + 2 * (n0 * p.ldb);
-    const int my_k = 8 * place(lane >> 3, piece);               // first k of the piece this lane fetches (rows step by 8)
+    const int my_k = 8 * from_piece;                              // first k of the piece this lane fetches
 
     auto load = [&](int seg, int step, int buf) {
         const char* const a = a0 + 2 * (p.a_plane[seg] + (long long)step * STEP);
@@ -80,17 +80,17 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
             for (int i = 0; i < LB; ++i) dma16(b, b_off[i], to + BM * ROW_BYTES + (i * WAVES + wave) * 1024);
         } else {
             // the end of the summed axis: pieces beyond it are zero on both sides
-            char* const at = lds + buf * STAGE;
-            const bool inside = step * STEP + my_k < p.K;
+            if (step * STEP + my_k < p.K) {
 #pragma unroll
-            for (int i = 0; i < LA; ++i) {
-                if (inside) dma16(a, a_off[i], to + (i * WAVES + wave) * 1024);
-                else *reinterpret_cast<u32x4*>(at + (i * WAVES + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-            }
+                for (int i = 0; i < LA; ++i) dma16(a, a_off[i], to + (i * WAVES + wave) * 1024);
 #pragma unroll
-            for (int i = 0; i < LB; ++i) {
-                if (inside) dma16(b, b_off[i], to + BM * ROW_BYTES + (i * WAVES + wave) * 1024);
-                else *reinterpret_cast<u32x4*>(at + BM * ROW_BYTES + (i * WAVES + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+                for (int i = 0; i < LB; ++i) dma16(b, b_off[i], to + BM * ROW_BYTES + (i * WAVES + wave) * 1024);
+            } else {
+                char* const at = lds + buf * STAGE + wave * 1024 + lane * 16;
+#pragma unroll
+                for (int i = 0; i < LA; ++i) *reinterpret_cast<u32x4*>(at + i * WAVES * 1024) = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < LB; ++i) *reinterpret_cast<u32x4*>(at + BM * ROW_BYTES + i * WAVES * 1024) = u32x4{0, 0, 0, 0};
             }
         }
     };
@@ -102,14 +102,40 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
     const int rounds = s1 > s0 ? p.segments * (s1 - s0) : 0;
+    const int clear_at = p.segments > 1 ? rounds - (s1 - s0) : -1;
     int seg = 0, step = s0;                            // of the stage that is loaded next
-    if (rounds) load(seg, step, 0);
-    int clear_at = p.segments > 1 ? (p.segments - 1) * (s1 - s0) : -1;
-    for (int t = 0; t < rounds; ++t) {
+    auto load_next = [&](int buf) {
+        load(seg, step, buf);
+        if (++step == s1) { step = s0; ++seg; }
+    };
+
+    // A stage is 2 MI groups of NI matrix instructions: half kk (32 k), sixteen rows i of A.  The order is written out and held: after
+    // each group the reads of the operands of a later one are issued, A into a ring of MI registers, `AHEAD` groups ahead, B a half
+    // ahead, so that matrix instructions do not wait for LDS.  The one barrier of a stage stands before its last groups, when all
+    // of it has been read: the next stage has arrived then, its first reads go out behind the last groups, and the buffer is free
+    // for the stage after it.
+    constexpr int GROUPS = 2 * MI, AHEAD = MI - 2, LAST = MI == 8 ? 3 : 2;
+    u32x4 fa[MI], fb[2][NI];
+    // fragments: row l16 of sixteen, piece 4 kk + grp; the rest is the same for all lanes
+    const int frag_a = (wm * (BM / WM) + l16) * ROW_BYTES + 16 * place(l16, grp);
+    const int frag_b = (BM + wn * (BN / WN) + l16) * ROW_BYTES + 16 * place(l16, grp);
+    auto read_a = [&](const char* at, int g) {
+        fa[g % MI] = *reinterpret_cast<const u32x4*>(at + (frag_a ^ 64 * (g / MI)) + g % MI * 16 * ROW_BYTES);
+    };
+    auto read_b = [&](const char* at, int kk, int j) {
+        fb[kk][j] = *reinterpret_cast<const u32x4*>(at + (frag_b ^ 64 * kk) + j * 16 * ROW_BYTES);
+    };
+    if (rounds) {
+        load_next(0);
         lds_dma_wait_all();
         __syncthreads();
-        if (++step == s1) { step = s0; ++seg; }
-        if (t + 1 < rounds) load(seg, step, (t + 1) & 1);
+        if (rounds > 1) load_next(1);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) read_b(lds, 0, j);
+#pragma unroll
+        for (int g = 0; g < AHEAD; ++g) read_a(lds, g);
+    }
+    for (int t = 0; t < rounds; ++t) {
         if (t == clear_at) {
 #pragma unroll
             for (int i = 0; i < MI; ++i)
@@ -119,28 +145,34 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
                     for (int c = 0; c < 4; ++c) acc[i][j][c] = fabsf(acc[i][j][c]) < __builtin_inff() ? acc[i][j][c] : 0.f;
         }
         const char* const at = lds + (t & 1) * STAGE;
-#pragma unroll
-        for (int kk = 0; kk < STEP / 32; ++kk) {
-            u32x4 fa[MI], fb[NI];
-#pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int r = wn * (BN / WN) + j * 16 + l16;
-                fb[j] = *reinterpret_cast<const u32x4*>(at + (BM + r) * ROW_BYTES + 16 * place(r, kk * 4 + grp));
+        const char* const next = lds + (~t & 1) * STAGE;      // (after the last stage: read, not used)
+        static_range<0, GROUPS>([&](auto group) {
+            constexpr int g = decltype(group)::value;
+            if constexpr (g == GROUPS - LAST) {
+                lds_dma_wait_all();
+                __syncthreads();
+                if (t + 2 < rounds) load_next(t & 1);
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int r = wm * (BM / WM) + i * 16 + l16;
-                fa[i] = *reinterpret_cast<const u32x4*>(at + r * ROW_BYTES + 16 * place(r, kk * 4 + grp));
+            for (int j = 0; j < NI; ++j) acc[g % MI][j] = multiply<F16>(fb[g / MI][j], fa[g % MI], acc[g % MI][j]);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (g < NI) read_b(at, 1, g);
+            if constexpr (g + AHEAD < GROUPS) read_a(at, g + AHEAD);
+            if constexpr (g == GROUPS - LAST) {
+#pragma unroll
+                for (int j = 0; j < NI; ++j) read_b(next, 0, j);
             }
+            if constexpr (g >= GROUPS - LAST) {
+                constexpr int done = g - (GROUPS - LAST);                   // reads of A's next fragments: evenly over the last groups
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NI; ++j) acc[i][j] = multiply<F16>(fb[j], fa[i], acc[i][j]);
-        }
+                for (int i = AHEAD * done / LAST; i < AHEAD * (done + 1) / LAST; ++i) read_a(next, i);
+            }
+        });
     }
 
-    const int mw = m0 + wm * (BM / WM) + l16, nw = n0 + wn * (BN / WN) + 4 * grp;
     if (p.splits > 1) {
+        const int mw = m0 + wm * (BM / WM) + l16, nw = n0 + wn * (BN / WN) + 4 * grp;
         const long long ld = (p.N + 3) / 4 * 4;
         float* const out = p.partial + (long long)blockIdx.y * p.M * ld;
 #pragma unroll
@@ -152,69 +184,66 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
             }
         return;
     }
+
+    // The sums go through LDS, as many rows at a time as fit, so that a thread finishes eight neighbouring columns and a wave's loads
+    // and stores are whole rows.  16-byte piece c of row r lies at c ^ (r & 15).
+    constexpr int PASSES = BM * BN * 4 > 2 * (int)STAGE ? 2 : 1, PI = MI / PASSES, PASS_ROWS = WM * PI * 16;
+    constexpr int LANES = BN / 8, AT_ONCE = 64 * WAVES / LANES;             // threads of a row, rows of an iteration
+    static_assert(PASS_ROWS * BN * 4 <= 2 * (int)STAGE && PASS_ROWS % AT_ONCE == 0, "a pass fits the stages' buffers");
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds);
+    const int n = n0 + (tid % LANES) * 8;
+    float bias[8];
+    load_bias<DT>(p.f, n, bias);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        const int m = mw + i * 16;
-        const bool row = m < p.M;
+    for (int pass = 0; pass < PASSES; ++pass) {
+        if (pass || rounds) __syncthreads();
 #pragma unroll
-        for (int j = 0; j < NI; j += 2) {
-            float z[2][4];
-            float most = 0.f;
+        for (int i = 0; i < PI; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int n = nw + (j + h) * 16;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) z[h][c] = acc[i][j + h][c];
-                if (row && n < p.N) finish_sum<DT>(p.f, m, n, z[h]);
-                if (p.f.zq) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) most = n + c < p.N ? fmaxf(most, finite_magnitude(z[h][c])) : most;
-                }
+            for (int j = 0; j < NI; ++j) {
+                const int r = (wm * PI + i) * 16 + l16, c = wn * (BN / WN / 4) + j * 4 + grp;
+                sums[r * (BN / 4) + (c ^ l16)] = acc[pass * PI + i][j];
             }
-            if (p.f.zq) {
-                most = fmaxf(most, __shfl_xor(most, 16));
-                most = fmaxf(most, __shfl_xor(most, 32));
+        __syncthreads();
+        by_activation(p.f.act, [&](auto act) {
+#pragma unroll 1
+            for (int r = tid / LANES; r < PASS_ROWS; r += AT_ONCE) {
+                const int c = 2 * (tid % LANES);
+                const f32x4 lo = sums[r * (BN / 4) + (c ^ (r & 15))], hi = sums[r * (BN / 4) + ((c + 1) ^ (r & 15))];
+                float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                const int m = m0 + r / (PI * 16) * (BM / WM) + pass * PI * 16 + r % (PI * 16);
+                finish_eight<DT, decltype(act)::value>(p.f, m, n, bias, z);
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int n = nw + (j + h) * 16;
-                if (row && n < p.N) {
-                    if (p.f.zq) finish_checkpoint<DT>(p.f, m, n, z[h], most, h == 0 && grp == 0);
-                    finish_store<DT>(p.f, m, n, z[h]);
-                }
-            }
-        }
+        });
     }
 }
 
 // The sums of the workgroups that shared a tile's K, added in their order, and the epilogue.
 template <int DT>
 __global__ void __launch_bounds__(256)
-dense_join_kernel(DenseProduct p)
+dense_join_kernel(DenseProduct p, int wide_log)
 {
+    const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), rows = 256 >> wide_log;
+    const int n = (int)((blockIdx.x * (unsigned)wide + tx) * 8);
     const long long ld = (p.N + 3) / 4 * 4;
-    const int n = (blockIdx.x * 256 + threadIdx.x) * 4;
-    for (int m = blockIdx.y; m < p.M; m += gridDim.y) {
-        float z[4] = {0.f, 0.f, 0.f, 0.f};
-        if (n < p.N) {
-            const float* from = p.partial + m * ld + n;
-            for (int s = 0; s < p.splits; ++s, from += p.M * ld) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(from);
+    float bias[8];
+    load_bias<DT>(p.f, n, bias);
+    by_activation(p.f.act, [&](auto act) {
+        for (long long m = (long long)blockIdx.y * rows + (threadIdx.x >> wide_log); m - (threadIdx.x >> wide_log) < p.M; m += (long long)gridDim.y * rows) {
+            float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (m < p.M && n < p.N) {
+                const float* from = p.partial + m * ld + n;
+                const bool both = n + 4 < p.N;
+#pragma unroll 4
+                for (int s = 0; s < p.splits; ++s, from += p.M * ld) {
+                    const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = both ? *reinterpret_cast<const f32x4*>(from + 4) : f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) z[c] += v[c];
+                    for (int c = 0; c < 4; ++c) { z[c] += lo[c]; z[4 + c] += hi[c]; }
+                }
             }
-            finish_sum<DT>(p.f, m, n, z);
+            finish_eight<DT, decltype(act)::value>(p.f, (int)(m < p.M ? m : p.M), n, bias, z);
         }
-        if (p.f.zq) {
-            float most = 0.f;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) most = n + c < p.N ? fmaxf(most, finite_magnitude(z[c])) : most;
-#pragma unroll
-            for (int d = 1; d < 8; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-            if (n < p.N) finish_checkpoint<DT>(p.f, m, n, z, most, (threadIdx.x & 7) == 0);
-        }
-        if (n < p.N) finish_store<DT>(p.f, m, n, z);
-    }
+    });
 }
 
 template <bool F16, int DT, int BM, int BN, int WM, int WN>
@@ -269,10 +298,14 @@ hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipS
 
 hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st)
 {
-    const dim3 grid((unsigned)((p.N + 1023) / 1024), (unsigned)(p.M < 65535 ? p.M : 65535));
-    if (dtype == IOLB_F32) dense_join_kernel<IOLB_F32><<<grid, 256, 0, st>>>(p);
-    else if (dtype == IOLB_F16) dense_join_kernel<IOLB_F16><<<grid, 256, 0, st>>>(p);
-    else dense_join_kernel<IOLB_BF16><<<grid, 256, 0, st>>>(p);
+    int wide_log = 2;                               // threads of a row: whole blocks of 32 columns
+    while (wide_log < 8 && (8LL << wide_log) < p.N) ++wide_log;
+    const int rows = 256 >> wide_log;
+    const long long gy = ((long long)p.M + rows - 1) / rows;
+    const dim3 grid((unsigned)((p.N + (8LL << wide_log) - 1) / (8LL << wide_log)), (unsigned)(gy < 65535 ? gy : 65535));
+    if (dtype == IOLB_F32) dense_join_kernel<IOLB_F32><<<grid, 256, 0, st>>>(p, wide_log);
+    else if (dtype == IOLB_F16) dense_join_kernel<IOLB_F16><<<grid, 256, 0, st>>>(p, wide_log);
+    else dense_join_kernel<IOLB_BF16><<<grid, 256, 0, st>>>(p, wide_log);
     return hipGetLastError();
 }
 
