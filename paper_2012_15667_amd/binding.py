@@ -515,61 +515,59 @@ def _act_code(act):
 
 
 def _rows(t, name, dtype, device, shape=None):
-    """(address, values between rows) of a matrix on the GPU whose rows are contiguous."""
-    torch = _torch or _load_torch()
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2):
-        raise TypeError("%s must be a matrix of %s on the GPU" % (name, dtype))
-    if t.device != device:
-        raise ValueError(name + " is on another GPU")
-    rows, cols = t.shape
-    if shape is not None and (rows, cols) != shape:
-        raise ValueError("%s has the wrong shape" % name)
-    if rows == 0 or cols == 0:
-        return t.data_ptr(), cols
-    along, step = t.stride()[1], t.stride()[0]
-    if (cols > 1 and along != 1) or (rows > 1 and step < cols):
+    """(address, values between rows, rows, columns) of a matrix on GPU number `device` whose rows are contiguous."""
+    if not (isinstance(t, _torch.Tensor) and t.dtype == dtype and t.get_device() == device >= 0):
+        raise TypeError("%s must be a matrix of %s on the same GPU" % (name, dtype))
+    size = t.shape
+    if len(size) != 2 or (shape is not None and size != shape):
+        raise (TypeError if len(size) != 2 else ValueError)(name + " has the wrong shape")
+    rows, cols = size
+    step, along = t.stride()
+    if rows <= 1 or cols == 0:
+        step = cols
+    if (along != 1 and cols > 1 and rows) or step < cols:
         raise TypeError(name + " must have contiguous rows that do not overlap")
-    return t.data_ptr(), step if rows > 1 else cols
+    return t.data_ptr(), step, rows, cols
 
 
 def _dense(t, name, dtype, device, shape):
-    torch = _torch or _load_torch()
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
-        raise TypeError("%s must be a contiguous tensor of %s on the GPU" % (name, dtype))
-    if t.device != device:
-        raise ValueError(name + " is on another GPU")
-    if tuple(t.shape) != shape:
+    if not (isinstance(t, _torch.Tensor) and t.dtype == dtype and t.get_device() == device >= 0 and t.is_contiguous()):
+        raise TypeError("%s must be a contiguous tensor of %s on the same GPU" % (name, dtype))
+    if t.shape != shape:
         raise ValueError(name + " has the wrong shape")
     return t.data_ptr()
 
 
 def _checkpoint_of(c, name, device, rows, cols):
-    torch = _torch or _load_torch()
     if not (isinstance(c, tuple) and len(c) == 2):
         raise TypeError(name + " must be a Checkpoint")
-    return (_dense(c[0], name + ".q", torch.int8, device, (rows, cols)),
-            _dense(c[1], name + ".e", torch.uint8, device, (rows, -(-cols // CHECKPOINT_BLOCK))))
+    return (_dense(c[0], name + ".q", _torch.int8, device, (rows, cols)),
+            _dense(c[1], name + ".e", _torch.uint8, device, (rows, -(-cols // CHECKPOINT_BLOCK))))
 
 
-def _new_checkpoint(rows, cols, device):
-    torch = _torch or _load_torch()
-    return Checkpoint(torch.empty((rows, cols), dtype=torch.int8, device=device),
-                      torch.empty((rows, -(-cols // CHECKPOINT_BLOCK)), dtype=torch.uint8, device=device))
+def _new_checkpoint(like, rows, cols):
+    return Checkpoint(like.new_empty((rows, cols), dtype=_torch.int8),
+                      like.new_empty((rows, -(-cols // CHECKPOINT_BLOCK)), dtype=_torch.uint8))
 
 
 def _use_stream_on(device):
-    if device.index != (_torch or _load_torch()).cuda.current_device():
+    torch = _torch
+    if device != torch.cuda.current_device():
         raise ValueError("the tensors are not on the current GPU")
-    _use_current_stream()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _check(lib().iolb_set_stream(raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream))
 
 
-def _call_with_workspace(call, query, args, device):
-    # (the workspace comes from torch's allocator, which hands memory out again in the order of the stream)
-    torch = _torch or _load_torch()
-    need = ctypes.c_size_t(0)
-    _check(query(ctypes.byref(args), ctypes.byref(need)))
-    ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
-    _check(call(ctypes.byref(args), ws.data_ptr() if ws is not None else None, need.value))
+def _call_with_workspace(call, query, args, like):
+    # A call that needs a workspace and has none launches nothing, so most small ones are made in one go.  The workspace comes from
+    # torch's allocator, which hands memory out again in the order of the stream.
+    code = call(args, None, 0)
+    if code == -4:
+        need = ctypes.c_size_t(0)
+        _check(query(args, need))
+        ws = like.new_empty(need.value, dtype=_torch.uint8)
+        code = call(args, ws.data_ptr(), need.value)
+    _check(code)
 
 
 def linear(x, w, bias=None, act="none", residual=None, residual_first=False, checkpoint=False, y=None):
@@ -577,27 +575,27 @@ def linear(x, w, bias=None, act="none", residual=None, residual_first=False, che
     bias [N], residual [M][N]; all float32, all float16 or all bfloat16, rows contiguous.  checkpoint=True returns (y,
     Checkpoint of what the activation was applied to).  y may be given, and may be the residual."""
     torch = _torch or _load_torch()
-    if not isinstance(x, torch.Tensor) or not isinstance(w, torch.Tensor):
-        raise TypeError("x and w must be tensors")
-    dtype, device = x.dtype, x.device
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a tensor")
+    dtype, device = x.dtype, x.get_device()
     code = _dtype_code(dtype)
-    px, ldx = _rows(x, "x", dtype, device)
-    pw, ldw = _rows(w, "w", dtype, device)
-    M, K = x.shape
-    N = w.shape[0]
-    if w.shape[1] != K:
+    px, ldx, M, K = _rows(x, "x", dtype, device)
+    pw, ldw, N, C = _rows(w, "w", dtype, device)
+    if C != K:
         raise ValueError("x and w have different numbers of columns")
     pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else None
-    pr, ldr = _rows(residual, "residual", dtype, device, (M, N)) if residual is not None else (None, 0)
+    pr, ldr = _rows(residual, "residual", dtype, device, (M, N))[:2] if residual is not None else (None, 0)
     if y is None:
-        y = torch.empty((M, N), dtype=dtype, device=device)
-    py, ldy = _rows(y, "y", dtype, device, (M, N))
-    z = _new_checkpoint(M, N, device) if checkpoint else None
-    args = LinearArgs(M, N, K, code, _act_code(act), int(bool(residual_first)), px, pw, pb, pr, py, ldx, ldw, ldr, ldy,
+        y = x.new_empty((M, N))
+        py, ldy = y.data_ptr(), N
+    else:
+        py, ldy = _rows(y, "y", dtype, device, (M, N))[:2]
+    z = _new_checkpoint(x, M, N) if checkpoint else None
+    args = LinearArgs(M, N, K, code, _act_code(act), 1 if residual_first else 0, px, pw, pb, pr, py, ldx, ldw, ldr, ldy,
                       z.q.data_ptr() if checkpoint else None, z.e.data_ptr() if checkpoint else None)
     L = lib()
     _use_stream_on(device)
-    _call_with_workspace(L.iolb_linear, L.iolb_linear_workspace_bytes, args, device)
+    _call_with_workspace(L.iolb_linear, L.iolb_linear_workspace_bytes, args, x)
     return (y, z) if checkpoint else y
 
 
@@ -606,11 +604,11 @@ def checkpoint_pack(x):
     torch = _torch or _load_torch()
     if not isinstance(x, torch.Tensor):
         raise TypeError("x must be a tensor")
+    device = x.get_device()
     code = _dtype_code(x.dtype)
-    px, ldx = _rows(x, "x", x.dtype, x.device)
-    rows, cols = x.shape
-    c = _new_checkpoint(rows, cols, x.device)
-    _use_stream_on(x.device)
+    px, ldx, rows, cols = _rows(x, "x", x.dtype, device)
+    c = _new_checkpoint(x, rows, cols)
+    _use_stream_on(device)
     _check(lib().iolb_checkpoint_pack(px, ldx, rows, cols, code, c.q.data_ptr(), c.e.data_ptr()))
     return c
 
@@ -621,14 +619,16 @@ def checkpoint_unpack(c, dtype=None, act="none", y=None):
     if not (isinstance(c, tuple) and len(c) == 2 and isinstance(c[0], torch.Tensor) and c[0].dim() == 2):
         raise TypeError("c must be a Checkpoint")
     rows, cols = c[0].shape
-    device = c[0].device
+    device = c[0].get_device()
     if dtype is None:
         dtype = y.dtype if y is not None else torch.float32
     code = _dtype_code(dtype)
     pq, pe = _checkpoint_of(c, "c", device, rows, cols)
     if y is None:
-        y = torch.empty((rows, cols), dtype=dtype, device=device)
-    py, ldy = _rows(y, "y", dtype, device, (rows, cols))
+        y = c[0].new_empty((rows, cols), dtype=dtype)
+        py, ldy = y.data_ptr(), cols
+    else:
+        py, ldy = _rows(y, "y", dtype, device, (rows, cols))[:2]
     _use_stream_on(device)
     _check(lib().iolb_checkpoint_unpack(pq, pe, rows, cols, _act_code(act), code, py, ldy))
     return y
@@ -639,15 +639,13 @@ def linear_backward(dy, w, x=None, z=None, act="none", x_act="none", want_dx=Tru
     [M][K] (the input is x_act of it) and z of what the activation was applied to [M][N] (None for act="none").
     dz = dy act'(z) is the gradient of a residual that was added first.  x is needed for dw, w for the sizes and dx."""
     torch = _torch or _load_torch()
-    if not isinstance(dy, torch.Tensor) or not isinstance(w, torch.Tensor):
-        raise TypeError("dy and w must be tensors")
-    dtype, device = dy.dtype, dy.device
+    if not isinstance(dy, torch.Tensor):
+        raise TypeError("dy must be a tensor")
+    dtype, device = dy.dtype, dy.get_device()
     code = _dtype_code(dtype)
-    pdy, ldy = _rows(dy, "dy", dtype, device)
-    pw, ldw = _rows(w, "w", dtype, device)
-    M, N = dy.shape
-    K = w.shape[1]
-    if w.shape[0] != N:
+    pdy, ldy, M, N = _rows(dy, "dy", dtype, device)
+    pw, ldw, outputs, K = _rows(w, "w", dtype, device)
+    if outputs != N:
         raise ValueError("dy and w have different numbers of outputs")
     a = _act_code(act)
     if a and z is None:
@@ -656,14 +654,11 @@ def linear_backward(dy, w, x=None, z=None, act="none", x_act="none", want_dx=Tru
         raise ValueError("dw needs x")
     xq, xe = _checkpoint_of(x, "x", device, M, K) if x is not None else (None, None)
     zq, ze = _checkpoint_of(z, "z", device, M, N) if z is not None else (None, None)
-
-    def out(want, *shape):
-        return torch.empty(shape, dtype=dtype, device=device) if want else None
-
-    g = LinearGrads(out(want_dx, M, K), out(want_dw, N, K), out(want_db, N), out(want_dz, M, N))
+    g = LinearGrads(dy.new_empty((M, K)) if want_dx else None, dy.new_empty((N, K)) if want_dw else None,
+                    dy.new_empty((N,)) if want_db else None, dy.new_empty((M, N)) if want_dz else None)
     args = LinearBackwardArgs(M, N, K, code, a, _act_code(x_act), pdy, pw, ldy, ldw, xq, xe, zq, ze,
-                              *(t.data_ptr() if t is not None else None for t in g))
+                              *[t.data_ptr() if t is not None else None for t in g])
     L = lib()
     _use_stream_on(device)
-    _call_with_workspace(L.iolb_linear_backward, L.iolb_linear_backward_workspace_bytes, args, device)
+    _call_with_workspace(L.iolb_linear_backward, L.iolb_linear_backward_workspace_bytes, args, dy)
     return g

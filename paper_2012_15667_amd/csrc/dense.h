@@ -49,7 +49,7 @@ struct DenseProduct {
 };
 
 // Blocks of the tile kernel.
-enum { DENSE_TILE_256, DENSE_TILE_128, DENSE_TILE_64, DENSE_TILES };
+enum { DENSE_TILE_256, DENSE_TILE_128, DENSE_TILE_64x128, DENSE_TILE_64, DENSE_TILES };
 struct DenseTilePlan { int tile, splits; };
 DenseTilePlan dense_tile_plan(int M, int N, int K, int segments);
 inline size_t dense_partial_bytes(int splits, long long M, long long N) { return (size_t)splits * M * ((N + 3) / 4 * 4) * 4; }
@@ -69,6 +69,8 @@ hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st);
 // Values v[r][c], rows x cols, from one of three sources:
 enum { DENSE_FROM_TENSOR, DENSE_FROM_CHECKPOINT, DENSE_FROM_GRADIENT };
 struct DenseLayout {
+    int source;
+    int planes;                             // 1 or 3 (fp32: bf16 parts; 1 where the values are exact in bf16)
     int rows, cols;
     const void* src;                        // tensor: v = src;  gradient: v = src * act'(checkpoint), or src where q is null
     long long ld;
@@ -84,8 +86,14 @@ struct DenseLayout {
     void* copy;                             // v in the tensor's own type, [rows][cols], or null
     float* colsum;                          // [ceil(rows / 64)][cols]: sums over 64 rows each, or null
 };
-// dtype: of src, copy and (16-bit types) the planes; planes: 1 or 3 (fp32: bf16 parts; 1 where the values are exact in bf16).
-hipError_t launch_dense_layout(int source, int dtype, int planes, const DenseLayout& l, hipStream_t st);
+// Up to three of them in one launch.
+constexpr int MAX_LAYOUTS = 3;
+struct DenseLayouts {
+    int count;
+    DenseLayout of[MAX_LAYOUTS];
+};
+// dtype: of src, copy and (16-bit types) the planes.
+hipError_t launch_dense_layouts(int dtype, const DenseLayouts& l, hipStream_t st);
 // out[c] = sum of colsum over its `blocks` rows, in `dtype`.
 hipError_t launch_dense_colsum(const float* colsum, int blocks, int cols, void* out, int dtype, hipStream_t st);
 

@@ -108,16 +108,17 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     if (!launch) return IOLB_OK;
 
     const hipStream_t st = call_stream();
+    DenseLayouts layouts{};
     const auto lay = [&](const void* src, int64_t ld, int64_t rows, void* to) {
-        DenseLayout l{};
+        DenseLayout& l = layouts.of[layouts.count++];
+        l.source = DENSE_FROM_TENSOR; l.planes = planes;
         l.rows = (int)rows; l.cols = (int)a.K;
-        l.src = src; l.ld = ld;
-        l.vec_src = ld * size_of(a.dtype) % 16 == 0 && aligned_to(src, 16);
+        l.src = src; l.ld = ld; l.vec_src = pieces_of_16(src, ld);
         l.rowmajor = to; l.ld_rm = Kp;
-        return launch_dense_layout(DENSE_FROM_TENSOR, a.dtype, planes, l, st);
     };
-    if (!x_direct) DENSE_HIP(lay(a.x, a.ldx, a.M, xp));
-    if (!w_direct) DENSE_HIP(lay(a.w, a.ldw, a.N, wp));
+    if (!x_direct) lay(a.x, a.ldx, a.M, xp);
+    if (!w_direct) lay(a.w, a.ldw, a.N, wp);
+    if (layouts.count) DENSE_HIP(launch_dense_layouts(a.dtype, layouts, st));
     DENSE_HIP(launch_dense_product(p, plan.tile, a.dtype, st));
     return IOLB_OK;
 }
@@ -208,8 +209,10 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     if (!launch) return IOLB_OK;
 
     const hipStream_t st = call_stream();
+    DenseLayouts layouts{};
     if (a.M > 0 && a.N > 0 && (dz_to || dzt || dz_copy || sums)) {
-        DenseLayout l{};
+        DenseLayout& l = layouts.of[layouts.count++];
+        l.source = DENSE_FROM_GRADIENT; l.planes = planes;
         l.rows = (int)a.M; l.cols = (int)a.N;
         l.src = a.dy; l.ld = a.ldy;
         l.vec_src = a.ldy * size_of(a.dtype) % 16 == 0 && aligned_to(a.dy, 16);
@@ -219,8 +222,24 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         l.transposed = dzt; l.ld_tr = Mp;
         l.copy = dz_copy;
         l.colsum = sums;
-        DENSE_HIP(launch_dense_layout(DENSE_FROM_GRADIENT, a.dtype, planes, l, st));
     }
+    if (wt) {
+        DenseLayout& l = layouts.of[layouts.count++];
+        l.source = DENSE_FROM_TENSOR; l.planes = planes;
+        l.rows = (int)a.N; l.cols = (int)a.K;
+        l.src = a.w; l.ld = a.ldw;
+        l.vec_src = a.ldw * size_of(a.dtype) % 16 == 0 && aligned_to(a.w, 16);
+        l.transposed = wt; l.ld_tr = Np;
+    }
+    if (want_dw && a.M > 0) {
+        DenseLayout& l = layouts.of[layouts.count++];
+        l.source = DENSE_FROM_CHECKPOINT; l.planes = planes_x;
+        l.rows = (int)a.M; l.cols = (int)a.K;
+        l.q = a.xq; l.e = a.xe; l.act = a.x_act;
+        l.vec_q = a.K % 8 == 0 && aligned_to(a.xq, 8);
+        l.transposed = xt; l.ld_tr = Mp;
+    }
+    if (layouts.count) DENSE_HIP(launch_dense_layouts(a.dtype, layouts, st));
     if (a.db && a.N > 0) DENSE_HIP(launch_dense_colsum(sums, row_blocks, (int)a.N, a.db, a.dtype, st));
     const auto finish = [&](void* out, int64_t m, int64_t n) {
         DenseFinish f{};
@@ -233,22 +252,10 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         px.f = finish(a.dx, a.M, a.K);
         DENSE_HIP(launch_dense_rows(px, true, rows_x.join, a.dtype, st));
     } else if (want_dx) {
-        DenseLayout l{};
-        l.rows = (int)a.N; l.cols = (int)a.K;
-        l.src = a.w; l.ld = a.ldw;
-        l.vec_src = a.ldw * size_of(a.dtype) % 16 == 0 && aligned_to(a.w, 16);
-        l.transposed = wt; l.ld_tr = Np;
-        DENSE_HIP(launch_dense_layout(DENSE_FROM_TENSOR, a.dtype, planes, l, st));
         px.f = finish(a.dx, a.M, a.K);
         DENSE_HIP(launch_dense_product(px, plan_x.tile, a.dtype, st));
     }
     if (want_dw) {
-        DenseLayout l{};
-        l.rows = (int)a.M; l.cols = (int)a.K;
-        l.q = a.xq; l.e = a.xe; l.act = a.x_act;
-        l.vec_q = a.K % 8 == 0 && aligned_to(a.xq, 8);
-        l.transposed = xt; l.ld_tr = Mp;
-        DENSE_HIP(launch_dense_layout(DENSE_FROM_CHECKPOINT, a.dtype, planes_x, l, st));
         pw.f = finish(a.dw, a.N, a.K);
         DENSE_HIP(launch_dense_product(pw, plan_w.tile, a.dtype, st));
     }

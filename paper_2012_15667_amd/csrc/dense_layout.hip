@@ -38,23 +38,34 @@ __device__ __forceinline__ void load_checkpoint(const int8_t* p, float unit, int
     }
 }
 
-template <int DT, int PLANES>
-__device__ __forceinline__ void plane_bits(float v, unsigned short (&bits)[PLANES])
+template <int DT>
+__device__ __forceinline__ void plane_bits(float v, unsigned short (&bits)[DT == IOLB_F32 ? 3 : 1])
 {
-    if constexpr (PLANES == 3) dense_parts(v, bits[0], bits[1], bits[2]);
+    if constexpr (DT == IOLB_F32) dense_parts(v, bits[0], bits[1], bits[2]);
     else if constexpr (DT == IOLB_F16) bits[0] = __builtin_bit_cast(unsigned short, (_Float16)v);
     else bits[0] = __builtin_bit_cast(unsigned short, (__bf16)v);
 }
 
-template <int SOURCE, int DT, int PLANES>
+struct LayoutLaunch {
+    DenseLayouts all;
+    unsigned first[MAX_LAYOUTS];                   // workgroup at which each starts
+};
+
+template <int DT>
 __global__ void __launch_bounds__(256)
-dense_layout_kernel(DenseLayout g, int blocks_c)
+dense_layout_kernel(LayoutLaunch launch)
 {
     typedef typename DenseType<DT>::type T;
+    constexpr int PLANES = DT == IOLB_F32 ? 3 : 1;
     __shared__ __align__(16) unsigned short turned[PLANES][64][PITCH];
     __shared__ float sums[32][64 + 1];
+    int which = 0;
+#pragma unroll
+    for (int i = 1; i < MAX_LAYOUTS; ++i) which = i < launch.all.count && blockIdx.x >= launch.first[i] ? i : which;
+    const DenseLayout& g = launch.all.of[which];
+    const unsigned block = blockIdx.x - launch.first[which], blocks_c = (unsigned)((g.cols + 63) / 64);
     const int tid = threadIdx.x, c8 = (tid & 7) * 8, r_in = tid >> 3;
-    const int c0 = (int)(blockIdx.x % blocks_c) * 64, r0 = (int)(blockIdx.x / blocks_c) * 64;
+    const int c0 = (int)(block % blocks_c) * 64, r0 = (int)(block / blocks_c) * 64;
     const int c = c0 + c8, have = g.cols - c;                      // may be negative
     const long long blocks_q = (g.cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
     float column[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -64,31 +75,34 @@ dense_layout_kernel(DenseLayout g, int blocks_c)
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         const bool live = r < g.rows && have > 0;
         if (live) {
-            if constexpr (SOURCE != DENSE_FROM_CHECKPOINT)
-                load_eight(static_cast<const T*>(g.src) + r * g.ld + c, have, g.vec_src, v);
-            if (SOURCE == DENSE_FROM_CHECKPOINT || (SOURCE == DENSE_FROM_GRADIENT && g.q)) {
+            if (g.source != DENSE_FROM_CHECKPOINT) load_eight(static_cast<const T*>(g.src) + r * g.ld + c, have, g.vec_src, v);
+            if (g.q) {
                 float z[8];
                 const float unit = two_to((int)g.e[r * blocks_q + c / CKPT_BLOCK] - 127);
                 load_checkpoint(g.q + (long long)r * g.cols + c, unit, have, g.vec_q, z);
-                by_activation(g.act, [&](auto act) {
+                by_activation(g.act, [&](auto act) __attribute__((always_inline)) {
+                    constexpr int ACT = decltype(act)::value;
+                    if (g.source == DENSE_FROM_CHECKPOINT) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if constexpr (SOURCE == DENSE_FROM_CHECKPOINT) v[i] = activate<decltype(act)::value>(z[i]);
-                        else v[i] = i < have ? through_activation<decltype(act)::value>(v[i], z[i]) : 0.f;
+                        for (int i = 0; i < 8; ++i) v[i] = activate<ACT>(z[i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = i < have ? through_activation<ACT>(v[i], z[i]) : 0.f;
                     }
                 });
             }
         }
         unsigned short bits[8][PLANES];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) plane_bits<DT, PLANES>(v[i], bits[i]);
+        for (int i = 0; i < 8; ++i) plane_bits<DT>(v[i], bits[i]);
         if (live && g.rowmajor) {
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
                 u32x4 w;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] = bits[2 * i][p] | (unsigned)bits[2 * i + 1][p] << 16;
-                *reinterpret_cast<u32x4*>(static_cast<unsigned short*>(g.rowmajor) + (p * (long long)g.rows + r) * g.ld_rm + c) = w;
+                if (p < g.planes)
+                    *reinterpret_cast<u32x4*>(static_cast<unsigned short*>(g.rowmajor) + (p * (long long)g.rows + r) * g.ld_rm + c) = w;
             }
         }
         if (live && g.copy) {
@@ -101,7 +115,8 @@ dense_layout_kernel(DenseLayout g, int blocks_c)
 #pragma unroll
             for (int p = 0; p < PLANES; ++p)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) turned[p][c8 + i][in] = bits[i][p];
+                for (int i = 0; i < 8; ++i)
+                    if (p < g.planes) turned[p][c8 + i][in] = bits[i][p];
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) column[i] += v[i];
@@ -119,8 +134,9 @@ dense_layout_kernel(DenseLayout g, int blocks_c)
             if (c0 + tc < g.cols && r0 + c8 < g.rows) {
 #pragma unroll
                 for (int p = 0; p < PLANES; ++p)
-                    *reinterpret_cast<u32x4*>(static_cast<unsigned short*>(g.transposed) + (p * (long long)g.cols + c0 + tc) * g.ld_tr + r0 + c8) =
-                        *reinterpret_cast<const u32x4*>(&turned[p][tc][c8]);
+                    if (p < g.planes)
+                        *reinterpret_cast<u32x4*>(static_cast<unsigned short*>(g.transposed) + (p * (long long)g.cols + c0 + tc) * g.ld_tr + r0 + c8) =
+                            *reinterpret_cast<const u32x4*>(&turned[p][tc][c8]);
             }
         }
     }
@@ -201,7 +217,7 @@ checkpoint_unpack_kernel(const int8_t* q, const uint8_t* e, int rows, int cols, 
         load_checkpoint(q + r * cols + c, two_to((int)e[r * blocks + c / CKPT_BLOCK] - 127), have, vec_q, v);
         T* const to = static_cast<T*>(y) + r * ldy + c;
         T8 t;
-        by_activation(act, [&](auto a) {
+        by_activation(act, [&](auto a) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) t[i] = (T)activate<decltype(a)::value>(v[i]);
         });
@@ -228,34 +244,22 @@ RowGrid row_grid(int rows, int cols)
 bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 int size_of(int dtype) { return dtype == IOLB_F32 ? 4 : 2; }
 
-template <int SOURCE, int DT>
-hipError_t layout(int planes, const DenseLayout& l, hipStream_t st)
-{
-    const long long bc = (l.cols + 63) / 64, n = bc * ((l.rows + 63) / 64);
-    if (n > 0x7fffffffLL) return hipErrorInvalidValue;
-    if (n == 0) return hipSuccess;
-    if constexpr (DT == IOLB_F32) {
-        if (planes == 3) dense_layout_kernel<SOURCE, DT, 3><<<(unsigned)n, 256, 0, st>>>(l, (int)bc);
-        else dense_layout_kernel<SOURCE, DT, 1><<<(unsigned)n, 256, 0, st>>>(l, (int)bc);
-    } else {
-        dense_layout_kernel<SOURCE, DT, 1><<<(unsigned)n, 256, 0, st>>>(l, (int)bc);
-    }
-    return hipGetLastError();
-}
-
 }  // namespace
 
-hipError_t launch_dense_layout(int source, int dtype, int planes, const DenseLayout& l, hipStream_t st)
+hipError_t launch_dense_layouts(int dtype, const DenseLayouts& l, hipStream_t st)
 {
-#define BY_TYPE(S)                                                                \
-    (dtype == IOLB_F32 ? layout<S, IOLB_F32>(planes, l, st) : dtype == IOLB_F16 ? layout<S, IOLB_F16>(planes, l, st) \
-                                                                              : layout<S, IOLB_BF16>(planes, l, st))
-    switch (source) {
-    case DENSE_FROM_TENSOR: return BY_TYPE(DENSE_FROM_TENSOR);
-    case DENSE_FROM_CHECKPOINT: return BY_TYPE(DENSE_FROM_CHECKPOINT);
-    default: return BY_TYPE(DENSE_FROM_GRADIENT);
+    LayoutLaunch a{l, {}};
+    long long n = 0;
+    for (int i = 0; i < l.count; ++i) {
+        a.first[i] = (unsigned)n;
+        n += ((l.of[i].cols + 63LL) / 64) * ((l.of[i].rows + 63LL) / 64);
+        if (n > 0x7fffffffLL) return hipErrorInvalidValue;
     }
-#undef BY_TYPE
+    if (n == 0) return hipSuccess;
+    if (dtype == IOLB_F32) dense_layout_kernel<IOLB_F32><<<(unsigned)n, 256, 0, st>>>(a);
+    else if (dtype == IOLB_F16) dense_layout_kernel<IOLB_F16><<<(unsigned)n, 256, 0, st>>>(a);
+    else dense_layout_kernel<IOLB_BF16><<<(unsigned)n, 256, 0, st>>>(a);
+    return hipGetLastError();
 }
 
 hipError_t launch_dense_colsum(const float* colsum, int blocks, int cols, void* out, int dtype, hipStream_t st)

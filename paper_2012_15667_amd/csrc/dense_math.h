@@ -246,7 +246,7 @@ __device__ __forceinline__ void finish_four(const DenseFinish& f, int m, int n, 
 #pragma unroll
     for (int i = 0; i < 4; ++i) z[i] = sum[i] + b[i];
     if (f.residual && f.first) add_residual<DT>(f, m, n, z);
-    by_activation(f.act, [&](auto act) { store_columns<DT, decltype(act)::value>(f, m, n, z); });
+    by_activation(f.act, [&](auto act) __attribute__((always_inline)) { store_columns<DT, decltype(act)::value>(f, m, n, z); });
 }
 
 // Eight columns of row m, which four neighbouring lanes continue to a checkpoint's block.  Every lane of the wave calls.

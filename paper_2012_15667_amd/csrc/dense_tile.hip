@@ -114,7 +114,8 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
     // ahead, so that matrix instructions do not wait for LDS.  The one barrier of a stage stands before its last groups, when all
     // of it has been read: the next stage has arrived then, its first reads go out behind the last groups, and the buffer is free
     // for the stage after it.
-    constexpr int GROUPS = 2 * MI, AHEAD = MI - 2, LAST = MI == 8 ? 3 : 2;
+    constexpr int GROUPS = 2 * MI, AHEAD = MI > 2 ? MI - 2 : 1, LAST = MI == 8 ? 3 : MI == 4 ? 2 : 1;
+    static_assert(AHEAD < MI && LAST <= AHEAD && NI <= GROUPS - LAST, "a stage is read before its barrier");
     u32x4 fa[MI], fb[2][NI];
     // fragments: row l16 of sixteen, piece 4 kk + grp; the rest is the same for all lanes
     const int frag_a = (wm * (BM / WM) + l16) * ROW_BYTES + 16 * place(l16, grp);
@@ -205,7 +206,7 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
                 sums[r * (BN / 4) + (c ^ l16)] = acc[pass * PI + i][j];
             }
         __syncthreads();
-        by_activation(p.f.act, [&](auto act) {
+        by_activation(p.f.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll 1
             for (int r = tid / LANES; r < PASS_ROWS; r += AT_ONCE) {
                 const int c = 2 * (tid % LANES);
@@ -226,9 +227,9 @@ dense_join_kernel(DenseProduct p, int wide_log)
     const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), rows = 256 >> wide_log;
     const int n = (int)((blockIdx.x * (unsigned)wide + tx) * 8);
     const long long ld = (p.N + 3) / 4 * 4;
-    float bias[8];
-    load_bias<DT>(p.f, n, bias);
-    by_activation(p.f.act, [&](auto act) {
+    by_activation(p.f.act, [&](auto act) __attribute__((always_inline)) {
+        float bias[8];
+        load_bias<DT>(p.f, n, bias);
         for (long long m = (long long)blockIdx.y * rows + (threadIdx.x >> wide_log); m - (threadIdx.x >> wide_log) < p.M; m += (long long)gridDim.y * rows) {
             float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (m < p.M && n < p.N) {
@@ -264,7 +265,8 @@ hipError_t launch_tile(const DenseProduct& p, int tile, hipStream_t st)
     switch (tile) {
     case DENSE_TILE_256: return launch<F16, DT, 256, 256, 2, 4>(p, st);
     case DENSE_TILE_128: return launch<F16, DT, 128, 128, 2, 2>(p, st);
-    default: return launch<F16, DT, 64, 128, 1, 4>(p, st);
+    case DENSE_TILE_64x128: return launch<F16, DT, 64, 128, 1, 4>(p, st);
+    default: return launch<F16, DT, 64, 64, 2, 2>(p, st);
     }
 }
 
@@ -277,8 +279,8 @@ DenseTilePlan dense_tile_plan(int M, int N, int K, int segments)
     const auto tiles = [&](int bm, int bn) { return (long long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     DenseTilePlan plan{DENSE_TILE_256, 1};
     if (tiles(256, 256) >= 192) return plan;
-    plan.tile = M <= 64 ? DENSE_TILE_64 : DENSE_TILE_128;
-    const long long n = plan.tile == DENSE_TILE_64 ? tiles(64, 128) : tiles(128, 128);
+    plan.tile = M <= 64 ? DENSE_TILE_64x128 : DENSE_TILE_128;
+    const long long n = plan.tile == DENSE_TILE_64x128 ? tiles(64, 128) : tiles(128, 128);
     const int steps = (K + STEP - 1) / STEP;
     // at least four stages (of all segments together) a share
     const long long most = (long long)steps * segments / 4 < steps ? (long long)steps * segments / 4 : steps;

@@ -549,7 +549,7 @@ def test_c_calls_refuse_without_touching_the_gpu():
     for bad in (dict(dtype=3), dict(dtype=-1), dict(act=5), dict(act=-1), dict(K=1 << 23, ldx=1 << 23, ldw=1 << 23), dict(M=1 << 31)):
         assert linear(**bad) == -2, bad
     assert linear(M=0, y=None) == 0 and linear(N=0, w=None) == 0
-    assert linear(K=15, ldx=15, ldw=15) == -4                    # parts of fp32 operands need a workspace
+    assert linear(M=100) == -4                                   # parts of fp32 operands need a workspace
 
     def back(**k):
         a = dict(M=4, N=8, K=16, dtype=2, act=1, x_act=0, dy=p, w=p, ldy=8, ldw=16, xq=p, xe=p, zq=p, ze=p, dx=p, dw=p, db=p, dz=None)
@@ -562,7 +562,7 @@ def test_c_calls_refuse_without_touching_the_gpu():
         assert back(**bad) == -1, bad
     for bad in (dict(dtype=9), dict(act=9), dict(x_act=9), dict(M=1 << 23)):
         assert back(**bad) == -2, bad
-    assert back() == -4
+    assert back(M=100) == -4
     assert L.iolb_checkpoint_pack(None, 4, 4, 4, 0, p, p) == -1
     assert L.iolb_checkpoint_pack(p, 3, 4, 4, 0, p, p) == -1
     assert L.iolb_checkpoint_pack(p, 4, 4, 4, 7, p, p) == -2
