@@ -272,22 +272,32 @@ hipError_t launch_tile(const DenseProduct& p, int tile, hipStream_t st)
 
 }  // namespace
 
-// Blocks and shares.  A large block reads its operands less often; a small one, and K shared by several workgroups, fill
-// the 256 compute units.
+// Block and number of workgroups that share K: the least modelled time.  A stage takes a workgroup `alone` ns while it has a compute unit
+// to itself (bound by its chain of loads, reads and products) and `each` ns of the unit's time among several.  Sharing K costs a
+// second launch and the partial sums' way through memory.  Fitted to a sweep of 20 shapes, 64 <= M, N <= 25088, 64 <= K <= 16384; of these
+// the model's pick is within 8% of the best measured one.  Examples (us, bf16, 256 x 256 / 128 x 128 / 64 x 128 / 64 x 64, each with its
+// best share of K): 128 x 4096 x 4096 24.9 / 19.0 / 17.7 / 17.4, 1024 x 1024 x 1024 26.7 / 14.6 / 11.4 / 9.7, 2048 x 4096 x 4096 79 / 69 / 94 / 100.
+// Measured and not taken: three and four buffers for the small blocks, two workgroups of 128 x 128 with four (more stages on their way, fewer
+// workgroups on a compute unit): 2048 x 2048 x 2048 27.0 -> 28.2, 1024 x 4096 x 1024 15.8 -> 16.7, 4096 x 4096 x 256 20.1 -> 28.
 DenseTilePlan dense_tile_plan(int M, int N, int K, int segments)
 {
-    const auto tiles = [&](int bm, int bn) { return (long long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    struct Block { int m, n, alone, each; };
+    static const Block blocks[DENSE_TILES] = {{256, 256, 1450, 1550}, {128, 128, 720, 510}, {64, 128, 570, 350}, {64, 64, 490, 190}};
+    static const int shares[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    const long long steps = (K + STEP - 1) / STEP;
     DenseTilePlan plan{DENSE_TILE_256, 1};
-    if (tiles(256, 256) >= 192) return plan;
-    plan.tile = M <= 64 ? DENSE_TILE_64x128 : DENSE_TILE_128;
-    const long long n = plan.tile == DENSE_TILE_64x128 ? tiles(64, 128) : tiles(128, 128);
-    const int steps = (K + STEP - 1) / STEP;
-    // at least four stages (of all segments together) a share
-    const long long most = (long long)steps * segments / 4 < steps ? (long long)steps * segments / 4 : steps;
-    long long splits = 512 / n;
-    if (splits > most) splits = most;
-    if (splits > 64) splits = 64;
-    plan.splits = splits < 1 ? 1 : (int)splits;
+    long long least = -1;
+    for (int b = 0; b < DENSE_TILES; ++b) {
+        const Block& k = blocks[b];
+        const long long tiles = (long long)((M + k.m - 1) / k.m) * ((N + k.n - 1) / k.n);
+        for (const int s : shares) {
+            if (s > 1 && s > steps) break;
+            const long long on_unit = (tiles * s + 255) / 256, stage = k.each * on_unit > k.alone ? k.each * on_unit : k.alone;
+            long long ns = stage * ((steps + s - 1) / s) * segments;
+            if (s > 1) ns += 3000 + 80 * s + (long long)(8.0 * s * M * N / 5500);
+            if (least < 0 || ns < least) { least = ns; plan = {b, s}; }
+        }
+    }
     return plan;
 }
 
