@@ -183,7 +183,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     if (want_dx && few) {
         px.M = (int)a.M; px.N = (int)a.K; px.K = (int)a.N;
         px.a = dz; px.lda = ld_dz; px.vec_a = aligned_to(dz, 16) && (a.M == 1 || ld_dz * size_of(a.dtype) % 16 == 0);
-        px.b = a.w; px.ldb = a.ldw; px.vec_b = aligned_to(a.w, 4 * size_of(a.dtype)) && (a.N == 1 || a.ldw % 4 == 0);
+        px.b = a.w; px.ldb = a.ldw; px.vec_b = a.K % 4 == 0 && aligned_to(a.w, 4 * size_of(a.dtype)) && (a.N == 1 || a.ldw % 4 == 0);
         rows_x = dense_rows_plan(px.M, px.N, px.K, a.dtype, true, false);
         px.splits = rows_x.splits;
         if (rows_x.join) partial_x = dense_partial_bytes(px.splits, px.M, px.N);

@@ -8,6 +8,8 @@
 #include "dense_math.h"
 #include "kernels.h"
 
+#include <cmath>
+
 namespace iolb {
 
 namespace {
@@ -41,22 +43,18 @@ __device__ __forceinline__ void parts_of_two(float a, float b, unsigned& h, unsi
 // The operand of a lane for 32 k, in one part (16-bit types) or three.
 template <int DT> struct Fragment { u32x4 part[DT == IOLB_F32 ? 3 : 1]; };
 
-template <int DT, int MODE>
-__device__ __forceinline__ f32x4 multiply_parts(const Fragment<DT>& b, const Fragment<DT>& a, f32x4 c)
+// c[i] += a[i % NA] b[i / NA], smallest products of parts first; product by product, so that neighbouring matrix instructions do not wait for
+// each other's sums.
+template <int DT, int MODE, int NA, int NB>
+__device__ __forceinline__ void multiply_parts(const Fragment<DT> (&b)[NB], const Fragment<DT> (&a)[NA], f32x4* const (&c)[NA * NB])
 {
-    if constexpr (DT != IOLB_F32) {
-        return multiply<DT == IOLB_F16>(b.part[0], a.part[0], c);
-    } else {
-        if constexpr (MODE != LEADING_PRODUCT) {
-            c = multiply<false>(b.part[2], a.part[0], c);
-            c = multiply<false>(b.part[0], a.part[2], c);
-            c = multiply<false>(b.part[1], a.part[1], c);
-            c = multiply<false>(b.part[1], a.part[0], c);
-            c = multiply<false>(b.part[0], a.part[1], c);
-        }
-        if constexpr (MODE != SMALL_PRODUCTS) c = multiply<false>(b.part[0], a.part[0], c);
-        return c;
-    }
+    constexpr int part_b[6] = {2, 0, 1, 1, 0, 0}, part_a[6] = {0, 2, 1, 0, 1, 0};
+    constexpr int from = DT != IOLB_F32 || MODE == LEADING_PRODUCT ? 5 : 0, to = DT == IOLB_F32 && MODE == SMALL_PRODUCTS ? 5 : 6;
+#pragma unroll
+    for (int q = from; q < to; ++q)
+#pragma unroll
+        for (int i = 0; i < NA * NB; ++i)
+            *c[i] = multiply<DT == IOLB_F16>(b[i / NA].part[DT == IOLB_F32 ? part_b[q] : 0], a[i % NA].part[DT == IOLB_F32 ? part_a[q] : 0], *c[i]);
 }
 
 // Eight values of a row as they lie in memory.  fp32: two runs of four, so that four lanes read 64 neighbouring bytes at a time.
@@ -66,11 +64,13 @@ template <int DT> struct Raw { u32x4 v[DT == IOLB_F32 ? 2 : 1]; };
 template <int DT>
 __device__ __forceinline__ int k_of(int g, int i) { return DT == IOLB_F32 ? (i < 4 ? 4 * g + i : 12 + 4 * g + i) : 8 * g + i; }
 
-// Piece g of 32 values that start at p, of which `have` exist (the others are zero).
-template <int DT>
-__device__ __forceinline__ void load_raw(Raw<DT>& r, const typename DenseType<DT>::type* p, int g, int have, bool vec)
+// Piece g of 32 values that start at p.  WHOLE: all there, in 16-byte pieces.  Otherwise `have` of the 32 exist and the others are zero.
+// The two kinds never meet in one loop: where loads one by one join a path of whole pieces, the compiler waits for all that are on
+// their way, and what was asked for ahead is lost.
+template <int DT, bool WHOLE>
+__device__ __forceinline__ void load_raw(Raw<DT>& r, const typename DenseType<DT>::type* p, int g, int have)
 {
-    if (vec && have >= 32) {
+    if constexpr (WHOLE) {
         if constexpr (DT == IOLB_F32) {
             r.v[0] = *reinterpret_cast<const u32x4*>(p + 4 * g);
             r.v[1] = *reinterpret_cast<const u32x4*>(p + 16 + 4 * g);
@@ -88,6 +88,15 @@ __device__ __forceinline__ void load_raw(Raw<DT>& r, const typename DenseType<DT
             r.v[0][i] = lo | hi << 16;
         }
     }
+}
+
+// What was loaded ahead is first used here and not earlier: the compiler, free to, moves the arithmetic on it up to the load, across the barrier
+// and into the step before, and waits for it there.
+template <int DT>
+__device__ __forceinline__ void used_from_here(Raw<DT>& r)
+{
+#pragma unroll
+    for (auto& v : r.v) asm volatile("" : "+v"(v));
 }
 
 template <int DT, bool SAFE>
@@ -115,6 +124,13 @@ __device__ __forceinline__ void clear_not_finite(f32x4& c)
     for (int i = 0; i < 4; ++i) c[i] = fabsf(c[i]) < __builtin_inff() ? c[i] : 0.f;
 }
 
+// Steps from s0 on up to the one returned can be read in whole pieces.
+__device__ __forceinline__ int whole_steps(const DenseProduct& p, int s0, int s1)
+{
+    const int full = p.vec_a && p.vec_b ? p.K / STEP : 0;
+    return full < s0 ? s0 : full < s1 ? full : s1;
+}
+
 __device__ __forceinline__ void keep_partial(const DenseProduct& p, int split, int m, int n, const f32x4& c)
 {
     const long long ld = (p.N + 3) / 4 * 4;
@@ -136,49 +152,53 @@ dense_few_kernel(DenseProduct p, int join)
     const int n0 = blockIdx.x * 16;
     const int steps_all = (p.K + STEP - 1) / STEP;
     const int s0 = (int)((long long)steps_all * blockIdx.y / p.splits), s1 = (int)((long long)steps_all * (blockIdx.y + 1) / p.splits);
-    const int row_b = n0 + l16 < p.N ? n0 + l16 : p.N - 1;            // (sums of rows that do not exist are not stored)
-    const bool live_a = l16 < p.M;
-    const T* const b = static_cast<const T*>(p.b) + row_b * p.ldb;
-    const T* const a = static_cast<const T*>(p.a) + (live_a ? l16 : 0) * p.lda;
+    // rows that do not exist are read from the last one: their sums are not stored
+    const T* const b = static_cast<const T*>(p.b) + (n0 + l16 < p.N ? n0 + l16 : p.N - 1) * p.ldb;
+    const T* const a = static_cast<const T*>(p.a) + (l16 < p.M ? l16 : p.M - 1) * p.lda;
 
-    Raw<DT> rb[AHEAD][2], ra[AHEAD][2];
-    auto load = [&](int s, Raw<DT> (&to_b)[2], Raw<DT> (&to_a)[2]) {
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            const int k = s * STEP + 32 * kk, have = p.K - k;
-            load_raw<DT>(to_b[kk], b + k, grp, have, p.vec_b);
-            if (live_a) load_raw<DT>(to_a[kk], a + k, grp, have, p.vec_a);
-        }
-    };
-    auto sums = [&](auto mode) {
+    const int whole_to = whole_steps(p, s0, s1);
+    // the sums of steps from ... to - 1, of which this wave has every eighth
+    auto range = [&](auto mode, auto whole, int from, int to, f32x4 (&c)[2]) __attribute__((always_inline)) {
         constexpr int MODE = decltype(mode)::value;
-        f32x4 c[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+        Raw<DT> rb[AHEAD][2], ra[AHEAD][2];
+        auto load = [&](int s, Raw<DT> (&to_b)[2], Raw<DT> (&to_a)[2]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (s0 + wave + i * WAVES < s1) load(s0 + wave + i * WAVES, rb[i], ra[i]);
-        for (int s = s0 + wave; s < s1; s += AHEAD * WAVES) {
+            for (int kk = 0; kk < 2; ++kk) {
+                const int k = s * STEP + 32 * kk;
+                load_raw<DT, decltype(whole)::value>(to_b[kk], b + k, grp, p.K - k);
+                load_raw<DT, decltype(whole)::value>(to_a[kk], a + k, grp, p.K - k);
+            }
+        };
+        if (from + wave >= to) return;
+        // (beyond its last step a wave loads that again: without a condition on them, loads ahead stay in their registers)
+        const int last = to - 1 - (to - 1 - from - wave) % WAVES;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) load(from + wave + i * WAVES < to ? from + wave + i * WAVES : last, rb[i], ra[i]);
+        for (int s = from + wave; s < to; s += AHEAD * WAVES) {
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
-                if (s + i * WAVES < s1) {
+                const bool live = s + i * WAVES < to;
 #pragma unroll
-                    for (int kk = 0; kk < 2; ++kk) {
-                        Fragment<DT> fb, fa;
-                        cut<DT, MODE != ALL_PRODUCTS>(rb[i][kk], fb);
-                        cut<DT, MODE != ALL_PRODUCTS>(ra[i][kk], fa);
-                        c[kk] = multiply_parts<DT, MODE>(fb, fa, c[kk]);
-                    }
-                    if (s + (i + AHEAD) * WAVES < s1) load(s + (i + AHEAD) * WAVES, rb[i], ra[i]);
+                for (int kk = 0; kk < 2; ++kk) {
+                    Fragment<DT> fb[1], fa[1];
+                    used_from_here<DT>(rb[i][kk]);
+                    used_from_here<DT>(ra[i][kk]);
+                    cut<DT, MODE != ALL_PRODUCTS>(rb[i][kk], fb[0]);
+                    cut<DT, MODE != ALL_PRODUCTS>(ra[i][kk], fa[0]);
+                    if (live) multiply_parts<DT, MODE, 1, 1>(fb, fa, {&c[kk]});
                 }
+                __builtin_amdgcn_sched_barrier(0);            // loads ahead are issued here, not where their registers are used
+                load(s + (i + AHEAD) * WAVES < to ? s + (i + AHEAD) * WAVES : last, rb[i], ra[i]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+    };
+    auto sums = [&](auto mode) __attribute__((always_inline)) {
+        f32x4 c[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+        range(mode, std::true_type{}, s0, whole_to, c);
+        range(mode, std::false_type{}, whole_to, s1, c);
         return c[0] + c[1];
     };
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-            for (auto& v : ra[i][kk].v) v = u32x4{0, 0, 0, 0};          // rows of A that do not exist
     f32x4 c = sums(std::integral_constant<int, ALL_PRODUCTS>{});
     if constexpr (DT == IOLB_F32) {
         if (__any(!all_finite(c))) {                                     // (nothing is shared yet: a wave may decide for itself)
@@ -205,15 +225,25 @@ dense_few_kernel(DenseProduct p, int join)
 // ahead and of B one or two are kept in registers.  Along (not across): a wave takes sixteen rows of B.  Across: 64 columns of
 // B, four neighbours a lane, so that the eight rows a lane reads are its operand's eight k for each of the four without
 // an exchange between lanes.
+constexpr int NC = 2;                                  // columns of B that a lane reads side by side, across
+constexpr int rows_waves(bool across) { return across ? 4 : 8; }
+constexpr int rows_columns(bool across) { return across ? 4 * 16 * NC : 128; }            // of a workgroup
+// workgroups on a compute unit, by their registers: of 16 rows or less, of 17 to 32, of more
+constexpr int rows_resident(int dtype, int tiles, bool across)
+{
+    return across ? (dtype == IOLB_F32 ? (tiles > 2 ? 3 : 4) : (tiles > 2 ? 4 : 5)) : (dtype == IOLB_F32 ? (tiles > 2 ? 1 : 2) : 2);
+}
+
 template <int DT, int MT, bool ACROSS>
-__global__ void __launch_bounds__(ACROSS ? 256 : 512, 2)
+__global__ void __launch_bounds__(64 * rows_waves(ACROSS), rows_waves(ACROSS) * rows_resident(DT, MT, ACROSS) / 4)
 dense_rows_kernel(DenseProduct p, int join)
 {
     typedef typename DenseType<DT>::type T;
-    constexpr int WAVES = ACROSS ? 4 : 8, THREADS = 64 * WAVES, COLS = ACROSS ? 64 : 16, PARTS = DT == IOLB_F32 ? 3 : 1;
+    constexpr int WAVES = rows_waves(ACROSS), THREADS = 64 * WAVES, COLS = ACROSS ? 16 * NC : 16, PARTS = DT == IOLB_F32 ? 3 : 1;
     constexpr int ROWS = 16 * MT, ITEMS = ROWS * 8, PER = (ITEMS + THREADS - 1) / THREADS;
-    constexpr int NF = ACROSS ? 4 : 1;                                   // fragments of B side by side
-    constexpr int UNITS = 2;                                             // loads of B: 32 k each
+    constexpr int NF = ACROSS ? NC : 1;                                  // fragments of B side by side
+    constexpr int WORDS = DT == IOLB_F32 ? NF : NF / 2;                   // of a lane and row of B, across
+    constexpr int UNITS = 2;
     __shared__ __align__(16) u32x4 rows[2][PARTS][ROWS * 8];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -224,106 +254,114 @@ dense_rows_kernel(DenseProduct p, int join)
     const T* const a = static_cast<const T*>(p.a);
     const T* const b = static_cast<const T*>(p.b);
 
-    // ---- B in registers
-    struct Unit { Raw<DT> along; u32x4 across[ACROSS ? 8 : 1]; };
-    Unit ub[UNITS];
+    // rows (columns) that do not exist are read from the last one: their sums are not stored
     const int along_row = n0 + l16 < p.N ? n0 + l16 : p.N - 1;
-    const int first_col = n0 + 4 * l16;
-    auto load_b = [&](int k, Unit& u) {                                  // k: of the unit's first
-        if constexpr (!ACROSS) {
-            load_raw<DT>(u.along, b + along_row * p.ldb + k, grp, p.K - k, p.vec_b);
-        } else {
+    const int first_col = n0 + NC * l16;
+    const int whole_to = whole_steps(p, s0, s1);
+    f32x4 acc[MT][NF];
+
+    auto range = [&](auto mode, auto whole, int from, int to) __attribute__((always_inline)) {
+        constexpr int MODE = decltype(mode)::value;
+        constexpr bool SAFE = MODE != ALL_PRODUCTS, WHOLE = decltype(whole)::value;
+        if (from >= to) return;
+        // ---- B in registers: 32 k of sixteen rows, or of 64 columns
+        struct Unit { Raw<DT> along; unsigned across[8][ACROSS ? WORDS : 1]; };
+        Unit ub[UNITS];
+        auto load_b = [&](int k, Unit& u) __attribute__((always_inline)) {                     // k: of the unit's first
+            if constexpr (!ACROSS) {
+                load_raw<DT, WHOLE>(u.along, b + along_row * p.ldb + k, grp, p.K - k);
+            } else if constexpr (WHOLE) {
+                typedef unsigned Words __attribute__((ext_vector_type(WORDS)));
+                const T* const at = b + (k + 8 * grp) * p.ldb + (first_col < p.N ? first_col : p.N - NC);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int row = k + 8 * grp + i;
-                const T* const from = b + (row < p.K ? row : p.K - 1) * p.ldb + first_col;
-                u32x4 v = {0, 0, 0, 0};
-                if (row < p.K) {
-                    if (p.vec_b && first_col + 4 <= p.N) {
-                        if constexpr (DT == IOLB_F32) {
-                            v = *reinterpret_cast<const u32x4*>(from);
-                        } else {
-                            const u32x2 t = *reinterpret_cast<const u32x2*>(from);
-                            v[0] = t[0]; v[1] = t[1];
-                        }
-                    } else if constexpr (DT == IOLB_F32) {
+                for (int i = 0; i < 8; ++i) {
+                    const Words t = *reinterpret_cast<const Words*>(at + i * p.ldb);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) v[j] = first_col + j < p.N ? __float_as_uint(from[j]) : 0u;
+                    for (int w = 0; w < WORDS; ++w) u.across[i][w] = t[w];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int row = k + 8 * grp + i;
+                    const bool in = row < p.K;
+                    const T* const at = b + (in ? row : 0) * p.ldb + first_col;
+                    if constexpr (DT == IOLB_F32) {
+#pragma unroll
+                        for (int j = 0; j < WORDS; ++j) u.across[i][j] = in && first_col + j < p.N ? __float_as_uint(at[j]) : 0u;
                     } else {
-                        const unsigned short* const q = reinterpret_cast<const unsigned short*>(from);
+                        const unsigned short* const q = reinterpret_cast<const unsigned short*>(at);
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const unsigned lo = first_col + 2 * j < p.N ? q[2 * j] : 0u, hi = first_col + 2 * j + 1 < p.N ? q[2 * j + 1] : 0u;
-                            v[j] = lo | hi << 16;
+                        for (int j = 0; j < WORDS; ++j) {
+                            const unsigned lo = in && first_col + 2 * j < p.N ? q[2 * j] : 0u, hi = in && first_col + 2 * j + 1 < p.N ? q[2 * j + 1] : 0u;
+                            u.across[i][j] = lo | hi << 16;
                         }
                     }
                 }
-                u.across[i] = v;
             }
-        }
-    };
-    // ---- A: registers, then LDS
-    Raw<DT> ra[PER];
-    auto load_a = [&](int s) {
+        };
+        // ---- A: registers, then LDS (across: plain order of k, as the eight rows of B that a lane reads are neighbours)
+        Raw<DT> ra[PER];
+        auto load_a = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int item = tid + i * THREADS, row = m0 + (item >> 3), piece = item & 7, k = s * STEP + 32 * (piece >> 2);
-            if (ITEMS % THREADS == 0 || item < ITEMS) {
-                if (row < p.M) {
-                    if constexpr (ACROSS && DT == IOLB_F32) {
-                        // plain order of k: the eight rows of B that a lane reads are neighbours
-                        const float* const from = a + row * p.lda + k + 8 * (piece & 3);
-                        const int have = p.K - k - 8 * (piece & 3);
-                        if (p.vec_a && have >= 8) {
-                            ra[i].v[0] = *reinterpret_cast<const u32x4*>(from);
-                            ra[i].v[1] = *reinterpret_cast<const u32x4*>(from + 4);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) ra[i].v[j / 4][j % 4] = j < have ? __float_as_uint(from[j]) : 0u;
-                        }
+            for (int i = 0; i < PER; ++i) {
+                const int item = tid + i * THREADS, row = m0 + (item >> 3), piece = item & 7, g = piece & 3;
+                const T* const at = a + (row < p.M ? row : p.M - 1) * p.lda + s * STEP + 32 * (piece >> 2);
+                const int have = p.K - s * STEP - 32 * (piece >> 2);
+                if constexpr (ACROSS && DT == IOLB_F32) {
+                    if constexpr (WHOLE) {
+                        ra[i].v[0] = *reinterpret_cast<const u32x4*>(at + 8 * g);
+                        ra[i].v[1] = *reinterpret_cast<const u32x4*>(at + 8 * g + 4);
                     } else {
-                        load_raw<DT>(ra[i], a + row * p.lda + k, piece & 3, p.K - k, p.vec_a);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) ra[i].v[j / 4][j % 4] = 8 * g + j < have ? __float_as_uint(at[8 * g + j]) : 0u;
                     }
                 } else {
-#pragma unroll
-                    for (auto& v : ra[i].v) v = u32x4{0, 0, 0, 0};
+                    load_raw<DT, WHOLE>(ra[i], at, g, have);
                 }
             }
-        }
-    };
-
-    f32x4 acc[MT][NF];
-    auto sums = [&](auto mode) {
-        constexpr int MODE = decltype(mode)::value;
-        constexpr bool SAFE = MODE != ALL_PRODUCTS;
-        auto store_a = [&](int buf) {
+        };
+        auto store_a = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const int item = tid + i * THREADS, row = item >> 3, piece = item & 7;
                 if (ITEMS % THREADS == 0 || item < ITEMS) {
                     Fragment<DT> f;
+                    used_from_here<DT>(ra[i]);
                     cut<DT, SAFE>(ra[i], f);
 #pragma unroll
                     for (int q = 0; q < PARTS; ++q) rows[buf][q][row * 8 + place(row, piece)] = f.part[q];
                 }
             }
         };
-        if (s0 >= s1) return;
-        load_a(s0);
+        __syncthreads();                                      // (an earlier range's last step may still be read)
+        load_a(from);
+        store_a(from & 1);
+        // In the order of the loop, A before B: a wait for A at its head then leaves B on its way.  (Beyond the last step the last one is
+        // loaded again: without a condition on them, loads ahead stay in their registers.)
+        load_a(from + 1 < to ? from + 1 : from);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) load_b(s0 * STEP + 32 * u, ub[u]);
-        store_a(s0 & 1);
-        if (s0 + 1 < s1) load_a(s0 + 1);
-        for (int s = s0; s < s1; ++s) {
+        for (int u = 0; u < UNITS; ++u) {
+            load_b(from * STEP + 32 * u, ub[u]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        for (int s = from; s < to; ++s) {
+            const int after = s + 1 < to ? s + 1 : s;
             __syncthreads();
-            if (s + 1 < s1) store_a((s + 1) & 1);
-            if (s + 2 < s1) load_a(s + 2);
+            store_a((s + 1) & 1);
+            load_a(s + 2 < to ? s + 2 : after);
+            __builtin_amdgcn_sched_barrier(0);                // loads ahead are issued here, not where their registers are used
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
                 Fragment<DT> fb[NF];
                 if constexpr (!ACROSS) {
+                    used_from_here<DT>(ub[u].along);
                     cut<DT, SAFE>(ub[u].along, fb[0]);
                 } else {
+#pragma unroll
+                    for (auto& row : ub[u].across)
+#pragma unroll
+                        for (unsigned& v : row) asm volatile("" : "+v"(v));
 #pragma unroll
                     for (int j = 0; j < NF; ++j)
 #pragma unroll
@@ -339,18 +377,30 @@ dense_rows_kernel(DenseProduct p, int join)
                             }
                         }
                 }
-                if (s + 1 < s1) load_b((s + 1) * STEP + 32 * u, ub[u]);
+                __builtin_amdgcn_sched_barrier(0);
+                load_b(after * STEP + 32 * u, ub[u]);
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int TOGETHER = ACROSS ? 1 : MT;     // rows' fragments in registers at a time
 #pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    Fragment<DT> fa;
-                    const int row = 16 * t + l16;
+                for (int t = 0; t < MT; t += TOGETHER) {
+                    Fragment<DT> fa[TOGETHER];
+                    f32x4* sum[TOGETHER * NF];
 #pragma unroll
-                    for (int q = 0; q < PARTS; ++q) fa.part[q] = rows[s & 1][q][row * 8 + place(row, 4 * u + grp)];
+                    for (int i = 0; i < TOGETHER; ++i) {
+                        const int row = 16 * (t + i) + l16;
 #pragma unroll
-                    for (int j = 0; j < NF; ++j) acc[t][j] = multiply_parts<DT, MODE>(fb[j], fa, acc[t][j]);
+                        for (int q = 0; q < PARTS; ++q) fa[i].part[q] = rows[s & 1][q][row * 8 + place(row, 4 * u + grp)];
+#pragma unroll
+                        for (int j = 0; j < NF; ++j) sum[j * TOGETHER + i] = &acc[t + i][j];
+                    }
+                    multiply_parts<DT, MODE, TOGETHER, NF>(fb, fa, sum);
                 }
             }
         }
+    };
+    auto sums = [&](auto mode) __attribute__((always_inline)) {
+        range(mode, std::true_type{}, s0, whole_to);
+        range(mode, std::false_type{}, whole_to, s1);
     };
     auto clear = [&](bool all) {
 #pragma unroll
@@ -373,7 +423,6 @@ dense_rows_kernel(DenseProduct p, int join)
             clear(true);
             sums(std::integral_constant<int, SMALL_PRODUCTS>{});
             clear(false);
-            __syncthreads();
             sums(std::integral_constant<int, LEADING_PRODUCT>{});
         }
     }
@@ -382,10 +431,13 @@ dense_rows_kernel(DenseProduct p, int join)
         const int m = m0 + 16 * t + l16;
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
-            // across: column 4 (4 grp + i) + j of the wave's is value i of fragment j
-            const int n = n0 + (ACROSS ? 16 * grp + 4 * i : 4 * grp);
+            // across: column NC (4 grp + r) + j of the wave's is value r of fragment j
+            const int n = n0 + (ACROSS ? 4 * NC * grp + 4 * i : 4 * grp);
             f32x4 c = acc[t][0];
-            if constexpr (ACROSS) c = f32x4{acc[t][0][i], acc[t][1][i], acc[t][2][i], acc[t][3][i]};
+            if constexpr (ACROSS) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) c[v] = acc[t][(4 * i + v) % NC][(4 * i + v) / NC];
+            }
             if (join) {
                 keep_partial(p, blockIdx.y, m, n, c);
             } else {
@@ -405,35 +457,43 @@ hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
         return hipGetLastError();
     }
     const int mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
-    const unsigned cols = across ? 256 : 128;
+    const int cols = rows_columns(across), threads = 64 * rows_waves(across);
     const dim3 grid((p.N + cols - 1) / cols, p.splits, (p.M + 16 * mt - 1) / (16 * mt));
     if (across) {
-        if (mt == 1) dense_rows_kernel<DT, 1, true><<<grid, 256, 0, st>>>(p, join);
-        else if (mt == 2) dense_rows_kernel<DT, 2, true><<<grid, 256, 0, st>>>(p, join);
-        else dense_rows_kernel<DT, 4, true><<<grid, 256, 0, st>>>(p, join);
+        if (mt == 1) dense_rows_kernel<DT, 1, true><<<grid, threads, 0, st>>>(p, join);
+        else if (mt == 2) dense_rows_kernel<DT, 2, true><<<grid, threads, 0, st>>>(p, join);
+        else dense_rows_kernel<DT, 4, true><<<grid, threads, 0, st>>>(p, join);
     } else {
-        if (mt <= 2) dense_rows_kernel<DT, 2, false><<<grid, 512, 0, st>>>(p, join);
-        else dense_rows_kernel<DT, 4, false><<<grid, 512, 0, st>>>(p, join);
+        if (mt <= 2) dense_rows_kernel<DT, 2, false><<<grid, threads, 0, st>>>(p, join);
+        else dense_rows_kernel<DT, 4, false><<<grid, threads, 0, st>>>(p, join);
     }
     return hipGetLastError();
 }
 
 }  // namespace
 
-// Enough workgroups to have all compute units read, as long as each keeps eight steps (a wave of the first kernel: one).
+// How many workgroups share K: the least modelled time.  They run in rounds of as many as the compute units hold.  What a step takes a round
+// lies between its share of the memory's bandwidth (4.9 TB/s) and its own latency `alone`; a step's worth goes before the first.  Sharing K costs a second
+// launch and the partial sums' way through memory.  Fitted to a sweep of 22 products of 1 to 64 rows and 0.5 M to 103 M weights, 1 to 64 shares.
 DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint)
 {
-    const int steps = (K + STEP - 1) / STEP;
-    const bool few = !across && M <= FEW;
-    const int cols = few ? 16 : across ? 256 : 128;
-    const long long blocks = (N + cols - 1) / cols;
-    const int wanted = few ? 256 : 512;
-    long long splits = (wanted + blocks - 1) / blocks;
-    const long long most = few ? steps / 32 : steps / 8;
-    if (blocks * 2 > wanted || splits > most) splits = blocks * 2 > wanted ? 1 : most;
-    if (splits < 1) splits = 1;
-    (void)dtype;
-    return {(int)splits, splits > 1 || checkpoint};
+    const bool few = !across && M <= FEW, wide = dtype == IOLB_F32;
+    const int tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+    const double alone = few ? (wide ? 1500 : 800) : !across ? (wide ? 1000 : 840) : !wide ? 550 : tiles == 1 ? 1050 : tiles == 2 ? 1350 : 1900;
+    const long long steps = (K + STEP - 1) / STEP, cols = few ? 16 : rows_columns(across);
+    const long long blocks = (N + cols - 1) / cols, waves = few ? 8 : 1;           // (few: the waves share the steps)
+    const long long capacity = 256 * (few ? 2 : rows_resident(dtype, tiles, across));
+    const double step_ns = (double)cols * waves * STEP * (wide ? 4 : 2) / 4900;                        // of one workgroup
+    int best = 1;
+    double least = -1;
+    for (int s = 1; s <= 64 && s <= steps; ++s) {
+        const long long groups = blocks * s, each = (steps + s * waves - 1) / (s * waves) + 1, rest = groups % capacity;
+        double ns = (double)(groups / capacity * each) * std::hypot(alone, capacity * step_ns);
+        if (rest) ns += each * std::hypot(alone, rest * step_ns);
+        if (s > 1) ns += 2000 + 80 * s + 8.0 * s * M * N / 10000;
+        if (least < 0 || ns < least) { least = ns; best = s; }
+    }
+    return {best, best > 1 || checkpoint};
 }
 
 hipError_t launch_dense_rows(const DenseProduct& p, bool across, bool join, int dtype, hipStream_t st)
