@@ -64,6 +64,10 @@ struct DenseRowsPlan { int splits; bool join; };
 DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint);
 hipError_t launch_dense_rows(const DenseProduct& p, bool across, bool join, int dtype, hipStream_t st);
 hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st);
+// The same for a short summed axis, 0 < K <= DENSE_ROWS_MOST: operands in planes, `plane_a` and `plane_b` elements apart; no bias, activation,
+// residual or checkpoint.  At most DENSE_OUTER_ROWS rows of A.
+constexpr long long DENSE_OUTER_ROWS = 65535 * 128LL;
+hipError_t launch_dense_outer(const DenseProduct& p, int planes_b, long long plane_a, long long plane_b, int dtype, hipStream_t st);
 
 // ---- operands laid out for the product --------------------------------------------------------------
 // Values v[r][c], rows x cols, from one of three sources:

@@ -180,6 +180,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     DenseTilePlan plan_x{}, plan_w{};
     DenseRowsPlan rows_x{};
     size_t partial_x = 0, partial_w = 0;
+    bool outer = false;
     if (want_dx && few) {
         px.M = (int)a.M; px.N = (int)a.K; px.K = (int)a.N;
         px.a = dz; px.lda = ld_dz; px.vec_a = aligned_to(dz, 16) && (a.M == 1 || ld_dz * size_of(a.dtype) % 16 == 0);
@@ -199,8 +200,9 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         pw.M = (int)a.N; pw.N = (int)a.K; pw.K = (int)Mp;
         pw.a = dzt; pw.lda = Mp; pw.b = xt; pw.ldb = Mp;
         segments(&pw, planes, planes_x, a.N * Mp, a.K * Mp);
+        outer = few && a.M > 0 && a.N <= DENSE_OUTER_ROWS;
         plan_w = dense_tile_plan(pw.M, pw.N, pw.K, pw.segments);
-        pw.splits = plan_w.splits;
+        pw.splits = outer ? 1 : plan_w.splits;
         if (pw.splits > 1) partial_w = dense_partial_bytes(pw.splits, pw.M, pw.N);
     }
     // one after the other on the stream: they share the room for partial sums
@@ -257,7 +259,8 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     }
     if (want_dw) {
         pw.f = finish(a.dw, a.N, a.K);
-        DENSE_HIP(launch_dense_product(pw, plan_w.tile, a.dtype, st));
+        if (outer) DENSE_HIP(launch_dense_outer(pw, planes_x, a.N * Mp, a.K * Mp, a.dtype, st));
+        else DENSE_HIP(launch_dense_product(pw, plan_w.tile, a.dtype, st));
     }
     return IOLB_OK;
 }

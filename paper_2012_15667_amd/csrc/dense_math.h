@@ -194,20 +194,21 @@ __device__ __forceinline__ float largest_of(const float (&z)[W], int have)
     return most;
 }
 
-// Eight columns; the block's largest finite magnitude is `most`, and its first lane writes the exponent.
-template <int DT>
-__device__ __forceinline__ void store_codes(const DenseFinish& f, int m, int n, const float (&z)[8], float most)
+// The block's largest finite magnitude is `most`, and its first lane writes the exponent.
+template <int DT, int W>
+__device__ __forceinline__ void store_codes(const DenseFinish& f, int m, int n, const float (&z)[W], float most)
 {
+    typedef unsigned Words __attribute__((ext_vector_type(W / 4)));
     const int e = ckpt_exponent<DT>(most), have = f.N - n;
-    u32x2 code = {0, 0};
+    Words code = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) code[i / 4] |= ckpt_code<DT>(z[i], e) << 8 * (i % 4);
+    for (int i = 0; i < W; ++i) code[i / 4] |= ckpt_code<DT>(z[i], e) << 8 * (i % 4);
     int8_t* const to = f.zq + (long long)m * f.N + n;
     if (f.vec_q) {
-        *reinterpret_cast<u32x2*>(to) = code;
+        *reinterpret_cast<Words*>(to) = code;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < W; ++i)
             if (i < have) to[i] = (int8_t)(code[i / 4] >> 8 * (i % 4));
     }
     if (n % CKPT_BLOCK == 0) f.ze[(long long)m * ((f.N + CKPT_BLOCK - 1) / CKPT_BLOCK) + n / CKPT_BLOCK] = (uint8_t)(e + 127);
@@ -249,18 +250,21 @@ __device__ __forceinline__ void finish_four(const DenseFinish& f, int m, int n, 
     by_activation(f.act, [&](auto act) __attribute__((always_inline)) { store_columns<DT, decltype(act)::value>(f, m, n, z); });
 }
 
-// Eight columns of row m, which four neighbouring lanes continue to a checkpoint's block.  Every lane of the wave calls.
-template <int DT, int ACT>
-__device__ __forceinline__ void finish_eight(const DenseFinish& f, int m, int n, const float (&bias)[8], float (&z)[8])
+// Columns that a lane finishes: 16 bytes of the output.
+template <int DT> constexpr int FINISH_COLUMNS = DT == IOLB_F32 ? 4 : 8;
+
+// W columns of row m, which 32 / W neighbouring lanes continue to a checkpoint's block.  Every lane of the wave calls.
+template <int DT, int ACT, int W>
+__device__ __forceinline__ void finish_columns(const DenseFinish& f, int m, int n, const float (&bias)[W], float (&z)[W])
 {
     const bool live = m < f.M && n < f.N;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] += bias[i];
+    for (int i = 0; i < W; ++i) z[i] += bias[i];
     if (live && f.residual && f.first) add_residual<DT>(f, m, n, z);
     if (f.zq) {
         float most = largest_of(z, f.N - n);
-        most = fmaxf(most, __shfl_xor(most, 1));
-        most = fmaxf(most, __shfl_xor(most, 2));
+#pragma unroll
+        for (int d = 1; d < CKPT_BLOCK / W; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
         if (live) store_codes<DT>(f, m, n, z, most);
     }
     if (live) store_columns<DT, ACT>(f, m, n, z);

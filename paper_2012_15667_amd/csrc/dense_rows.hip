@@ -447,6 +447,111 @@ dense_rows_kernel(DenseProduct p, int join)
     }
 }
 
+// ---- products of which the summed axis is short (the weights' gradient of up to 64 rows): bound by writing C ---------
+// A is [M][K], B [N][K], K at most 64, both in planes.  A wave keeps sixteen NT rows of A in registers and goes along a run of columns: their
+// fragments of B come from L2, two groups of 32 ahead, there is neither LDS nor a barrier, and the stores stream.  A lane ends with
+// neighbouring columns of one row: 16 bytes of the output at a time (16-bit types: rows r of two tiles are columns 8 (r / 4) + r % 4 and
+// four further).
+constexpr int OUTER_RUN = 256;                         // columns of a workgroup
+
+template <int DT, int PB, int KK>
+__global__ void __launch_bounds__(256, PB == 3 ? 2 : 3)
+dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
+{
+    constexpr int PA = DT == IOLB_F32 ? 3 : 1, NT = DT == IOLB_F32 ? 2 : 4, AHEAD = 2;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4;
+    const int m0 = (blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 16 * NT;
+    if (m0 >= p.M) return;
+    const unsigned short* const a = static_cast<const unsigned short*>(p.a);
+    const unsigned short* const b = static_cast<const unsigned short*>(p.b);
+    u32x4 fa[NT][KK][PA];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int q = 0; q < PA; ++q) {
+                const int row = m0 + 16 * t + l16, k = 32 * kk + 8 * grp;
+                fa[t][kk][q] = k < p.K ? *reinterpret_cast<const u32x4*>(a + q * plane_a + (row < p.M ? row : p.M - 1) * p.lda + k) : u32x4{0, 0, 0, 0};
+            }
+    const int n_from = blockIdx.x * OUTER_RUN, n_to = n_from + OUTER_RUN < p.N ? n_from + OUTER_RUN : p.N;
+    u32x4 fb[AHEAD][2][KK][PB];
+    // (pieces beyond the summed axis: zero in A, any finite values here, so those of its first piece; B's rows beyond its last: that one's)
+    auto load = [&](int n, u32x4 (&to)[2][KK][PB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int col = n + (DT == IOLB_F32 ? 16 * j + l16 : 8 * (l16 >> 2) + 4 * j + (l16 & 3));
+            const unsigned short* const row = b + (col < p.N ? col : p.N - 1) * p.ldb;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                const int k = 32 * kk + 8 * grp;
+#pragma unroll
+                for (int q = 0; q < PB; ++q) to[j][kk][q] = *reinterpret_cast<const u32x4*>(row + q * plane_b + (k < p.K ? k : 0));
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load(n_from + 32 * i, fb[i]);
+    for (int n0 = n_from; n0 < n_to; n0 += 32 * AHEAD) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int n = n0 + 32 * i;
+            f32x4 c[NT][2] = {};
+            constexpr int part_a[6] = {2, 0, 1, 1, 0, 0}, part_b[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+            for (int q = 0; q < 6; ++q) {
+                if (part_a[q] >= PA || part_b[q] >= PB) continue;
+                if (q == 5 && PB == 3) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) clear_not_finite(c[t][j]);
+                }
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            c[t][j] = multiply<DT == IOLB_F16>(fb[i][j][kk][part_b[q]], fa[t][kk][part_a[q]], c[t][j]);
+            }
+            load(n + 32 * AHEAD < n_to ? n + 32 * AHEAD : n_from, fb[i]);
+            if (n < n_to) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int m = m0 + 16 * t + l16;
+                    if constexpr (DT == IOLB_F32) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float z[4] = {c[t][j][0], c[t][j][1], c[t][j][2], c[t][j][3]};
+                            const int col = n + 16 * j + 4 * grp;
+                            if (m < p.M && col < p.N) store_columns<DT, IOLB_ACT_NONE>(p.f, m, col, z);
+                        }
+                    } else {
+                        float z[8];
+#pragma unroll
+                        for (int v = 0; v < 8; ++v) z[v] = c[t][v / 4][v % 4];
+                        const int col = n + 8 * grp;
+                        if (m < p.M && col < p.N) store_columns<DT, IOLB_ACT_NONE>(p.f, m, col, z);
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <int DT, int PB>
+hipError_t launch_outer(const DenseProduct& p, long long plane_a, long long plane_b, hipStream_t st)
+{
+    const int rows = 4 * 16 * (DT == IOLB_F32 ? 2 : 4);
+    const long long gy = ((long long)p.M + rows - 1) / rows;
+    if (gy > 65535) return hipErrorInvalidValue;
+    const dim3 grid((p.N + OUTER_RUN - 1) / OUTER_RUN, (unsigned)gy);
+    if (p.K <= 32) dense_outer_kernel<DT, PB, 1><<<grid, 256, 0, st>>>(p, plane_a, plane_b);
+    else dense_outer_kernel<DT, PB, 2><<<grid, 256, 0, st>>>(p, plane_a, plane_b);
+    return hipGetLastError();
+}
+
 constexpr int FEW = 16;                                // rows of the first kernel
 
 template <int DT>
@@ -494,6 +599,13 @@ DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool 
         if (least < 0 || ns < least) { least = ns; best = s; }
     }
     return {best, best > 1 || checkpoint};
+}
+
+hipError_t launch_dense_outer(const DenseProduct& p, int planes_b, long long plane_a, long long plane_b, int dtype, hipStream_t st)
+{
+    if (dtype == IOLB_F32)
+        return planes_b == 3 ? launch_outer<IOLB_F32, 3>(p, plane_a, plane_b, st) : launch_outer<IOLB_F32, 1>(p, plane_a, plane_b, st);
+    return dtype == IOLB_F16 ? launch_outer<IOLB_F16, 1>(p, plane_a, plane_b, st) : launch_outer<IOLB_BF16, 1>(p, plane_a, plane_b, st);
 }
 
 hipError_t launch_dense_rows(const DenseProduct& p, bool across, bool join, int dtype, hipStream_t st)

@@ -186,14 +186,14 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
         return;
     }
 
-    // The sums go through LDS, as many rows at a time as fit, so that a thread finishes eight neighbouring columns and a wave's loads
+    // The sums go through LDS, as many rows at a time as fit, so that a thread finishes 16 bytes of a row and a wave's loads
     // and stores are whole rows.  16-byte piece c of row r lies at c ^ (r & 15).
     constexpr int PASSES = BM * BN * 4 > 2 * (int)STAGE ? 2 : 1, PI = MI / PASSES, PASS_ROWS = WM * PI * 16;
-    constexpr int LANES = BN / 8, AT_ONCE = 64 * WAVES / LANES;             // threads of a row, rows of an iteration
+    constexpr int W = FINISH_COLUMNS<DT>, LANES = BN / W, AT_ONCE = 64 * WAVES / LANES;   // threads of a row, rows of an iteration
     static_assert(PASS_ROWS * BN * 4 <= 2 * (int)STAGE && PASS_ROWS % AT_ONCE == 0, "a pass fits the stages' buffers");
     f32x4* const sums = reinterpret_cast<f32x4*>(lds);
-    const int n = n0 + (tid % LANES) * 8;
-    float bias[8];
+    const int n = n0 + (tid % LANES) * W;
+    float bias[W];
     load_bias<DT>(p.f, n, bias);
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
@@ -209,11 +209,15 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
         by_activation(p.f.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll 1
             for (int r = tid / LANES; r < PASS_ROWS; r += AT_ONCE) {
-                const int c = 2 * (tid % LANES);
-                const f32x4 lo = sums[r * (BN / 4) + (c ^ (r & 15))], hi = sums[r * (BN / 4) + ((c + 1) ^ (r & 15))];
-                float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                float z[W];
+#pragma unroll
+                for (int h = 0; h < W / 4; ++h) {
+                    const f32x4 four = sums[r * (BN / 4) + ((W / 4 * (tid % LANES) + h) ^ (r & 15))];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[4 * h + i] = four[i];
+                }
                 const int m = m0 + r / (PI * 16) * (BM / WM) + pass * PI * 16 + r % (PI * 16);
-                finish_eight<DT, decltype(act)::value>(p.f, m, n, bias, z);
+                finish_columns<DT, decltype(act)::value>(p.f, m, n, bias, z);
             }
         });
     }
@@ -242,7 +246,7 @@ dense_join_kernel(DenseProduct p, int wide_log)
                     for (int c = 0; c < 4; ++c) { z[c] += lo[c]; z[4 + c] += hi[c]; }
                 }
             }
-            finish_eight<DT, decltype(act)::value>(p.f, (int)(m < p.M ? m : p.M), n, bias, z);
+            finish_columns<DT, decltype(act)::value>(p.f, (int)(m < p.M ? m : p.M), n, bias, z);
         }
     });
 }
