@@ -44,6 +44,8 @@ struct DenseProduct {
     long long a_plane[MAX_SEGMENTS], b_plane[MAX_SEGMENTS];   // where the segment's planes start, in elements
     int splits;                             // workgroups that share a tile's K; their sums go to `partial` if > 1
     float* partial;                         // [splits][M][N rounded up to 4]
+    int block_columns, per;                 // kernels for few rows: workgroups take runs of `per` steps, block after block of columns,
+                                            // and a block's pieces are as many as runs meet it (block_columns 0: `splits`)
     int vec_a, vec_b;                       // kernels for few rows: whole 16-byte pieces of the operand may be read
     DenseFinish f;
 };
@@ -57,10 +59,11 @@ inline size_t dense_partial_bytes(int splits, long long M, long long N) { return
 hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st);
 
 // The same for few rows of A: both operands as the caller holds them (fp32 too: taken apart in the kernels), any K, bound by reading
-// B.  across: B is [K][N], summed along its rows.  K is shared by `splits` workgroups.  Sums go to `partial` if join is set
-// (always with splits > 1 or a checkpoint).
+// B.  across: B is [K][N], summed along its rows.  K is shared by workgroups, at most `splits` to a sum.  Sums go to `partial` if join is
+// set (always with splits > 1 or a checkpoint).
 constexpr int DENSE_ROWS_MOST = 64;
-struct DenseRowsPlan { int splits; bool join; };
+constexpr int DENSE_ROWS_STEP = 64;         // k of a step
+struct DenseRowsPlan { int splits, per; bool join; int block_columns; };
 DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint);
 hipError_t launch_dense_rows(const DenseProduct& p, bool across, bool join, int dtype, hipStream_t st);
 hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st);

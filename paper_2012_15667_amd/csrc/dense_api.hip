@@ -87,7 +87,7 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
         p.b = a.w; p.ldb = a.ldw; p.vec_b = a.N == 1 ? aligned_to(a.w, 16) : pieces_of_16(a.w, a.ldw);
         p.K = (int)a.K;
         const DenseRowsPlan plan = dense_rows_plan(p.M, p.N, p.K, a.dtype, false, a.zq != nullptr);
-        p.splits = plan.splits;
+        p.splits = plan.splits; p.per = plan.per; p.block_columns = plan.block_columns;
         if (plan.join) p.partial = static_cast<float*>(pieces.take(dense_partial_bytes(plan.splits, a.M, a.N)));
         *need = pieces.used;
         if (launch) DENSE_HIP(launch_dense_rows(p, false, plan.join, a.dtype, call_stream()));
@@ -186,7 +186,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         px.a = dz; px.lda = ld_dz; px.vec_a = aligned_to(dz, 16) && (a.M == 1 || ld_dz * size_of(a.dtype) % 16 == 0);
         px.b = a.w; px.ldb = a.ldw; px.vec_b = a.K % 4 == 0 && aligned_to(a.w, 4 * size_of(a.dtype)) && (a.N == 1 || a.ldw % 4 == 0);
         rows_x = dense_rows_plan(px.M, px.N, px.K, a.dtype, true, false);
-        px.splits = rows_x.splits;
+        px.splits = rows_x.splits; px.per = rows_x.per; px.block_columns = rows_x.block_columns;
         if (rows_x.join) partial_x = dense_partial_bytes(px.splits, px.M, px.N);
     } else if (want_dx) {
         px.M = (int)a.M; px.N = (int)a.K; px.K = (int)Np;

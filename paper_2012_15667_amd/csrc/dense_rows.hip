@@ -231,7 +231,7 @@ constexpr int rows_columns(bool across) { return across ? 4 * 16 * NC : 128; }  
 // workgroups on a compute unit, by their registers: of 16 rows or less, of 17 to 32, of more
 constexpr int rows_resident(int dtype, int tiles, bool across)
 {
-    return across ? (dtype == IOLB_F32 ? (tiles > 2 ? 3 : 4) : (tiles > 2 ? 4 : 5)) : (dtype == IOLB_F32 ? (tiles > 2 ? 1 : 2) : 2);
+    return across ? (dtype == IOLB_F32 ? (tiles > 2 ? 2 : 3) : (tiles > 2 ? 3 : 4)) : (dtype == IOLB_F32 ? (tiles > 2 ? 1 : 2) : 2);
 }
 
 template <int DT, int MT, bool ACROSS>
@@ -247,13 +247,15 @@ dense_rows_kernel(DenseProduct p, int join)
     __shared__ __align__(16) u32x4 rows[2][PARTS][ROWS * 8];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n0 = (blockIdx.x * WAVES + wave) * COLS;
-    const int m0 = blockIdx.z * ROWS;
-    const int steps_all = (p.K + STEP - 1) / STEP;
-    const int s0 = (int)((long long)steps_all * blockIdx.y / p.splits), s1 = (int)((long long)steps_all * (blockIdx.y + 1) / p.splits);
     const T* const a = static_cast<const T*>(p.a);
     const T* const b = static_cast<const T*>(p.b);
-
+    const long long steps = p.K > 0 ? (p.K + STEP - 1) / STEP : 1, total = steps * ((p.N + WAVES * COLS - 1) / (WAVES * COLS));
+    const long long end = (blockIdx.x + 1LL) * p.per < total ? (blockIdx.x + 1LL) * p.per : total;
+    // the workgroup's run of steps, block by block
+    for (long long at_step = (long long)blockIdx.x * p.per; at_step < end;) {
+    const int block = (int)(at_step / steps), s0 = (int)(at_step % steps), s1 = (int)(steps < s0 + end - at_step ? steps : s0 + end - at_step);
+    at_step += s1 - s0;
+    const int n0 = (block * WAVES + wave) * COLS;
     // rows (columns) that do not exist are read from the last one: their sums are not stored
     const int along_row = n0 + l16 < p.N ? n0 + l16 : p.N - 1;
     const int first_col = n0 + NC * l16;
@@ -304,7 +306,7 @@ dense_rows_kernel(DenseProduct p, int join)
         auto load_a = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int item = tid + i * THREADS, row = m0 + (item >> 3), piece = item & 7, g = piece & 3;
+                const int item = tid + i * THREADS, row = item >> 3, piece = item & 7, g = piece & 3;
                 const T* const at = a + (row < p.M ? row : p.M - 1) * p.lda + s * STEP + 32 * (piece >> 2);
                 const int have = p.K - s * STEP - 32 * (piece >> 2);
                 if constexpr (ACROSS && DT == IOLB_F32) {
@@ -428,7 +430,7 @@ dense_rows_kernel(DenseProduct p, int join)
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int m = m0 + 16 * t + l16;
+        const int m = 16 * t + l16;
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
             // across: column NC (4 grp + r) + j of the wave's is value r of fragment j
@@ -439,11 +441,12 @@ dense_rows_kernel(DenseProduct p, int join)
                 for (int v = 0; v < 4; ++v) c[v] = acc[t][(4 * i + v) % NC][(4 * i + v) / NC];
             }
             if (join) {
-                keep_partial(p, blockIdx.y, m, n, c);
+                keep_partial(p, (int)(blockIdx.x - block * steps / p.per), m, n, c);
             } else {
                 finish_four<DT>(p.f, m, n, c);
             }
         }
+    }
     }
 }
 
@@ -452,10 +455,8 @@ dense_rows_kernel(DenseProduct p, int join)
 // fragments of B come from L2, two groups of 32 ahead, there is neither LDS nor a barrier, and the stores stream.  A lane ends with
 // neighbouring columns of one row: 16 bytes of the output at a time (16-bit types: rows r of two tiles are columns 8 (r / 4) + r % 4 and
 // four further).
-constexpr int OUTER_RUN = 256;                         // columns of a workgroup
-
 template <int DT, int PB, int KK>
-__global__ void __launch_bounds__(256, PB == 3 ? 2 : 3)
+__global__ void __launch_bounds__(256, PB == 3 ? 1 : KK == 2 ? 2 : 3)
 dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
 {
     constexpr int PA = DT == IOLB_F32 ? 3 : 1, NT = DT == IOLB_F32 ? 2 : 4, AHEAD = 2;
@@ -474,7 +475,7 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
                 const int row = m0 + 16 * t + l16, k = 32 * kk + 8 * grp;
                 fa[t][kk][q] = k < p.K ? *reinterpret_cast<const u32x4*>(a + q * plane_a + (row < p.M ? row : p.M - 1) * p.lda + k) : u32x4{0, 0, 0, 0};
             }
-    const int n_from = blockIdx.x * OUTER_RUN, n_to = n_from + OUTER_RUN < p.N ? n_from + OUTER_RUN : p.N;
+    const int n_from = blockIdx.x * p.per, n_to = n_from + p.per < p.N ? n_from + p.per : p.N;
     u32x4 fb[AHEAD][2][KK][PB];
     // (pieces beyond the summed axis: zero in A, any finite values here, so those of its first piece; B's rows beyond its last: that one's)
     auto load = [&](int n, u32x4 (&to)[2][KK][PB]) __attribute__((always_inline)) {
@@ -492,6 +493,14 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) load(n_from + 32 * i, fb[i]);
+    // WHOLE: every store is a 16-byte piece that exists.  (Under conditions the stores' number is not known, and a wait for a load would be
+    // one for the stores before it.)
+    auto run = [&](auto whole) __attribute__((always_inline)) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    auto store = [&](int m, int col, auto& z) __attribute__((always_inline)) {
+        if constexpr (WHOLE) store_whole<DT>(p.f, m, col, z);
+        else if (m < p.M && col < p.N) store_columns<DT, IOLB_ACT_NONE>(p.f, m, col, z);
+    };
     for (int n0 = n_from; n0 < n_to; n0 += 32 * AHEAD) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
@@ -516,7 +525,7 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
                             c[t][j] = multiply<DT == IOLB_F16>(fb[i][j][kk][part_b[q]], fa[t][kk][part_a[q]], c[t][j]);
             }
             load(n + 32 * AHEAD < n_to ? n + 32 * AHEAD : n_from, fb[i]);
-            if (n < n_to) {
+            if (WHOLE || n < n_to) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const int m = m0 + 16 * t + l16;
@@ -525,28 +534,34 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
                         for (int j = 0; j < 2; ++j) {
                             float z[4] = {c[t][j][0], c[t][j][1], c[t][j][2], c[t][j][3]};
                             const int col = n + 16 * j + 4 * grp;
-                            if (m < p.M && col < p.N) store_columns<DT, IOLB_ACT_NONE>(p.f, m, col, z);
+                            store(m, col, z);
                         }
                     } else {
                         float z[8];
 #pragma unroll
                         for (int v = 0; v < 8; ++v) z[v] = c[t][v / 4][v % 4];
                         const int col = n + 8 * grp;
-                        if (m < p.M && col < p.N) store_columns<DT, IOLB_ACT_NONE>(p.f, m, col, z);
+                        store(m, col, z);
                     }
                 }
             }
         }
     }
+    };
+    if (p.f.vec_y && m0 + 16 * NT <= p.M && (n_to - n_from) % (32 * AHEAD) == 0) run(std::true_type{});
+    else run(std::false_type{});
 }
 
 template <int DT, int PB>
-hipError_t launch_outer(const DenseProduct& p, long long plane_a, long long plane_b, hipStream_t st)
+hipError_t launch_outer(DenseProduct p, long long plane_a, long long plane_b, hipStream_t st)
 {
     const int rows = 4 * 16 * (DT == IOLB_F32 ? 2 : 4);
     const long long gy = ((long long)p.M + rows - 1) / rows;
     if (gy > 65535) return hipErrorInvalidValue;
-    const dim3 grid((p.N + OUTER_RUN - 1) / OUTER_RUN, (unsigned)gy);
+    // a wave's run of columns: eight waves to a SIMD, as each starts with a wait for its rows of A
+    const long long run = ((long long)p.N * gy * 4 / 8192 + 63) / 64 * 64;
+    p.per = (int)(run < 64 ? 64 : run > 4096 ? 4096 : run);
+    const dim3 grid((unsigned)(((long long)p.N + p.per - 1) / p.per), (unsigned)gy);
     if (p.K <= 32) dense_outer_kernel<DT, PB, 1><<<grid, 256, 0, st>>>(p, plane_a, plane_b);
     else dense_outer_kernel<DT, PB, 2><<<grid, 256, 0, st>>>(p, plane_a, plane_b);
     return hipGetLastError();
@@ -563,7 +578,8 @@ hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
     }
     const int mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
     const int cols = rows_columns(across), threads = 64 * rows_waves(across);
-    const dim3 grid((p.N + cols - 1) / cols, p.splits, (p.M + 16 * mt - 1) / (16 * mt));
+    const long long total = (p.K > 0 ? (p.K + STEP - 1LL) / STEP : 1) * ((p.N + cols - 1LL) / cols);       // (a sum over nothing: one empty step)
+    const unsigned grid = (unsigned)((total + p.per - 1) / p.per);
     if (across) {
         if (mt == 1) dense_rows_kernel<DT, 1, true><<<grid, threads, 0, st>>>(p, join);
         else if (mt == 2) dense_rows_kernel<DT, 2, true><<<grid, threads, 0, st>>>(p, join);
@@ -577,28 +593,41 @@ hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
 
 }  // namespace
 
-// How many workgroups share K: the least modelled time.  They run in rounds of as many as the compute units hold.  What a step takes a round
-// lies between its share of the memory's bandwidth (4.9 TB/s) and its own latency `alone`; a step's worth goes before the first.  Sharing K costs a second
-// launch and the partial sums' way through memory.  Fitted to a sweep of 22 products of 1 to 64 rows and 0.5 M to 103 M weights, 1 to 64 shares.
+// How the steps are dealt out: the least modelled time.  Up to sixteen rows: `splits` workgroups share the K of sixteen columns.  Beyond: the steps of
+// all blocks of columns, one after the other, are cut into equal runs, one a workgroup, so that every compute unit has the same to do (with
+// whole shares of K, 196 blocks of 25088 columns left some with twice the others': 117 us at 64 rows, 87 dealt out evenly).  What a step
+// takes lies between its share of the memory's bandwidth (4.9 TB/s) and its own latency `alone`; one goes before the first.  A second launch
+// adds the partial sums, which go through memory.  Fitted to a sweep of 22 products of 1 to 64 rows and 0.5 M to 103 M weights, 1 to 64 shares.
 DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint)
 {
     const bool few = !across && M <= FEW, wide = dtype == IOLB_F32;
     const int tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
     const double alone = few ? (wide ? 1500 : 800) : !across ? (wide ? 1000 : 840) : !wide ? 550 : tiles == 1 ? 1050 : tiles == 2 ? 1350 : 1900;
-    const long long steps = (K + STEP - 1) / STEP, cols = few ? 16 : rows_columns(across);
+    const long long steps = K > 0 ? (K + STEP - 1) / STEP : 1, cols = few ? 16 : rows_columns(across);
     const long long blocks = (N + cols - 1) / cols, waves = few ? 8 : 1;           // (few: the waves share the steps)
     const long long capacity = 256 * (few ? 2 : rows_resident(dtype, tiles, across));
     const double step_ns = (double)cols * waves * STEP * (wide ? 4 : 2) / 4900;                        // of one workgroup
-    int best = 1;
+    DenseRowsPlan best{1, 0, checkpoint, 0};
     double least = -1;
-    for (int s = 1; s <= 64 && s <= steps; ++s) {
-        const long long groups = blocks * s, each = (steps + s * waves - 1) / (s * waves) + 1, rest = groups % capacity;
-        double ns = (double)(groups / capacity * each) * std::hypot(alone, capacity * step_ns);
-        if (rest) ns += each * std::hypot(alone, rest * step_ns);
-        if (s > 1) ns += 2000 + 80 * s + 8.0 * s * M * N / 10000;
-        if (least < 0 || ns < least) { least = ns; best = s; }
+    const auto consider = [&](long long groups, long long each, int pieces, const DenseRowsPlan& plan) {
+        double ns = (double)(groups / capacity * (each + 1)) * std::hypot(alone, capacity * step_ns);
+        if (groups % capacity) ns += (each + 1) * std::hypot(alone, groups % capacity * step_ns);
+        if (pieces > 1) ns += 2000 + 80 * pieces + 8.0 * pieces * M * N / 10000;
+        if (least < 0 || ns < least) { least = ns; best = plan; }
+    };
+    if (few) {
+        for (int s = 1; s <= 64 && s <= steps; ++s)
+            consider(blocks * s, (steps + s * waves - 1) / (s * waves), s, {s, 0, s > 1 || checkpoint, 0});
+    } else {
+        consider(blocks, steps, 1, {1, (int)steps, checkpoint, (int)cols});
+        for (long long groups = 32; groups <= capacity; groups += groups < 256 ? 32 : 256) {
+            const long long per = (blocks * steps + groups - 1) / groups;
+            if (per >= steps) continue;
+            const int pieces = (int)((steps + per - 2) / per + 1);            // of a block, at most
+            consider((blocks * steps + per - 1) / per, per, pieces, {pieces, (int)per, true, (int)cols});
+        }
     }
-    return {best, best > 1 || checkpoint};
+    return best;
 }
 
 hipError_t launch_dense_outer(const DenseProduct& p, int planes_b, long long plane_a, long long plane_b, int dtype, hipStream_t st)

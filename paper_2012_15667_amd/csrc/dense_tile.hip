@@ -234,13 +234,19 @@ dense_join_kernel(DenseProduct p, int wide_log)
     by_activation(p.f.act, [&](auto act) __attribute__((always_inline)) {
         float bias[8];
         load_bias<DT>(p.f, n, bias);
+        int pieces = p.splits;
+        if (p.block_columns && n < p.N) {
+            // the runs that meet the block of columns n is in (all eight are in one)
+            const long long steps = p.K > 0 ? (p.K + DENSE_ROWS_STEP - 1) / DENSE_ROWS_STEP : 1, first = n / p.block_columns * steps;
+            pieces = (int)((first + steps - 1) / p.per - first / p.per) + 1;
+        }
         for (long long m = (long long)blockIdx.y * rows + (threadIdx.x >> wide_log); m - (threadIdx.x >> wide_log) < p.M; m += (long long)gridDim.y * rows) {
             float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (m < p.M && n < p.N) {
                 const float* from = p.partial + m * ld + n;
                 const bool both = n + 4 < p.N;
 #pragma unroll 4
-                for (int s = 0; s < p.splits; ++s, from += p.M * ld) {
+                for (int s = 0; s < pieces; ++s, from += p.M * ld) {
                     const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = both ? *reinterpret_cast<const f32x4*>(from + 4) : f32x4{0, 0, 0, 0};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) { z[c] += lo[c]; z[4 + c] += hi[c]; }
