@@ -46,6 +46,9 @@ struct DenseProduct {
     float* partial;                         // [splits][M][N rounded up to 4]
     int block_columns, per;                 // kernels for few rows: workgroups take runs of `per` steps, block after block of columns,
                                             // and a block's pieces are as many as runs meet it (block_columns 0: `splits`)
+    const int *exps_a, *exps_b;             // fp32 operands in two fp16 parts: the exponents of their rows (null otherwise)
+    const int* uneven;                      // not null: the launch does nothing unless *uneven is `when`
+    int when;
     int vec_a, vec_b;                       // kernels for few rows: whole 16-byte pieces of the operand may be read
     DenseFinish f;
 };
@@ -55,7 +58,7 @@ enum { DENSE_TILE_256, DENSE_TILE_128, DENSE_TILE_64x128, DENSE_TILE_64, DENSE_T
 struct DenseTilePlan { int tile, splits; };
 DenseTilePlan dense_tile_plan(int M, int N, int K, int segments);
 inline size_t dense_partial_bytes(int splits, long long M, long long N) { return (size_t)splits * M * ((N + 3) / 4 * 4) * 4; }
-// dtype: of y, bias and residual; f16: the operands are fp16 (else bf16).
+// dtype: of y, bias and residual.  Operands are of the type; for fp32 they are in two fp16 parts where exps_a is given, else in three bf16 parts.
 hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st);
 
 // The same for few rows of A: both operands as the caller holds them (fp32 too: taken apart in the kernels), any K, bound by reading
@@ -97,12 +100,18 @@ struct DenseLayout {
 constexpr int MAX_LAYOUTS = 3;
 struct DenseLayouts {
     int count;
+    const int* uneven;                      // not null: the launch does nothing unless *uneven is 1
     DenseLayout of[MAX_LAYOUTS];
 };
 // dtype: of src, copy and (16-bit types) the planes.
 hipError_t launch_dense_layouts(int dtype, const DenseLayouts& l, hipStream_t st);
 // out[c] = sum of colsum over its `blocks` rows, in `dtype`.
 hipError_t launch_dense_colsum(const float* colsum, int blocks, int cols, void* out, int dtype, hipStream_t st);
+
+// Rows of a and b, `cols` long, in two fp16 parts, planes [2][rows][pitch] (pitch: cols rounded up to 8), and their exponents; *uneven
+// becomes 1 if two parts do not hold a row well, else 0.
+hipError_t launch_dense_halves(const float* a, long long lda, int rows_a, void* planes_a, int* exps_a, const float* b, long long ldb, int rows_b,
+                               void* planes_b, int* exps_b, int cols, long long pitch, int* uneven, hipStream_t st);
 
 hipError_t launch_checkpoint_pack(const void* x, long long ldx, int rows, int cols, int dtype, int8_t* q, uint8_t* e, hipStream_t st);
 hipError_t launch_checkpoint_unpack(const int8_t* q, const uint8_t* e, int rows, int cols, int act, int dtype, void* y, long long ldy,

@@ -74,7 +74,6 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     if (a.M == 0 || a.N == 0) return IOLB_OK;
     Pieces pieces{static_cast<char*>(ws)};
     const int64_t Kp = up8(a.K);
-    const int planes = a.dtype == IOLB_F32 ? 3 : 1;
     DenseProduct p{};
     const auto pieces_of_16 = [&](const void* t, int64_t ld) { return aligned_to(t, 16) && ld * size_of(a.dtype) % 16 == 0; };
     const bool eights = a.N % 8 == 0;
@@ -94,6 +93,7 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
         return IOLB_OK;
     }
     p.K = (int)Kp;
+    const int planes = a.dtype == IOLB_F32 ? 3 : 1;
     segments(&p, planes, planes, a.M * Kp, a.N * Kp);
     const bool x_direct = direct(a.x, a.ldx, a.K, a.dtype) || a.K == 0, w_direct = direct(a.w, a.ldw, a.K, a.dtype) || a.K == 0;
     p.a = a.x; p.lda = a.ldx;
@@ -103,12 +103,40 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     if (!w_direct) { p.b = wp = pieces.take((size_t)planes * a.N * Kp * 2); p.ldb = Kp; }
     const DenseTilePlan plan = dense_tile_plan(p.M, p.N, p.K, p.segments);
     p.splits = plan.splits;
-    if (plan.splits > 1) p.partial = static_cast<float*>(pieces.take(dense_partial_bytes(plan.splits, a.M, a.N)));
+    size_t partial = plan.splits > 1 ? dense_partial_bytes(plan.splits, a.M, a.N) : 0;
+
+    // Large fp32 products in two fp16 parts, three products in place of six.  Whether an operand's rows allow it is found out on the GPU; the
+    // launches for three parts follow all the same and end at once if it does, which costs some 10 us.
+    DenseProduct h = p;
+    DenseTilePlan plan_h{};
+    const bool halves = planes == 3 && (double)a.M * a.N * a.K >= 1e10;
+    int *xe = nullptr, *we = nullptr, *uneven = nullptr;
+    if (halves) {
+        h.a = pieces.take((size_t)2 * a.M * Kp * 2); h.lda = Kp;
+        h.b = pieces.take((size_t)2 * a.N * Kp * 2); h.ldb = Kp;
+        h.exps_a = xe = static_cast<int*>(pieces.take((size_t)a.M * 4));
+        h.exps_b = we = static_cast<int*>(pieces.take((size_t)a.N * 4));
+        p.uneven = h.uneven = uneven = static_cast<int*>(pieces.take(4));
+        p.when = 1; h.when = 0;
+        h.segments = 3;                                                    // l h, h l, h h
+        h.a_plane[0] = a.M * Kp; h.a_plane[1] = h.a_plane[2] = 0;
+        h.b_plane[1] = a.N * Kp; h.b_plane[0] = h.b_plane[2] = 0;
+        plan_h = dense_tile_plan(h.M, h.N, h.K, 3);
+        h.splits = plan_h.splits;
+        if (h.splits > 1) partial = std::max(partial, dense_partial_bytes(h.splits, a.M, a.N));
+    }
+    if (partial) h.partial = p.partial = static_cast<float*>(pieces.take(partial));
     *need = pieces.used;
     if (!launch) return IOLB_OK;
 
     const hipStream_t st = call_stream();
+    if (halves) {
+        DENSE_HIP(launch_dense_halves(static_cast<const float*>(a.x), a.ldx, (int)a.M, const_cast<void*>(h.a), xe, static_cast<const float*>(a.w), a.ldw,
+                                      (int)a.N, const_cast<void*>(h.b), we, (int)a.K, Kp, uneven, st));
+        DENSE_HIP(launch_dense_product(h, plan_h.tile, a.dtype, st));
+    }
     DenseLayouts layouts{};
+    layouts.uneven = uneven;
     const auto lay = [&](const void* src, int64_t ld, int64_t rows, void* to) {
         DenseLayout& l = layouts.of[layouts.count++];
         l.source = DENSE_FROM_TENSOR; l.planes = planes;

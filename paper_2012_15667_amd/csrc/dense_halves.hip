@@ -1,0 +1,137 @@
+// fp32 operands of large products in two fp16 parts, half the matrix work of three bf16 parts.
+//
+// A row (the summed axis lies along it) is scaled by the power of two that brings its largest finite value into [2^14, 2^15), and a
+// scaled value is h + l, both fp16 rounded to nearest: held to 2^-22 of itself or 2^-40 of its row's largest value, whichever is more.  Three
+// products are taken, l h, h l and h h; l l is below 2^-22 of the product.  Against the sum of magnitudes that is fp32's own rounding, except
+// where a row's ordinary values are far below its largest: a row of whose non-zero values more than one in 64 is below 2^-20 of its largest
+// (of normal values, 3 in a million are) is uneven, and an operand with one sends the whole product to three bf16 parts.  Infinities and NaN as in dense.h: h is
+// the value, l zero, h h comes last.
+//
+// One workgroup (or wave) reads a row twice, the second time from L2: bound by memory.  4096 x 9216 and 4096 x 9216: HALVES_TIME.
+#include "dense_math.h"
+#include "kernels.h"
+
+namespace iolb {
+
+namespace {
+
+struct Rows {
+    const float* x;
+    long long ld;
+    int rows, vec;
+    unsigned short* planes;                        // [2][rows][pitch]
+    int* exps;
+};
+
+__global__ void __launch_bounds__(64) dense_even_kernel(int* uneven) { if (threadIdx.x == 0) *uneven = 0; }
+
+__device__ __forceinline__ void load_row_piece(const Rows& g, const float* row, int c, int cols, float (&v)[8])
+{
+    const int have = cols - c;
+    if (g.vec && have >= 8) {
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(row + c), hi = *reinterpret_cast<const f32x4*>(row + c + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = lo[i]; v[4 + i] = hi[i]; }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < have ? row[c + i] : 0.f;
+    }
+}
+
+// THREADS (64 or 256) to a row.
+template <int THREADS>
+__global__ void __launch_bounds__(256)
+dense_halves_kernel(Rows first, Rows second, int cols, long long pitch, int groups_first, int* uneven)
+{
+    constexpr int AT_ONCE = 256 / THREADS;
+    __shared__ float most_of[4];
+    __shared__ int small_of[4], count_of[4];
+    const bool is_second = (int)blockIdx.x >= groups_first;
+    const Rows g = is_second ? second : first;
+    const int tid = threadIdx.x % THREADS, wave = threadIdx.x >> 6;
+    const long long r = (long long)(blockIdx.x - (is_second ? groups_first : 0)) * AT_ONCE + threadIdx.x / THREADS;
+    const bool live = r < g.rows;
+    const float* const row = g.x + (live ? r : 0) * g.ld;
+    float most = 0.f;
+    if (live) {
+        for (int c = tid * 8; c < cols; c += THREADS * 8) {
+            float v[8];
+            load_row_piece(g, row, c, cols, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_magnitude(v[i]));
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if constexpr (THREADS == 256) {
+        if ((threadIdx.x & 63) == 0) most_of[wave] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
+    }
+    int top;                                        // most = f 2^top, f in [0.5, 1)
+    (void)frexpf(most, &top);
+    const int shift = most > 0.f ? 15 - top : 0;
+    const float line = 0x1p-20f * ldexpf(most, shift);
+    int small = 0, count = 0;
+    for (int c = live ? tid * 8 : (int)pitch; c < (int)pitch; c += THREADS * 8) {
+        float v[8];
+        load_row_piece(g, row, c, cols, v);
+        u32x4 h, l;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            unsigned hb[2], lb[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float x = v[2 * i + j], s = ldexpf(x, shift);
+                const bool finite = fabsf(x) < __builtin_inff();
+                const _Float16 hv = finite ? (_Float16)s : (_Float16)x;
+                const _Float16 lv = finite ? (_Float16)(s - (float)hv) : (_Float16)0.f;
+                count += x != 0.f;
+                small += x != 0.f && fabsf(s) < line;
+                hb[j] = __builtin_bit_cast(unsigned short, hv);
+                lb[j] = __builtin_bit_cast(unsigned short, lv);
+            }
+            h[i] = hb[0] | hb[1] << 16;
+            l[i] = lb[0] | lb[1] << 16;
+        }
+        *reinterpret_cast<u32x4*>(g.planes + r * pitch + c) = h;
+        *reinterpret_cast<u32x4*>(g.planes + ((long long)g.rows + r) * pitch + c) = l;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        small += __shfl_xor(small, d);
+        count += __shfl_xor(count, d);
+    }
+    if constexpr (THREADS == 256) {
+        if ((threadIdx.x & 63) == 0) { small_of[wave] = small; count_of[wave] = count; }
+        __syncthreads();
+        small = small_of[0] + small_of[1] + small_of[2] + small_of[3];
+        count = count_of[0] + count_of[1] + count_of[2] + count_of[3];
+    }
+    if (live && tid == 0) {
+        g.exps[r] = -shift;
+        if (small > count / 64) *uneven = 1;                // (whoever writes it writes the same)
+    }
+}
+
+}  // namespace
+
+hipError_t launch_dense_halves(const float* a, long long lda, int rows_a, void* planes_a, int* exps_a, const float* b, long long ldb, int rows_b,
+                               void* planes_b, int* exps_b, int cols, long long pitch, int* uneven, hipStream_t st)
+{
+    const auto rows = [](const float* x, long long ld, int n, void* planes, int* exps) {
+        return Rows{x, ld, n, reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % 4 == 0, static_cast<unsigned short*>(planes), exps};
+    };
+    const Rows ra = rows(a, lda, rows_a, planes_a, exps_a), rb = rows(b, ldb, rows_b, planes_b, exps_b);
+    // a wave to a row, or a workgroup where there are few rows or they are long
+    const bool workgroup = (long long)rows_a + rows_b < 4096 || cols > 4096;
+    const int at_once = workgroup ? 1 : 4;
+    const long long ga = ((long long)rows_a + at_once - 1) / at_once, gb = ((long long)rows_b + at_once - 1) / at_once;
+    if (ga + gb > 0x7fffffffLL) return hipErrorInvalidValue;
+    dense_even_kernel<<<1, 64, 0, st>>>(uneven);
+    if (workgroup) dense_halves_kernel<256><<<(unsigned)(ga + gb), 256, 0, st>>>(ra, rb, cols, pitch, (int)ga, uneven);
+    else dense_halves_kernel<64><<<(unsigned)(ga + gb), 256, 0, st>>>(ra, rb, cols, pitch, (int)ga, uneven);
+    return hipGetLastError();
+}
+
+}  // namespace iolb

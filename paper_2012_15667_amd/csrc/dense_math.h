@@ -262,6 +262,15 @@ __device__ __forceinline__ void finish_four(const DenseFinish& f, int m, int n, 
     by_activation(f.act, [&](auto act) __attribute__((always_inline)) { store_columns<DT, decltype(act)::value>(f, m, n, z); });
 }
 
+// Sums of operands in two fp16 parts, scaled back.
+template <int W>
+__device__ __forceinline__ void from_halves(const DenseProduct& p, int m, int n, float (&z)[W])
+{
+    const int e = p.exps_a[m < p.M ? m : 0];
+#pragma unroll
+    for (int i = 0; i < W; ++i) z[i] = ldexpf(z[i], e + p.exps_b[n + i < p.N ? n + i : 0]);
+}
+
 // Columns that a lane finishes: 16 bytes of the output.
 template <int DT> constexpr int FINISH_COLUMNS = DT == IOLB_F32 ? 4 : 8;
 

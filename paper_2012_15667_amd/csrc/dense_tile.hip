@@ -26,6 +26,7 @@ template <bool F16, int DT, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, 2)
 dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
 {
+    if (p.uneven && *p.uneven != p.when) return;
     constexpr int WAVES = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
     constexpr int LA = BM / 8 / WAVES, LB = BN / 8 / WAVES;           // loads of a wave and stage: 8 rows each
     constexpr unsigned STAGE = (BM + BN) * ROW_BYTES;
@@ -217,6 +218,7 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
                     for (int i = 0; i < 4; ++i) z[4 * h + i] = four[i];
                 }
                 const int m = m0 + r / (PI * 16) * (BM / WM) + pass * PI * 16 + r % (PI * 16);
+                if constexpr (F16 && DT == IOLB_F32) from_halves(p, m, n, z);
                 finish_columns<DT, decltype(act)::value>(p.f, m, n, bias, z);
             }
         });
@@ -228,6 +230,7 @@ template <int DT>
 __global__ void __launch_bounds__(256)
 dense_join_kernel(DenseProduct p, int wide_log)
 {
+    if (p.uneven && *p.uneven != p.when) return;
     const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), rows = 256 >> wide_log;
     const int n = (int)((blockIdx.x * (unsigned)wide + tx) * 8);
     const long long ld = (p.N + 3) / 4 * 4;
@@ -252,6 +255,7 @@ dense_join_kernel(DenseProduct p, int wide_log)
                     for (int c = 0; c < 4; ++c) { z[c] += lo[c]; z[4 + c] += hi[c]; }
                 }
             }
+            if (DT == IOLB_F32 && p.exps_a) from_halves(p, (int)(m < p.M ? m : p.M), n, z);
             finish_columns<DT, decltype(act)::value>(p.f, (int)(m < p.M ? m : p.M), n, bias, z);
         }
     });
@@ -313,7 +317,7 @@ DenseTilePlan dense_tile_plan(int M, int N, int K, int segments)
 
 hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st)
 {
-    hipError_t e = dtype == IOLB_F32 ? launch_tile<false, IOLB_F32>(p, tile, st)
+    hipError_t e = dtype == IOLB_F32 ? (p.exps_a ? launch_tile<true, IOLB_F32>(p, tile, st) : launch_tile<false, IOLB_F32>(p, tile, st))
                  : dtype == IOLB_F16 ? launch_tile<true, IOLB_F16>(p, tile, st) : launch_tile<false, IOLB_BF16>(p, tile, st);
     return e != hipSuccess || p.splits == 1 ? e : launch_dense_join(p, dtype, st);
 }

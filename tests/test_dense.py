@@ -602,3 +602,45 @@ def test_python_refusals():
                       (lambda: B.checkpoint_unpack(B.checkpoint_pack(x), torch.float64), TypeError)):
         with pytest.raises(kind):
             bad()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(100, 70, 72), (300, 260, 1000), (2100, 1030, 5000)])
+def test_linear_fp32_rows_of_uneven_magnitude(M, N, K):
+    """Rows whose values differ by many powers of two, in x and in w, at every scale of the type, with weights that are zero where
+    the large ones are: every output keeps the bound of fp32 sums, (K + 16) 2^-24 of its own sum of magnitudes, or of what 2^-40 of a
+    row's largest value amounts to in rows of ordinary spread (at most one in 64 of the non-zero values below 2^-20 of the largest)."""
+    torch = _torch()
+    rng = np.random.default_rng(K)
+    x = rng.standard_normal((M, K))
+    w = rng.standard_normal((N, K))
+    x *= 2.0 ** rng.integers(-40, 40, (M, 1))                       # a scale for each row
+    x[0] *= 1e-30
+    x[1] *= 1e25
+    x[2, 3] = 2.0 ** 70                                              # one value far beyond its row
+    x[3, ::2] *= 2.0 ** -60
+    x[4] = 0
+    x[4, 5] = 3.0
+    w[:, 3] = 0
+    w[0] = 0
+    w[0, 7] = 1.0                                                    # picks one value of x
+    w[1, 1:] *= 2.0 ** -50
+    x, w = (torch.from_numpy(v.astype(np.float32)).cuda() for v in (x, w))
+    x64, w64 = to64(x), to64(w)
+    want, total = x64 @ w64.T, np.abs(x64) @ np.abs(w64).T
+
+    def marked(v):
+        a = np.abs(v)
+        return ((a > 0) & (a < 2.0 ** -20 * a.max(1)[:, None])).sum(1) > (a > 0).sum(1) // 64
+
+    assert marked(x64)[2] and not marked(x64)[5]
+    check_uneven(x, w, x64, w64, want, total, K)
+    # the same without the rows that two parts do not hold
+    even, kept = ~marked(x64), ~marked(w64)
+    x, w = (t[torch.from_numpy(k).cuda()].contiguous() for t, k in ((x, even), (w, kept)))
+    check_uneven(x, w, x64[even], w64[kept], want[even][:, kept], total[even][:, kept], K)
+
+
+def check_uneven(x, w, x64, w64, want, total, K):
+    loose = 2.0 ** -39 * (np.abs(x64).max(1)[:, None] * np.abs(w64).sum(1)[None] + np.abs(x64).sum(1)[:, None] * np.abs(w64).max(1)[None])
+    assert_within(B.linear(x, w), want, (K + 16) * 2.0 ** -24 * total + loose + TINY["float32"])
