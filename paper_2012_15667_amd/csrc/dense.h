@@ -64,13 +64,25 @@ hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipS
 // The same for few rows of A: both operands as the caller holds them (fp32 too: taken apart in the kernels), any K, bound by reading
 // B.  across: B is [K][N], summed along its rows.  K is shared by workgroups, at most `splits` to a sum.  Sums go to `partial` if join is
 // set (always with splits > 1 or a checkpoint).
-constexpr int DENSE_ROWS_MOST = 64;
+constexpr int DENSE_FEW = 16;               // rows of the kernel for the fewest
+// Whether a product with M rows and an N x K weight runs on them, or on the product kernel with its operands laid out.  fp32: the layout of the
+// weights in parts costs more than all of the product up to some hundred rows (4096 x 4096, us: 64 rows 24 against 69, 128 36 / 78, 256 62 / 97;
+// 512 x 512, 256 rows 12 / 16).  16-bit types: the product kernel reads weights in place (4096 x 4096, 20 rows 15.7 against 12.6), but across
+// they would be transposed: 4096 x 4096, 64 rows 15.5 against 28, 128 24.8 / 31, 256 40 / 37; 1000 x 2048, 20 rows 13.1 / 13.2, 64 17.9 / 14.2;
+// 1001 x 1003, whose rows are not aligned, 20 rows 16.6 / 13.2.
+inline bool dense_rows_wanted(long long M, long long N, long long K, int dtype, bool across, bool aligned)
+{
+    if (dtype == IOLB_F32) return M <= 512;
+    if (!across) return M <= DENSE_FEW;
+    return aligned && (M <= 32 || (M <= 128 && N * K >= (1 << 22)));
+}
+constexpr int DENSE_OUTER_MOST = 64;
 constexpr int DENSE_ROWS_STEP = 64;         // k of a step
 struct DenseRowsPlan { int splits, per; bool join; int block_columns; };
 DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint);
 hipError_t launch_dense_rows(const DenseProduct& p, bool across, bool join, int dtype, hipStream_t st);
 hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st);
-// The same for a short summed axis, 0 < K <= DENSE_ROWS_MOST: operands in planes, `plane_a` and `plane_b` elements apart; no bias, activation,
+// The same for a short summed axis, 0 < K <= DENSE_OUTER_MOST: operands in planes, `plane_a` and `plane_b` elements apart; no bias, activation,
 // residual or checkpoint.  At most DENSE_OUTER_ROWS rows of A.
 constexpr long long DENSE_OUTER_ROWS = 65535 * 128LL;
 hipError_t launch_dense_outer(const DenseProduct& p, int planes_b, long long plane_a, long long plane_b, int dtype, hipStream_t st);

@@ -81,7 +81,7 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
                       eights && aligned_to(a.bias, 16), eights && pieces_of_16(a.residual, a.M == 1 ? 8 : a.ldr),
                       eights && pieces_of_16(a.y, a.M == 1 ? 8 : a.ldy), eights && aligned_to(a.zq, 8)};
     p.M = (int)a.M; p.N = (int)a.N;
-    if (a.M <= DENSE_ROWS_MOST) {
+    if (dense_rows_wanted(a.M, a.N, a.K, a.dtype, false, true)) {
         p.a = a.x; p.lda = a.ldx; p.vec_a = a.M == 1 ? aligned_to(a.x, 16) : pieces_of_16(a.x, a.ldx);
         p.b = a.w; p.ldb = a.ldw; p.vec_b = a.N == 1 ? aligned_to(a.w, 16) : pieces_of_16(a.w, a.ldw);
         p.K = (int)a.K;
@@ -177,7 +177,8 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     // the input's checkpoint is exact in one bf16 part, unless a smooth activation has to be taken of it
     const int planes_x = planes == 3 && a.x_act != IOLB_ACT_NONE && a.x_act != IOLB_ACT_RELU ? 3 : 1;
     const int64_t Mp = up8(a.M), Np = up8(a.N);
-    const bool want_dx = a.dx && a.M > 0 && a.K > 0, few = a.M <= DENSE_ROWS_MOST, want_dw = a.dw && a.N > 0 && a.K > 0;
+    const bool vec_w = a.K % 4 == 0 && aligned_to(a.w, 4 * size_of(a.dtype)) && (a.N == 1 || a.ldw % 4 == 0);
+    const bool want_dx = a.dx && a.M > 0 && a.K > 0, few = dense_rows_wanted(a.M, a.N, a.K, a.dtype, true, vec_w), want_dw = a.dw && a.N > 0 && a.K > 0;
     const bool has_z = a.act != IOLB_ACT_NONE;
 
     // dz = dy act'(z) along the rows for dx (dy itself where that is it), transposed for dW
@@ -212,7 +213,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     if (want_dx && few) {
         px.M = (int)a.M; px.N = (int)a.K; px.K = (int)a.N;
         px.a = dz; px.lda = ld_dz; px.vec_a = aligned_to(dz, 16) && (a.M == 1 || ld_dz * size_of(a.dtype) % 16 == 0);
-        px.b = a.w; px.ldb = a.ldw; px.vec_b = a.K % 4 == 0 && aligned_to(a.w, 4 * size_of(a.dtype)) && (a.N == 1 || a.ldw % 4 == 0);
+        px.b = a.w; px.ldb = a.ldw; px.vec_b = vec_w;
         rows_x = dense_rows_plan(px.M, px.N, px.K, a.dtype, true, false);
         px.splits = rows_x.splits; px.per = rows_x.per; px.block_columns = rows_x.block_columns;
         if (rows_x.join) partial_x = dense_partial_bytes(px.splits, px.M, px.N);
@@ -228,7 +229,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         pw.M = (int)a.N; pw.N = (int)a.K; pw.K = (int)Mp;
         pw.a = dzt; pw.lda = Mp; pw.b = xt; pw.ldb = Mp;
         segments(&pw, planes, planes_x, a.N * Mp, a.K * Mp);
-        outer = few && a.M > 0 && a.N <= DENSE_OUTER_ROWS;
+        outer = a.M > 0 && a.M <= DENSE_OUTER_MOST && a.N <= DENSE_OUTER_ROWS;
         plan_w = dense_tile_plan(pw.M, pw.N, pw.K, pw.segments);
         pw.splits = outer ? 1 : plan_w.splits;
         if (pw.splits > 1) partial_w = dense_partial_bytes(pw.splits, pw.M, pw.N);

@@ -251,13 +251,12 @@ __device__ __forceinline__ void store_whole(const DenseFinish& f, int m, int n, 
 
 // Four columns without a checkpoint, for a wave that holds them in one lane.
 template <int DT>
-__device__ __forceinline__ void finish_four(const DenseFinish& f, int m, int n, const f32x4& sum)
+__device__ __forceinline__ void finish_four(const DenseFinish& f, int m, int n, const float (&bias)[4], const f32x4& sum)
 {
     if (m >= f.M || n >= f.N) return;
-    float z[4], b[4];
-    load_bias<DT>(f, n, b);
+    float z[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) z[i] = sum[i] + b[i];
+    for (int i = 0; i < 4; ++i) z[i] = sum[i] + bias[i];
     if (f.residual && f.first) add_residual<DT>(f, m, n, z);
     by_activation(f.act, [&](auto act) __attribute__((always_inline)) { store_columns<DT, decltype(act)::value>(f, m, n, z); });
 }

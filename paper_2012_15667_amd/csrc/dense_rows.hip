@@ -157,6 +157,8 @@ dense_few_kernel(DenseProduct p, int join)
     const T* const a = static_cast<const T*>(p.a) + (l16 < p.M ? l16 : p.M - 1) * p.lda;
 
     const int whole_to = whole_steps(p, s0, s1);
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};                              // (on its way while the products are taken)
+    if (!join && n0 + 4 * grp < p.N) load_bias<DT>(p.f, n0 + 4 * grp, bias);
     // the sums of steps from ... to - 1, of which this wave has every eighth
     auto range = [&](auto mode, auto whole, int from, int to, f32x4 (&c)[2]) __attribute__((always_inline)) {
         constexpr int MODE = decltype(mode)::value;
@@ -216,11 +218,11 @@ dense_few_kernel(DenseProduct p, int join)
     if (join) {
         keep_partial(p, blockIdx.y, m, n, c);
     } else {
-        finish_four<DT>(p.f, m, n, c);
+        finish_four<DT>(p.f, m, n, bias, c);
     }
 }
 
-// ---- up to 64 rows: A through LDS, each wave its own columns of C -------------------------------------------------
+// ---- more rows: A through LDS, 64 rows at a time, each wave its own columns of C -------------------------------------------------
 // A step is 64 k.  A's rows are cut into parts once for the workgroup and lie in two LDS buffers in turn; the loads of A two steps
 // ahead and of B one or two are kept in registers.  Along (not across): a wave takes sixteen rows of B.  Across: 64 columns of
 // B, four neighbours a lane, so that the eight rows a lane reads are its operand's eight k for each of the four without
@@ -231,7 +233,7 @@ constexpr int rows_columns(bool across) { return across ? 4 * 16 * NC : 128; }  
 // workgroups on a compute unit, by their registers: of 16 rows or less, of 17 to 32, of more
 constexpr int rows_resident(int dtype, int tiles, bool across)
 {
-    return across ? (dtype == IOLB_F32 ? (tiles > 2 ? 2 : 3) : (tiles > 2 ? 3 : 4)) : (dtype == IOLB_F32 ? (tiles > 2 ? 1 : 2) : 2);
+    return across ? (dtype == IOLB_F32 ? (tiles > 2 ? 2 : 3) : (tiles > 2 ? 3 : 4)) : (tiles > 2 ? 1 : 2);
 }
 
 template <int DT, int MT, bool ACROSS>
@@ -249,6 +251,7 @@ dense_rows_kernel(DenseProduct p, int join)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const T* const a = static_cast<const T*>(p.a);
     const T* const b = static_cast<const T*>(p.b);
+    const int m0 = blockIdx.y * ROWS;
     const long long steps = p.K > 0 ? (p.K + STEP - 1) / STEP : 1, total = steps * ((p.N + WAVES * COLS - 1) / (WAVES * COLS));
     const long long end = (blockIdx.x + 1LL) * p.per < total ? (blockIdx.x + 1LL) * p.per : total;
     // the workgroup's run of steps, block by block
@@ -306,7 +309,7 @@ dense_rows_kernel(DenseProduct p, int join)
         auto load_a = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int item = tid + i * THREADS, row = item >> 3, piece = item & 7, g = piece & 3;
+                const int item = tid + i * THREADS, row = m0 + (item >> 3), piece = item & 7, g = piece & 3;
                 const T* const at = a + (row < p.M ? row : p.M - 1) * p.lda + s * STEP + 32 * (piece >> 2);
                 const int have = p.K - s * STEP - 32 * (piece >> 2);
                 if constexpr (ACROSS && DT == IOLB_F32) {
@@ -430,7 +433,7 @@ dense_rows_kernel(DenseProduct p, int join)
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int m = 16 * t + l16;
+        const int m = m0 + 16 * t + l16;
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
             // across: column NC (4 grp + r) + j of the wave's is value r of fragment j
@@ -443,7 +446,9 @@ dense_rows_kernel(DenseProduct p, int join)
             if (join) {
                 keep_partial(p, (int)(blockIdx.x - block * steps / p.per), m, n, c);
             } else {
-                finish_four<DT>(p.f, m, n, c);
+                float bias[4] = {0.f, 0.f, 0.f, 0.f};
+                if (n < p.N) load_bias<DT>(p.f, n, bias);
+                finish_four<DT>(p.f, m, n, bias, c);
             }
         }
     }
@@ -567,26 +572,26 @@ hipError_t launch_outer(DenseProduct p, long long plane_a, long long plane_b, hi
     return hipGetLastError();
 }
 
-constexpr int FEW = 16;                                // rows of the first kernel
-
 template <int DT>
 hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
 {
-    if (!across && p.M <= FEW) {
+    if (!across && p.M <= DENSE_FEW) {
         dense_few_kernel<DT><<<dim3((p.N + 15) / 16, p.splits), 512, 0, st>>>(p, join);
         return hipGetLastError();
     }
     const int mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
     const int cols = rows_columns(across), threads = 64 * rows_waves(across);
     const long long total = (p.K > 0 ? (p.K + STEP - 1LL) / STEP : 1) * ((p.N + cols - 1LL) / cols);       // (a sum over nothing: one empty step)
-    const unsigned grid = (unsigned)((total + p.per - 1) / p.per);
+    const dim3 grid((unsigned)((total + p.per - 1) / p.per), (p.M + 16 * mt - 1) / (16 * mt));
     if (across) {
         if (mt == 1) dense_rows_kernel<DT, 1, true><<<grid, threads, 0, st>>>(p, join);
         else if (mt == 2) dense_rows_kernel<DT, 2, true><<<grid, threads, 0, st>>>(p, join);
         else dense_rows_kernel<DT, 4, true><<<grid, threads, 0, st>>>(p, join);
-    } else {
+    } else if constexpr (DT == IOLB_F32) {
         if (mt <= 2) dense_rows_kernel<DT, 2, false><<<grid, threads, 0, st>>>(p, join);
         else dense_rows_kernel<DT, 4, false><<<grid, threads, 0, st>>>(p, join);
+    } else {
+        return hipErrorInvalidValue;                  // 16-bit types, along: up to DENSE_FEW rows only
     }
     return hipGetLastError();
 }
@@ -600,12 +605,12 @@ hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
 // adds the partial sums, which go through memory.  Fitted to a sweep of 22 products of 1 to 64 rows and 0.5 M to 103 M weights, 1 to 64 shares.
 DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint)
 {
-    const bool few = !across && M <= FEW, wide = dtype == IOLB_F32;
+    const bool few = !across && M <= DENSE_FEW, wide = dtype == IOLB_F32;
     const int tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    const double alone = few ? (wide ? 1500 : 800) : !across ? (wide ? 1000 : 840) : !wide ? 550 : tiles == 1 ? 1050 : tiles == 2 ? 1350 : 1900;
+    const double alone = few ? (wide ? 1500 : 800) : !across ? 1000 : !wide ? 550 : tiles == 1 ? 1050 : tiles == 2 ? 1350 : 1900;
     const long long steps = K > 0 ? (K + STEP - 1) / STEP : 1, cols = few ? 16 : rows_columns(across);
     const long long blocks = (N + cols - 1) / cols, waves = few ? 8 : 1;           // (few: the waves share the steps)
-    const long long capacity = 256 * (few ? 2 : rows_resident(dtype, tiles, across));
+    const long long capacity = 256 * (few ? 2 : rows_resident(dtype, tiles, across)) / ((M + 63) / 64);   // (each 64 rows have workgroups of their own)
     const double step_ns = (double)cols * waves * STEP * (wide ? 4 : 2) / 4900;                        // of one workgroup
     DenseRowsPlan best{1, 0, checkpoint, 0};
     double least = -1;
