@@ -31,7 +31,6 @@ struct DenseFinish {
     long long ldr, ldy;
     int M, N;
     int act, first;                         // first: the residual is added before the activation
-    int vec_bias, vec_res, vec_y, vec_q;    // eight neighbouring columns may be read / written as whole 16- or 8-byte pieces
 };
 
 // C[m][n] = sum over segments and k of A[m][k] B[n][k]; both operands contiguous along k, 16-byte aligned rows.
@@ -49,7 +48,6 @@ struct DenseProduct {
     const int *exps_a, *exps_b;             // fp32 operands in two fp16 parts: the exponents of their rows (null otherwise)
     const int* uneven;                      // not null: the launch does nothing unless *uneven is `when`
     int when;
-    int vec_a, vec_b;                       // kernels for few rows: whole 16-byte pieces of the operand may be read
     DenseFinish f;
 };
 
@@ -68,13 +66,12 @@ constexpr int DENSE_FEW = 16;               // rows of the kernel for the fewest
 // Whether a product with M rows and an N x K weight runs on them, or on the product kernel with its operands laid out.  fp32: the layout of the
 // weights in parts costs more than all of the product up to some hundred rows (4096 x 4096, us: 64 rows 24 against 69, 128 36 / 78, 256 62 / 97;
 // 512 x 512, 256 rows 12 / 16).  16-bit types: the product kernel reads weights in place (4096 x 4096, 20 rows 15.7 against 12.6), but across
-// they would be transposed: 4096 x 4096, 64 rows 15.5 against 28, 128 24.8 / 31, 256 40 / 37; 1000 x 2048, 20 rows 13.1 / 13.2, 64 17.9 / 14.2;
-// 1001 x 1003, whose rows are not aligned, 20 rows 16.6 / 13.2.
-inline bool dense_rows_wanted(long long M, long long N, long long K, int dtype, bool across, bool aligned)
+// they would be transposed: 4096 x 4096, 64 rows 15.5 against 28, 128 24.8 / 31, 256 40 / 37; 1000 x 2048, 20 rows 13.1 / 13.2, 64 17.9 / 14.2.
+inline bool dense_rows_wanted(long long M, long long N, long long K, int dtype, bool across)
 {
     if (dtype == IOLB_F32) return M <= 512;
     if (!across) return M <= DENSE_FEW;
-    return aligned && (M <= 32 || (M <= 128 && N * K >= (1 << 22)));
+    return M <= 32 || (M <= 128 && N * K >= (1 << 22));
 }
 constexpr int DENSE_OUTER_MOST = 64;
 constexpr int DENSE_ROWS_STEP = 64;         // k of a step
@@ -96,10 +93,8 @@ struct DenseLayout {
     int rows, cols;
     const void* src;                        // tensor: v = src;  gradient: v = src * act'(checkpoint), or src where q is null
     long long ld;
-    int vec_src;                            // eight neighbouring columns may be read at once
     const int8_t* q;                        // checkpoint: v = act(value)
     const uint8_t* e;
-    int vec_q;
     int act;
     void* rowmajor;                         // [planes][rows][ld_rm], or null; columns up to the next multiple of 8 are zero
     long long ld_rm;

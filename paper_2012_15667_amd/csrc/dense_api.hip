@@ -75,15 +75,11 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     Pieces pieces{static_cast<char*>(ws)};
     const int64_t Kp = up8(a.K);
     DenseProduct p{};
-    const auto pieces_of_16 = [&](const void* t, int64_t ld) { return aligned_to(t, 16) && ld * size_of(a.dtype) % 16 == 0; };
-    const bool eights = a.N % 8 == 0;
-    p.f = DenseFinish{a.bias, a.residual, a.y, a.zq, a.ze, a.ldr, a.ldy, (int)a.M, (int)a.N, a.act, a.residual_first != 0,
-                      eights && aligned_to(a.bias, 16), eights && pieces_of_16(a.residual, a.M == 1 ? 8 : a.ldr),
-                      eights && pieces_of_16(a.y, a.M == 1 ? 8 : a.ldy), eights && aligned_to(a.zq, 8)};
+    p.f = DenseFinish{a.bias, a.residual, a.y, a.zq, a.ze, a.ldr, a.ldy, (int)a.M, (int)a.N, a.act, a.residual_first != 0};
     p.M = (int)a.M; p.N = (int)a.N;
-    if (dense_rows_wanted(a.M, a.N, a.K, a.dtype, false, true)) {
-        p.a = a.x; p.lda = a.ldx; p.vec_a = a.M == 1 ? aligned_to(a.x, 16) : pieces_of_16(a.x, a.ldx);
-        p.b = a.w; p.ldb = a.ldw; p.vec_b = a.N == 1 ? aligned_to(a.w, 16) : pieces_of_16(a.w, a.ldw);
+    if (dense_rows_wanted(a.M, a.N, a.K, a.dtype, false)) {
+        p.a = a.x; p.lda = a.ldx;
+        p.b = a.w; p.ldb = a.ldw;
         p.K = (int)a.K;
         const DenseRowsPlan plan = dense_rows_plan(p.M, p.N, p.K, a.dtype, false, a.zq != nullptr);
         p.splits = plan.splits; p.per = plan.per; p.block_columns = plan.block_columns;
@@ -141,7 +137,7 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
         DenseLayout& l = layouts.of[layouts.count++];
         l.source = DENSE_FROM_TENSOR; l.planes = planes;
         l.rows = (int)rows; l.cols = (int)a.K;
-        l.src = src; l.ld = ld; l.vec_src = pieces_of_16(src, ld);
+        l.src = src; l.ld = ld;
         l.rowmajor = to; l.ld_rm = Kp;
     };
     if (!x_direct) lay(a.x, a.ldx, a.M, xp);
@@ -177,8 +173,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     // the input's checkpoint is exact in one bf16 part, unless a smooth activation has to be taken of it
     const int planes_x = planes == 3 && a.x_act != IOLB_ACT_NONE && a.x_act != IOLB_ACT_RELU ? 3 : 1;
     const int64_t Mp = up8(a.M), Np = up8(a.N);
-    const bool vec_w = a.K % 4 == 0 && aligned_to(a.w, 4 * size_of(a.dtype)) && (a.N == 1 || a.ldw % 4 == 0);
-    const bool want_dx = a.dx && a.M > 0 && a.K > 0, few = dense_rows_wanted(a.M, a.N, a.K, a.dtype, true, vec_w), want_dw = a.dw && a.N > 0 && a.K > 0;
+    const bool want_dx = a.dx && a.M > 0 && a.K > 0, few = dense_rows_wanted(a.M, a.N, a.K, a.dtype, true), want_dw = a.dw && a.N > 0 && a.K > 0;
     const bool has_z = a.act != IOLB_ACT_NONE;
 
     // dz = dy act'(z) along the rows for dx (dy itself where that is it), transposed for dW
@@ -212,8 +207,8 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     bool outer = false;
     if (want_dx && few) {
         px.M = (int)a.M; px.N = (int)a.K; px.K = (int)a.N;
-        px.a = dz; px.lda = ld_dz; px.vec_a = aligned_to(dz, 16) && (a.M == 1 || ld_dz * size_of(a.dtype) % 16 == 0);
-        px.b = a.w; px.ldb = a.ldw; px.vec_b = vec_w;
+        px.a = dz; px.lda = ld_dz;
+        px.b = a.w; px.ldb = a.ldw;
         rows_x = dense_rows_plan(px.M, px.N, px.K, a.dtype, true, false);
         px.splits = rows_x.splits; px.per = rows_x.per; px.block_columns = rows_x.block_columns;
         if (rows_x.join) partial_x = dense_partial_bytes(px.splits, px.M, px.N);
@@ -246,9 +241,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         l.source = DENSE_FROM_GRADIENT; l.planes = planes;
         l.rows = (int)a.M; l.cols = (int)a.N;
         l.src = a.dy; l.ld = a.ldy;
-        l.vec_src = a.ldy * size_of(a.dtype) % 16 == 0 && aligned_to(a.dy, 16);
         l.q = has_z ? a.zq : nullptr; l.e = a.ze; l.act = a.act;
-        l.vec_q = a.N % 8 == 0 && aligned_to(a.zq, 8);
         l.rowmajor = dz_to; l.ld_rm = Np;
         l.transposed = dzt; l.ld_tr = Mp;
         l.copy = dz_copy;
@@ -259,7 +252,6 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         l.source = DENSE_FROM_TENSOR; l.planes = planes;
         l.rows = (int)a.N; l.cols = (int)a.K;
         l.src = a.w; l.ld = a.ldw;
-        l.vec_src = a.ldw * size_of(a.dtype) % 16 == 0 && aligned_to(a.w, 16);
         l.transposed = wt; l.ld_tr = Np;
     }
     if (want_dw && a.M > 0) {
@@ -267,7 +259,6 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         l.source = DENSE_FROM_CHECKPOINT; l.planes = planes_x;
         l.rows = (int)a.M; l.cols = (int)a.K;
         l.q = a.xq; l.e = a.xe; l.act = a.x_act;
-        l.vec_q = a.K % 8 == 0 && aligned_to(a.xq, 8);
         l.transposed = xt; l.ld_tr = Mp;
     }
     if (layouts.count) DENSE_HIP(launch_dense_layouts(a.dtype, layouts, st));
@@ -276,7 +267,6 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         DenseFinish f{};
         f.y = out; f.ldy = n; f.M = (int)m; f.N = (int)n;
         f.act = IOLB_ACT_NONE;
-        f.vec_y = n % 8 == 0 && aligned_to(out, 16);
         return f;
     };
     if (want_dx && few) {

@@ -18,25 +18,12 @@ namespace {
 struct Rows {
     const float* x;
     long long ld;
-    int rows, vec;
+    int rows;
     unsigned short* planes;                        // [2][rows][pitch]
     int* exps;
 };
 
 __global__ void __launch_bounds__(64) dense_even_kernel(int* uneven) { if (threadIdx.x == 0) *uneven = 0; }
-
-__device__ __forceinline__ void load_row_piece(const Rows& g, const float* row, int c, int cols, float (&v)[8])
-{
-    const int have = cols - c;
-    if (g.vec && have >= 8) {
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(row + c), hi = *reinterpret_cast<const f32x4*>(row + c + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = lo[i]; v[4 + i] = hi[i]; }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < have ? row[c + i] : 0.f;
-    }
-}
 
 // THREADS (64 or 256) to a row.
 template <int THREADS>
@@ -56,7 +43,7 @@ dense_halves_kernel(Rows first, Rows second, int cols, long long pitch, int grou
     if (live) {
         for (int c = tid * 8; c < cols; c += THREADS * 8) {
             float v[8];
-            load_row_piece(g, row, c, cols, v);
+            load_columns(row + c, cols - c, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_magnitude(v[i]));
         }
@@ -75,7 +62,7 @@ dense_halves_kernel(Rows first, Rows second, int cols, long long pitch, int grou
     int small = 0, count = 0;
     for (int c = live ? tid * 8 : (int)pitch; c < (int)pitch; c += THREADS * 8) {
         float v[8];
-        load_row_piece(g, row, c, cols, v);
+        load_columns(row + c, cols - c, v);
         u32x4 h, l;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -120,7 +107,7 @@ hipError_t launch_dense_halves(const float* a, long long lda, int rows_a, void* 
                                void* planes_b, int* exps_b, int cols, long long pitch, int* uneven, hipStream_t st)
 {
     const auto rows = [](const float* x, long long ld, int n, void* planes, int* exps) {
-        return Rows{x, ld, n, reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % 4 == 0, static_cast<unsigned short*>(planes), exps};
+        return Rows{x, ld, n, static_cast<unsigned short*>(planes), exps};
     };
     const Rows ra = rows(a, lda, rows_a, planes_a, exps_a), rb = rows(b, ldb, rows_b, planes_b, exps_b);
     // a wave to a row, or a workgroup where there are few rows or they are long

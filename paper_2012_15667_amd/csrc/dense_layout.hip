@@ -13,23 +13,26 @@ namespace {
 constexpr int PITCH = 72;                          // 16-bit values of a transposed row in LDS: 144 bytes
 
 template <class T>
-__device__ __forceinline__ void load_eight(const T* p, int have, bool vec, float (&v)[8])
+__device__ __forceinline__ void store_eight(T* p, int have, const float (&v)[8])
 {
-    if (vec && have >= 8) {
-        typedef T T8 __attribute__((ext_vector_type(8), aligned(16)));
-        const T8 t = *reinterpret_cast<const T8*>(p);
+    typename Piece<T, 8>::type t;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+    for (int i = 0; i < 8; ++i) t[i] = (T)v[i];
+    if (have >= 8) {
+        *reinterpret_cast<typename Piece<T, 8>::type*>(p) = t;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < have ? (float)p[i] : 0.f;
+        for (int i = 0; i < 8; ++i)
+            if (i < have) p[i] = t[i];
     }
 }
 
-__device__ __forceinline__ void load_checkpoint(const int8_t* p, float unit, int have, bool vec, float (&v)[8])
+typedef unsigned Codes __attribute__((ext_vector_type(2), aligned(1)));          // eight 8-bit codes, at any address
+
+__device__ __forceinline__ void load_checkpoint(const int8_t* p, float unit, int have, float (&v)[8])
 {
-    if (vec && have >= 8) {
-        const u32x2 t = *reinterpret_cast<const u32x2*>(p);
+    if (have >= 8) {
+        const Codes t = *reinterpret_cast<const Codes*>(p);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = ckpt_value((int)(t[i / 4] << (24 - 8 * (i % 4))) >> 24, unit);
     } else {
@@ -76,11 +79,11 @@ dense_layout_kernel(LayoutLaunch launch)
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         const bool live = r < g.rows && have > 0;
         if (live) {
-            if (g.source != DENSE_FROM_CHECKPOINT) load_eight(static_cast<const T*>(g.src) + r * g.ld + c, have, g.vec_src, v);
+            if (g.source != DENSE_FROM_CHECKPOINT) load_columns(static_cast<const T*>(g.src) + r * g.ld + c, have, v);
             if (g.q) {
                 float z[8];
                 const float unit = two_to((int)g.e[r * blocks_q + c / CKPT_BLOCK] - 127);
-                load_checkpoint(g.q + (long long)r * g.cols + c, unit, have, g.vec_q, z);
+                load_checkpoint(g.q + (long long)r * g.cols + c, unit, have, z);
                 by_activation(g.act, [&](auto act) __attribute__((always_inline)) {
                     constexpr int ACT = decltype(act)::value;
                     if (g.source == DENSE_FROM_CHECKPOINT) {
@@ -107,10 +110,7 @@ dense_layout_kernel(LayoutLaunch launch)
             }
         }
         if (live && g.copy) {
-            T* const to = static_cast<T*>(g.copy) + (long long)r * g.cols + c;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < have) to[i] = (T)v[i];
+            store_eight(static_cast<T*>(g.copy) + (long long)r * g.cols + c, have, v);
         }
         if (g.transposed) {
 #pragma unroll
@@ -171,7 +171,7 @@ dense_colsum_kernel(const float* colsum, int blocks, int cols, void* out)
 // Four lanes share a block of 32, eight values each.  A workgroup covers `wide` threads of a row and 256 / wide rows.
 template <int DT>
 __global__ void __launch_bounds__(256)
-checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t* q, uint8_t* e, int wide_log, int vec_x, int vec_q)
+checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t* q, uint8_t* e, int wide_log)
 {
     typedef typename DenseType<DT>::type T;
     const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), ty = threadIdx.x >> wide_log;
@@ -180,7 +180,7 @@ checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t*
     for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r - ty < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
         const int have = r < rows ? cols - c : 0;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (have > 0) load_eight(static_cast<const T*>(x) + r * ldx + c, have, vec_x, v);
+        if (have > 0) load_columns(static_cast<const T*>(x) + r * ldx + c, have, v);
         float most = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_magnitude(v[i]));
@@ -188,12 +188,12 @@ checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t*
         most = fmaxf(most, __shfl_xor(most, 2));
         if (have <= 0) continue;
         const int ex = ckpt_exponent<DT>(most);
-        u32x2 code = {0, 0};
+        Codes code = {0, 0};
 #pragma unroll
         for (int i = 0; i < 8; ++i) code[i / 4] |= ckpt_code<DT>(v[i], ex) << 8 * (i % 4);
         int8_t* const to = q + r * cols + c;
-        if (vec_q && have >= 8) {
-            *reinterpret_cast<u32x2*>(to) = code;
+        if (have >= 8) {
+            *reinterpret_cast<Codes*>(to) = code;
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -205,30 +205,21 @@ checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t*
 
 template <int DT>
 __global__ void __launch_bounds__(256)
-checkpoint_unpack_kernel(const int8_t* q, const uint8_t* e, int rows, int cols, int act, void* y, long long ldy, int wide_log, int vec_q, int vec_y)
+checkpoint_unpack_kernel(const int8_t* q, const uint8_t* e, int rows, int cols, int act, void* y, long long ldy, int wide_log)
 {
     typedef typename DenseType<DT>::type T;
-    typedef T T8 __attribute__((ext_vector_type(8), aligned(16)));
     const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), ty = threadIdx.x >> wide_log;
     const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 8), have = cols - c;
     const long long blocks = (cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
     if (have <= 0) return;
     for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
         float v[8];
-        load_checkpoint(q + r * cols + c, two_to((int)e[r * blocks + c / CKPT_BLOCK] - 127), have, vec_q, v);
-        T* const to = static_cast<T*>(y) + r * ldy + c;
-        T8 t;
+        load_checkpoint(q + r * cols + c, two_to((int)e[r * blocks + c / CKPT_BLOCK] - 127), have, v);
         by_activation(act, [&](auto a) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = (T)activate<decltype(a)::value>(v[i]);
+            for (int i = 0; i < 8; ++i) v[i] = activate<decltype(a)::value>(v[i]);
         });
-        if (vec_y && have >= 8) {
-            *reinterpret_cast<T8*>(to) = t;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < have) to[i] = t[i];
-        }
+        store_eight(static_cast<T*>(y) + r * ldy + c, have, v);
     }
 }
 
@@ -242,8 +233,6 @@ RowGrid row_grid(int rows, int cols)
     return {dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), wide_log};
 }
 
-bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-int size_of(int dtype) { return dtype == IOLB_F32 ? 4 : 2; }
 
 }  // namespace
 
@@ -275,10 +264,9 @@ hipError_t launch_dense_colsum(const float* colsum, int blocks, int cols, void* 
 hipError_t launch_checkpoint_pack(const void* x, long long ldx, int rows, int cols, int dtype, int8_t* q, uint8_t* e, hipStream_t st)
 {
     const RowGrid g = row_grid(rows, cols);
-    const int vec_x = aligned_to(x, 16) && ldx * size_of(dtype) % 16 == 0, vec_q = aligned_to(q, 8) && cols % 8 == 0;
-    if (dtype == IOLB_F32) checkpoint_pack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log, vec_x, vec_q);
-    else if (dtype == IOLB_F16) checkpoint_pack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log, vec_x, vec_q);
-    else checkpoint_pack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log, vec_x, vec_q);
+    if (dtype == IOLB_F32) checkpoint_pack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log);
+    else if (dtype == IOLB_F16) checkpoint_pack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log);
+    else checkpoint_pack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log);
     return hipGetLastError();
 }
 
@@ -286,10 +274,9 @@ hipError_t launch_checkpoint_unpack(const int8_t* q, const uint8_t* e, int rows,
                                     hipStream_t st)
 {
     const RowGrid g = row_grid(rows, cols);
-    const int vec_q = aligned_to(q, 8) && cols % 8 == 0, vec_y = aligned_to(y, 16) && ldy * size_of(dtype) % 16 == 0;
-    if (dtype == IOLB_F32) checkpoint_unpack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log, vec_q, vec_y);
-    else if (dtype == IOLB_F16) checkpoint_unpack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log, vec_q, vec_y);
-    else checkpoint_unpack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log, vec_q, vec_y);
+    if (dtype == IOLB_F32) checkpoint_unpack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log);
+    else if (dtype == IOLB_F16) checkpoint_unpack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log);
+    else checkpoint_unpack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log);
     return hipGetLastError();
 }
 

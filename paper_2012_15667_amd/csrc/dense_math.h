@@ -148,13 +148,15 @@ __device__ __forceinline__ f32x4 multiply(const u32x4& a, const u32x4& b, const 
 __device__ __forceinline__ int place(int row, int piece) { return piece ^ (row & 7); }
 
 // ---- the end of a product: W (4 or 8) neighbouring columns n ... of row m --------------------------------
-// `vec` flags of DenseFinish hold for eight columns, and so for four.
+// W values of T in one piece, at any address that is one for a T: rows start where their length and the caller's strides put them, and global
+// memory takes such accesses (a row of 1151 fp16 weights read value by value cost 68 us where pieces take PIECES).
+template <class T, int W> struct Piece { typedef T type __attribute__((ext_vector_type(W), aligned(sizeof(T)))); };
+
 template <int W, class T>
-__device__ __forceinline__ void load_columns(const T* p, int have, bool vec, float (&v)[W])
+__device__ __forceinline__ void load_columns(const T* p, int have, float (&v)[W])
 {
-    typedef T TW __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
-    if (vec && have > 0) {
-        const TW t = *reinterpret_cast<const TW*>(p);
+    if (have >= W) {
+        const auto t = *reinterpret_cast<const typename Piece<T, W>::type*>(p);
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] = (float)t[i];
     } else {
@@ -168,7 +170,7 @@ __device__ __forceinline__ void load_bias(const DenseFinish& f, int n, float (&b
 {
     typedef typename DenseType<DT>::type T;
     if (f.bias) {
-        load_columns(static_cast<const T*>(f.bias) + n, f.N - n, f.vec_bias, b);
+        load_columns(static_cast<const T*>(f.bias) + n, f.N - n, b);
     } else {
 #pragma unroll
         for (int i = 0; i < W; ++i) b[i] = 0.f;
@@ -180,7 +182,7 @@ __device__ __forceinline__ void add_residual(const DenseFinish& f, int m, int n,
 {
     typedef typename DenseType<DT>::type T;
     float v[W];
-    load_columns(static_cast<const T*>(f.residual) + m * f.ldr + n, f.N - n, f.vec_res, v);
+    load_columns(static_cast<const T*>(f.residual) + m * f.ldr + n, f.N - n, v);
 #pragma unroll
     for (int i = 0; i < W; ++i) z[i] += v[i];
 }
@@ -198,13 +200,13 @@ __device__ __forceinline__ float largest_of(const float (&z)[W], int have)
 template <int DT, int W>
 __device__ __forceinline__ void store_codes(const DenseFinish& f, int m, int n, const float (&z)[W], float most)
 {
-    typedef unsigned Words __attribute__((ext_vector_type(W / 4)));
+    typedef unsigned Words __attribute__((ext_vector_type(W / 4), aligned(1)));
     const int e = ckpt_exponent<DT>(most), have = f.N - n;
     Words code = {};
 #pragma unroll
     for (int i = 0; i < W; ++i) code[i / 4] |= ckpt_code<DT>(z[i], e) << 8 * (i % 4);
     int8_t* const to = f.zq + (long long)m * f.N + n;
-    if (f.vec_q) {
+    if (have >= W) {
         *reinterpret_cast<Words*>(to) = code;
     } else {
 #pragma unroll
@@ -219,13 +221,13 @@ template <int DT, int ACT, int W>
 __device__ __forceinline__ void store_columns(const DenseFinish& f, int m, int n, float (&z)[W])
 {
     typedef typename DenseType<DT>::type T;
-    typedef T TW __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
+    typedef typename Piece<T, W>::type TW;
     const int have = f.N - n;
 #pragma unroll
     for (int i = 0; i < W; ++i) z[i] = activate<ACT>(z[i]);
     if (f.residual && !f.first) add_residual<DT>(f, m, n, z);
     T* y = static_cast<T*>(f.y) + m * f.ldy + n;
-    if (f.vec_y) {
+    if (have >= W) {
         TW t;
 #pragma unroll
         for (int i = 0; i < W; ++i) t[i] = (T)z[i];
@@ -242,7 +244,7 @@ template <int DT, int W>
 __device__ __forceinline__ void store_whole(const DenseFinish& f, int m, int n, const float (&z)[W])
 {
     typedef typename DenseType<DT>::type T;
-    typedef T TW __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
+    typedef typename Piece<T, W>::type TW;
     TW t;
 #pragma unroll
     for (int i = 0; i < W; ++i) t[i] = (T)z[i];

@@ -64,6 +64,15 @@ template <int DT> struct Raw { u32x4 v[DT == IOLB_F32 ? 2 : 1]; };
 template <int DT>
 __device__ __forceinline__ int k_of(int g, int i) { return DT == IOLB_F32 ? (i < 4 ? 4 * g + i : 12 + 4 * g + i) : 8 * g + i; }
 
+// N 32-bit words from any address that is one for a T.
+template <int N, class T>
+__device__ __forceinline__ auto words_at(const T* p)
+{
+    typedef unsigned Words __attribute__((ext_vector_type(N)));
+    typedef unsigned Anywhere __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    return (Words)*reinterpret_cast<const Anywhere*>(p);
+}
+
 // Piece g of 32 values that start at p.  WHOLE: all there, in 16-byte pieces.  Otherwise `have` of the 32 exist and the others are zero.
 // The two kinds never meet in one loop: where loads one by one join a path of whole pieces, the compiler waits for all that are on
 // their way, and what was asked for ahead is lost.
@@ -72,10 +81,10 @@ __device__ __forceinline__ void load_raw(Raw<DT>& r, const typename DenseType<DT
 {
     if constexpr (WHOLE) {
         if constexpr (DT == IOLB_F32) {
-            r.v[0] = *reinterpret_cast<const u32x4*>(p + 4 * g);
-            r.v[1] = *reinterpret_cast<const u32x4*>(p + 16 + 4 * g);
+            r.v[0] = words_at<4>(p + 4 * g);
+            r.v[1] = words_at<4>(p + 16 + 4 * g);
         } else {
-            r.v[0] = *reinterpret_cast<const u32x4*>(p + 8 * g);
+            r.v[0] = words_at<4>(p + 8 * g);
         }
     } else if constexpr (DT == IOLB_F32) {
 #pragma unroll
@@ -125,9 +134,9 @@ __device__ __forceinline__ void clear_not_finite(f32x4& c)
 }
 
 // Steps from s0 on up to the one returned can be read in whole pieces.
-__device__ __forceinline__ int whole_steps(const DenseProduct& p, int s0, int s1)
+__device__ __forceinline__ int whole_steps(const DenseProduct& p, int s0, int s1, bool any = true)
 {
-    const int full = p.vec_a && p.vec_b ? p.K / STEP : 0;
+    const int full = any ? p.K / STEP : 0;
     return full < s0 ? s0 : full < s1 ? full : s1;
 }
 
@@ -262,7 +271,8 @@ dense_rows_kernel(DenseProduct p, int join)
     // rows (columns) that do not exist are read from the last one: their sums are not stored
     const int along_row = n0 + l16 < p.N ? n0 + l16 : p.N - 1;
     const int first_col = n0 + NC * l16;
-    const int whole_to = whole_steps(p, s0, s1);
+    const int whole_to = whole_steps(p, s0, s1, !ACROSS || p.N >= NC);
+    const bool edge = ACROSS && first_col == p.N - 1;            // (a pair of columns ends there: it is read one column earlier)
     f32x4 acc[MT][NF];
 
     auto range = [&](auto mode, auto whole, int from, int to) __attribute__((always_inline)) {
@@ -276,11 +286,10 @@ dense_rows_kernel(DenseProduct p, int join)
             if constexpr (!ACROSS) {
                 load_raw<DT, WHOLE>(u.along, b + along_row * p.ldb + k, grp, p.K - k);
             } else if constexpr (WHOLE) {
-                typedef unsigned Words __attribute__((ext_vector_type(WORDS)));
-                const T* const at = b + (k + 8 * grp) * p.ldb + (first_col < p.N ? first_col : p.N - NC);
+                const T* const at = b + (k + 8 * grp) * p.ldb + (first_col < p.N - NC ? first_col : p.N - NC);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const Words t = *reinterpret_cast<const Words*>(at + i * p.ldb);
+                    const auto t = words_at<WORDS>(at + i * p.ldb);
 #pragma unroll
                     for (int w = 0; w < WORDS; ++w) u.across[i][w] = t[w];
                 }
@@ -314,8 +323,8 @@ dense_rows_kernel(DenseProduct p, int join)
                 const int have = p.K - s * STEP - 32 * (piece >> 2);
                 if constexpr (ACROSS && DT == IOLB_F32) {
                     if constexpr (WHOLE) {
-                        ra[i].v[0] = *reinterpret_cast<const u32x4*>(at + 8 * g);
-                        ra[i].v[1] = *reinterpret_cast<const u32x4*>(at + 8 * g + 4);
+                        ra[i].v[0] = words_at<4>(at + 8 * g);
+                        ra[i].v[1] = words_at<4>(at + 8 * g + 4);
                     } else {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) ra[i].v[j / 4][j % 4] = 8 * g + j < have ? __float_as_uint(at[8 * g + j]) : 0u;
@@ -364,9 +373,11 @@ dense_rows_kernel(DenseProduct p, int join)
                     cut<DT, SAFE>(ub[u].along, fb[0]);
                 } else {
 #pragma unroll
-                    for (auto& row : ub[u].across)
+                    for (auto& row : ub[u].across) {
 #pragma unroll
                         for (unsigned& v : row) asm volatile("" : "+v"(v));
+                        if constexpr (WHOLE) row[0] = !edge ? row[0] : WORDS == 2 ? row[WORDS - 1] : row[0] >> 16;
+                    }
 #pragma unroll
                     for (int j = 0; j < NF; ++j)
 #pragma unroll
@@ -553,7 +564,7 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
         }
     }
     };
-    if (p.f.vec_y && m0 + 16 * NT <= p.M && (n_to - n_from) % (32 * AHEAD) == 0) run(std::true_type{});
+    if (m0 + 16 * NT <= p.M && (n_to - n_from) % (32 * AHEAD) == 0) run(std::true_type{});
     else run(std::false_type{});
 }
 
