@@ -59,16 +59,17 @@ inline size_t dense_partial_bytes(int splits, long long M, long long N) { return
 // dtype: of y, bias and residual.  Operands are of the type; for fp32 they are in two fp16 parts where exps_a is given, else in three bf16 parts.
 hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st);
 
-// The same for few rows of A: both operands as the caller holds them (fp32 too: taken apart in the kernels), any K, bound by reading
-// B.  across: B is [K][N], summed along its rows.  K is shared by workgroups, at most `splits` to a sum.  Sums go to `partial` if join is
+// The same for few rows of A: both operands as the caller holds them (fp32 too: taken apart in the kernels), K at least 8,
+// bound by reading B.  across: B is [K][N], summed along its rows, N at least 2.  K is shared by workgroups, at most `splits` to a sum.  Sums go to `partial` if join is
 // set (always with splits > 1 or a checkpoint).
 constexpr int DENSE_FEW = 16;               // rows of the kernel for the fewest
 // Whether a product with M rows and an N x K weight runs on them, or on the product kernel with its operands laid out.  fp32: the layout of the
 // weights in parts costs more than all of the product up to some hundred rows (4096 x 4096, us: 64 rows 24 against 69, 128 36 / 78, 256 62 / 97;
-// 512 x 512, 256 rows 12 / 16).  16-bit types: the product kernel reads weights in place (4096 x 4096, 20 rows 15.7 against 12.6), but across
+// 512 x 512, 256 rows 12 / 16).  Their rows are read in pieces of eight values, or two across: shorter ones are left to the product kernel.  16-bit types: the product kernel reads weights in place (4096 x 4096, 20 rows 15.7 against 12.6), but across
 // they would be transposed: 4096 x 4096, 64 rows 15.5 against 28, 128 24.8 / 31, 256 40 / 37; 1000 x 2048, 20 rows 13.1 / 13.2, 64 17.9 / 14.2.
 inline bool dense_rows_wanted(long long M, long long N, long long K, int dtype, bool across)
 {
+    if (across ? N < 8 || K < 2 : K < 8) return false;
     if (dtype == IOLB_F32) return M <= 512;
     if (!across) return M <= DENSE_FEW;
     return M <= 32 || (M <= 128 && N * K >= (1 << 22));

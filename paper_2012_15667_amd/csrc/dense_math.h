@@ -149,7 +149,7 @@ __device__ __forceinline__ int place(int row, int piece) { return piece ^ (row &
 
 // ---- the end of a product: W (4 or 8) neighbouring columns n ... of row m --------------------------------
 // W values of T in one piece, at any address that is one for a T: rows start where their length and the caller's strides put them, and global
-// memory takes such accesses (a row of 1151 fp16 weights read value by value cost 68 us where pieces take PIECES).
+// memory takes such accesses (a row of 1151 fp16 weights read value by value on 4 rows for 14464 outputs cost 68 us, in pieces 22).
 template <class T, int W> struct Piece { typedef T type __attribute__((ext_vector_type(W), aligned(sizeof(T)))); };
 
 template <int W, class T>

@@ -60,10 +60,6 @@ __device__ __forceinline__ void multiply_parts(const Fragment<DT> (&b)[NB], cons
 // Eight values of a row as they lie in memory.  fp32: two runs of four, so that four lanes read 64 neighbouring bytes at a time.
 template <int DT> struct Raw { u32x4 v[DT == IOLB_F32 ? 2 : 1]; };
 
-// k of value i of piece g (0 ... 3) of 32
-template <int DT>
-__device__ __forceinline__ int k_of(int g, int i) { return DT == IOLB_F32 ? (i < 4 ? 4 * g + i : 12 + 4 * g + i) : 8 * g + i; }
-
 // N 32-bit words from any address that is one for a T.
 template <int N, class T>
 __device__ __forceinline__ auto words_at(const T* p)
@@ -73,28 +69,65 @@ __device__ __forceinline__ auto words_at(const T* p)
     return (Words)*reinterpret_cast<const Anywhere*>(p);
 }
 
-// Piece g of 32 values that start at p.  WHOLE: all there, in 16-byte pieces.  Otherwise `have` of the 32 exist and the others are zero.
-// The two kinds never meet in one loop: where loads one by one join a path of whole pieces, the compiler waits for all that are on
-// their way, and what was asked for ahead is lost.
-template <int DT, bool WHOLE>
+// The same four words of 16-bit values at odd addresses, by aligned accesses: memory takes the others at a third of the rate (4 x 14464 x 1152 fp16
+// with rows 1153 apart 33 us, with this 20; 1154 apart 14).  The fifth word is read only where a value of the four lies in it.
+template <class T>
+__device__ __forceinline__ u32x4 words_at_odd(const T* p)
+{
+    const size_t at = reinterpret_cast<size_t>(p);
+    const unsigned off = (unsigned)at & 2;
+    const unsigned* const q = reinterpret_cast<const unsigned*>(at - off);
+    const u32x4 d = words_at<4>(q);
+    const unsigned last = q[off ? 4 : 3];
+    return u32x4{__builtin_amdgcn_alignbyte(d[1], d[0], off), __builtin_amdgcn_alignbyte(d[2], d[1], off), __builtin_amdgcn_alignbyte(d[3], d[2], off),
+                 __builtin_amdgcn_alignbyte(last, d[3], off)};
+}
+
+// How a step is read.  WHOLE: all of it exists.  ENDING: pieces are read from where they still end with the row (rows have eight values or more) and
+// moved down; what comes in is zero (4 x 14464 x 1151 fp16, whose last step was read value by value: 37 us, now 26).  The kinds have loops of
+// their own: where two meet in one, the compiler waits for all loads on their way, and what was asked for ahead is lost.
+enum { WHOLE, ENDING };
+
+// 128 bits moved down by 16 n (0 ... 8) bits.
+__device__ __forceinline__ u32x4 moved_down(const u32x4& v, int n)
+{
+    unsigned long long lo = v[0] | (unsigned long long)v[1] << 32, hi = v[2] | (unsigned long long)v[3] << 32;
+    const int s = 16 * (n & 3);
+    lo = s ? lo >> s | hi << (64 - s) : lo;
+    hi = s ? hi >> s : hi;
+    if (n & 4) { lo = hi; hi = 0; }
+    if (n & 8) lo = hi = 0;
+    return u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+
+// The N values at p (16 bytes) of a row in which `have` are left from there on; the others are zero.
+template <int N, bool ODD = false, class T>
+__device__ __forceinline__ u32x4 ending_at(const T* p, int have)
+{
+    const int in = have < 0 ? 0 : have < N ? have : N;
+    const T* const at = p + (have < N ? have : N) - N;
+    if constexpr (ODD) return moved_down(words_at_odd(at), (N - in) * (8 / N));
+    else return moved_down(words_at<4>(at), (N - in) * (8 / N));
+}
+
+// Piece g of 32 values that start at p, of which `have` exist.
+template <int DT, int KIND, bool ODD = false>
 __device__ __forceinline__ void load_raw(Raw<DT>& r, const typename DenseType<DT>::type* p, int g, int have)
 {
-    if constexpr (WHOLE) {
+    if constexpr (KIND == WHOLE) {
         if constexpr (DT == IOLB_F32) {
             r.v[0] = words_at<4>(p + 4 * g);
             r.v[1] = words_at<4>(p + 16 + 4 * g);
         } else {
-            r.v[0] = words_at<4>(p + 8 * g);
+            if constexpr (ODD) r.v[0] = words_at_odd(p + 8 * g);
+            else r.v[0] = words_at<4>(p + 8 * g);
         }
-    } else if constexpr (DT == IOLB_F32) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i / 4][i % 4] = k_of<DT>(g, i) < have ? __float_as_uint(p[k_of<DT>(g, i)]) : 0u;
     } else {
-        const unsigned short* const q = reinterpret_cast<const unsigned short*>(p) + 8 * g;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned lo = 8 * g + 2 * i < have ? q[2 * i] : 0u, hi = 8 * g + 2 * i + 1 < have ? q[2 * i + 1] : 0u;
-            r.v[0][i] = lo | hi << 16;
+        if constexpr (DT == IOLB_F32) {
+            r.v[0] = ending_at<4>(p + 4 * g, have - 4 * g);
+            r.v[1] = ending_at<4>(p + 16 + 4 * g, have - 16 - 4 * g);
+        } else {
+            r.v[0] = ending_at<8, ODD>(p + 8 * g, have - 8 * g);
         }
     }
 }
@@ -133,12 +166,14 @@ __device__ __forceinline__ void clear_not_finite(f32x4& c)
     for (int i = 0; i < 4; ++i) c[i] = fabsf(c[i]) < __builtin_inff() ? c[i] : 0.f;
 }
 
-// Steps from s0 on up to the one returned can be read in whole pieces.
-__device__ __forceinline__ int whole_steps(const DenseProduct& p, int s0, int s1, bool any = true)
+// Steps from s0 on up to the one returned exist whole.
+__device__ __forceinline__ int whole_steps(const DenseProduct& p, int s0, int s1)
 {
-    const int full = any ? p.K / STEP : 0;
+    const int full = p.K / STEP;
     return full < s0 ? s0 : full < s1 ? full : s1;
 }
+
+template <int N> using Constant = std::integral_constant<int, N>;
 
 __device__ __forceinline__ void keep_partial(const DenseProduct& p, int split, int m, int n, const f32x4& c)
 {
@@ -149,7 +184,7 @@ __device__ __forceinline__ void keep_partial(const DenseProduct& p, int split, i
 // ---- up to sixteen rows: the eight waves of a workgroup share K of sixteen columns of C -----------------------
 // A step of a wave is 64 k: of B sixteen rows (16 lanes) by 64 or 128 neighbouring bytes at a time (4 lanes), of A likewise, from L2.
 // The waves take the steps in turn, so that a workgroup reads runs of 8 * 64 values of a row.
-template <int DT>
+template <int DT, bool ODD>
 __global__ void __launch_bounds__(512)
 dense_few_kernel(DenseProduct p, int join)
 {
@@ -169,23 +204,24 @@ dense_few_kernel(DenseProduct p, int join)
     float bias[4] = {0.f, 0.f, 0.f, 0.f};                              // (on its way while the products are taken)
     if (!join && n0 + 4 * grp < p.N) load_bias<DT>(p.f, n0 + 4 * grp, bias);
     // the sums of steps from ... to - 1, of which this wave has every eighth
-    auto range = [&](auto mode, auto whole, int from, int to, f32x4 (&c)[2]) __attribute__((always_inline)) {
-        constexpr int MODE = decltype(mode)::value;
+    auto range = [&](auto mode, auto kind, int from, int to, f32x4 (&c)[2]) __attribute__((always_inline)) {
+        constexpr int MODE = decltype(mode)::value, KIND = decltype(kind)::value;
         Raw<DT> rb[AHEAD][2], ra[AHEAD][2];
         auto load = [&](int s, Raw<DT> (&to_b)[2], Raw<DT> (&to_a)[2]) __attribute__((always_inline)) {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
                 const int k = s * STEP + 32 * kk;
-                load_raw<DT, decltype(whole)::value>(to_b[kk], b + k, grp, p.K - k);
-                load_raw<DT, decltype(whole)::value>(to_a[kk], a + k, grp, p.K - k);
+                load_raw<DT, KIND, ODD>(to_b[kk], b + k, grp, p.K - k);
+                load_raw<DT, KIND, ODD>(to_a[kk], a + k, grp, p.K - k);
             }
         };
-        if (from + wave >= to) return;
+        const int first = from + ((wave - (from - s0)) & (WAVES - 1));          // (an ending goes to the wave that is next)
+        if (first >= to) return;
         // (beyond its last step a wave loads that again: without a condition on them, loads ahead stay in their registers)
-        const int last = to - 1 - (to - 1 - from - wave) % WAVES;
+        const int last = to - 1 - (to - 1 - first) % WAVES;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) load(from + wave + i * WAVES < to ? from + wave + i * WAVES : last, rb[i], ra[i]);
-        for (int s = from + wave; s < to; s += AHEAD * WAVES) {
+        for (int i = 0; i < AHEAD; ++i) load(first + i * WAVES < to ? first + i * WAVES : last, rb[i], ra[i]);
+        for (int s = first; s < to; s += AHEAD * WAVES) {
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 const bool live = s + i * WAVES < to;
@@ -206,8 +242,8 @@ dense_few_kernel(DenseProduct p, int join)
     };
     auto sums = [&](auto mode) __attribute__((always_inline)) {
         f32x4 c[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
-        range(mode, std::true_type{}, s0, whole_to, c);
-        range(mode, std::false_type{}, whole_to, s1, c);
+        range(mode, Constant<WHOLE>{}, s0, whole_to, c);
+        range(mode, Constant<ENDING>{}, whole_to, s1, c);
         return c[0] + c[1];
     };
     f32x4 c = sums(std::integral_constant<int, ALL_PRODUCTS>{});
@@ -261,7 +297,7 @@ dense_rows_kernel(DenseProduct p, int join)
     const T* const a = static_cast<const T*>(p.a);
     const T* const b = static_cast<const T*>(p.b);
     const int m0 = blockIdx.y * ROWS;
-    const long long steps = p.K > 0 ? (p.K + STEP - 1) / STEP : 1, total = steps * ((p.N + WAVES * COLS - 1) / (WAVES * COLS));
+    const long long steps = (p.K + STEP - 1) / STEP, total = steps * ((p.N + WAVES * COLS - 1) / (WAVES * COLS));
     const long long end = (blockIdx.x + 1LL) * p.per < total ? (blockIdx.x + 1LL) * p.per : total;
     // the workgroup's run of steps, block by block
     for (long long at_step = (long long)blockIdx.x * p.per; at_step < end;) {
@@ -271,45 +307,28 @@ dense_rows_kernel(DenseProduct p, int join)
     // rows (columns) that do not exist are read from the last one: their sums are not stored
     const int along_row = n0 + l16 < p.N ? n0 + l16 : p.N - 1;
     const int first_col = n0 + NC * l16;
-    const int whole_to = whole_steps(p, s0, s1, !ACROSS || p.N >= NC);
+    const int whole_to = whole_steps(p, s0, s1);
     const bool edge = ACROSS && first_col == p.N - 1;            // (a pair of columns ends there: it is read one column earlier)
     f32x4 acc[MT][NF];
 
-    auto range = [&](auto mode, auto whole, int from, int to) __attribute__((always_inline)) {
-        constexpr int MODE = decltype(mode)::value;
-        constexpr bool SAFE = MODE != ALL_PRODUCTS, WHOLE = decltype(whole)::value;
+    auto range = [&](auto mode, auto kind, int from, int to) __attribute__((always_inline)) {
+        constexpr int MODE = decltype(mode)::value, KIND = decltype(kind)::value;
+        constexpr bool SAFE = MODE != ALL_PRODUCTS;
         if (from >= to) return;
         // ---- B in registers: 32 k of sixteen rows, or of 64 columns
         struct Unit { Raw<DT> along; unsigned across[8][ACROSS ? WORDS : 1]; };
         Unit ub[UNITS];
         auto load_b = [&](int k, Unit& u) __attribute__((always_inline)) {                     // k: of the unit's first
             if constexpr (!ACROSS) {
-                load_raw<DT, WHOLE>(u.along, b + along_row * p.ldb + k, grp, p.K - k);
-            } else if constexpr (WHOLE) {
-                const T* const at = b + (k + 8 * grp) * p.ldb + (first_col < p.N - NC ? first_col : p.N - NC);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const auto t = words_at<WORDS>(at + i * p.ldb);
-#pragma unroll
-                    for (int w = 0; w < WORDS; ++w) u.across[i][w] = t[w];
-                }
+                load_raw<DT, KIND>(u.along, b + along_row * p.ldb + k, grp, p.K - k);
             } else {
+                const T* const at = b + (first_col < p.N - NC ? first_col : p.N - NC);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int row = k + 8 * grp + i;
-                    const bool in = row < p.K;
-                    const T* const at = b + (in ? row : 0) * p.ldb + first_col;
-                    if constexpr (DT == IOLB_F32) {
+                    const auto t = words_at<WORDS>(at + (KIND == WHOLE || row < p.K ? row : p.K - 1) * p.ldb);
 #pragma unroll
-                        for (int j = 0; j < WORDS; ++j) u.across[i][j] = in && first_col + j < p.N ? __float_as_uint(at[j]) : 0u;
-                    } else {
-                        const unsigned short* const q = reinterpret_cast<const unsigned short*>(at);
-#pragma unroll
-                        for (int j = 0; j < WORDS; ++j) {
-                            const unsigned lo = in && first_col + 2 * j < p.N ? q[2 * j] : 0u, hi = in && first_col + 2 * j + 1 < p.N ? q[2 * j + 1] : 0u;
-                            u.across[i][j] = lo | hi << 16;
-                        }
-                    }
+                    for (int w = 0; w < WORDS; ++w) u.across[i][w] = KIND == WHOLE || row < p.K ? t[w] : 0u;
                 }
             }
         };
@@ -322,15 +341,15 @@ dense_rows_kernel(DenseProduct p, int join)
                 const T* const at = a + (row < p.M ? row : p.M - 1) * p.lda + s * STEP + 32 * (piece >> 2);
                 const int have = p.K - s * STEP - 32 * (piece >> 2);
                 if constexpr (ACROSS && DT == IOLB_F32) {
-                    if constexpr (WHOLE) {
+                    if constexpr (KIND == WHOLE) {
                         ra[i].v[0] = words_at<4>(at + 8 * g);
                         ra[i].v[1] = words_at<4>(at + 8 * g + 4);
                     } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) ra[i].v[j / 4][j % 4] = 8 * g + j < have ? __float_as_uint(at[8 * g + j]) : 0u;
+                        ra[i].v[0] = ending_at<4>(at + 8 * g, have - 8 * g);
+                        ra[i].v[1] = ending_at<4>(at + 8 * g + 4, have - 8 * g - 4);
                     }
                 } else {
-                    load_raw<DT, WHOLE>(ra[i], at, g, have);
+                    load_raw<DT, KIND>(ra[i], at, g, have);
                 }
             }
         };
@@ -376,7 +395,7 @@ dense_rows_kernel(DenseProduct p, int join)
                     for (auto& row : ub[u].across) {
 #pragma unroll
                         for (unsigned& v : row) asm volatile("" : "+v"(v));
-                        if constexpr (WHOLE) row[0] = !edge ? row[0] : WORDS == 2 ? row[WORDS - 1] : row[0] >> 16;
+                        row[0] = !edge ? row[0] : WORDS == 2 ? row[WORDS - 1] : row[0] >> 16;
                     }
 #pragma unroll
                     for (int j = 0; j < NF; ++j)
@@ -415,8 +434,8 @@ dense_rows_kernel(DenseProduct p, int join)
         }
     };
     auto sums = [&](auto mode) __attribute__((always_inline)) {
-        range(mode, std::true_type{}, s0, whole_to);
-        range(mode, std::false_type{}, whole_to, s1);
+        range(mode, Constant<WHOLE>{}, s0, whole_to);
+        range(mode, Constant<ENDING>{}, whole_to, s1);
     };
     auto clear = [&](bool all) {
 #pragma unroll
@@ -509,12 +528,12 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) load(n_from + 32 * i, fb[i]);
-    // WHOLE: every store is a 16-byte piece that exists.  (Under conditions the stores' number is not known, and a wait for a load would be
+    // EVERY: every store is a 16-byte piece that exists.  (Under conditions the stores' number is not known, and a wait for a load would be
     // one for the stores before it.)
-    auto run = [&](auto whole) __attribute__((always_inline)) {
-    constexpr bool WHOLE = decltype(whole)::value;
+    auto run = [&](auto every) __attribute__((always_inline)) {
+    constexpr bool EVERY = decltype(every)::value;
     auto store = [&](int m, int col, auto& z) __attribute__((always_inline)) {
-        if constexpr (WHOLE) store_whole<DT>(p.f, m, col, z);
+        if constexpr (EVERY) store_whole<DT>(p.f, m, col, z);
         else if (m < p.M && col < p.N) store_columns<DT, IOLB_ACT_NONE>(p.f, m, col, z);
     };
     for (int n0 = n_from; n0 < n_to; n0 += 32 * AHEAD) {
@@ -541,7 +560,7 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
                             c[t][j] = multiply<DT == IOLB_F16>(fb[i][j][kk][part_b[q]], fa[t][kk][part_a[q]], c[t][j]);
             }
             load(n + 32 * AHEAD < n_to ? n + 32 * AHEAD : n_from, fb[i]);
-            if (WHOLE || n < n_to) {
+            if (EVERY || n < n_to) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const int m = m0 + 16 * t + l16;
@@ -587,12 +606,15 @@ template <int DT>
 hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
 {
     if (!across && p.M <= DENSE_FEW) {
-        dense_few_kernel<DT><<<dim3((p.N + 15) / 16, p.splits), 512, 0, st>>>(p, join);
+        const dim3 grid((p.N + 15) / 16, p.splits);
+        const bool odd = DT != IOLB_F32 && ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b)) % 4 || p.ldb % 2 || (p.M > 1 && p.lda % 2));
+        if (odd) dense_few_kernel<DT, DT != IOLB_F32><<<grid, 512, 0, st>>>(p, join);
+        else dense_few_kernel<DT, false><<<grid, 512, 0, st>>>(p, join);
         return hipGetLastError();
     }
     const int mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
     const int cols = rows_columns(across), threads = 64 * rows_waves(across);
-    const long long total = (p.K > 0 ? (p.K + STEP - 1LL) / STEP : 1) * ((p.N + cols - 1LL) / cols);       // (a sum over nothing: one empty step)
+    const long long total = (p.K + STEP - 1LL) / STEP * ((p.N + cols - 1LL) / cols);
     const dim3 grid((unsigned)((total + p.per - 1) / p.per), (p.M + 16 * mt - 1) / (16 * mt));
     if (across) {
         if (mt == 1) dense_rows_kernel<DT, 1, true><<<grid, threads, 0, st>>>(p, join);
@@ -619,7 +641,7 @@ DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool 
     const bool few = !across && M <= DENSE_FEW, wide = dtype == IOLB_F32;
     const int tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
     const double alone = few ? (wide ? 1500 : 800) : !across ? 1000 : !wide ? 550 : tiles == 1 ? 1050 : tiles == 2 ? 1350 : 1900;
-    const long long steps = K > 0 ? (K + STEP - 1) / STEP : 1, cols = few ? 16 : rows_columns(across);
+    const long long steps = (K + STEP - 1) / STEP, cols = few ? 16 : rows_columns(across);
     const long long blocks = (N + cols - 1) / cols, waves = few ? 8 : 1;           // (few: the waves share the steps)
     const long long capacity = 256 * (few ? 2 : rows_resident(dtype, tiles, across)) / ((M + 63) / 64);   // (each 64 rows have workgroups of their own)
     const double step_ns = (double)cols * waves * STEP * (wide ? 4 : 2) / 4900;                        // of one workgroup

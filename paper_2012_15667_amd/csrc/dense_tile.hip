@@ -240,7 +240,7 @@ dense_join_kernel(DenseProduct p, int wide_log)
         int pieces = p.splits;
         if (p.block_columns && n < p.N) {
             // the runs that meet the block of columns n is in (all eight are in one)
-            const long long steps = p.K > 0 ? (p.K + DENSE_ROWS_STEP - 1) / DENSE_ROWS_STEP : 1, first = n / p.block_columns * steps;
+            const long long steps = (p.K + DENSE_ROWS_STEP - 1) / DENSE_ROWS_STEP, first = n / p.block_columns * steps;
             pieces = (int)((first + steps - 1) / p.per - first / p.per) + 1;
         }
         for (long long m = (long long)blockIdx.y * rows + (threadIdx.x >> wide_log); m - (threadIdx.x >> wide_log) < p.M; m += (long long)gridDim.y * rows) {
