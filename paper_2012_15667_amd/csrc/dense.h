@@ -103,6 +103,8 @@ struct DenseLayout {
     long long ld_tr;
     void* copy;                             // v in the tensor's own type, [rows][cols], or null
     float* colsum;                          // [ceil(rows / 64)][cols]: sums over 64 rows each, or null
+    void* total;                            // up to 64 rows: the sums in the tensor's type instead, or null
+    int odd;                                // set by the launcher: 16-bit values of src may start at odd addresses
 };
 // Up to three of them in one launch.
 constexpr int MAX_LAYOUTS = 3;

@@ -198,7 +198,9 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
     }
     if (want_dx && !few) wt = pieces.take((size_t)planes * a.K * Np * 2);
     const int row_blocks = (int)((a.M + 63) / 64);
-    float* const sums = static_cast<float*>(a.db ? pieces.take((size_t)row_blocks * a.N * 4) : nullptr);
+    // (up to 64 rows the first stage's sums are the sums)
+    const bool one_block = row_blocks == 1;
+    float* const sums = static_cast<float*>(a.db && !one_block ? pieces.take((size_t)row_blocks * a.N * 4) : nullptr);
 
     DenseProduct px{}, pw{};
     DenseTilePlan plan_x{}, plan_w{};
@@ -236,7 +238,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
 
     const hipStream_t st = call_stream();
     DenseLayouts layouts{};
-    if (a.M > 0 && a.N > 0 && (dz_to || dzt || dz_copy || sums)) {
+    if (a.M > 0 && a.N > 0 && (dz_to || dzt || dz_copy || a.db)) {
         DenseLayout& l = layouts.of[layouts.count++];
         l.source = DENSE_FROM_GRADIENT; l.planes = planes;
         l.rows = (int)a.M; l.cols = (int)a.N;
@@ -245,7 +247,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         l.rowmajor = dz_to; l.ld_rm = Np;
         l.transposed = dzt; l.ld_tr = Mp;
         l.copy = dz_copy;
-        l.colsum = sums;
+        l.colsum = sums; l.total = one_block ? a.db : nullptr;
     }
     if (wt) {
         DenseLayout& l = layouts.of[layouts.count++];
@@ -262,7 +264,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         l.transposed = xt; l.ld_tr = Mp;
     }
     if (layouts.count) DENSE_HIP(launch_dense_layouts(a.dtype, layouts, st));
-    if (a.db && a.N > 0) DENSE_HIP(launch_dense_colsum(sums, row_blocks, (int)a.N, a.db, a.dtype, st));
+    if (a.db && a.N > 0 && !one_block) DENSE_HIP(launch_dense_colsum(sums, row_blocks, (int)a.N, a.db, a.dtype, st));
     const auto finish = [&](void* out, int64_t m, int64_t n) {
         DenseFinish f{};
         f.y = out; f.ldy = n; f.M = (int)m; f.N = (int)n;

@@ -79,7 +79,19 @@ dense_layout_kernel(LayoutLaunch launch)
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         const bool live = r < g.rows && have > 0;
         if (live) {
-            if (g.source != DENSE_FROM_CHECKPOINT) load_columns(static_cast<const T*>(g.src) + r * g.ld + c, have, v);
+            if (g.source != DENSE_FROM_CHECKPOINT) {
+                const T* const from = static_cast<const T*>(g.src) + r * g.ld + c;
+                if (sizeof(T) == 2 && g.odd && have >= 8) {
+                    typedef T T8 __attribute__((ext_vector_type(8)));
+                    if constexpr (sizeof(T) == 2) {
+                        const T8 t = __builtin_bit_cast(T8, words_at_odd(from));
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+                    }
+                } else {
+                    load_columns(from, have, v);
+                }
+            }
             if (g.q) {
                 float z[8];
                 const float unit = two_to((int)g.e[r * blocks_q + c / CKPT_BLOCK] - 127);
@@ -122,7 +134,7 @@ dense_layout_kernel(LayoutLaunch launch)
 #pragma unroll
         for (int i = 0; i < 8; ++i) column[i] += v[i];
     }
-    if (g.colsum) {
+    if (g.colsum || g.total) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sums[r_in][c8 + i] = column[i];
     }
@@ -141,10 +153,11 @@ dense_layout_kernel(LayoutLaunch launch)
             }
         }
     }
-    if (g.colsum && tid < 64 && c0 + tid < g.cols) {
+    if ((g.colsum || g.total) && tid < 64 && c0 + tid < g.cols) {
         float s = 0.f;
         for (int i = 0; i < 32; ++i) s += sums[i][tid];
-        g.colsum[(long long)(r0 / 64) * g.cols + c0 + tid] = s;
+        if (g.total) static_cast<T*>(g.total)[c0 + tid] = (T)s;
+        else g.colsum[(long long)(r0 / 64) * g.cols + c0 + tid] = s;
     }
 }
 
@@ -241,6 +254,7 @@ hipError_t launch_dense_layouts(int dtype, const DenseLayouts& l, hipStream_t st
     LayoutLaunch a{l, {}};
     long long n = 0;
     for (int i = 0; i < l.count; ++i) {
+        a.all.of[i].odd = reinterpret_cast<uintptr_t>(l.of[i].src) % 4 || l.of[i].ld % 2;
         a.first[i] = (unsigned)n;
         n += ((l.of[i].cols + 63LL) / 64) * ((l.of[i].rows + 63LL) / 64);
         if (n > 0x7fffffffLL) return hipErrorInvalidValue;

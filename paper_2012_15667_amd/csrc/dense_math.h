@@ -147,6 +147,29 @@ __device__ __forceinline__ f32x4 multiply(const u32x4& a, const u32x4& b, const 
 // Where 16-byte piece c of a 128-byte row lies in LDS: sixteen rows' pieces of the same c fall on different banks.
 __device__ __forceinline__ int place(int row, int piece) { return piece ^ (row & 7); }
 
+// N 32-bit words from any address that is one for a T.
+template <int N, class T>
+__device__ __forceinline__ auto words_at(const T* p)
+{
+    typedef unsigned Words __attribute__((ext_vector_type(N)));
+    typedef unsigned Anywhere __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    return (Words)*reinterpret_cast<const Anywhere*>(p);
+}
+
+// The same four words of 16-bit values at odd addresses, by aligned accesses: memory takes the others at a third of the rate (4 x 14464 x 1152 fp16
+// with rows 1153 apart 33 us, with this 20; 1154 apart 14).  The fifth word is read only where a value of the four lies in it.
+template <class T>
+__device__ __forceinline__ u32x4 words_at_odd(const T* p)
+{
+    const size_t at = reinterpret_cast<size_t>(p);
+    const unsigned off = (unsigned)at & 2;
+    const unsigned* const q = reinterpret_cast<const unsigned*>(at - off);
+    const u32x4 d = words_at<4>(q);
+    const unsigned last = q[off ? 4 : 3];
+    return u32x4{__builtin_amdgcn_alignbyte(d[1], d[0], off), __builtin_amdgcn_alignbyte(d[2], d[1], off), __builtin_amdgcn_alignbyte(d[3], d[2], off),
+                 __builtin_amdgcn_alignbyte(last, d[3], off)};
+}
+
 // ---- the end of a product: W (4 or 8) neighbouring columns n ... of row m --------------------------------
 // W values of T in one piece, at any address that is one for a T: rows start where their length and the caller's strides put them, and global
 // memory takes such accesses (a row of 1151 fp16 weights read value by value on 4 rows for 14464 outputs cost 68 us, in pieces 22).

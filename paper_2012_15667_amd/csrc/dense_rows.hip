@@ -60,29 +60,6 @@ __device__ __forceinline__ void multiply_parts(const Fragment<DT> (&b)[NB], cons
 // Eight values of a row as they lie in memory.  fp32: two runs of four, so that four lanes read 64 neighbouring bytes at a time.
 template <int DT> struct Raw { u32x4 v[DT == IOLB_F32 ? 2 : 1]; };
 
-// N 32-bit words from any address that is one for a T.
-template <int N, class T>
-__device__ __forceinline__ auto words_at(const T* p)
-{
-    typedef unsigned Words __attribute__((ext_vector_type(N)));
-    typedef unsigned Anywhere __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-    return (Words)*reinterpret_cast<const Anywhere*>(p);
-}
-
-// The same four words of 16-bit values at odd addresses, by aligned accesses: memory takes the others at a third of the rate (4 x 14464 x 1152 fp16
-// with rows 1153 apart 33 us, with this 20; 1154 apart 14).  The fifth word is read only where a value of the four lies in it.
-template <class T>
-__device__ __forceinline__ u32x4 words_at_odd(const T* p)
-{
-    const size_t at = reinterpret_cast<size_t>(p);
-    const unsigned off = (unsigned)at & 2;
-    const unsigned* const q = reinterpret_cast<const unsigned*>(at - off);
-    const u32x4 d = words_at<4>(q);
-    const unsigned last = q[off ? 4 : 3];
-    return u32x4{__builtin_amdgcn_alignbyte(d[1], d[0], off), __builtin_amdgcn_alignbyte(d[2], d[1], off), __builtin_amdgcn_alignbyte(d[3], d[2], off),
-                 __builtin_amdgcn_alignbyte(last, d[3], off)};
-}
-
 // How a step is read.  WHOLE: all of it exists.  ENDING: pieces are read from where they still end with the row (rows have eight values or more) and
 // moved down; what comes in is zero (4 x 14464 x 1151 fp16, whose last step was read value by value: 37 us, now 26).  The kinds have loops of
 // their own: where two meet in one, the compiler waits for all loads on their way, and what was asked for ahead is lost.
@@ -593,8 +570,10 @@ hipError_t launch_outer(DenseProduct p, long long plane_a, long long plane_b, hi
     const int rows = 4 * 16 * (DT == IOLB_F32 ? 2 : 4);
     const long long gy = ((long long)p.M + rows - 1) / rows;
     if (gy > 65535) return hipErrorInvalidValue;
-    // a wave's run of columns: eight waves to a SIMD, as each starts with a wait for its rows of A
-    const long long run = ((long long)p.N * gy * 4 / 8192 + 63) / 64 * 64;
+    // a wave's run of columns: each starts with a wait for its rows of A, so there are at most eight waves to a SIMD, and two where that would make
+    // runs shorter than 256 columns (4096 x 4096 fp32, runs of 64 31 us, of 256 28)
+    const long long columns = (long long)p.N * gy * 4, eight = (columns / 8192 + 63) / 64 * 64, two = (columns / 2048 + 63) / 64 * 64;
+    const long long run = eight >= 256 ? eight : two < 256 ? two : 256;
     p.per = (int)(run < 64 ? 64 : run > 4096 ? 4096 : run);
     const dim3 grid((unsigned)(((long long)p.N + p.per - 1) / p.per), (unsigned)gy);
     if (p.K <= 32) dense_outer_kernel<DT, PB, 1><<<grid, 256, 0, st>>>(p, plane_a, plane_b);
