@@ -194,16 +194,11 @@ checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t*
         const int have = r < rows ? cols - c : 0;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (have > 0) load_columns(static_cast<const T*>(x) + r * ldx + c, have, v);
-        float most = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_magnitude(v[i]));
-        most = fmaxf(most, __shfl_xor(most, 1));
-        most = fmaxf(most, __shfl_xor(most, 2));
+        unsigned words[2];
+        int ex;
+        ckpt_codes<DT, 8, 4>(v, have, words, ex);
         if (have <= 0) continue;
-        const int ex = ckpt_exponent<DT>(most);
-        Codes code = {0, 0};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) code[i / 4] |= ckpt_code<DT>(v[i], ex) << 8 * (i % 4);
+        const Codes code = {words[0], words[1]};
         int8_t* const to = q + r * cols + c;
         if (have >= 8) {
             *reinterpret_cast<Codes*>(to) = code;

@@ -17,31 +17,31 @@ template <> struct DenseType<IOLB_F16> { typedef _Float16 type; };
 template <> struct DenseType<IOLB_BF16> { typedef __bf16 type; };
 
 // ---- activations, in 32 bits ----------------------------------------------------------------------
-// Phi(z) = P(normal <= z) by formula 7.1.26 of Abramowitz and Stegun (error of erf at most 1.5e-7), evaluated for -|z| so that
-// nothing cancels in the lower tail.
-__device__ __forceinline__ float normal_below(float z, float gauss /* e^(-z^2 / 2) */)
+// P(normal > |z|) by formula 7.1.26 of Abramowitz and Stegun (error of erf at most 1.5e-7): nothing cancels in the tail.
+__device__ __forceinline__ float normal_tail(float z, float gauss /* e^(-z^2 / 2) */)
 {
-    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678f * fabsf(z));
-    const float p = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-    const float tail = 0.5f * p * gauss;
-    return z > 0.f ? 1.f - tail : tail;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+    const float p = t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f))));
+    return p * gauss;
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+__device__ __forceinline__ float gauss_of(float z) { return __builtin_amdgcn_exp2f(z * z * -0.72134752f); }     // e^(-z^2 / 2)
+
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
 
 constexpr float GELU_TANH_K = 1.5957691216f;      // 2 sqrt(2 / pi): (1 + tanh u) / 2 is the sigmoid of 2 u
 
-// Smooth activations tend to zero at -inf, where their formula is 0 x inf.
+// Smooth activations tend to zero at -inf, where their formula is 0 x inf: the factor z is kept from going beyond -10^4 (which gives zero), while a
+// NaN, which such a comparison drops, comes through the other factor.
 template <int ACT>
 __device__ __forceinline__ float activate(float z)
 {
     if constexpr (ACT == IOLB_ACT_NONE) return z;
     if constexpr (ACT == IOLB_ACT_RELU) return z <= 0.f ? 0.f : z;
-    float y;
-    if constexpr (ACT == IOLB_ACT_SILU) y = z * sigmoid(z);
-    if constexpr (ACT == IOLB_ACT_GELU) y = z * normal_below(z, __expf(-0.5f * z * z));
-    if constexpr (ACT == IOLB_ACT_GELU_TANH) y = z * sigmoid(GELU_TANH_K * (z + 0.044715f * z * z * z));
-    return z == -__builtin_inff() ? 0.f : y;
+    if constexpr (ACT == IOLB_ACT_SILU) return fmaxf(z, -1e4f) * sigmoid(z);
+    // z Phi(z) = max(z, 0) - |z| P(normal > |z|)
+    if constexpr (ACT == IOLB_ACT_GELU) return __builtin_fmaf(-fminf(fabsf(z), 1e4f), normal_tail(z, gauss_of(z)), fmaxf(z, 0.f));
+    if constexpr (ACT == IOLB_ACT_GELU_TANH) return fmaxf(z, -1e4f) * sigmoid(z * __builtin_fmaf(GELU_TANH_K * 0.044715f, z * z, GELU_TANH_K));
 }
 
 // dy act'(z).  Beyond |z| = 60 the slopes are 0 or 1 to every bit; cutting z there keeps its powers finite.
@@ -58,11 +58,11 @@ __device__ __forceinline__ float through_activation(float dy, float z)
         slope = s * (1.f + z * (1.f - s));
     }
     if constexpr (ACT == IOLB_ACT_GELU) {
-        const float g = __expf(-0.5f * z * z);
-        slope = normal_below(z, g) + z * g * 0.3989422804f;
+        const float g = gauss_of(z), tail = normal_tail(z, g);
+        slope = __builtin_fmaf(z * g, 0.3989422804f, z > 0.f ? 1.f - tail : tail);
     }
     if constexpr (ACT == IOLB_ACT_GELU_TANH) {
-        const float s = sigmoid(GELU_TANH_K * (z + 0.044715f * z * z * z));
+        const float s = sigmoid(z * __builtin_fmaf(GELU_TANH_K * 0.044715f, z * z, GELU_TANH_K));
         slope = s + z * s * (1.f - s) * GELU_TANH_K * (1.f + 0.134145f * z * z);
     }
     return dy * slope;
@@ -107,15 +107,53 @@ __device__ __forceinline__ int ckpt_exponent(float most)
     return e < r.lo ? r.lo : e > r.hi ? r.hi : e;
 }
 
-// x 2^-e rounded to nearest even, as the low byte.  At the largest exponent 64 2^e is beyond the type: 63 there.
-template <int DT>
-__device__ __forceinline__ unsigned ckpt_code(float x, int e)
+// W neighbouring values of a block, of which the lane's `have` exist; LANES lanes hold the block.  Returns their codes, four to a word, and
+// the block's exponent.  Every lane of the wave calls.
+//   A block of finite values below the largest exponent is the rule: its largest magnitude is the largest of the bits, and 1.5 2^23 added to
+// x 2^-e (one rounding, to nearest even) leaves the code in the low byte.  Where a lane of the wave meets anything else, all take the other
+// way: values that are not finite are left out of the largest and become -128, and at the largest exponent, where 64 2^e is beyond the type,
+// codes end at 63.
+template <int DT, int W, int LANES>
+__device__ __forceinline__ void ckpt_codes(const float (&x)[W], int have, unsigned (&codes)[W / 4], int& exponent)
 {
-    const float top = e == ckpt_range<DT>().hi ? 63.f : 127.f;
-    float q = __builtin_rintf(x * two_to(-e));
-    q = q > top ? top : q < -top ? -top : q;
-    const int code = fabsf(x) < __builtin_inff() ? (int)q : -128;
-    return (unsigned)code & 0xffu;
+    unsigned bits = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const unsigned b = __float_as_uint(x[i]) & 0x7fffffffu;
+        bits = i < have && b > bits ? b : bits;
+    }
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) {
+        const unsigned b = (unsigned)__shfl_xor((int)bits, d);
+        bits = b > bits ? b : bits;
+    }
+    int e = ckpt_exponent<DT>(__uint_as_float(bits));
+    unsigned c[W];
+    if (!__any(bits >= 0x7f800000u || e == ckpt_range<DT>().hi)) {
+        const float unit = two_to(-e);
+#pragma unroll
+        for (int i = 0; i < W; ++i) c[i] = __float_as_uint(__builtin_fmaf(x[i], unit, 12582912.f));
+    } else {
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) most = i < have ? fmaxf(most, finite_magnitude(x[i])) : most;
+#pragma unroll
+        for (int d = 1; d < LANES; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        e = ckpt_exponent<DT>(most);
+        const float unit = two_to(-e), top = e == ckpt_range<DT>().hi ? 63.f : 127.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            float q = __builtin_rintf(x[i] * unit);
+            q = q > top ? top : q < -top ? -top : q;
+            c[i] = fabsf(x[i]) < __builtin_inff() ? (unsigned)(int)q : 0x80u;
+        }
+    }
+    exponent = e;
+#pragma unroll
+    for (int w = 0; w < W / 4; ++w) {
+        const unsigned lo = __builtin_amdgcn_perm(c[4 * w + 1], c[4 * w], 0x0c0c0400u), hi = __builtin_amdgcn_perm(c[4 * w + 3], c[4 * w + 2], 0x04000c0cu);
+        codes[w] = lo | hi;
+    }
 }
 
 __device__ __forceinline__ float ckpt_value(int code, float unit) { return code == -128 ? __builtin_nanf("") : (float)code * unit; }
@@ -210,31 +248,22 @@ __device__ __forceinline__ void add_residual(const DenseFinish& f, int m, int n,
     for (int i = 0; i < W; ++i) z[i] += v[i];
 }
 
+// W columns' codes, and from the block's first lane its exponent.
 template <int W>
-__device__ __forceinline__ float largest_of(const float (&z)[W], int have)
-{
-    float most = 0.f;
-#pragma unroll
-    for (int i = 0; i < W; ++i) most = i < have ? fmaxf(most, finite_magnitude(z[i])) : most;
-    return most;
-}
-
-// The block's largest finite magnitude is `most`, and its first lane writes the exponent.
-template <int DT, int W>
-__device__ __forceinline__ void store_codes(const DenseFinish& f, int m, int n, const float (&z)[W], float most)
+__device__ __forceinline__ void store_codes(const DenseFinish& f, int m, int n, const unsigned (&codes)[W / 4], int e)
 {
     typedef unsigned Words __attribute__((ext_vector_type(W / 4), aligned(1)));
-    const int e = ckpt_exponent<DT>(most), have = f.N - n;
-    Words code = {};
-#pragma unroll
-    for (int i = 0; i < W; ++i) code[i / 4] |= ckpt_code<DT>(z[i], e) << 8 * (i % 4);
+    const int have = f.N - n;
     int8_t* const to = f.zq + (long long)m * f.N + n;
     if (have >= W) {
-        *reinterpret_cast<Words*>(to) = code;
+        Words t;
+#pragma unroll
+        for (int w = 0; w < W / 4; ++w) t[w] = codes[w];
+        *reinterpret_cast<Words*>(to) = t;
     } else {
 #pragma unroll
         for (int i = 0; i < W; ++i)
-            if (i < have) to[i] = (int8_t)(code[i / 4] >> 8 * (i % 4));
+            if (i < have) to[i] = (int8_t)(codes[i / 4] >> 8 * (i % 4));
     }
     if (n % CKPT_BLOCK == 0) f.ze[(long long)m * ((f.N + CKPT_BLOCK - 1) / CKPT_BLOCK) + n / CKPT_BLOCK] = (uint8_t)(e + 127);
 }
@@ -307,10 +336,10 @@ __device__ __forceinline__ void finish_columns(const DenseFinish& f, int m, int 
     for (int i = 0; i < W; ++i) z[i] += bias[i];
     if (live && f.residual && f.first) add_residual<DT>(f, m, n, z);
     if (f.zq) {
-        float most = largest_of(z, f.N - n);
-#pragma unroll
-        for (int d = 1; d < CKPT_BLOCK / W; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-        if (live) store_codes<DT>(f, m, n, z, most);
+        unsigned codes[W / 4];
+        int e;
+        ckpt_codes<DT, W, CKPT_BLOCK / W>(z, f.N - n, codes, e);
+        if (live) store_codes<W>(f, m, n, codes, e);
     }
     if (live) store_columns<DT, ACT>(f, m, n, z);
 }
