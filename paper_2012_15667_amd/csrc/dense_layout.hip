@@ -211,32 +211,45 @@ checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t*
     }
 }
 
+// Two lanes share a block, sixteen codes each, so that a lane's load is 16 bytes too.
 template <int DT>
 __global__ void __launch_bounds__(256)
 checkpoint_unpack_kernel(const int8_t* q, const uint8_t* e, int rows, int cols, int act, void* y, long long ldy, int wide_log)
 {
     typedef typename DenseType<DT>::type T;
     const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), ty = threadIdx.x >> wide_log;
-    const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 8), have = cols - c;
+    const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 16), have = cols - c;
     const long long blocks = (cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
     if (have <= 0) return;
     for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
-        float v[8];
-        load_checkpoint(q + r * cols + c, two_to((int)e[r * blocks + c / CKPT_BLOCK] - 127), have, v);
+        const float unit = two_to((int)e[r * blocks + c / CKPT_BLOCK] - 127);
+        const int8_t* const from = q + r * cols + c;
+        float v[2][8];
+        if (have >= 16) {
+            const u32x4 t = words_at<4>(from);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i / 8][i % 8] = ckpt_value((int)(t[i / 4] << (24 - 8 * (i % 4))) >> 24, unit);
+        } else {
+            load_checkpoint(from, unit, have, v[0]);
+            load_checkpoint(from + 8, unit, have - 8, v[1]);
+        }
         by_activation(act, [&](auto a) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate<decltype(a)::value>(v[i]);
+            for (int i = 0; i < 16; ++i) v[i / 8][i % 8] = activate<decltype(a)::value>(v[i / 8][i % 8]);
         });
-        store_eight(static_cast<T*>(y) + r * ldy + c, have, v);
+        T* const to = static_cast<T*>(y) + r * ldy + c;
+        store_eight(to, have, v[0]);
+        store_eight(to + 8, have - 8, v[1]);
     }
 }
 
 struct RowGrid { dim3 grid; int wide_log; };
-RowGrid row_grid(int rows, int cols)
+// each: columns of a thread
+RowGrid row_grid(int rows, int cols, long long each)
 {
     int wide_log = 2;                               // whole blocks of 32
-    while (wide_log < 8 && (8LL << wide_log) < cols) ++wide_log;
-    const long long gx = (cols + (8LL << wide_log) - 1) / (8LL << wide_log), per = 256 >> wide_log;
+    while (wide_log < 8 && (each << wide_log) < cols) ++wide_log;
+    const long long gx = (cols + (each << wide_log) - 1) / (each << wide_log), per = 256 >> wide_log;
     const long long gy = (rows + per - 1) / per;
     return {dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), wide_log};
 }
@@ -272,7 +285,7 @@ hipError_t launch_dense_colsum(const float* colsum, int blocks, int cols, void* 
 
 hipError_t launch_checkpoint_pack(const void* x, long long ldx, int rows, int cols, int dtype, int8_t* q, uint8_t* e, hipStream_t st)
 {
-    const RowGrid g = row_grid(rows, cols);
+    const RowGrid g = row_grid(rows, cols, 8);
     if (dtype == IOLB_F32) checkpoint_pack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log);
     else if (dtype == IOLB_F16) checkpoint_pack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log);
     else checkpoint_pack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, q, e, g.wide_log);
@@ -282,7 +295,7 @@ hipError_t launch_checkpoint_pack(const void* x, long long ldx, int rows, int co
 hipError_t launch_checkpoint_unpack(const int8_t* q, const uint8_t* e, int rows, int cols, int act, int dtype, void* y, long long ldy,
                                     hipStream_t st)
 {
-    const RowGrid g = row_grid(rows, cols);
+    const RowGrid g = row_grid(rows, cols, 16);
     if (dtype == IOLB_F32) checkpoint_unpack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log);
     else if (dtype == IOLB_F16) checkpoint_unpack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log);
     else checkpoint_unpack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(q, e, rows, cols, act, y, ldy, g.wide_log);
