@@ -7,7 +7,8 @@
 // (of normal values, 3 in a million are) is uneven, and an operand with one sends the whole product to three bf16 parts.  Infinities and NaN as in dense.h: h is
 // the value, l zero, h h comes last.
 //
-// One workgroup (or wave) reads a row twice, the second time from L2: bound by memory.  4096 x 9216 and 4096 x 9216: HALVES_TIME.
+// One workgroup (or wave) reads a row twice, the second time from L2: bound by memory: 4096 x 9216 twice 136 us, of 128 for
+// what it reads and writes.
 #include "dense_math.h"
 #include "kernels.h"
 

@@ -190,6 +190,10 @@ def test_linear_blocks_of_all_sizes_and_long_sums(dtype):
     check_linear(rng, 4097, 3200, 96, dtype, act="relu")              # the largest blocks, ragged
     check_linear(rng, 130, 200, 9000, dtype, act="gelu_tanh")         # K shared by workgroups
     check_linear(rng, 30, 200, 20000, dtype, checkpoint=True)
+    check_linear(rng, 513, 130, 1000, dtype, act="silu", residual="first", checkpoint=True)
+    check_linear(rng, 2200, 1000, 4600, dtype, act="relu", residual="after", checkpoint=True, gap=3)
+    check_linear(rng, 700, 5, 7, dtype)
+    check_linear(rng, 700, 300, 3, dtype, checkpoint=True)
 
 
 @pytest.mark.gpu
@@ -221,7 +225,7 @@ def test_linear_empty(dtype, M, N, K):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("M", [2, 30, 140])
+@pytest.mark.parametrize("M", [2, 30, 140, 600])
 def test_linear_of_values_that_are_not_finite(dtype, M):
     """Infinities and NaN go where the formula takes them and nowhere else; 0 inf is NaN; the largest finite values stay finite."""
     torch = _torch()
@@ -420,6 +424,10 @@ def test_backward_of_what_is_wanted_only(dtype, dx, dw, db):
 @pytest.mark.parametrize("dtype", TYPES)
 def test_backward_blocks_of_all_sizes(dtype):
     rng = np.random.default_rng(8)
+    check_backward(rng, 600, 77, 5, dtype, act="gelu", x_act="silu")
+    check_backward(rng, 600, 5, 77, dtype, act="relu")
+    check_backward(rng, 100, 2100, 2049, dtype, act="silu", gap=1)
+    check_backward(rng, 33, 8, 2, dtype, act="gelu")
     check_backward(rng, 3200, 4097, 96, dtype, act="silu")
     check_backward(rng, 9000, 130, 70, dtype, act="gelu_tanh")
 
@@ -643,3 +651,33 @@ def test_linear_fp32_rows_of_uneven_magnitude(M, N, K):
     x64, w64, want, total = x64[even], w64[kept], want[even][:, kept], total[even][:, kept]
     loose = 2.0 ** -39 * (np.abs(x64).max(1)[:, None] * np.abs(w64).sum(1)[None] + np.abs(x64).sum(1)[:, None] * np.abs(w64).max(1)[None])
     assert_within(B.linear(x, w), want, (K + 16) * 2.0 ** -24 * total + loose + TINY["float32"])
+
+
+@pytest.mark.gpu
+def test_large_fp32_products_of_values_that_are_not_finite():
+    """Two fp16 parts: infinities and NaN give what fp32 arithmetic gives in their rows and columns, and change nothing elsewhere."""
+    torch = _torch()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    x = torch.randn((2200, 4600), generator=g, device="cuda")
+    w = torch.randn((1000, 4600), generator=g, device="cuda")
+    w[:, 9] = torch.where(torch.arange(1000, device="cuda") % 2 == 0, 0.0, -2.0)
+    clean = B.linear(x, w)
+    x[5, 9] = float("inf")
+    x[300, 77] = float("nan")
+    w[44, 3] = float("-inf")
+    y = B.linear(x, w)
+    assert bool(torch.isnan(y[5, 0::2][torch.arange(500, device="cuda") != 22]).all()) and bool((y[5, 1::2] == float("-inf")).all())
+    assert bool(torch.isnan(y[300]).all()) and bool(torch.isinf(y[6:300, 44]).all())
+    rows = torch.ones(2200, dtype=torch.bool, device="cuda")
+    rows[[5, 300]] = False
+    columns = torch.ones(1000, dtype=torch.bool, device="cuda")
+    columns[44] = False
+    assert torch.equal(y[rows][:, columns], clean[rows][:, columns])
+    # the largest finite values, and sums beyond the type
+    x[:] = torch.finfo(torch.float32).max
+    w[:] = 0
+    w[:, 0] = 1
+    w[3, 1] = 1
+    y = B.linear(x, w)
+    assert bool((y[:, :3] == x[0, 0]).all()) and bool((y[:, 3] == float("inf")).all())
