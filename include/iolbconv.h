@@ -231,8 +231,10 @@ int iolb_winograd_matrices(int m, float* A, float* L, float* B);
  * backward pass needs held in 8 bits.  Tensors are fp32, fp16 or bf16, all of a call of one type, and hold rows of
  * contiguous values whose starts are ld... values apart (at least the row's length; any alignment of the type's own size).  Sums are
  * held in fp32 and rounded once to the tensor's type.  fp32 operands go to the matrix cores as the sum of three bf16 parts, which
- * hold them to the last bit from 2^-110 up; below that the absolute error stays under 2^-133.  Infinities and NaN give
- * what fp32 arithmetic gives.  Extents may be zero: no output then, or (a sum over nothing) bias and residual alone.
+ * hold them to the last bit from 2^-110 up; below that the absolute error stays under 2^-133.  Large fp32 products of iolb_linear (M above
+ * 512, M N K at least 3e9) take two fp16 parts instead, which hold a value to 2^-22 of itself or 2^-40 of its row's largest, whichever
+ * is more; where an operand has a row of which more than one in 64 non-zero values lies below 2^-20 of the row's largest, the call
+ * finds that on the device and takes three bf16 parts after all.  Infinities and NaN give what fp32 arithmetic gives.  Extents may be zero: no output then, or (a sum over nothing) bias and residual alone.
  * These calls allocate nothing: scratch is the caller's, 256-byte aligned, at least as large as the ..._workspace_bytes
  * call of the same arguments says (it may be 0: NULL then).  It depends on addresses too: tensors whose rows
  * do not start on 16 bytes are copied.  They enqueue kernels only, on the stream of iolb_set_stream, and can be captured. */
