@@ -2,8 +2,9 @@
 //
 // Products run on the 16-bit matrix cores with sums in fp32.  bf16 and fp16 tensors go there as they are; an fp32 tensor as
 // the sum of three bf16 parts, x = h + m + l, eight significant bits each, of whose nine products the six that reach fp32
-// precision are taken (the other three are below 2^-24 of the product), smallest first.  A part is a "plane" of its own
-// in memory, and a product of two planes a "segment" of the sum.
+// precision are taken (the other three are below 2^-24 of the product), smallest first; in large forward products as two fp16 parts
+// scaled by rows, of which three products are taken (dense_halves.hip).  A part is a "plane" of its own in memory, and a product of
+// two planes a "segment" of the sum.
 //
 // Not finite: h of an infinity or NaN is that value, m and l are zero.  h h then gives what fp32 arithmetic gives, while
 // the other products may turn 0 x inf into NaN or add infinities of the wrong sign; so h h comes last, and sums that are not

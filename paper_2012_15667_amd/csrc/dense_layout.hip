@@ -9,7 +9,8 @@ namespace {
 // ---- layout -----------------------------------------------------------------------------------------
 // A workgroup takes 64 x 64 values: a thread reads eight neighbouring columns of two rows, forms the values (a tensor's, a
 // checkpoint's through an activation, or a gradient's through the activation's slope), and writes them as planes along the
-// rows; the transposed planes go through LDS, and the column sums (the bias gradient's first stage) too.
+// rows; the transposed planes go through LDS, and the column sums (the bias gradient's first stage) too.  The three layouts of a bf16
+// gradient, M 8192, N 8192, K 4096 (dz both ways, the input and the weights transposed): 158 us in one launch, 587 MB, 3.7 TB/s.
 constexpr int PITCH = 72;                          // 16-bit values of a transposed row in LDS: 144 bytes
 
 template <class T>
@@ -181,7 +182,8 @@ dense_colsum_kernel(const float* colsum, int blocks, int cols, void* out)
 }
 
 // ---- checkpoints -------------------------------------------------------------------------------------
-// Four lanes share a block of 32, eight values each.  A workgroup covers `wide` threads of a row and 256 / wide rows.
+// Four lanes share a block of 32, eight values each.  A workgroup covers `wide` threads of a row and 256 / wide rows.  Bound by memory:
+// 16384 x 8192 bf16 81 us, 5.0 TB/s.
 template <int DT>
 __global__ void __launch_bounds__(256)
 checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t* q, uint8_t* e, int wide_log)
@@ -211,7 +213,8 @@ checkpoint_pack_kernel(const void* x, long long ldx, int rows, int cols, int8_t*
     }
 }
 
-// Two lanes share a block, sixteen codes each, so that a lane's load is 16 bytes too.
+// Two lanes share a block, sixteen codes each, so that a lane's load is 16 bytes too.  16384 x 8192 to bf16: 84 us, 4.8 TB/s; through gelu 101, where
+// the vector instructions count too.  (Eight codes a lane 107 without an activation, four rows of a lane at a time 156.)
 template <int DT>
 __global__ void __launch_bounds__(256)
 checkpoint_unpack_kernel(const int8_t* q, const uint8_t* e, int rows, int cols, int act, void* y, long long ldy, int wide_log)
@@ -253,7 +256,6 @@ RowGrid row_grid(int rows, int cols, long long each)
     const long long gy = (rows + per - 1) / per;
     return {dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), wide_log};
 }
-
 
 }  // namespace
 

@@ -3,6 +3,10 @@
 // straight to the registers of the one wave that multiplies it, as the caller holds it; fp32 values are cut into their three
 // bf16 parts there (5.5 vector instructions a value).
 //
+// Measured, kernel alone: 1 x 4096 -> 4096 bf16 8.2 us (4.1 TB/s of weights), 1 x 512 -> 1000 fp32 4.7 us (latency: the launch, one trip to memory,
+// the waves' sums through LDS); 64 x 25088 -> 4096 fp32 96 us and a join of 5 (4.3 TB/s; its six bf16 products would take 66 us at the large
+// products' rate); across, 64 x 4096 -> 25088 fp32 113 us and a join of 8 (3.7 TB/s: a step waits for its own loads, see `alone` below).
+//
 // Infinities, NaN and values whose leading part rounds to infinity make sums that are not finite; a workgroup that meets one
 // takes its sums again, now with parts that are zero beside such values, and the product of leading parts last (dense.h).
 #include "dense_math.h"
@@ -160,7 +164,8 @@ __device__ __forceinline__ void keep_partial(const DenseProduct& p, int split, i
 
 // ---- up to sixteen rows: the eight waves of a workgroup share K of sixteen columns of C -----------------------
 // A step of a wave is 64 k: of B sixteen rows (16 lanes) by 64 or 128 neighbouring bytes at a time (4 lanes), of A likewise, from L2.
-// The waves take the steps in turn, so that a workgroup reads runs of 8 * 64 values of a row.
+// The waves take the steps in turn, so that a workgroup reads runs of 8 * 64 values of a row.  Sixteen waves are no faster, and neither are steps
+// three, four or six ahead.
 template <int DT, bool ODD>
 __global__ void __launch_bounds__(512)
 dense_few_kernel(DenseProduct p, int join)
@@ -246,9 +251,9 @@ dense_few_kernel(DenseProduct p, int join)
 
 // ---- more rows: A through LDS, 64 rows at a time, each wave its own columns of C -------------------------------------------------
 // A step is 64 k.  A's rows are cut into parts once for the workgroup and lie in two LDS buffers in turn; the loads of A two steps
-// ahead and of B one or two are kept in registers.  Along (not across): a wave takes sixteen rows of B.  Across: 64 columns of
-// B, four neighbours a lane, so that the eight rows a lane reads are its operand's eight k for each of the four without
-// an exchange between lanes.
+// ahead and of B one are kept in registers.  Along (not across): a wave takes sixteen rows of B.  Across: 32 columns of
+// B, two neighbours a lane, so that the eight rows a lane reads are its operand's eight k for each of the two without
+// an exchange between lanes (four neighbours a lane read longer runs, but leave half as many workgroups to a compute unit: slower).
 constexpr int NC = 2;                                  // columns of B that a lane reads side by side, across
 constexpr int rows_waves(bool across) { return across ? 4 : 8; }
 constexpr int rows_columns(bool across) { return across ? 4 * 16 * NC : 128; }            // of a workgroup
@@ -292,7 +297,7 @@ dense_rows_kernel(DenseProduct p, int join)
         constexpr int MODE = decltype(mode)::value, KIND = decltype(kind)::value;
         constexpr bool SAFE = MODE != ALL_PRODUCTS;
         if (from >= to) return;
-        // ---- B in registers: 32 k of sixteen rows, or of 64 columns
+        // ---- B in registers: 32 k of sixteen rows, or of 32 columns
         struct Unit { Raw<DT> along; unsigned across[8][ACROSS ? WORDS : 1]; };
         Unit ub[UNITS];
         auto load_b = [&](int k, Unit& u) __attribute__((always_inline)) {                     // k: of the unit's first
@@ -465,8 +470,9 @@ dense_rows_kernel(DenseProduct p, int join)
 // ---- products of which the summed axis is short (the weights' gradient of up to 64 rows): bound by writing C ---------
 // A is [M][K], B [N][K], K at most 64, both in planes.  A wave keeps sixteen NT rows of A in registers and goes along a run of columns: their
 // fragments of B come from L2, two groups of 32 ahead, there is neither LDS nor a barrier, and the stores stream.  A lane ends with
-// neighbouring columns of one row: 16 bytes of the output at a time (16-bit types: rows r of two tiles are columns 8 (r / 4) + r % 4 and
+// neighbouring columns of one row, so it writes 16 bytes of the output at a time (16-bit types: rows r of two tiles are columns 8 (r / 4) + r % 4 and
 // four further).
+// 4096 x 25088 in fp32 from 64 rows (411 MB written): 109 us, 3.8 TB/s; a fill of as much takes 62.
 template <int DT, int PB, int KK>
 __global__ void __launch_bounds__(256, PB == 3 ? 1 : KK == 2 ? 2 : 3)
 dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
@@ -612,7 +618,7 @@ hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
 
 // How the steps are dealt out: the least modelled time.  Up to sixteen rows: `splits` workgroups share the K of sixteen columns.  Beyond: the steps of
 // all blocks of columns, one after the other, are cut into equal runs, one a workgroup, so that every compute unit has the same to do (with
-// whole shares of K, 196 blocks of 25088 columns left some with twice the others': 117 us at 64 rows, 87 dealt out evenly).  What a step
+// whole shares of K, 196 blocks of 25088 columns left some with twice the others': 64 x 4096 -> 25088 fp32 across 117 us, dealt out evenly 113).  What a step
 // takes lies between its share of the memory's bandwidth (4.9 TB/s) and its own latency `alone`; one goes before the first.  A second launch
 // adds the partial sums, which go through memory.  Fitted to a sweep of 22 products of 1 to 64 rows and 0.5 M to 103 M weights, 1 to 64 shares.
 DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint)

@@ -5,7 +5,12 @@
 // way while stage t is multiplied.  A row of a stage is 128 bytes, eight pieces of 16; piece c of row r lies in place
 // c ^ (r & 7), so that the sixteen rows a fragment read touches fall on different banks.  The LDS end of such a load is fixed by
 // the lane, so it is the address in memory that is exchanged.  Products are taken with B as the first operand: a lane then holds
-// four neighbouring columns of one row, which it finishes and stores at once.
+// four neighbouring columns of one row.
+//
+// Measured: 8192 x 16384 -> 4096 fp16 898-922 us (1190-1220 TFLOP/s; bf16 and fp16 products of 8192 x 8192 x 8192 by the vendor's library reach 1235 and 1390 on
+// the card), 8192 x 4096 -> 16384 bf16 862 us, with gelu 911, 8192 x 4096 -> 8192 bf16 406 (1350 TFLOP/s): bound by the matrix cores at the clock
+// that the card's power leaves them.  With every stage read from the same addresses, so that all loads come from L2, they
+// take 4 to 10% less.  Small ones, 1023 x 1001 -> 777 fp16 13.3 us, wait for their chain of stages.
 #include "dense_math.h"
 #include "kernels.h"
 #include "lds_dma.h"
@@ -39,7 +44,7 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
     const int wm = wave / WN, wn = wave % WN;
 
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of neighbouring tiles, in bands of eight tile rows, so that
-    // its L2 holds the operands of a compact patch.
+    // its L2 holds the operands of a compact patch.  (Bands of four and six rows are within 2%, of 16 and 32 slower.)
     int bm, bn;
     {
         const int n = gridDim.x, q = n >> 3, r = n & 7, xcd = blockIdx.x & 7;
@@ -292,7 +297,8 @@ hipError_t launch_tile(const DenseProduct& p, int tile, hipStream_t st)
 // the model's pick is within 8% of the best measured one.  Examples (us, bf16, 256 x 256 / 128 x 128 / 64 x 128 / 64 x 64, each with its
 // best share of K): 128 x 4096 x 4096 24.9 / 19.0 / 17.7 / 17.4, 1024 x 1024 x 1024 26.7 / 14.6 / 11.4 / 9.7, 2048 x 4096 x 4096 79 / 69 / 94 / 100.
 // Measured and not taken: three and four buffers for the small blocks, two workgroups of 128 x 128 with four (more stages on their way, fewer
-// workgroups on a compute unit): 2048 x 2048 x 2048 27.0 -> 28.2, 1024 x 4096 x 1024 15.8 -> 16.7, 4096 x 4096 x 256 20.1 -> 28.
+// workgroups on a compute unit): 2048 x 2048 x 2048 27.0 -> 28.2, 1024 x 4096 x 1024 15.8 -> 16.7, 4096 x 4096 x 256 20.1 -> 28; a third buffer
+// of A for the largest block (all of the LDS): 8192 x 16384 x 4096 862 -> 911; a higher wave priority around the products: 2 to 3% slower.
 DenseTilePlan dense_tile_plan(int M, int N, int K, int segments)
 {
     struct Block { int m, n, alone, each; };
