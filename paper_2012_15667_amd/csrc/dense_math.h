@@ -291,18 +291,6 @@ __device__ __forceinline__ void store_columns(const DenseFinish& f, int m, int n
     }
 }
 
-// All W of them, in one piece, as they are.
-template <int DT, int W>
-__device__ __forceinline__ void store_whole(const DenseFinish& f, int m, int n, const float (&z)[W])
-{
-    typedef typename DenseType<DT>::type T;
-    typedef typename Piece<T, W>::type TW;
-    TW t;
-#pragma unroll
-    for (int i = 0; i < W; ++i) t[i] = (T)z[i];
-    *reinterpret_cast<TW*>(static_cast<T*>(f.y) + m * f.ldy + n) = t;
-}
-
 // Four columns without a checkpoint, for a wave that holds them in one lane.
 template <int DT>
 __device__ __forceinline__ void finish_four(const DenseFinish& f, int m, int n, const float (&bias)[4], const f32x4& sum)

@@ -469,15 +469,29 @@ dense_rows_kernel(DenseProduct p, int join)
 
 // ---- products of which the summed axis is short (the weights' gradient of up to 64 rows): bound by writing C ---------
 // A is [M][K], B [N][K], K at most 64, both in planes.  A wave keeps sixteen NT rows of A in registers and goes along a run of columns: their
-// fragments of B come from L2, two groups of 32 ahead, there is neither LDS nor a barrier, and the stores stream.  A lane ends with
-// neighbouring columns of one row, so it writes 16 bytes of the output at a time (16-bit types: rows r of two tiles are columns 8 (r / 4) + r % 4 and
-// four further).
-// 4096 x 25088 in fp32 from 64 rows (411 MB written): 109 us, 3.8 TB/s; a fill of as much takes 62.
+// fragments of B come from L2, 64 columns ahead, there is neither LDS nor a barrier, and the stores stream.  A lane ends with 16 bytes of
+// neighbouring columns of one row (16-bit types: rows r of two tiles are columns 8 (r / 4) + r % 4 and four further), four lanes with 64; the lanes of
+// two rows exchange pieces, so that a store writes whole lines of 128 bytes.
+// Calls with their layouts, 4096 x 25088 from 64 rows, fp32 (411 MB written, a fill takes 62 us): 92 us, with stores of 64 bytes 99; bf16 59 of 63.
+// Neighbouring lanes: the even one keeps a and gives b, the odd one keeps b and gives a; a is of the even lane's row then, b of the odd one's.
+__device__ __forceinline__ void exchange(u32x4& a, u32x4& b, bool odd)
+{
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const unsigned give = odd ? a[r] : b[r];
+        const unsigned got = (unsigned)__builtin_amdgcn_mov_dpp((int)give, 0xB1, 0xf, 0xf, true);      // (lane ^ 1's)
+        a[r] = odd ? got : a[r];
+        b[r] = odd ? b[r] : got;
+    }
+}
+
 template <int DT, int PB, int KK>
 __global__ void __launch_bounds__(256, PB == 3 ? 1 : KK == 2 ? 2 : 3)
 dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
 {
-    constexpr int PA = DT == IOLB_F32 ? 3 : 1, NT = DT == IOLB_F32 ? 2 : 4, AHEAD = 2;
+    constexpr int PA = DT == IOLB_F32 ? 3 : 1, NT = DT == IOLB_F32 ? 2 : 4, AHEAD = DT == IOLB_F32 ? 2 : 1;
+    constexpr int TILES = DT == IOLB_F32 ? 2 : 4, COLUMNS = 16 * TILES, EACH = DT == IOLB_F32 ? 4 : 8;       // EACH: columns of a piece of 16 bytes
+    typedef typename DenseType<DT>::type T;
     const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4;
     const int m0 = (blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 16 * NT;
     if (m0 >= p.M) return;
@@ -494,12 +508,12 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
                 fa[t][kk][q] = k < p.K ? *reinterpret_cast<const u32x4*>(a + q * plane_a + (row < p.M ? row : p.M - 1) * p.lda + k) : u32x4{0, 0, 0, 0};
             }
     const int n_from = blockIdx.x * p.per, n_to = n_from + p.per < p.N ? n_from + p.per : p.N;
-    u32x4 fb[AHEAD][2][KK][PB];
+    u32x4 fb[AHEAD][TILES][KK][PB];
     // (pieces beyond the summed axis: zero in A, any finite values here, so those of its first piece; B's rows beyond its last: that one's)
-    auto load = [&](int n, u32x4 (&to)[2][KK][PB]) __attribute__((always_inline)) {
+    auto load = [&](int n, u32x4 (&to)[TILES][KK][PB]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int col = n + (DT == IOLB_F32 ? 16 * j + l16 : 8 * (l16 >> 2) + 4 * j + (l16 & 3));
+        for (int j = 0; j < TILES; ++j) {
+            const int col = n + (DT == IOLB_F32 ? 16 * j + l16 : 32 * (j / 2) + 8 * (l16 >> 2) + 4 * (j % 2) + (l16 & 3));
             const unsigned short* const row = b + (col < p.N ? col : p.N - 1) * p.ldb;
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
@@ -510,20 +524,16 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
         }
     };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) load(n_from + 32 * i, fb[i]);
+    for (int i = 0; i < AHEAD; ++i) load(n_from + COLUMNS * i, fb[i]);
     // EVERY: every store is a 16-byte piece that exists.  (Under conditions the stores' number is not known, and a wait for a load would be
     // one for the stores before it.)
     auto run = [&](auto every) __attribute__((always_inline)) {
     constexpr bool EVERY = decltype(every)::value;
-    auto store = [&](int m, int col, auto& z) __attribute__((always_inline)) {
-        if constexpr (EVERY) store_whole<DT>(p.f, m, col, z);
-        else if (m < p.M && col < p.N) store_columns<DT, IOLB_ACT_NONE>(p.f, m, col, z);
-    };
-    for (int n0 = n_from; n0 < n_to; n0 += 32 * AHEAD) {
+    for (int n0 = n_from; n0 < n_to; n0 += COLUMNS * AHEAD) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int n = n0 + 32 * i;
-            f32x4 c[NT][2] = {};
+            const int n = n0 + COLUMNS * i;
+            f32x4 c[NT][TILES] = {};
             constexpr int part_a[6] = {2, 0, 1, 1, 0, 0}, part_b[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
             for (int q = 0; q < 6; ++q) {
@@ -532,41 +542,51 @@ dense_outer_kernel(DenseProduct p, long long plane_a, long long plane_b)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) clear_not_finite(c[t][j]);
+                        for (int j = 0; j < TILES; ++j) clear_not_finite(c[t][j]);
                 }
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
+                        for (int j = 0; j < TILES; ++j)
                             c[t][j] = multiply<DT == IOLB_F16>(fb[i][j][kk][part_b[q]], fa[t][kk][part_a[q]], c[t][j]);
             }
-            load(n + 32 * AHEAD < n_to ? n + 32 * AHEAD : n_from, fb[i]);
+            load(n + COLUMNS * AHEAD < n_to ? n + COLUMNS * AHEAD : n_from, fb[i]);
             if (EVERY || n < n_to) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const int m = m0 + 16 * t + l16;
-                    if constexpr (DT == IOLB_F32) {
+                    const auto value = [&](int piece, int v) { return c[t][DT == IOLB_F32 ? piece : 2 * piece + v / 4][v % 4]; };
+                    if constexpr (EVERY) {
+                        typedef typename Piece<T, EACH>::type TW;
+                        u32x4 z[2];
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            float z[4] = {c[t][j][0], c[t][j][1], c[t][j][2], c[t][j][3]};
-                            const int col = n + 16 * j + 4 * grp;
-                            store(m, col, z);
+                        for (int g = 0; g < 2; ++g) {
+                            TW w;
+#pragma unroll
+                            for (int v = 0; v < EACH; ++v) w[v] = (T)value(g, v);
+                            z[g] = __builtin_bit_cast(u32x4, w);
                         }
+                        exchange(z[0], z[1], l16 & 1);
+                        T* const to = static_cast<T*>(p.f.y) + (m0 + 16 * t + (l16 & ~1)) * p.f.ldy + n + EACH * (4 * (l16 & 1) + grp);
+                        *reinterpret_cast<TW*>(to) = __builtin_bit_cast(TW, z[0]);
+                        *reinterpret_cast<TW*>(to + p.f.ldy) = __builtin_bit_cast(TW, z[1]);
                     } else {
-                        float z[8];
 #pragma unroll
-                        for (int v = 0; v < 8; ++v) z[v] = c[t][v / 4][v % 4];
-                        const int col = n + 8 * grp;
-                        store(m, col, z);
+                        for (int g = 0; g < 2; ++g) {
+                            const int m = m0 + 16 * t + l16, col = n + EACH * (4 * g + grp);
+                            float z[EACH];
+#pragma unroll
+                            for (int v = 0; v < EACH; ++v) z[v] = value(g, v);
+                            if (m < p.M && col < p.N) store_columns<DT, IOLB_ACT_NONE>(p.f, m, col, z);
+                        }
                     }
                 }
             }
         }
     }
     };
-    if (m0 + 16 * NT <= p.M && (n_to - n_from) % (32 * AHEAD) == 0) run(std::true_type{});
+    if (m0 + 16 * NT <= p.M && (n_to - n_from) % (COLUMNS * AHEAD) == 0) run(std::true_type{});
     else run(std::false_type{});
 }
 
