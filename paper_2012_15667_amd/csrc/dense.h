@@ -65,7 +65,7 @@ hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipS
 // set (always with splits > 1 or a checkpoint).
 constexpr int DENSE_FEW = 16;               // rows of the kernel for the fewest
 // Whether a product with M rows and an N x K weight runs on them, or on the product kernel with its operands laid out.  fp32: the layout of the
-// weights in parts costs more than all of the product up to some hundred rows (4096 x 4096, us: 64 rows 24 against 69, 128 36 / 78, 256 62 / 97;
+// weights in parts costs more than all of the product up to some hundred rows (4096 x 4096, us: 64 rows 24 against 69, 128 33 / 77, 256 54 / 84, 512 93 / 110;
 // 512 x 512, 256 rows 12 / 16).  Their rows are read in pieces of eight values, or two across: shorter ones are left to the product kernel.  16-bit types: the product kernel reads weights in place (4096 x 4096, 20 rows 15.7 against 12.6), but across
 // they would be transposed: 4096 x 4096, 64 rows 15.5 against 28, 128 24.8 / 31, 256 40 / 37; 1000 x 2048, 20 rows 13.1 / 13.2, 64 17.9 / 14.2.
 inline bool dense_rows_wanted(long long M, long long N, long long K, int dtype, bool across)

@@ -251,26 +251,28 @@ dense_few_kernel(DenseProduct p, int join)
 
 // ---- more rows: A through LDS, 64 rows at a time, each wave its own columns of C -------------------------------------------------
 // A step is 64 k.  A's rows are cut into parts once for the workgroup and lie in two LDS buffers in turn; the loads of A two steps
-// ahead and of B one are kept in registers.  Along (not across): a wave takes sixteen rows of B.  Across: 32 columns of
+// ahead and of B one are kept in registers.  Along (not across): a wave takes sixteen or thirty-two rows of B.  Across: 32 columns of
 // B, two neighbours a lane, so that the eight rows a lane reads are its operand's eight k for each of the two without
 // an exchange between lanes (four neighbours a lane read longer runs, but leave half as many workgroups to a compute unit: slower).
 constexpr int NC = 2;                                  // columns of B that a lane reads side by side, across
 constexpr int rows_waves(bool across) { return across ? 4 : 8; }
-constexpr int rows_columns(bool across) { return across ? 4 * 16 * NC : 128; }            // of a workgroup
+// Fragments of B of a wave.  Along, each reads all of A's from LDS, and from 65 rows on that binds: with two they serve twice the columns, but there are half as
+// many workgroups.  One against two, fp32, us: 256 x 6456 -> 12224 322 / 233, 96 x 25088 -> 4096 181 / 154, 256 x 4096 -> 4096 57 / 54,
+// 128 x 4096 -> 4096 34 / 35, 256 x 2048 -> 2048 22 / 28; 64 x 6456 -> 12224 86 / 89.
+constexpr int rows_side(long long M, long long N, long long K, bool across) { return across ? NC : M > 64 && M * N * K >= 4000000000LL ? 2 : 1; }
 // workgroups on a compute unit, by their registers: of 16 rows or less, of 17 to 32, of more
 constexpr int rows_resident(int dtype, int tiles, bool across)
 {
     return across ? (dtype == IOLB_F32 ? (tiles > 2 ? 2 : 3) : (tiles > 2 ? 3 : 4)) : (tiles > 2 ? 1 : 2);
 }
 
-template <int DT, int MT, bool ACROSS>
+template <int DT, int MT, bool ACROSS, int NF>
 __global__ void __launch_bounds__(64 * rows_waves(ACROSS), rows_waves(ACROSS) * rows_resident(DT, MT, ACROSS) / 4)
 dense_rows_kernel(DenseProduct p, int join)
 {
     typedef typename DenseType<DT>::type T;
-    constexpr int WAVES = rows_waves(ACROSS), THREADS = 64 * WAVES, COLS = ACROSS ? 16 * NC : 16, PARTS = DT == IOLB_F32 ? 3 : 1;
+    constexpr int WAVES = rows_waves(ACROSS), THREADS = 64 * WAVES, COLS = 16 * NF, PARTS = DT == IOLB_F32 ? 3 : 1;
     constexpr int ROWS = 16 * MT, ITEMS = ROWS * 8, PER = (ITEMS + THREADS - 1) / THREADS;
-    constexpr int NF = ACROSS ? NC : 1;                                  // fragments of B side by side
     constexpr int WORDS = DT == IOLB_F32 ? NF : NF / 2;                   // of a lane and row of B, across
     constexpr int UNITS = 2;
     __shared__ __align__(16) u32x4 rows[2][PARTS][ROWS * 8];
@@ -287,7 +289,9 @@ dense_rows_kernel(DenseProduct p, int join)
     at_step += s1 - s0;
     const int n0 = (block * WAVES + wave) * COLS;
     // rows (columns) that do not exist are read from the last one: their sums are not stored
-    const int along_row = n0 + l16 < p.N ? n0 + l16 : p.N - 1;
+    int along_row[NF];
+#pragma unroll
+    for (int j = 0; j < NF; ++j) along_row[j] = n0 + 16 * j + l16 < p.N ? n0 + 16 * j + l16 : p.N - 1;
     const int first_col = n0 + NC * l16;
     const int whole_to = whole_steps(p, s0, s1);
     const bool edge = ACROSS && first_col == p.N - 1;            // (a pair of columns ends there: it is read one column earlier)
@@ -297,12 +301,13 @@ dense_rows_kernel(DenseProduct p, int join)
         constexpr int MODE = decltype(mode)::value, KIND = decltype(kind)::value;
         constexpr bool SAFE = MODE != ALL_PRODUCTS;
         if (from >= to) return;
-        // ---- B in registers: 32 k of sixteen rows, or of 32 columns
-        struct Unit { Raw<DT> along; unsigned across[8][ACROSS ? WORDS : 1]; };
+        // ---- B in registers: 32 k of sixteen NF rows, or of 32 columns
+        struct Unit { Raw<DT> along[ACROSS ? 1 : NF]; unsigned across[8][ACROSS ? WORDS : 1]; };
         Unit ub[UNITS];
         auto load_b = [&](int k, Unit& u) __attribute__((always_inline)) {                     // k: of the unit's first
             if constexpr (!ACROSS) {
-                load_raw<DT, KIND>(u.along, b + along_row * p.ldb + k, grp, p.K - k);
+#pragma unroll
+                for (int j = 0; j < NF; ++j) load_raw<DT, KIND>(u.along[j], b + along_row[j] * p.ldb + k, grp, p.K - k);
             } else {
                 const T* const at = b + (first_col < p.N - NC ? first_col : p.N - NC);
 #pragma unroll
@@ -370,8 +375,11 @@ dense_rows_kernel(DenseProduct p, int join)
             for (int u = 0; u < UNITS; ++u) {
                 Fragment<DT> fb[NF];
                 if constexpr (!ACROSS) {
-                    used_from_here<DT>(ub[u].along);
-                    cut<DT, SAFE>(ub[u].along, fb[0]);
+#pragma unroll
+                    for (int j = 0; j < NF; ++j) {
+                        used_from_here<DT>(ub[u].along[j]);
+                        cut<DT, SAFE>(ub[u].along[j], fb[j]);
+                    }
                 } else {
 #pragma unroll
                     for (auto& row : ub[u].across) {
@@ -449,8 +457,8 @@ dense_rows_kernel(DenseProduct p, int join)
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
             // across: column NC (4 grp + r) + j of the wave's is value r of fragment j
-            const int n = n0 + (ACROSS ? 4 * NC * grp + 4 * i : 4 * grp);
-            f32x4 c = acc[t][0];
+            const int n = n0 + (ACROSS ? 4 * NC * grp + 4 * i : 16 * i + 4 * grp);
+            f32x4 c = acc[t][i];
             if constexpr (ACROSS) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) c[v] = acc[t][(4 * i + v) % NC][(4 * i + v) / NC];
@@ -473,6 +481,7 @@ dense_rows_kernel(DenseProduct p, int join)
 // neighbouring columns of one row (16-bit types: rows r of two tiles are columns 8 (r / 4) + r % 4 and four further), four lanes with 64; the lanes of
 // two rows exchange pieces, so that a store writes whole lines of 128 bytes.
 // Calls with their layouts, 4096 x 25088 from 64 rows, fp32 (411 MB written, a fill takes 62 us): 92 us, with stores of 64 bytes 99; bf16 59 of 63.
+
 // Neighbouring lanes: the even one keeps a and gives b, the odd one keeps b and gives a; a is of the even lane's row then, b of the odd one's.
 __device__ __forceinline__ void exchange(u32x4& a, u32x4& b, bool odd)
 {
@@ -618,16 +627,17 @@ hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
         return hipGetLastError();
     }
     const int mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
-    const int cols = rows_columns(across), threads = 64 * rows_waves(across);
+    const int side = rows_side(p.M, p.N, p.K, across), cols = rows_waves(across) * 16 * side, threads = 64 * rows_waves(across);
     const long long total = (p.K + STEP - 1LL) / STEP * ((p.N + cols - 1LL) / cols);
     const dim3 grid((unsigned)((total + p.per - 1) / p.per), (p.M + 16 * mt - 1) / (16 * mt));
     if (across) {
-        if (mt == 1) dense_rows_kernel<DT, 1, true><<<grid, threads, 0, st>>>(p, join);
-        else if (mt == 2) dense_rows_kernel<DT, 2, true><<<grid, threads, 0, st>>>(p, join);
-        else dense_rows_kernel<DT, 4, true><<<grid, threads, 0, st>>>(p, join);
+        if (mt == 1) dense_rows_kernel<DT, 1, true, NC><<<grid, threads, 0, st>>>(p, join);
+        else if (mt == 2) dense_rows_kernel<DT, 2, true, NC><<<grid, threads, 0, st>>>(p, join);
+        else dense_rows_kernel<DT, 4, true, NC><<<grid, threads, 0, st>>>(p, join);
     } else if constexpr (DT == IOLB_F32) {
-        if (mt <= 2) dense_rows_kernel<DT, 2, false><<<grid, threads, 0, st>>>(p, join);
-        else dense_rows_kernel<DT, 4, false><<<grid, threads, 0, st>>>(p, join);
+        if (mt <= 2) dense_rows_kernel<DT, 2, false, 1><<<grid, threads, 0, st>>>(p, join);
+        else if (side == 1) dense_rows_kernel<DT, 4, false, 1><<<grid, threads, 0, st>>>(p, join);
+        else dense_rows_kernel<DT, 4, false, 2><<<grid, threads, 0, st>>>(p, join);
     } else {
         return hipErrorInvalidValue;                  // 16-bit types, along: up to DENSE_FEW rows only
     }
@@ -645,8 +655,8 @@ DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool 
 {
     const bool few = !across && M <= DENSE_FEW, wide = dtype == IOLB_F32;
     const int tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    const double alone = few ? (wide ? 1000 : 600) : !across ? 1000 : !wide ? 550 : tiles == 1 ? 1050 : tiles == 2 ? 1350 : 1900;
-    const long long steps = (K + STEP - 1) / STEP, cols = few ? 16 : rows_columns(across);
+    const double alone = few ? (wide ? 1000 : 600) : !across ? (rows_side(M, N, K, false) == 2 ? 1600 : 1000) : !wide ? 550 : tiles == 1 ? 1050 : tiles == 2 ? 1350 : 1900;
+    const long long steps = (K + STEP - 1) / STEP, cols = few ? 16 : rows_waves(across) * 16 * rows_side(M, N, K, across);
     const long long blocks = (N + cols - 1) / cols, waves = few ? 8 : 1;           // (few: the waves share the steps)
     const long long capacity = 256 * (few ? 2 : rows_resident(dtype, tiles, across)) / ((M + 63) / 64);   // (each 64 rows have workgroups of their own)
     const double step_ns = (double)cols * waves * STEP * (wide ? 4 : 2) / 4900;                        // of one workgroup

@@ -681,3 +681,34 @@ def test_large_fp32_products_of_values_that_are_not_finite():
     w[3, 1] = 1
     y = B.linear(x, w)
     assert bool((y[:, :3] == x[0, 0]).all()) and bool((y[:, 3] == float("inf")).all())
+
+
+@pytest.mark.gpu
+def test_linear_fp32_of_some_hundred_rows():
+    """65 to 512 rows with so many products that a wave takes two groups of columns: ragged extents, each epilogue, shared K."""
+    rng = np.random.default_rng(21)
+    check_linear(rng, 70, 8011, 7205, "float32", act="gelu", residual="first", checkpoint=True, gap=3)
+    check_linear(rng, 129, 260, 120003, "float32", act="relu", residual="after")
+    check_linear(rng, 511, 16001, 490, "float32", lead=1)
+
+
+@pytest.mark.gpu
+def test_linear_fp32_of_some_hundred_rows_not_finite():
+    torch = _torch()
+    x, w = torch.ones(100, 8008, device="cuda"), torch.ones(5001, 8008, device="cuda")
+    w[1::2] = -1
+    x[7, 8001] = float("inf")
+    w[4990, 3] = float("nan")
+    w[4999, 5] = float("-inf")
+    x[9, 5] = 0
+    y = B.linear(x, w)
+    plain = torch.arange(5001, device="cuda")
+    even, odd = plain % 2 == 0, plain % 2 == 1
+    even[4990] = odd[4999] = False
+    assert bool((y[7, even] == float("inf")).all()) and bool((y[7, odd] == float("-inf")).all())
+    assert bool(torch.isnan(y[:, 4990]).all()) and bool(torch.isnan(y[9, 4999]))
+    others = torch.arange(100, device="cuda")
+    others = others[(others != 7) & (others != 9)]
+    assert bool((y[others][:, 4999] == float("-inf")).all())
+    assert bool((y[others][:, even] == 8008).all()) and bool((y[others][:, odd] == -8008).all())
+    assert bool((y[9, even] == 8007).all())
