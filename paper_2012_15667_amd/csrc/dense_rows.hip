@@ -5,7 +5,8 @@
 //
 // Measured, kernel alone: 1 x 4096 -> 4096 bf16 8.2 us (4.1 TB/s of weights), 1 x 512 -> 1000 fp32 4.7 us (latency: the launch, one trip to memory,
 // the waves' sums through LDS); 64 x 25088 -> 4096 fp32 96 us and a join of 5 (4.3 TB/s; its six bf16 products would take 66 us at the large
-// products' rate); across, 64 x 4096 -> 25088 fp32 113 us and a join of 8 (3.7 TB/s: a step waits for its own loads, see `alone` below).
+// products' rate); across, 64 x 4096 -> 25088 fp32 with its join 111-115 us (3.6 TB/s; with every load of B from the same 64 rows, in cache,
+// it took 107 of 116: matrix and vector instructions bind it).
 //
 // Infinities, NaN and values whose leading part rounds to infinity make sums that are not finite; a workgroup that meets one
 // takes its sums again, now with parts that are zero beside such values, and the product of leading parts last (dense.h).
@@ -295,6 +296,8 @@ dense_rows_kernel(DenseProduct p, int join)
     const int first_col = n0 + NC * l16;
     const int whole_to = whole_steps(p, s0, s1);
     const bool edge = ACROSS && first_col == p.N - 1;            // (a pair of columns ends there: it is read one column earlier)
+    const T* const across_col = ACROSS ? b + (first_col < p.N - NC ? first_col : p.N - NC) : b;
+    const T* const across_at = across_col + 8 * grp * p.ldb;
     f32x4 acc[MT][NF];
 
     auto range = [&](auto mode, auto kind, int from, int to) __attribute__((always_inline)) {
@@ -309,11 +312,12 @@ dense_rows_kernel(DenseProduct p, int join)
 #pragma unroll
                 for (int j = 0; j < NF; ++j) load_raw<DT, KIND>(u.along[j], b + along_row[j] * p.ldb + k, grp, p.K - k);
             } else {
-                const T* const at = b + (first_col < p.N - NC ? first_col : p.N - NC);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int row = k + 8 * grp + i;
-                    const auto t = words_at<WORDS>(at + (KIND == WHOLE || row < p.K ? row : p.K - 1) * p.ldb);
+                    // (whole: a lane's part of the address stays, the step's part is the same for all lanes)
+                    const T* const at = KIND == WHOLE ? across_at + (long long)(k + i) * p.ldb : across_col + (row < p.K ? row : p.K - 1) * p.ldb;
+                    const auto t = words_at<WORDS>(at);
 #pragma unroll
                     for (int w = 0; w < WORDS; ++w) u.across[i][w] = KIND == WHOLE || row < p.K ? t[w] : 0u;
                 }
@@ -404,22 +408,18 @@ dense_rows_kernel(DenseProduct p, int join)
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 load_b(after * STEP + 32 * u, ub[u]);
-                __builtin_amdgcn_sched_barrier(0);
-                constexpr int TOGETHER = ACROSS ? 1 : MT;     // rows' fragments in registers at a time
+                if constexpr (!ACROSS) __builtin_amdgcn_sched_barrier(0);
+                Fragment<DT> fa[MT];
+                f32x4* sum[MT * NF];
 #pragma unroll
-                for (int t = 0; t < MT; t += TOGETHER) {
-                    Fragment<DT> fa[TOGETHER];
-                    f32x4* sum[TOGETHER * NF];
+                for (int i = 0; i < MT; ++i) {
+                    const int row = 16 * i + l16;
 #pragma unroll
-                    for (int i = 0; i < TOGETHER; ++i) {
-                        const int row = 16 * (t + i) + l16;
+                    for (int q = 0; q < PARTS; ++q) fa[i].part[q] = rows[s & 1][q][row * 8 + place(row, 4 * u + grp)];
 #pragma unroll
-                        for (int q = 0; q < PARTS; ++q) fa[i].part[q] = rows[s & 1][q][row * 8 + place(row, 4 * u + grp)];
-#pragma unroll
-                        for (int j = 0; j < NF; ++j) sum[j * TOGETHER + i] = &acc[t + i][j];
-                    }
-                    multiply_parts<DT, MODE, TOGETHER, NF>(fb, fa, sum);
+                    for (int j = 0; j < NF; ++j) sum[j * MT + i] = &acc[i][j];
                 }
+                multiply_parts<DT, MODE, MT, NF>(fb, fa, sum);
             }
         }
     };
