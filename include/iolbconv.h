@@ -232,9 +232,9 @@ int iolb_winograd_matrices(int m, float* A, float* L, float* B);
  * contiguous values whose starts are ld... values apart (at least the row's length; any alignment of the type's own size).  Sums are
  * held in fp32 and rounded once to the tensor's type.  fp32 operands go to the matrix cores as the sum of three bf16 parts, which
  * hold them to the last bit from 2^-110 up; below that the absolute error stays under 2^-133.  Large fp32 products of iolb_linear (M above
- * 512, M N K at least 3e9) take two fp16 parts instead, which hold a value to 2^-22 of itself or 2^-40 of its row's largest, whichever
- * is more; where an operand has a row of which more than one in 64 non-zero values lies below 2^-20 of the row's largest, the call
- * finds that on the device and takes three bf16 parts after all.  Infinities and NaN give what fp32 arithmetic gives.  Extents may be zero: no output then, or (a sum over nothing) bias and residual alone.
+ * 512 or K below 8, M N K at least 3e9) take two fp16 parts instead, which hold a value to 2^-22 of itself unless it is far below its row's
+ * largest.  Every sum is within 2^-19 of its sum of magnitudes beside the rounding of fp32 sums: where an operand has rows with many such
+ * values, or sums are too small for what was cut, the call finds that on the device and takes the product, or those sums, in full.  Infinities and NaN give what fp32 arithmetic gives.  Extents may be zero: no output then, or (a sum over nothing) bias and residual alone.
  * These calls allocate nothing: scratch is the caller's, 256-byte aligned, at least as large as the ..._workspace_bytes
  * call of the same arguments says (it may be 0: NULL then).  It depends on addresses too: tensors whose rows
  * do not start on 16 bytes are copied.  They enqueue kernels only, on the stream of iolb_set_stream, and can be captured. */

@@ -34,6 +34,9 @@ struct DenseFinish {
     int act, first;                         // first: the residual is added before the activation
 };
 
+// A row in two fp16 parts: its values are those of the parts times 2^exponent; what the parts leave out, scaled like them (dense_halves.hip).
+struct DenseScale { int exponent; float lost; };
+
 // C[m][n] = sum over segments and k of A[m][k] B[n][k]; both operands contiguous along k, 16-byte aligned rows.
 struct DenseProduct {
     const void* a;
@@ -46,8 +49,14 @@ struct DenseProduct {
     float* partial;                         // [splits][M][N rounded up to 4]
     int block_columns, per;                 // kernels for few rows: workgroups take runs of `per` steps, block after block of columns,
                                             // and a block's pieces are as many as runs meet it (block_columns 0: `splits`)
-    const int *exps_a, *exps_b;             // fp32 operands in two fp16 parts: the exponents of their rows (null otherwise)
-    const int* uneven;                      // not null: the launch does nothing unless *uneven is `when`
+    // fp32 operands in two fp16 parts: their rows' scales (null otherwise), and the operands themselves, `values_k` long, for sums that are taken again
+    const DenseScale *scales_a, *scales_b;
+    const float *values_a, *values_b;
+    long long ld_values_a, ld_values_b;
+    int values_k;
+    // not null: [0] operands that two parts do not hold, [1] blocks of sums that were left out.  `when` 0: the launch in two parts, nothing if [0];
+    // 1: in three, nothing unless [0] or [1], and where not [0] only the blocks marked in `left`.
+    int *uneven, *left;
     int when;
     DenseFinish f;
 };
@@ -57,8 +66,10 @@ enum { DENSE_TILE_256, DENSE_TILE_128, DENSE_TILE_64x128, DENSE_TILE_64, DENSE_T
 struct DenseTilePlan { int tile, splits; };
 DenseTilePlan dense_tile_plan(int M, int N, int K, int segments);
 inline size_t dense_partial_bytes(int splits, long long M, long long N) { return (size_t)splits * M * ((N + 3) / 4 * 4) * 4; }
-// dtype: of y, bias and residual.  Operands are of the type; for fp32 they are in two fp16 parts where exps_a is given, else in three bf16 parts.
+// dtype: of y, bias and residual.  Operands are of the type; for fp32 they are in two fp16 parts where scales_a is given, else in three bf16 parts.
 hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st);
+// Blocks of sums that are finished together, marks in `left`.
+long long dense_finish_blocks(const DenseTilePlan& plan, int M, int N);
 
 // The same for few rows of A: both operands as the caller holds them (fp32 too: taken apart in the kernels), K at least 8,
 // bound by reading B.  across: B is [K][N], summed along its rows, N at least 2.  K is shared by workgroups, at most `splits` to a sum.  Sums go to `partial` if join is
@@ -111,7 +122,7 @@ struct DenseLayout {
 constexpr int MAX_LAYOUTS = 3;
 struct DenseLayouts {
     int count;
-    const int* uneven;                      // not null: the launch does nothing unless *uneven is 1
+    const int* uneven;                      // not null: the launch does nothing unless one of the two is set
     DenseLayout of[MAX_LAYOUTS];
 };
 // dtype: of src, copy and (16-bit types) the planes.
@@ -119,10 +130,16 @@ hipError_t launch_dense_layouts(int dtype, const DenseLayouts& l, hipStream_t st
 // out[c] = sum of colsum over its `blocks` rows, in `dtype`.
 hipError_t launch_dense_colsum(const float* colsum, int blocks, int cols, void* out, int dtype, hipStream_t st);
 
-// Rows of a and b, `cols` long, in two fp16 parts, planes [2][rows][pitch] (pitch: cols rounded up to 8), and their exponents; *uneven
-// becomes 1 if two parts do not hold a row well, else 0.
-hipError_t launch_dense_halves(const float* a, long long lda, int rows_a, void* planes_a, int* exps_a, const float* b, long long ldb, int rows_b,
-                               void* planes_b, int* exps_b, int cols, long long pitch, int* uneven, hipStream_t st);
+// Rows of a tensor, `cols` long, in two fp16 parts, planes [2][rows][pitch] (pitch: cols rounded up to 8), their scales;
+// uneven[0] becomes 1 if two parts do not hold a row well, else 0, and uneven[1] 0.
+struct DenseHalves {
+    const float* x;
+    long long ld;
+    int rows;
+    unsigned short* planes;
+    DenseScale* scales;
+};
+hipError_t launch_dense_halves(const DenseHalves& a, const DenseHalves& b, int cols, long long pitch, int* uneven, hipStream_t st);
 
 hipError_t launch_checkpoint_pack(const void* x, long long ldx, int rows, int cols, int dtype, int8_t* q, uint8_t* e, hipStream_t st);
 hipError_t launch_checkpoint_unpack(const int8_t* q, const uint8_t* e, int rows, int cols, int act, int dtype, void* y, long long ldy,

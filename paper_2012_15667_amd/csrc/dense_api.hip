@@ -97,40 +97,42 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     void *xp = nullptr, *wp = nullptr;
     if (!x_direct) { p.a = xp = pieces.take((size_t)planes * a.M * Kp * 2); p.lda = Kp; }
     if (!w_direct) { p.b = wp = pieces.take((size_t)planes * a.N * Kp * 2); p.ldb = Kp; }
-    const DenseTilePlan plan = dense_tile_plan(p.M, p.N, p.K, p.segments);
-    p.splits = plan.splits;
-    size_t partial = plan.splits > 1 ? dense_partial_bytes(plan.splits, a.M, a.N) : 0;
-
     // Large fp32 products in two fp16 parts, three products in place of six.  Whether an operand's rows allow it is found out on the GPU; the
-    // launches for three parts follow all the same and end at once if it does, which costs some 10 us.  Three parts against two, us:
+    // launches for three parts follow all the same and end at once if it does and no block of sums was left to them, which costs some 10 us.  Three parts against two, us:
     // 1024 x 1024 x 1024 36 / 38, 2048 x 1024 x 1024 48 / 48, 4096 x 1024 x 1024 74 / 58, 2048 x 2048 x 2048 120 / 97, 4096 x 4096 x 4096 668 / 398.
-    DenseProduct h = p;
-    DenseTilePlan plan_h{};
+    DenseProduct h{};
     const bool halves = planes == 3 && (double)a.M * a.N * a.K >= 3e9;
-    int *xe = nullptr, *we = nullptr, *uneven = nullptr;
+    const DenseTilePlan plan = dense_tile_plan(p.M, p.N, p.K, halves ? 3 : p.segments);         // (one for both: they finish the same blocks)
+    p.splits = plan.splits;
+    int* uneven = nullptr;
+    DenseHalves hx{static_cast<const float*>(a.x), a.ldx, (int)a.M}, hw{static_cast<const float*>(a.w), a.ldw, (int)a.N};
     if (halves) {
-        h.a = pieces.take((size_t)2 * a.M * Kp * 2); h.lda = Kp;
-        h.b = pieces.take((size_t)2 * a.N * Kp * 2); h.ldb = Kp;
-        h.exps_a = xe = static_cast<int*>(pieces.take((size_t)a.M * 4));
-        h.exps_b = we = static_cast<int*>(pieces.take((size_t)a.N * 4));
-        p.uneven = h.uneven = uneven = static_cast<int*>(pieces.take(4));
-        p.when = 1; h.when = 0;
+        for (DenseHalves* t : {&hx, &hw}) {
+            t->planes = static_cast<unsigned short*>(pieces.take((size_t)2 * t->rows * Kp * 2));
+            t->scales = static_cast<DenseScale*>(pieces.take((size_t)t->rows * sizeof(DenseScale)));
+        }
+        p.uneven = uneven = static_cast<int*>(pieces.take(8));
+        p.left = static_cast<int*>(pieces.take((size_t)dense_finish_blocks(plan, p.M, p.N) * 4));
+        p.when = 1;
+        h = p;
+        h.when = 0;
+        h.a = hx.planes; h.lda = Kp;
+        h.b = hw.planes; h.ldb = Kp;
+        h.scales_a = hx.scales; h.values_a = hx.x; h.ld_values_a = hx.ld;
+        h.scales_b = hw.scales; h.values_b = hw.x; h.ld_values_b = hw.ld;
+        h.values_k = (int)a.K;
         h.segments = 3;                                                    // l h, h l, h h
         h.a_plane[0] = a.M * Kp; h.a_plane[1] = h.a_plane[2] = 0;
         h.b_plane[1] = a.N * Kp; h.b_plane[0] = h.b_plane[2] = 0;
-        plan_h = dense_tile_plan(h.M, h.N, h.K, 3);
-        h.splits = plan_h.splits;
-        if (h.splits > 1) partial = std::max(partial, dense_partial_bytes(h.splits, a.M, a.N));
     }
-    if (partial) h.partial = p.partial = static_cast<float*>(pieces.take(partial));
+    if (plan.splits > 1) h.partial = p.partial = static_cast<float*>(pieces.take(dense_partial_bytes(plan.splits, a.M, a.N)));
     *need = pieces.used;
     if (!launch) return IOLB_OK;
 
     const hipStream_t st = call_stream();
     if (halves) {
-        DENSE_HIP(launch_dense_halves(static_cast<const float*>(a.x), a.ldx, (int)a.M, const_cast<void*>(h.a), xe, static_cast<const float*>(a.w), a.ldw,
-                                      (int)a.N, const_cast<void*>(h.b), we, (int)a.K, Kp, uneven, st));
-        DENSE_HIP(launch_dense_product(h, plan_h.tile, a.dtype, st));
+        DENSE_HIP(launch_dense_halves(hx, hw, (int)a.K, Kp, uneven, st));
+        DENSE_HIP(launch_dense_product(h, plan.tile, a.dtype, st));
     }
     DenseLayouts layouts{};
     layouts.uneven = uneven;

@@ -59,7 +59,7 @@ template <int DT>
 __global__ void __launch_bounds__(256)
 dense_layout_kernel(LayoutLaunch launch)
 {
-    if (launch.all.uneven && *launch.all.uneven != 1) return;
+    if (launch.all.uneven && !(launch.all.uneven[0] | launch.all.uneven[1])) return;
     typedef typename DenseType<DT>::type T;
     constexpr int PLANES = DT == IOLB_F32 ? 3 : 1;
     __shared__ __align__(16) unsigned short turned[PLANES][64][PITCH];

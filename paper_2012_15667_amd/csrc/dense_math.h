@@ -303,13 +303,36 @@ __device__ __forceinline__ void finish_four(const DenseFinish& f, int m, int n, 
     by_activation(f.act, [&](auto act) __attribute__((always_inline)) { store_columns<DT, decltype(act)::value>(f, m, n, z); });
 }
 
-// Sums of operands in two fp16 parts, scaled back.
-template <int W>
-__device__ __forceinline__ void from_halves(const DenseProduct& p, int m, int n, float (&z)[W])
+// ---- sums of operands in two fp16 parts ----------------------------------------------------------------
+__device__ __forceinline__ bool not_wanted(const DenseProduct& p)
 {
-    const int e = p.exps_a[m < p.M ? m : 0];
+    return p.uneven && ((p.uneven[0] | (p.when ? p.uneven[1] : 0)) != 0) != (p.when != 0);
+}
+
+// A scaled sum below this may owe more than 2^-20 of itself to what the parts left out: a row's loss times the other row's largest value, which is
+// below 2^15.  (A row of zeros: nothing is lost.)
+__device__ __forceinline__ float least_sum(float lost_a, float lost_b)
+{
+    return lost_a < 0.f || lost_b < 0.f ? 0.f : 0x1p35f * (lost_a + lost_b);
+}
+
+// Such a sum as fp32 products of the operands themselves: this wave's share of it among `waves`.
+__device__ __forceinline__ float share_again(const DenseProduct& p, int m, int n, int wave, int waves, int lane)
+{
+    const float *const a = p.values_a + m * p.ld_values_a, *const b = p.values_b + n * p.ld_values_b;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 256 * wave + 4 * lane; k + 4 <= p.values_k; k += 256 * waves) {
+        const u32x4 u = words_at<4>(a + k), v = words_at<4>(b + k);
 #pragma unroll
-    for (int i = 0; i < W; ++i) z[i] = ldexpf(z[i], e + p.exps_b[n + i < p.N ? n + i : 0]);
+        for (int i = 0; i < 4; ++i) s[i] = __builtin_fmaf(__uint_as_float(u[i]), __uint_as_float(v[i]), s[i]);
+    }
+    const int tail = p.values_k / 4 * 4 + lane;
+    if (wave == 0 && tail < p.values_k) s[0] = __builtin_fmaf(a[tail], b[tail], s[0]);
+    float sum = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    return sum;
 }
 
 // Columns that a lane finishes: 16 bytes of the output.

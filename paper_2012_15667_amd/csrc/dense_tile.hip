@@ -22,6 +22,30 @@ namespace {
 constexpr int STEP = 64;                               // k of a stage
 constexpr int ROW_BYTES = 2 * STEP;
 
+// Sums in two fp16 parts that may be too small for what the parts left out (dense_math.h) are taken again, up to one in 128 of a workgroup's by all of its
+// waves; blocks with more are left to three bf16 parts.
+template <int WAVES> struct Again { int m, n; float share[WAVES]; };
+constexpr int again_most(int outputs) { return outputs / 128; }
+constexpr int again_bytes(int outputs, int waves) { return 16 + again_most(outputs) * 4 * (2 + waves); }
+template <int WAVES>
+__device__ __forceinline__ float whole(const Again<WAVES>& again)
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += again.share[w];
+    return sum;
+}
+
+// How many times a block's sums go through LDS, and where the sums taken again are listed: behind them.
+constexpr int stage_bytes(int bm, int bn) { return (bm + bn) * ROW_BYTES; }
+constexpr int finish_passes(int bm, int bn) { return bm * bn * 4 > 2 * stage_bytes(bm, bn) ? 2 : 1; }
+constexpr int again_at(int bm, int bn) { return bm * bn * 4 / finish_passes(bm, bn); }
+constexpr int lds_bytes(int bm, int bn, int waves, bool halves)
+{
+    const int listed = halves ? again_at(bm, bn) + again_bytes(bm * bn, waves) : 0;
+    return listed > 2 * stage_bytes(bm, bn) ? listed : 2 * stage_bytes(bm, bn);
+}
+
 __device__ __forceinline__ void dma16(const char* base, unsigned offset, unsigned lds)
 {
     lds_dma_load_16(reinterpret_cast<const float*>(base), offset, lds);
@@ -31,10 +55,11 @@ template <bool F16, int DT, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, 2)
 dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
 {
-    if (p.uneven && *p.uneven != p.when) return;
+    if (not_wanted(p)) return;
+    constexpr bool HALVES = F16 && DT == IOLB_F32;
     constexpr int WAVES = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
     constexpr int LA = BM / 8 / WAVES, LB = BN / 8 / WAVES;           // loads of a wave and stage: 8 rows each
-    constexpr unsigned STAGE = (BM + BN) * ROW_BYTES;
+    constexpr unsigned STAGE = stage_bytes(BM, BN);
     static_assert(NI % 2 == 0 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "blocks of 32 columns, whole loads");
     extern __shared__ u32x4 lds16[];
     char* const lds = reinterpret_cast<char*>(lds16);
@@ -54,6 +79,8 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
         bm = 8 * band + in % high;
         bn = in / high;
     }
+    const int tile = bm * tiles_n + bn;
+    if (!HALVES && p.left && p.splits == 1 && !p.uneven[0] && !p.left[tile]) return;
     const int m0 = bm * BM, n0 = bn * BN;
     const int steps_all = (p.K + STEP - 1) / STEP;
     const int s0 = (int)((long long)steps_all * blockIdx.y / p.splits), s1 = (int)((long long)steps_all * (blockIdx.y + 1) / p.splits);
@@ -192,9 +219,53 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
         return;
     }
 
+    int* const again_count = reinterpret_cast<int*>(lds + again_at(BM, BN));
+    Again<WAVES>* const again = reinterpret_cast<Again<WAVES>*>(lds + again_at(BM, BN) + 16);
+    int taken_again = 0;
+    if constexpr (HALVES) {
+        const int mw = m0 + wm * (BM / WM) + l16, nw = n0 + wn * (BN / WN) + 4 * grp;
+        __syncthreads();
+        if (tid == 0) *again_count = 0;
+        __syncthreads();
+        DenseScale scale_a[MI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) scale_a[i] = p.scales_a[mw + i * 16 < p.M ? mw + i * 16 : p.M - 1];
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int n = nw + j * 16;
+            DenseScale scale_b[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) scale_b[c] = p.scales_b[n + c < p.N ? n + c : p.N - 1];
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int m = mw + i * 16;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (fabsf(acc[i][j][c]) < least_sum(scale_a[i].lost, scale_b[c].lost) && m < p.M && n + c < p.N) {
+                        const int at = atomicAdd(again_count, 1);
+                        if (at < again_most(BM * BN)) { again[at].m = m; again[at].n = n + c; }
+                    }
+                    acc[i][j][c] = ldexpf(acc[i][j][c], scale_a[i].exponent + scale_b[c].exponent);
+                }
+            }
+        }
+        __syncthreads();
+        taken_again = *again_count;
+        const bool left = taken_again > again_most(BM * BN);
+        if (tid == 0) {
+            p.left[tile] = left;
+            if (left) p.uneven[1] = 1;
+        }
+        if (left) return;
+        for (int i = 0; i < taken_again; ++i) {
+            const float share = share_again(p, again[i].m, again[i].n, wave, WAVES, lane);
+            if (lane == 0) again[i].share[wave] = share;
+        }
+    }
+
     // The sums go through LDS, as many rows at a time as fit, so that a thread finishes 16 bytes of a row and a wave's loads
     // and stores are whole rows.  16-byte piece c of row r lies at c ^ (r & 15).
-    constexpr int PASSES = BM * BN * 4 > 2 * (int)STAGE ? 2 : 1, PI = MI / PASSES, PASS_ROWS = WM * PI * 16;
+    constexpr int PASSES = finish_passes(BM, BN), PI = MI / PASSES, PASS_ROWS = WM * PI * 16;
     constexpr int W = FINISH_COLUMNS<DT>, LANES = BN / W, AT_ONCE = 64 * WAVES / LANES;   // threads of a row, rows of an iteration
     static_assert(PASS_ROWS * BN * 4 <= 2 * (int)STAGE && PASS_ROWS % AT_ONCE == 0, "a pass fits the stages' buffers");
     f32x4* const sums = reinterpret_cast<f32x4*>(lds);
@@ -212,6 +283,13 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
                 sums[r * (BN / 4) + (c ^ l16)] = acc[pass * PI + i][j];
             }
         __syncthreads();
+        if (HALVES && taken_again) {
+            for (int i = tid; i < taken_again; i += 64 * WAVES) {
+                const int m = again[i].m - m0, nn = again[i].n - n0, in = m % (BM / WM), r = m / (BM / WM) * (PI * 16) + in % (PI * 16);
+                if (in / (PI * 16) == pass) reinterpret_cast<float*>(&sums[r * (BN / 4) + (nn / 4 ^ (r & 15))])[nn & 3] = whole(again[i]);
+            }
+            __syncthreads();
+        }
         by_activation(p.f.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll 1
             for (int r = tid / LANES; r < PASS_ROWS; r += AT_ONCE) {
@@ -223,7 +301,6 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
                     for (int i = 0; i < 4; ++i) z[4 * h + i] = four[i];
                 }
                 const int m = m0 + r / (PI * 16) * (BM / WM) + pass * PI * 16 + r % (PI * 16);
-                if constexpr (F16 && DT == IOLB_F32) from_halves(p, m, n, z);
                 finish_columns<DT, decltype(act)::value>(p.f, m, n, bias, z);
             }
         });
@@ -231,17 +308,25 @@ dense_tile_kernel(DenseProduct p, int tiles_m, int tiles_n)
 }
 
 // The sums of the workgroups that shared a tile's K, added in their order, and the epilogue.
-template <int DT>
+template <int DT, bool HALVES = false>
 __global__ void __launch_bounds__(256)
 dense_join_kernel(DenseProduct p, int wide_log)
 {
-    if (p.uneven && *p.uneven != p.when) return;
+    if (not_wanted(p)) return;
+    constexpr int MOST = again_most(256 * 8);
+    __shared__ Again<4> again[HALVES ? MOST : 1];
+    __shared__ int again_count;
     const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), rows = 256 >> wide_log;
     const int n = (int)((blockIdx.x * (unsigned)wide + tx) * 8);
     const long long ld = (p.N + 3) / 4 * 4;
     by_activation(p.f.act, [&](auto act) __attribute__((always_inline)) {
         float bias[8];
         load_bias<DT>(p.f, n, bias);
+        DenseScale scale_b[HALVES ? 8 : 1];
+        if constexpr (HALVES) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) scale_b[c] = p.scales_b[n + c < p.N ? n + c : p.N - 1];
+        }
         int pieces = p.splits;
         if (p.block_columns && n < p.N) {
             // the runs that meet the block of columns n is in (all eight are in one)
@@ -249,6 +334,10 @@ dense_join_kernel(DenseProduct p, int wide_log)
             pieces = (int)((first + steps - 1) / p.per - first / p.per) + 1;
         }
         for (long long m = (long long)blockIdx.y * rows + (threadIdx.x >> wide_log); m - (threadIdx.x >> wide_log) < p.M; m += (long long)gridDim.y * rows) {
+            const long long block = (m - (threadIdx.x >> wide_log)) / rows * gridDim.x + blockIdx.x;
+            if (DT == IOLB_F32 && !HALVES && p.left && !p.uneven[0] && !p.left[block]) continue;
+            DenseScale scale_a{};
+            if constexpr (HALVES) scale_a = p.scales_a[m < p.M ? m : 0];
             float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (m < p.M && n < p.N) {
                 const float* from = p.partial + m * ld + n;
@@ -260,7 +349,42 @@ dense_join_kernel(DenseProduct p, int wide_log)
                     for (int c = 0; c < 4; ++c) { z[c] += lo[c]; z[4 + c] += hi[c]; }
                 }
             }
-            if (DT == IOLB_F32 && p.exps_a) from_halves(p, (int)(m < p.M ? m : p.M), n, z);
+            if constexpr (HALVES) {
+                unsigned small = 0;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    small |= m < p.M && n + c < p.N && fabsf(z[c]) < least_sum(scale_a.lost, scale_b[c].lost) ? 1u << c : 0u;
+                    z[c] = ldexpf(z[c], scale_a.exponent + scale_b[c].exponent);
+                }
+                const bool any = __syncthreads_or(small != 0);
+                int at = 0, count = 0;
+                if (any) {
+                    if (threadIdx.x == 0) again_count = 0;
+                    __syncthreads();
+                    if (small) {
+                        at = atomicAdd(&again_count, __builtin_popcount(small));
+                        int to = at;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            if (small >> c & 1 && to < MOST) { again[to].m = (int)m; again[to].n = n + c; ++to; }
+                    }
+                    __syncthreads();
+                    count = again_count;
+                    for (int i = 0; i < count && count <= MOST; ++i) {
+                        const float share = share_again(p, again[i].m, again[i].n, threadIdx.x >> 6, 4, threadIdx.x & 63);
+                        if ((threadIdx.x & 63) == 0) again[i].share[threadIdx.x >> 6] = share;
+                    }
+                    __syncthreads();
+                }
+                if (threadIdx.x == 0) {
+                    p.left[block] = count > MOST;
+                    if (count > MOST) p.uneven[1] = 1;
+                }
+                if (count > MOST) continue;
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (small >> c & 1) z[c] = whole(again[at++]);
+            }
             finish_columns<DT, decltype(act)::value>(p.f, (int)(m < p.M ? m : p.M), n, bias, z);
         }
     });
@@ -274,7 +398,7 @@ hipError_t launch(const DenseProduct& p, hipStream_t st)
     if (e != hipSuccess) return e;
     const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN;
     if ((long long)tm * tn > 0x7fffffffLL) return hipErrorInvalidValue;
-    kernel<<<dim3(tm * tn, p.splits), 64 * WM * WN, 2 * (BM + BN) * ROW_BYTES, st>>>(p, tm, tn);
+    kernel<<<dim3(tm * tn, p.splits), 64 * WM * WN, lds_bytes(BM, BN, WM * WN, F16 && DT == IOLB_F32), st>>>(p, tm, tn);
     return hipGetLastError();
 }
 
@@ -289,6 +413,9 @@ hipError_t launch_tile(const DenseProduct& p, int tile, hipStream_t st)
     }
 }
 
+struct Block { int m, n, alone, each; };
+constexpr Block blocks[DENSE_TILES] = {{256, 256, 1450, 1550}, {128, 128, 720, 510}, {64, 128, 570, 350}, {64, 64, 490, 190}};
+
 }  // namespace
 
 // Block and number of workgroups that share K: the least modelled time.  A stage takes a workgroup `alone` ns while it has a compute unit
@@ -301,8 +428,6 @@ hipError_t launch_tile(const DenseProduct& p, int tile, hipStream_t st)
 // of A for the largest block (all of the LDS): 8192 x 16384 x 4096 862 -> 911; a higher wave priority around the products: 2 to 3% slower.
 DenseTilePlan dense_tile_plan(int M, int N, int K, int segments)
 {
-    struct Block { int m, n, alone, each; };
-    static const Block blocks[DENSE_TILES] = {{256, 256, 1450, 1550}, {128, 128, 720, 510}, {64, 128, 570, 350}, {64, 64, 490, 190}};
     static const int shares[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
     const long long steps = (K + STEP - 1) / STEP;
     DenseTilePlan plan{DENSE_TILE_256, 1};
@@ -321,21 +446,35 @@ DenseTilePlan dense_tile_plan(int M, int N, int K, int segments)
     return plan;
 }
 
+static int join_wide_log(int N)
+{
+    int wide_log = 2;                               // threads of a row: whole blocks of 32 columns
+    while (wide_log < 8 && (8LL << wide_log) < N) ++wide_log;
+    return wide_log;
+}
+
+long long dense_finish_blocks(const DenseTilePlan& plan, int M, int N)
+{
+    const int wide_log = join_wide_log(N);
+    const long long m = plan.splits == 1 ? blocks[plan.tile].m : 256 >> wide_log, n = plan.splits == 1 ? blocks[plan.tile].n : 8LL << wide_log;
+    return ((M + m - 1) / m) * ((N + n - 1) / n);
+}
+
 hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st)
 {
-    hipError_t e = dtype == IOLB_F32 ? (p.exps_a ? launch_tile<true, IOLB_F32>(p, tile, st) : launch_tile<false, IOLB_F32>(p, tile, st))
+    hipError_t e = dtype == IOLB_F32 ? (p.scales_a ? launch_tile<true, IOLB_F32>(p, tile, st) : launch_tile<false, IOLB_F32>(p, tile, st))
                  : dtype == IOLB_F16 ? launch_tile<true, IOLB_F16>(p, tile, st) : launch_tile<false, IOLB_BF16>(p, tile, st);
     return e != hipSuccess || p.splits == 1 ? e : launch_dense_join(p, dtype, st);
 }
 
 hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st)
 {
-    int wide_log = 2;                               // threads of a row: whole blocks of 32 columns
-    while (wide_log < 8 && (8LL << wide_log) < p.N) ++wide_log;
+    const int wide_log = join_wide_log(p.N);
     const int rows = 256 >> wide_log;
     const long long gy = ((long long)p.M + rows - 1) / rows;
     const dim3 grid((unsigned)((p.N + (8LL << wide_log) - 1) / (8LL << wide_log)), (unsigned)(gy < 65535 ? gy : 65535));
-    if (dtype == IOLB_F32) dense_join_kernel<IOLB_F32><<<grid, 256, 0, st>>>(p, wide_log);
+    if (dtype == IOLB_F32 && p.scales_a) dense_join_kernel<IOLB_F32, true><<<grid, 256, 0, st>>>(p, wide_log);
+    else if (dtype == IOLB_F32) dense_join_kernel<IOLB_F32><<<grid, 256, 0, st>>>(p, wide_log);
     else if (dtype == IOLB_F16) dense_join_kernel<IOLB_F16><<<grid, 256, 0, st>>>(p, wide_log);
     else dense_join_kernel<IOLB_BF16><<<grid, 256, 0, st>>>(p, wide_log);
     return hipGetLastError();
