@@ -246,7 +246,7 @@ enum { IOLB_ACT_NONE = 0, IOLB_ACT_RELU = 1, IOLB_ACT_SILU = 2, IOLB_ACT_GELU = 
 /* z = x w^T + bias (+ residual if residual_first);  y = act(z) (+ residual otherwise).
  * x [M][K], w [N][K], bias [N] or NULL, residual [M][N] or NULL, y [M][N]; y may be the residual itself, and overlaps nothing
  * else.  zq, ze (both or neither): the checkpoint of z, from the fp32 sums, as iolb_checkpoint_pack lays it out.
- * M, N up to 2^30, K up to 2^22 (IOLB_EUNSUPPORTED beyond). */
+ * M, N up to 2^30, K up to 2^22, and no launch of 2^32 threads or more, as 2^27 columns for up to 16 rows would take (IOLB_EUNSUPPORTED beyond). */
 typedef struct iolb_linear_args {
     int64_t M, N, K;
     int32_t dtype, act, residual_first;
@@ -275,7 +275,7 @@ int iolb_checkpoint_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int6
  * dz [M][N] is the residual's gradient where that came before the activation.  Outputs are dense; each may be NULL, and w, xq
  * with it.  The slope of relu at 0 is 0, and a dy that it stops is not looked at.  16-bit types: dz is rounded to the type
  * once, before the products; db is summed before that.  Sums are added in a fixed order: equal calls give equal bits.
- * M, N up to 2^22, K up to 2^30 (IOLB_EUNSUPPORTED beyond). */
+ * M, N up to 2^22, K up to 2^30, and no launch of 2^32 threads or more (IOLB_EUNSUPPORTED beyond). */
 typedef struct iolb_linear_backward_args {
     int64_t M, N, K;
     int32_t dtype, act, x_act;

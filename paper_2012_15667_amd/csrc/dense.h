@@ -65,6 +65,7 @@ struct DenseProduct {
 enum { DENSE_TILE_256, DENSE_TILE_128, DENSE_TILE_64x128, DENSE_TILE_64, DENSE_TILES };
 struct DenseTilePlan { int tile, splits; };
 DenseTilePlan dense_tile_plan(int M, int N, int K, int segments);
+bool dense_tile_launchable(const DenseTilePlan& plan, int M, int N);           // whether a launch can count its threads
 inline size_t dense_partial_bytes(int splits, long long M, long long N) { return (size_t)splits * M * ((N + 3) / 4 * 4) * 4; }
 // dtype: of y, bias and residual.  Operands are of the type; for fp32 they are in two fp16 parts where scales_a is given, else in three bf16 parts.
 hipError_t launch_dense_product(const DenseProduct& p, int tile, int dtype, hipStream_t st);
@@ -90,6 +91,7 @@ constexpr int DENSE_OUTER_MOST = 64;
 constexpr int DENSE_ROWS_STEP = 64;         // k of a step
 struct DenseRowsPlan { int splits, per; bool join; int block_columns; };
 DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool checkpoint);
+bool dense_rows_launchable(const DenseRowsPlan& plan, int M, int N, int K, bool across);
 hipError_t launch_dense_rows(const DenseProduct& p, bool across, bool join, int dtype, hipStream_t st);
 hipError_t launch_dense_join(const DenseProduct& p, int dtype, hipStream_t st);
 // The same for a short summed axis, 0 < K <= DENSE_OUTER_MOST: operands in planes, `plane_a` and `plane_b` elements apart; no bias, activation,
@@ -139,6 +141,12 @@ struct DenseHalves {
     unsigned short* planes;
     DenseScale* scales;
 };
+// Workgroups of 256: a wave to a row, or all of it where there are few rows or they are long.
+inline bool dense_halves_by_workgroup(long long rows_a, long long rows_b, long long cols) { return rows_a + rows_b < 4096 || cols > 4096; }
+inline long long dense_halves_groups(long long rows_a, long long rows_b, long long cols)
+{
+    return dense_halves_by_workgroup(rows_a, rows_b, cols) ? rows_a + rows_b : (rows_a + 3) / 4 + (rows_b + 3) / 4;
+}
 hipError_t launch_dense_halves(const DenseHalves& a, const DenseHalves& b, int cols, long long pitch, int* uneven, hipStream_t st);
 
 hipError_t launch_checkpoint_pack(const void* x, long long ldx, int rows, int cols, int dtype, int8_t* q, uint8_t* e, hipStream_t st);

@@ -15,6 +15,9 @@ bool known_act(int act) { return act >= IOLB_ACT_NONE && act <= IOLB_ACT_GELU_TA
 int64_t size_of(int dtype) { return dtype == IOLB_F32 ? 4 : 2; }
 bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+// A launch counts its threads along an axis in 32 bits.
+bool launchable(int64_t workgroups, int threads) { return workgroups * threads <= 0xffffffffLL; }
+int64_t layout_groups(int64_t rows, int64_t cols) { return (rows + 63) / 64 * ((cols + 63) / 64); }
 
 // Hands out pieces of the caller's workspace; with no memory behind it, counts them.
 struct Pieces {
@@ -82,6 +85,7 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
         p.b = a.w; p.ldb = a.ldw;
         p.K = (int)a.K;
         const DenseRowsPlan plan = dense_rows_plan(p.M, p.N, p.K, a.dtype, false, a.zq != nullptr);
+        if (!dense_rows_launchable(plan, p.M, p.N, p.K, false)) return IOLB_EUNSUPPORTED;
         p.splits = plan.splits; p.per = plan.per; p.block_columns = plan.block_columns;
         if (plan.join) p.partial = static_cast<float*>(pieces.take(dense_partial_bytes(plan.splits, a.M, a.N)));
         *need = pieces.used;
@@ -101,8 +105,10 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     // launches for three parts follow all the same and end at once if it does and no block of sums was left to them, which costs some 10 us.  Three parts against two, us:
     // 1024 x 1024 x 1024 36 / 38, 2048 x 1024 x 1024 48 / 48, 4096 x 1024 x 1024 74 / 58, 2048 x 2048 x 2048 120 / 97, 4096 x 4096 x 4096 668 / 398.
     DenseProduct h{};
-    const bool halves = planes == 3 && (double)a.M * a.N * a.K >= 3e9;
+    const bool halves = planes == 3 && (double)a.M * a.N * a.K >= 3e9 && launchable(dense_halves_groups(a.M, a.N, a.K), 256);
     const DenseTilePlan plan = dense_tile_plan(p.M, p.N, p.K, halves ? 3 : p.segments);         // (one for both: they finish the same blocks)
+    if (!dense_tile_launchable(plan, p.M, p.N) || !launchable((x_direct ? 0 : layout_groups(a.M, a.K)) + (w_direct ? 0 : layout_groups(a.N, a.K)), 256))
+        return IOLB_EUNSUPPORTED;
     p.splits = plan.splits;
     int* uneven = nullptr;
     DenseHalves hx{static_cast<const float*>(a.x), a.ldx, (int)a.M}, hw{static_cast<const float*>(a.w), a.ldw, (int)a.N};
@@ -215,6 +221,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         px.a = dz; px.lda = ld_dz;
         px.b = a.w; px.ldb = a.ldw;
         rows_x = dense_rows_plan(px.M, px.N, px.K, a.dtype, true, false);
+        if (!dense_rows_launchable(rows_x, px.M, px.N, px.K, true)) return IOLB_EUNSUPPORTED;
         px.splits = rows_x.splits; px.per = rows_x.per; px.block_columns = rows_x.block_columns;
         if (rows_x.join) partial_x = dense_partial_bytes(px.splits, px.M, px.N);
     } else if (want_dx) {
@@ -222,6 +229,7 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         px.a = dz; px.lda = ld_dz; px.b = wt; px.ldb = Np;
         segments(&px, planes, planes, a.M * Np, a.K * Np);
         plan_x = dense_tile_plan(px.M, px.N, px.K, px.segments);
+        if (!dense_tile_launchable(plan_x, px.M, px.N)) return IOLB_EUNSUPPORTED;
         px.splits = plan_x.splits;
         if (px.splits > 1) partial_x = dense_partial_bytes(px.splits, px.M, px.N);
     }
@@ -231,9 +239,11 @@ int run_backward(const iolb_linear_backward_args& a, void* ws, size_t* need, boo
         segments(&pw, planes, planes_x, a.N * Mp, a.K * Mp);
         outer = a.M > 0 && a.M <= DENSE_OUTER_MOST && a.N <= DENSE_OUTER_ROWS;
         plan_w = dense_tile_plan(pw.M, pw.N, pw.K, pw.segments);
+        if (!outer && !dense_tile_launchable(plan_w, pw.M, pw.N)) return IOLB_EUNSUPPORTED;
         pw.splits = outer ? 1 : plan_w.splits;
         if (pw.splits > 1) partial_w = dense_partial_bytes(pw.splits, pw.M, pw.N);
     }
+    if (!launchable(layout_groups(a.M, a.N) + (wt ? layout_groups(a.N, a.K) : 0) + (want_dw ? layout_groups(a.M, a.K) : 0), 256)) return IOLB_EUNSUPPORTED;
     // one after the other on the stream: they share the room for partial sums
     px.partial = pw.partial = static_cast<float*>(pieces.take(std::max(partial_x, partial_w)));
     *need = pieces.used;
@@ -308,7 +318,8 @@ int checked_call(const Args* a, void* ws, size_t ws_bytes, int (*check)(const Ar
         const int rc = check(*a);
         if (rc != IOLB_OK) return rc;
         size_t need = 0;
-        run(*a, nullptr, &need, false);
+        const int planned = run(*a, nullptr, &need, false);
+        if (planned != IOLB_OK) return planned;
         if (need && (!ws || ws_bytes < need || !aligned_to(ws, 256))) return IOLB_EWORKSPACE;
         return run(*a, ws, &need, true);
     });

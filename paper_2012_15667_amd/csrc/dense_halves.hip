@@ -109,14 +109,12 @@ dense_halves_kernel(DenseHalves first, DenseHalves second, int cols, long long p
 
 hipError_t launch_dense_halves(const DenseHalves& a, const DenseHalves& b, int cols, long long pitch, int* uneven, hipStream_t st)
 {
-    // a wave to a row, or a workgroup where there are few rows or they are long
-    const bool workgroup = (long long)a.rows + b.rows < 4096 || cols > 4096;
-    const int at_once = workgroup ? 1 : 4;
-    const long long ga = ((long long)a.rows + at_once - 1) / at_once, gb = ((long long)b.rows + at_once - 1) / at_once;
-    if (ga + gb > 0x7fffffffLL) return hipErrorInvalidValue;
+    const bool workgroup = dense_halves_by_workgroup(a.rows, b.rows, cols);
+    const int groups_a = workgroup ? a.rows : (a.rows + 3) / 4;
+    const unsigned groups = (unsigned)dense_halves_groups(a.rows, b.rows, cols);
     dense_even_kernel<<<1, 64, 0, st>>>(uneven);
-    if (workgroup) dense_halves_kernel<256><<<(unsigned)(ga + gb), 256, 0, st>>>(a, b, cols, pitch, (int)ga, uneven);
-    else dense_halves_kernel<64><<<(unsigned)(ga + gb), 256, 0, st>>>(a, b, cols, pitch, (int)ga, uneven);
+    if (workgroup) dense_halves_kernel<256><<<groups, 256, 0, st>>>(a, b, cols, pitch, groups_a, uneven);
+    else dense_halves_kernel<64><<<groups, 256, 0, st>>>(a, b, cols, pitch, groups_a, uneven);
     return hipGetLastError();
 }
 

@@ -616,6 +616,14 @@ hipError_t launch_outer(DenseProduct p, long long plane_a, long long plane_b, hi
     return hipGetLastError();
 }
 
+// Workgroups of the kernel for more than DENSE_FEW rows along the first axis.
+long long rows_groups(int M, int N, int K, int per, bool across)
+{
+    const int cols = rows_waves(across) * 16 * rows_side(M, N, K, across);
+    const long long total = (K + STEP - 1LL) / STEP * ((N + cols - 1LL) / cols);
+    return (total + per - 1) / per;
+}
+
 template <int DT>
 hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
 {
@@ -627,9 +635,8 @@ hipError_t launch(const DenseProduct& p, bool across, bool join, hipStream_t st)
         return hipGetLastError();
     }
     const int mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
-    const int side = rows_side(p.M, p.N, p.K, across), cols = rows_waves(across) * 16 * side, threads = 64 * rows_waves(across);
-    const long long total = (p.K + STEP - 1LL) / STEP * ((p.N + cols - 1LL) / cols);
-    const dim3 grid((unsigned)((total + p.per - 1) / p.per), (p.M + 16 * mt - 1) / (16 * mt));
+    const int side = rows_side(p.M, p.N, p.K, across), threads = 64 * rows_waves(across);
+    const dim3 grid((unsigned)rows_groups(p.M, p.N, p.K, p.per, across), (p.M + 16 * mt - 1) / (16 * mt));
     if (across) {
         if (mt == 1) dense_rows_kernel<DT, 1, true, NC><<<grid, threads, 0, st>>>(p, join);
         else if (mt == 2) dense_rows_kernel<DT, 2, true, NC><<<grid, threads, 0, st>>>(p, join);
@@ -681,6 +688,12 @@ DenseRowsPlan dense_rows_plan(int M, int N, int K, int dtype, bool across, bool 
         }
     }
     return best;
+}
+
+bool dense_rows_launchable(const DenseRowsPlan& plan, int M, int N, int K, bool across)
+{
+    if (!across && M <= DENSE_FEW) return (N + 15LL) / 16 * 512 <= 0xffffffffLL;
+    return rows_groups(M, N, K, plan.per, across) * 64 * rows_waves(across) <= 0xffffffffLL;
 }
 
 hipError_t launch_dense_outer(const DenseProduct& p, int planes_b, long long plane_a, long long plane_b, int dtype, hipStream_t st)

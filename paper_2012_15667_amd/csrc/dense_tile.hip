@@ -446,6 +446,13 @@ DenseTilePlan dense_tile_plan(int M, int N, int K, int segments)
     return plan;
 }
 
+bool dense_tile_launchable(const DenseTilePlan& plan, int M, int N)
+{
+    const Block& b = blocks[plan.tile];
+    const long long tiles = ((long long)M + b.m - 1) / b.m * (((long long)N + b.n - 1) / b.n);
+    return tiles * (plan.tile == DENSE_TILE_256 ? 512 : 256) <= 0xffffffffLL;
+}
+
 static int join_wide_log(int N)
 {
     int wide_log = 2;                               // threads of a row: whole blocks of 32 columns
