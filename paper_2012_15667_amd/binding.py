@@ -570,10 +570,33 @@ def _call_with_workspace(call, query, args, like):
     _check(code)
 
 
+_NoGraph = None
+
+
+def _without_graph(y, given, inputs):
+    """y as a result of `inputs`, some of which require gradients, whose backward pass is an error: not a constant that ends the graph."""
+    global _NoGraph
+    if _NoGraph is None:
+        class NoGraph(_torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, y, given, *inputs):
+                if given:
+                    ctx.mark_dirty(y)
+                    return y
+                return y.view_as(y)
+
+            @staticmethod
+            def backward(ctx, *grads):
+                raise RuntimeError("linear() records no gradients: they are linear_backward's")
+        _NoGraph = NoGraph
+    return _NoGraph.apply(y, given, *inputs)
+
+
 def linear(x, w, bias=None, act="none", residual=None, residual_first=False, checkpoint=False, y=None):
     """y = act(x w^T + bias) + residual, or act(x w^T + bias + residual) with residual_first, for x [M][K], w [N][K],
     bias [N], residual [M][N]; all float32, all float16 or all bfloat16, rows contiguous.  checkpoint=True returns (y,
-    Checkpoint of what the activation was applied to).  y may be given, and may be the residual."""
+    Checkpoint of what the activation was applied to).  y may be given, and may be the residual.  Gradients come from
+    linear_backward(): a backward pass through y is an error."""
     torch = _torch or _load_torch()
     if not isinstance(x, torch.Tensor):
         raise TypeError("x must be a tensor")
@@ -588,14 +611,24 @@ def linear(x, w, bias=None, act="none", residual=None, residual_first=False, che
     if y is None:
         y = x.new_empty((M, N))
         py, ldy = y.data_ptr(), N
+        given = False
     else:
         py, ldy = _rows(y, "y", dtype, device, (M, N))[:2]
+        given = True
+    wanted = x.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad) or \
+        (residual is not None and residual.requires_grad) or (given and y.requires_grad)
+    if wanted:
+        wanted = torch.is_grad_enabled()
+        if wanted and given and y.requires_grad:
+            raise RuntimeError("y must not require gradients")
     z = _new_checkpoint(x, M, N) if checkpoint else None
     args = LinearArgs(M, N, K, code, _act_code(act), 1 if residual_first else 0, px, pw, pb, pr, py, ldx, ldw, ldr, ldy,
                       z.q.data_ptr() if checkpoint else None, z.e.data_ptr() if checkpoint else None)
     L = lib()
     _use_stream_on(device)
     _call_with_workspace(L.iolb_linear, L.iolb_linear_workspace_bytes, args, x)
+    if wanted:
+        y = _without_graph(y, given, (x, w, bias, residual))
     return (y, z) if checkpoint else y
 
 
