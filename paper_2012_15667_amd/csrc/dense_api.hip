@@ -113,10 +113,10 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     int* uneven = nullptr;
     DenseHalves hx{static_cast<const float*>(a.x), a.ldx, (int)a.M}, hw{static_cast<const float*>(a.w), a.ldw, (int)a.N};
     if (halves) {
-        for (DenseHalves* t : {&hx, &hw}) {
-            t->planes = static_cast<unsigned short*>(pieces.take((size_t)2 * t->rows * Kp * 2));
-            t->scales = static_cast<DenseScale*>(pieces.take((size_t)t->rows * sizeof(DenseScale)));
-        }
+        // (where the three parts go: those are laid out when the product of these is done)
+        hx.planes = static_cast<unsigned short*>(xp);
+        hw.planes = static_cast<unsigned short*>(wp);
+        for (DenseHalves* t : {&hx, &hw}) t->scales = static_cast<DenseScale*>(pieces.take((size_t)t->rows * sizeof(DenseScale)));
         p.uneven = uneven = static_cast<int*>(pieces.take(8));
         p.left = static_cast<int*>(pieces.take((size_t)dense_finish_blocks(plan, p.M, p.N) * 4));
         p.when = 1;
