@@ -240,7 +240,8 @@ int iolb_winograd_matrices(int m, float* A, float* L, float* B);
  * do not start on 16 bytes are copied.  They enqueue kernels only, on the stream of iolb_set_stream, and can be captured. */
 enum { IOLB_F32 = 0, IOLB_F16 = 1, IOLB_BF16 = 2 };
 /* silu: z / (1 + e^-z);  gelu: z Phi(z);  gelu_tanh: z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.  All three are 0 at
- * -infinity; a NaN stays one. */
+ * -infinity; a NaN stays one.  In fp32 they hold to 1e-6 |z| + 1e-7 (gelu's tail from a published formula: 5e-5 of the result at z = -3, 5e-4 at -4),
+ * their slopes to 4e-6. */
 enum { IOLB_ACT_NONE = 0, IOLB_ACT_RELU = 1, IOLB_ACT_SILU = 2, IOLB_ACT_GELU = 3, IOLB_ACT_GELU_TANH = 4 };
 
 /* z = x w^T + bias (+ residual if residual_first);  y = act(z) (+ residual otherwise).
@@ -261,9 +262,12 @@ int iolb_linear(const iolb_linear_args* args, void* workspace, size_t workspace_
 
 /* The 8-bit checkpoint of x [rows][cols]: q [rows][cols] and one byte for each 32 values of a row, e [rows][ceil(cols / 32)].
  * A value is q 2^(e - 127), q from -127 to 127, with the least exponent that brings the block's finite values within
- * that (at least 2^-126, for fp16 2^-24; at most 2^122, for fp16 2^10, where q stops at 63), rounded to nearest even: an error of at
- * most 1/127 of the block's largest value, 1/254 at best.  Values that are not finite become q = -128 and read back as NaN.
- * Every value is one of the tensor's type, and of bf16. */
+ * that (at least 2^-126, for fp16 2^-24; at most 2^122, for fp16 2^10, where q stops at 63), rounded to nearest even.  The error is at most
+ * half of 2^(e - 127): 1/127 of the block's largest value, 1/254 at best, with an exponent between the two ends; at the least one it may be all
+ * of a value up to 2^-127 (fp16 2^-25); at the largest one, where q stops, up to 2^(e - 127) (fp16: 65504 is held as 64512), and finite sums beyond
+ * the type, in iolb_linear's checkpoint, are held as 63 2^10 or 63 2^122 while y is infinite.  Values that are not finite become q = -128 and read back as NaN.
+ * Every value is one of the tensor's type, and of bf16.  A checkpoint does not say what type it was packed from: read as another one, its values are
+ * rounded to that, and as fp16 they are infinite from 65520 on. */
 int iolb_checkpoint_pack(const void* x, int64_t ldx, int64_t rows, int64_t cols, int dtype, int8_t* q, uint8_t* e);
 /* y [rows][cols] = act(values of the checkpoint). */
 int iolb_checkpoint_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, int act, int dtype, void* y, int64_t ldy);
@@ -273,8 +277,9 @@ int iolb_checkpoint_unpack(const int8_t* q, const uint8_t* e, int64_t rows, int6
  * was applied to, [M][N] (NULL with IOLB_ACT_NONE).
  *   dz = dy act'(z);  dx [M][K] = dz w;  dw [N][K] = dz^T x;  db [N] = sum of dz over its rows
  * dz [M][N] is the residual's gradient where that came before the activation.  Outputs are dense; each may be NULL, and w, xq
- * with it.  The slope of relu at 0 is 0, and a dy that it stops is not looked at.  16-bit types: dz is rounded to the type
- * once, before the products; db is summed before that.  Sums are added in a fixed order: equal calls give equal bits.
+ * with it.  The slope of relu at 0 is 0, and a dy that it stops is not looked at.  16-bit types: dz, and an input
+ * that is recomputed through silu, gelu or gelu_tanh, are rounded to the type once, before the products (as fp16 a dz below 2^-25 is 0: scale dy); db is summed
+ * before that.  Sums are added in a fixed order: equal calls give equal bits.
  * M, N up to 2^22, K up to 2^30, and no launch of 2^32 threads or more (IOLB_EUNSUPPORTED beyond). */
 typedef struct iolb_linear_backward_args {
     int64_t M, N, K;

@@ -45,7 +45,8 @@ class LinearBackwardArgs(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("xq", "xe", "zq", "ze", "dx", "dw", "db", "dz")]
 
 
-#: The 8-bit checkpoint of a tensor of rows: q int8 [rows][cols], e uint8 [rows][ceil(cols / 32)].
+#: The 8-bit checkpoint of a tensor of rows: q int8 [rows][cols], e uint8 [rows][ceil(cols / 32)].  It does not hold the type it was packed from: who
+#: reads it says of which type its values are to be, and as float16 those of another type may be infinite.
 Checkpoint = namedtuple("Checkpoint", "q e")
 #: What linear_backward returns; None for what was not wanted.
 LinearGrads = namedtuple("LinearGrads", "dx dw db dz")

@@ -42,6 +42,10 @@ __device__ __forceinline__ void load_checkpoint(const int8_t* p, float unit, int
     }
 }
 
+// 16-bit types: one part of the type, as a tensor of dz or of the layer's input would hold it in memory.  That is a second rounding beside the result's own, chosen
+// because two parts would double the matrix work (8192 x 4096 -> 8192 bf16: some 830 of 987 us).  Error of the gradients against 64 bits, relative 2-norm, with
+// unrounded operands / this: bf16 dx and dW through gelu 1.66e-3 / 2.33e-3, fp16 dW with the input through silu 2.07e-4 / 2.54e-4.  (A checkpoint's values
+// are exact in either type they were packed from, also through relu; db is summed from the unrounded values.)
 template <int DT>
 __device__ __forceinline__ void plane_bits(float v, unsigned short (&bits)[DT == IOLB_F32 ? 3 : 1])
 {
