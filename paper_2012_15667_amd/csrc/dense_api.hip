@@ -103,7 +103,7 @@ int run_linear(const iolb_linear_args& a, void* ws, size_t* need, bool launch)
     if (!w_direct) { p.b = wp = pieces.take((size_t)planes * a.N * Kp * 2); p.ldb = Kp; }
     // Large fp32 products in two fp16 parts, three products in place of six.  Whether an operand's rows allow it is found out on the GPU; the
     // launches for three parts follow all the same and end at once if it does and no block of sums was left to them, which costs some 10 us.  Three parts against two, us:
-    // 1024 x 1024 x 1024 36 / 38, 2048 x 1024 x 1024 48 / 48, 4096 x 1024 x 1024 74 / 58, 2048 x 2048 x 2048 120 / 97, 4096 x 4096 x 4096 668 / 398.
+    // 1024 x 1024 x 1024 37 / 40, 2048 x 1024 x 1024 50 / 49, 4096 x 1024 x 1024 74 / 57, 2048 x 2048 x 2048 115 / 96, 4096 x 4096 x 4096 633 / 395.
     DenseProduct h{};
     const bool halves = planes == 3 && (double)a.M * a.N * a.K >= 3e9 && launchable(dense_halves_groups(a.M, a.N, a.K), 256);
     const DenseTilePlan plan = dense_tile_plan(p.M, p.N, p.K, halves ? 3 : p.segments);         // (one for both: they finish the same blocks)

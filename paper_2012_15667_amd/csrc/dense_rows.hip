@@ -4,9 +4,9 @@
 // bf16 parts there (5.5 vector instructions a value).
 //
 // Measured, kernel alone: 1 x 4096 -> 4096 bf16 8.2 us (4.1 TB/s of weights), 1 x 512 -> 1000 fp32 4.7 us (latency: the launch, one trip to memory,
-// the waves' sums through LDS); 64 x 25088 -> 4096 fp32 96 us and a join of 5 (4.3 TB/s; its six bf16 products would take 66 us at the large
-// products' rate); across, 64 x 4096 -> 25088 fp32 with its join 111-115 us (3.6 TB/s; with every load of B from the same 64 rows, in cache,
-// it took 107 of 116: matrix and vector instructions bind it).
+// the waves' sums through LDS); 64 x 25088 -> 4096 fp32 96 us and a join of 5 (4.3 TB/s; its six bf16 products would take 48 us at the
+// rate of large library products); across, 64 x 4096 -> 25088 fp32 with its join 111-115 us by itself (3.6 TB/s; with every load of B from the same 64 rows,
+// in cache, 107 of 116: matrix and vector instructions bind it), and 139 in a whole backward call, whose other kernels leave less of B in the caches.
 //
 // Infinities, NaN and values whose leading part rounds to infinity make sums that are not finite; a workgroup that meets one
 // takes its sums again, now with parts that are zero beside such values, and the product of leading parts last (dense.h).
@@ -480,7 +480,8 @@ dense_rows_kernel(DenseProduct p, int join)
 // fragments of B come from L2, 64 columns ahead, there is neither LDS nor a barrier, and the stores stream.  A lane ends with 16 bytes of
 // neighbouring columns of one row (16-bit types: rows r of two tiles are columns 8 (r / 4) + r % 4 and four further), four lanes with 64; the lanes of
 // two rows exchange pieces, so that a store writes whole lines of 128 bytes.
-// Calls with their layouts, 4096 x 25088 from 64 rows, fp32 (411 MB written, a fill takes 62 us): 92 us, with stores of 64 bytes 99; bf16 59 of 63.
+// Calls with their layouts, 4096 x 25088 from 64 rows, fp32 (411 MB written, a fill takes 62 us): 92 us, with stores of 64 bytes 99; bf16 59 of 63.  In a whole
+// backward call, behind dx, the kernel alone takes 105.
 
 // Neighbouring lanes: the even one keeps a and gives b, the odd one keeps b and gives a; a is of the even lane's row then, b of the odd one's.
 __device__ __forceinline__ void exchange(u32x4& a, u32x4& b, bool odd)

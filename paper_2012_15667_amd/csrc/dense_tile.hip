@@ -7,10 +7,11 @@
 // the lane, so it is the address in memory that is exchanged.  Products are taken with B as the first operand: a lane then holds
 // four neighbouring columns of one row.
 //
-// Measured: 8192 x 16384 -> 4096 fp16 898-922 us (1190-1220 TFLOP/s; bf16 and fp16 products of 8192 x 8192 x 8192 by the vendor's library reach 1235 and 1390 on
-// the card), 8192 x 4096 -> 16384 bf16 862 us, with gelu 911, 8192 x 4096 -> 8192 bf16 406 (1350 TFLOP/s): bound by the matrix cores at the clock
-// that the card's power leaves them.  With every stage read from the same addresses, so that all loads come from L2, they
-// take 4 to 10% less.  Small ones, 1023 x 1001 -> 777 fp16 13.3 us, wait for their chain of stages.
+// Measured: 8192 x 16384 -> 4096 fp16 896-922 us (1190-1230 TFLOP/s), 8192 x 4096 -> 16384 bf16 855-925, with gelu 911, 8192 x 4096 -> 8192 bf16 410-445
+// (1240-1340 TFLOP/s); products of the vendor's library, in turn on the same card once that has run for some tenths of a second, 700, 692 and 342 (1570-1650; in
+// its first tens of milliseconds 8192 x 8192 x 8192 runs at 1235 in bf16 and 1390 in fp16).  So the matrix cores could do a quarter more, at this card's power too.
+// Of that, loads account for 4 to 10% (with every stage read from the same addresses, all from L2); the rest has not
+// been taken apart.  Small ones, 1023 x 1001 -> 777 fp16 13.3 us, wait for their chain of stages.
 #include "dense_math.h"
 #include "kernels.h"
 #include "lds_dma.h"
