@@ -52,3 +52,39 @@ def test_exactly_as_many_bytes_as_told(M, N, K, data):
         off = np.abs(y.double().cpu().numpy() - x64 @ w64.T) - (K + 16) * 2.0 ** -24 * (np.abs(x64) @ np.abs(w64).T)
         assert off.max() <= 2.0 ** -149
     assert B.lib().iolb_linear(ctypes.byref(args), ws.data_ptr(), need - 1) == -4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(2304, 1100, 1536), (600, 640, 9216)])
+def test_replays_of_a_graph_with_data_of_another_kind(M, N, K):
+    """What one replay finds of its operands (even, uneven, some sums or many to be taken again) is not the next one's."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    plain = [torch.randn(s, generator=g, device="cuda") for s in ((M, K), (N, K))]
+
+    def data(kind):
+        x, w = (t.clone() for t in plain)
+        if kind == "uneven":
+            x[1, ::3] *= 2.0 ** -40
+        if kind in ("few", "many"):
+            x[:, 5] *= 2.0 ** -40
+            rows = slice(0, N // 4) if kind == "many" else slice(0, 1)
+            w[rows] = 0
+            w[rows, 5] = 1
+        return x, w
+
+    x, w = data("even")
+    r = torch.randn((M, N), generator=g, device="cuda")
+    B.linear(x, w)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        y, z = B.linear(x, w, act="silu", residual=r, residual_first=True, checkpoint=True)
+    for kind in ("many", "even", "uneven", "few", "many", "few", "even"):
+        for to, t in zip((x, w), data(kind)):
+            to.copy_(t)
+        want, z_want = B.linear(x, w, act="silu", residual=r, residual_first=True, checkpoint=True)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(z.q, z_want.q) and torch.equal(z.e, z_want.e), kind
