@@ -32,7 +32,7 @@ extern "C" {
 
 #define IOLB_OK            0
 #define IOLB_EINVAL       -1   /* null pointer, non-positive extent, stride < 1, pad < 0, empty output */
-#define IOLB_EUNSUPPORTED -2   /* Winograd m outside {2,3,4,6}; algo, layout, type or activation outside its enum; dense layer too large */
+#define IOLB_EUNSUPPORTED -2   /* Winograd m outside {2,3,4,6}; algo, layout, type, activation or norm outside its enum; dense layer or tensor too large */
 #define IOLB_ENOTILE      -3   /* no tile fits the LDS / register budgets */
 #define IOLB_EWORKSPACE   -4   /* workspace missing or too small */
 #define IOLB_EHIP         -5   /* a HIP runtime call or launch failed; see iolb_last_hip_error */
@@ -294,6 +294,94 @@ typedef struct iolb_linear_backward_args {
 } iolb_linear_backward_args;
 int iolb_linear_backward_workspace_bytes(const iolb_linear_backward_args* args, size_t* bytes);
 int iolb_linear_backward(const iolb_linear_backward_args* args, void* workspace, size_t workspace_bytes);
+
+/* ---- Around the dense layers of a residual block --------------------------------------------------------
+ * Norms with gate and residual scale and their gradients, dropout, and dense layers in microscaled 4-bit floating point.  Types, rows, strides,
+ * extents of zero, workspaces, streams and capture: as above.  M, N, rows, cols up to 2^30 if not said otherwise. */
+enum { IOLB_NORM_NONE = 0, IOLB_NORM_RMS = 1, IOLB_NORM_LAYER = 2 };
+
+/* The end of a block and the start of the next, row by row of N values:
+ *   p = post(h) post_weight + post_bias;   x' = scale x + gate p;   y = pre(x') pre_weight + pre_bias
+ * IOLB_NORM_RMS: v / sqrt(mean of v^2 + eps);  IOLB_NORM_LAYER: (v - mean) / sqrt(variance + eps);  IOLB_NORM_NONE: v itself, without weight
+ * and bias (pre: there is no y).  x, h [M][N]; weights and biases [N], each may be NULL; gate [groups][N] or NULL: groups divides M, and
+ * row m takes the gate's row m / (M / groups).  x' is rounded to the type, and y is of x' as rounded: what a backward pass reads is what was normalised.
+ * x_out [M][N] may be x itself, and y and x_out overlap nothing else.  h NULL: y = pre(x) alone; post, gate, x_out are none then, and scale is 1.
+ * Sums in fp32, of squares too: fp32 rows with values beyond 2^63 may overflow, to 0 or NaN.  A row with a NaN becomes NaN. */
+typedef struct iolb_block_norm_args {
+    int64_t M, N, groups;
+    int32_t dtype, post, pre;
+    float scale, eps;
+    const void *x, *h, *post_weight, *post_bias, *gate, *pre_weight, *pre_bias;
+    void *x_out, *y;
+    int64_t ldx, ldh, ldo, ldy;
+} iolb_block_norm_args;
+int iolb_block_norm(const iolb_block_norm_args* args);
+
+/* Gradients of iolb_block_norm from dy [M][N] (of y; NULL with pre IOLB_NORM_NONE, or none), dx_out [M][N] (of x' from elsewhere, or NULL),
+ * x [M][N]: the x' that the forward call left (the x it was given, where h was NULL), and h [M][N] or NULL.  Statistics are taken again from these.
+ *   d = dx_out + (gradient of pre at x', of dy);  dx = scale d;  dh = (gradient of post at h, of gate d)
+ * and of weights, biases and gate the sums of their factors over the rows that share them.  Outputs are dense, dx, dh [M][N], dgate [groups][N], the
+ * others [N]; each may be NULL.  dh needs h, dgate the gate (and post_bias, where p had one), dpost_... a norm of h, dpre_... dy.
+ * Sums are added in a fixed order: equal calls give equal bits.  M, N up to 2^22.  Outputs overlap nothing. */
+typedef struct iolb_block_norm_backward_args {
+    int64_t M, N, groups;
+    int32_t dtype, post, pre;
+    float scale, eps;
+    const void *dy, *dx_out, *x, *h, *post_weight, *post_bias, *gate, *pre_weight;
+    int64_t lddy, lddx, ldx, ldh;
+    void *dx, *dh, *dgate, *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
+} iolb_block_norm_backward_args;
+int iolb_block_norm_backward_workspace_bytes(const iolb_block_norm_backward_args* args, size_t* bytes);
+int iolb_block_norm_backward(const iolb_block_norm_backward_args* args, void* workspace, size_t workspace_bytes);
+
+/* y = residual + (x scaled by 1 / (1 - p) where it stays, 0 where it is dropped); residual [rows][cols] or NULL.  The mask is not stored: the call with
+ * the same seed and offset on dy, without the residual, is the backward pass.
+ * Each value has 16 bits of Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, 2011) and stays where they are at least t = p 2^16, rounded; the scale is
+ * 2^16 / (2^16 - t), so that the mean is kept for the p that holds.  p of 1 drops all, of less at most 65535 of 65536.  Key: seed; counter: the offset in its upper
+ * 64 bits, in its lower ones r ceil(cols / 8) + c / 8 for the value in row r, column c, whose bits are the c % 8 th of eight, each word's lower half first.  So other
+ * offsets give other masks, and no stride matters.  counter: two 64-bit words on the device, read when the kernel runs, added to seed and offset (a graph
+ * that is replayed takes its masks from there); or NULL.
+ * A dropped x is not looked at (a NaN leaves 0).  y may be x or the residual, and overlaps nothing else.  zq, ze (both or neither): the checkpoint
+ * of y as rounded, as iolb_checkpoint_pack gives it. */
+typedef struct iolb_dropout_args {
+    int64_t rows, cols;
+    int32_t dtype;
+    double p;
+    uint64_t seed, offset;
+    const uint64_t* counter;
+    const void *x, *residual;
+    void* y;
+    int64_t ldx, ldr, ldy;
+    int8_t* zq;
+    uint8_t* ze;
+} iolb_dropout_args;
+int iolb_dropout(const iolb_dropout_args* args);
+
+/* Microscaled 4-bit floating point: 32 values of a row share a power of two 2^(s - 127), and each has a sign and a magnitude of 0, 0.5, 1, 1.5, 2, 3, 4 or 6 of it
+ * (codes 0 to 7, the sign is bit 3).  s is the least that brings the block within 7 (so nothing is off by more than half a step there either: 6 is
+ * the nearest of up to 7), values are rounded to nearest, ties to the even code.  A block with a value that is not finite has s = 255 and is NaN as a whole.  A block's
+ * largest value is off by 1/6 of itself at most; what lies below 1/28 of it may become 0.
+ * codes [rows][64 ceil(cols / 128)] bytes: column c in byte c / 2, the even one in the lower half; scales [rows][4 ceil(cols / 128)] bytes.  Rows
+ * are padded to 128 columns of zeros, which the products read: pack writes them.  codes 16-byte aligned, scales 4-byte. */
+int iolb_mx4_pack(const void* x, int64_t ldx, int64_t rows, int64_t cols, int dtype, uint8_t* codes, uint8_t* scales);
+/* y [rows][cols]: the values.  What the type does not reach (6 2^126, or 2^16 in fp16) becomes its largest value. */
+int iolb_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, int dtype, void* y, int64_t ldy);
+
+/* iolb_linear with both operands in that form: w_codes, w_scales as iolb_mx4_pack lays w [N][K] out, and x either likewise (x_codes, x_scales; x NULL) or
+ * a tensor [M][K] of the type, which the call brings into it first.  Products are exact, sums in fp32; bias, activation and residual
+ * as there; y may be the residual.  No gradients: weights in 4 bits are for answering.  M, N up to 2^30, K up to 2^22, and no launch of 2^32 threads. */
+typedef struct iolb_linear_mx4_args {
+    int64_t M, N, K;
+    int32_t dtype, act, residual_first;
+    const void* x;
+    int64_t ldx;
+    const uint8_t *x_codes, *x_scales, *w_codes, *w_scales;
+    const void *bias, *residual;
+    void* y;
+    int64_t ldr, ldy;
+} iolb_linear_mx4_args;
+int iolb_linear_mx4_workspace_bytes(const iolb_linear_mx4_args* args, size_t* bytes);
+int iolb_linear_mx4(const iolb_linear_mx4_args* args, void* workspace, size_t workspace_bytes);
 
 /* Stream (a hipStream_t) later calls enqueue on; NULL selects the null stream. */
 int iolb_set_stream(void* hip_stream);

@@ -23,10 +23,14 @@ EXPORTS = ["conv_direct", "conv_direct_noalloc", "conv_direct_noalloc_max_weight
            "iolb_timing_enable", "iolb_timing_read", "iolb_release_workspace", "iolb_strerror",
            "iolb_last_hip_error",
            "iolb_linear", "iolb_linear_workspace_bytes", "iolb_checkpoint_pack", "iolb_checkpoint_unpack",
-           "iolb_linear_backward", "iolb_linear_backward_workspace_bytes"]
+           "iolb_linear_backward", "iolb_linear_backward_workspace_bytes",
+           "iolb_block_norm", "iolb_block_norm_backward", "iolb_block_norm_backward_workspace_bytes", "iolb_dropout",
+           "iolb_mx4_pack", "iolb_mx4_unpack", "iolb_linear_mx4", "iolb_linear_mx4_workspace_bytes"]
 
 ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 CHECKPOINT_BLOCK = 32                       # values of a row that share a scale
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+MX4_BLOCK, MX4_WIDE = 32, 128               # values of a row that share a scale; columns that rows in 4 bits are padded to
 
 
 class LinearArgs(ctypes.Structure):
@@ -45,11 +49,50 @@ class LinearBackwardArgs(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("xq", "xe", "zq", "ze", "dx", "dw", "db", "dz")]
 
 
+class BlockNormArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("M", "N", "groups")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "post", "pre")] + \
+               [(n, ctypes.c_float) for n in ("scale", "eps")] + \
+               [(n, ctypes.c_void_p) for n in ("x", "h", "post_weight", "post_bias", "gate", "pre_weight", "pre_bias", "x_out", "y")] + \
+               [(n, ctypes.c_int64) for n in ("ldx", "ldh", "ldo", "ldy")]
+
+
+class BlockNormBackwardArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("M", "N", "groups")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "post", "pre")] + \
+               [(n, ctypes.c_float) for n in ("scale", "eps")] + \
+               [(n, ctypes.c_void_p) for n in ("dy", "dx_out", "x", "h", "post_weight", "post_bias", "gate", "pre_weight")] + \
+               [(n, ctypes.c_int64) for n in ("lddy", "lddx", "ldx", "ldh")] + \
+               [(n, ctypes.c_void_p) for n in ("dx", "dh", "dgate", "dpost_weight", "dpost_bias", "dpre_weight", "dpre_bias")]
+
+
+class DropoutArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "cols")] + [("dtype", ctypes.c_int32), ("p", ctypes.c_double)] + \
+               [(n, ctypes.c_uint64) for n in ("seed", "offset")] + \
+               [(n, ctypes.c_void_p) for n in ("counter", "x", "residual", "y")] + \
+               [(n, ctypes.c_int64) for n in ("ldx", "ldr", "ldy")] + [(n, ctypes.c_void_p) for n in ("zq", "ze")]
+
+
+class LinearMx4Args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("M", "N", "K")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "act", "residual_first")] + \
+               [("x", ctypes.c_void_p), ("ldx", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("x_codes", "x_scales", "w_codes", "w_scales", "bias", "residual", "y")] + \
+               [(n, ctypes.c_int64) for n in ("ldr", "ldy")]
+
+
 #: The 8-bit checkpoint of a tensor of rows: q int8 [rows][cols], e uint8 [rows][ceil(cols / 32)].  It does not hold the type it was packed from: who
 #: reads it says of which type its values are to be, and as float16 those of another type may be infinite.
 Checkpoint = namedtuple("Checkpoint", "q e")
 #: What linear_backward returns; None for what was not wanted.
 LinearGrads = namedtuple("LinearGrads", "dx dw db dz")
+#: What block_norm returns: the new residual stream and its norm; None for what there is not.
+BlockNorm = namedtuple("BlockNorm", "x y")
+#: What block_norm_backward returns; None for what was not wanted or has no input.
+BlockNormGrads = namedtuple("BlockNormGrads", "dx dh dgate dpost_weight dpost_bias dpre_weight dpre_bias")
+#: A tensor of rows in microscaled 4-bit floating point: codes uint8 [rows][64 ceil(cols / 128)], two a byte, the even column's in the lower half;
+#: scales uint8 [rows][4 ceil(cols / 128)]; cols, the columns that are values.  Those behind them are zeros.
+Mx4 = namedtuple("Mx4", "codes scales cols")
 
 
 class Shape(ctypes.Structure):
@@ -154,7 +197,8 @@ def lib():
                                                 ctypes.POINTER(ctypes.c_double)]
         L.iolb_release_workspace.restype = i
         L.iolb_release_workspace.argtypes = []
-        for name, args in (("iolb_linear", LinearArgs), ("iolb_linear_backward", LinearBackwardArgs)):
+        for name, args in (("iolb_linear", LinearArgs), ("iolb_linear_backward", LinearBackwardArgs), ("iolb_linear_mx4", LinearMx4Args),
+                           ("iolb_block_norm_backward", BlockNormBackwardArgs)):
             getattr(L, name).restype = i
             getattr(L, name).argtypes = [ctypes.POINTER(args), vp, sz]
             getattr(L, name + "_workspace_bytes").restype = i
@@ -163,6 +207,13 @@ def lib():
         L.iolb_checkpoint_pack.argtypes = [vp] + [ctypes.c_int64] * 3 + [i, vp, vp]
         L.iolb_checkpoint_unpack.restype = i
         L.iolb_checkpoint_unpack.argtypes = [vp, vp] + [ctypes.c_int64] * 2 + [i, i, vp, ctypes.c_int64]
+        for name, args in (("iolb_block_norm", BlockNormArgs), ("iolb_dropout", DropoutArgs)):
+            getattr(L, name).restype = i
+            getattr(L, name).argtypes = [ctypes.POINTER(args)]
+        L.iolb_mx4_pack.restype = i
+        L.iolb_mx4_pack.argtypes = [vp] + [ctypes.c_int64] * 3 + [i, vp, vp]
+        L.iolb_mx4_unpack.restype = i
+        L.iolb_mx4_unpack.argtypes = [vp, vp] + [ctypes.c_int64] * 2 + [i, vp, ctypes.c_int64]
         L.iolb_strerror.restype = ctypes.c_char_p
         L.iolb_strerror.argtypes = [i]
         L.iolb_last_hip_error.restype = ctypes.c_char_p
@@ -574,13 +625,14 @@ def _call_with_workspace(call, query, args, like):
 _NoGraph = None
 
 
-def _without_graph(y, given, inputs):
+def _without_graph(y, given, inputs, why="linear() records no gradients: they are linear_backward's"):
     """y as a result of `inputs`, some of which require gradients, whose backward pass is an error: not a constant that ends the graph."""
     global _NoGraph
     if _NoGraph is None:
         class NoGraph(_torch.autograd.Function):
             @staticmethod
-            def forward(ctx, y, given, *inputs):
+            def forward(ctx, why, y, given, *inputs):
+                ctx.why = why
                 if given:
                     ctx.mark_dirty(y)
                     return y
@@ -588,9 +640,9 @@ def _without_graph(y, given, inputs):
 
             @staticmethod
             def backward(ctx, *grads):
-                raise RuntimeError("linear() records no gradients: they are linear_backward's")
+                raise RuntimeError(ctx.why)
         _NoGraph = NoGraph
-    return _NoGraph.apply(y, given, *inputs)
+    return _NoGraph.apply(why, y, given, *inputs)
 
 
 def linear(x, w, bias=None, act="none", residual=None, residual_first=False, checkpoint=False, y=None):
@@ -696,3 +748,258 @@ def linear_backward(dy, w, x=None, z=None, act="none", x_act="none", want_dx=Tru
     _use_stream_on(device)
     _call_with_workspace(L.iolb_linear_backward, L.iolb_linear_backward_workspace_bytes, args, dy)
     return g
+
+
+# ---- around the dense layers of a residual block ----------------------------------------------------------
+
+def _norm_code(kind, name):
+    try:
+        return NORMS[kind]
+    except (KeyError, TypeError):
+        raise ValueError("%s must be one of %s" % (name, ", ".join(NORMS))) from None
+
+
+def _graph_wanted(inputs, given):
+    """Whether a result of `inputs` has to stand in autograd's graph; `given`: tensors that the results are written to."""
+    wanted = any(t is not None and t.requires_grad for t in (*inputs, *given)) and _torch.is_grad_enabled()
+    if wanted and any(y is not None and y.requires_grad for y in given):
+        raise RuntimeError("a tensor that is written to must not require gradients")
+    return wanted
+
+
+def _gate_of(gate, dtype, device, M, N):
+    """(address, groups)"""
+    if gate is None:
+        return None, 1
+    if isinstance(gate, _torch.Tensor) and gate.dim() == 2:
+        groups = gate.shape[0]
+        if groups < 1 or M % groups:
+            raise ValueError("the gate's rows must divide the rows of x")
+        return _dense(gate, "gate", dtype, device, (groups, N)), groups
+    return _dense(gate, "gate", dtype, device, (N,)), 1
+
+
+def block_norm(x, h=None, post="none", post_weight=None, post_bias=None, gate=None, scale=1.0, pre="rms", pre_weight=None, pre_bias=None,
+               eps=1e-6, x_out=None, y=None):
+    """The end of a block and the start of the next, row by row: BlockNorm(x', y) with
+
+        x' = scale x + gate post(h),   y = pre(x')
+
+    for the residual stream x [M][N] and the block's result h [M][N] (None: x' is None, and y = pre(x)).  post, pre: "rms", "layer" or "none" (post: h
+    itself; pre: y is None), with weights and biases [N] of their own, or none; gate [N], or [groups][N] where M / groups neighbouring rows share each of
+    its rows.  All float32, all float16 or all bfloat16, rows contiguous.  y is of x' as rounded to the type.  x_out, y may be given, and x_out may
+    be x.  Gradients come from block_norm_backward(): a backward pass through the results is an error."""
+    torch = _torch or _load_torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a tensor")
+    dtype, device = x.dtype, x.get_device()
+    code = _dtype_code(dtype)
+    px, ldx, M, N = _rows(x, "x", dtype, device)
+    kind_post, kind_pre = _norm_code(post, "post"), _norm_code(pre, "pre")
+    if h is None and (kind_post or gate is not None or x_out is not None or scale != 1.0):
+        raise ValueError("post, gate, scale and x_out go with h")
+    if not kind_post and (post_weight is not None or post_bias is not None):
+        raise ValueError("weight and bias go with a norm: post is none")
+    if not kind_pre and (pre_weight is not None or pre_bias is not None or y is not None):
+        raise ValueError("weight, bias and y go with a norm: pre is none")
+    if h is None and not kind_pre:
+        raise ValueError("there is nothing to do")
+    ph, ldh = _rows(h, "h", dtype, device, (M, N))[:2] if h is not None else (None, 0)
+    pgate, groups = _gate_of(gate, dtype, device, M, N)
+    columns = [_dense(t, n, dtype, device, (N,)) if t is not None else None
+               for t, n in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"), (pre_bias, "pre_bias"))]
+    inputs, given = (x, h, post_weight, post_bias, gate, pre_weight, pre_bias), (x_out, y)
+    wanted = _graph_wanted(inputs, given)
+    if h is None:
+        po, ldo = None, 0
+    elif x_out is None:
+        x_out = x.new_empty((M, N))
+        po, ldo = x_out.data_ptr(), N
+    else:
+        po, ldo = _rows(x_out, "x_out", dtype, device, (M, N))[:2]
+    if not kind_pre:
+        py, ldy = None, 0
+    elif y is None:
+        y = x.new_empty((M, N))
+        py, ldy = y.data_ptr(), N
+    else:
+        py, ldy = _rows(y, "y", dtype, device, (M, N))[:2]
+    args = BlockNormArgs(M, N, groups, code, kind_post, kind_pre, scale, eps, px, ph, columns[0], columns[1], pgate, columns[2], columns[3],
+                         po, py, ldx, ldh, ldo, ldy)
+    _use_stream_on(device)
+    _check(lib().iolb_block_norm(args))
+    if wanted:
+        why = "block_norm() records no gradients: they are block_norm_backward's"
+        if x_out is not None:
+            x_out = _without_graph(x_out, given[0] is not None, inputs, why)
+        if y is not None:
+            y = _without_graph(y, given[1] is not None, inputs, why)
+    return BlockNorm(x_out, y)
+
+
+def block_norm_backward(dy, dx_out, x, h=None, post="none", post_weight=None, post_bias=None, gate=None, scale=1.0, pre="rms",
+                        pre_weight=None, pre_bias=None, eps=1e-6, want_dx=True, want_weights=True):
+    """Gradients of block_norm(): BlockNormGrads from dy, the gradient of y (None where pre is "none", or where y was not used), and dx_out, that of x'
+    from where the stream goes on (None: from nowhere); x is the x' that block_norm returned (its x where h is None).  The other arguments are those
+    of block_norm.  dx and dh are there with want_dx, and with want_weights the gradients of those of gate, weights and biases that were given."""
+    torch = _torch or _load_torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a tensor")
+    dtype, device = x.dtype, x.get_device()
+    code = _dtype_code(dtype)
+    px, ldx, M, N = _rows(x, "x", dtype, device)
+    kind_post, kind_pre = _norm_code(post, "post"), _norm_code(pre, "pre")
+    if h is None and (kind_post or gate is not None or scale != 1.0):
+        raise ValueError("post, gate and scale go with h")
+    if not kind_post and (post_weight is not None or post_bias is not None):
+        raise ValueError("weight and bias go with a norm: post is none")
+    if not kind_pre and (pre_weight is not None or pre_bias is not None or dy is not None):
+        raise ValueError("weight, bias and dy go with a norm: pre is none")
+    if dy is None and dx_out is None:
+        raise ValueError("dy or dx_out is needed")
+    pdy, lddy = _rows(dy, "dy", dtype, device, (M, N))[:2] if dy is not None else (None, 0)
+    pdo, lddo = _rows(dx_out, "dx_out", dtype, device, (M, N))[:2] if dx_out is not None else (None, 0)
+    ph, ldh = _rows(h, "h", dtype, device, (M, N))[:2] if h is not None else (None, 0)
+    pgate, groups = _gate_of(gate, dtype, device, M, N)
+    columns = [_dense(t, n, dtype, device, (N,)) if t is not None else None
+               for t, n in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"), (pre_bias, "pre_bias"))]
+
+    def like(t, there=True):
+        return x.new_empty(t.shape) if t is not None and want_weights and there else None
+    g = BlockNormGrads(x.new_empty((M, N)) if want_dx else None, x.new_empty((M, N)) if want_dx and h is not None else None,
+                       like(gate), like(post_weight), like(post_bias), like(pre_weight, dy is not None), like(pre_bias, dy is not None))
+    args = BlockNormBackwardArgs(M, N, groups, code, kind_post, kind_pre, scale, eps, pdy, pdo, px, ph, columns[0], columns[1], pgate, columns[2],
+                                 lddy, lddo, ldx, ldh, *[t.data_ptr() if t is not None else None for t in g])
+    L = lib()
+    _use_stream_on(device)
+    _call_with_workspace(L.iolb_block_norm_backward, L.iolb_block_norm_backward_workspace_bytes, args, x)
+    return g
+
+
+def _word64(v, name):
+    if isinstance(v, bool) or not hasattr(v, "__index__"):
+        raise TypeError(name + " must be a whole number")
+    v = v.__index__()
+    if not 0 <= v < 1 << 64:
+        raise ValueError(name + " must fit 64 bits")
+    return v
+
+
+def dropout(x, p, seed, offset=0, counter=None, residual=None, checkpoint=False, y=None):
+    """y = residual + (x / (1 - p) where it stays, 0 where it is dropped), for x, residual [rows][cols], rows contiguous.  The mask is a function of
+    seed, offset and the value's place, and is not stored: dropout(dy, p, seed, offset) is the backward pass.  Take another offset for every call and
+    step.  counter: int64 [2] on the GPU, added to seed and offset when the kernel runs (a captured graph draws new masks by it).  p is taken to
+    16 bits, and the scale fits it.  checkpoint=True returns (y, Checkpoint of y), as linear_backward reads it.  y may be given, and may be x or the residual.  A
+    backward pass through y is an error."""
+    torch = _torch or _load_torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a tensor")
+    dtype, device = x.dtype, x.get_device()
+    code = _dtype_code(dtype)
+    px, ldx, rows, cols = _rows(x, "x", dtype, device)
+    p = float(p)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must be between 0 and 1")
+    seed, offset = _word64(seed, "seed"), _word64(offset, "offset")
+    pc = _dense(counter, "counter", torch.int64, device, (2,)) if counter is not None else None
+    pr, ldr = _rows(residual, "residual", dtype, device, (rows, cols))[:2] if residual is not None else (None, 0)
+    wanted = _graph_wanted((x, residual), (y,))
+    given = y is not None
+    if given:
+        py, ldy = _rows(y, "y", dtype, device, (rows, cols))[:2]
+    else:
+        y = x.new_empty((rows, cols))
+        py, ldy = y.data_ptr(), cols
+    z = _new_checkpoint(x, rows, cols) if checkpoint else None
+    args = DropoutArgs(rows, cols, code, p, seed, offset, pc, px, pr, py, ldx, ldr, ldy,
+                       z.q.data_ptr() if checkpoint else None, z.e.data_ptr() if checkpoint else None)
+    _use_stream_on(device)
+    _check(lib().iolb_dropout(args))
+    if wanted:
+        y = _without_graph(y, given, (x, residual), "dropout() records no gradients: they are dropout()'s of the same seed and offset")
+    return (y, z) if checkpoint else y
+
+
+def _mx4_of(c, name, device=None):
+    """(codes' address, scales' address, rows, columns) of an Mx4"""
+    if not (isinstance(c, tuple) and len(c) == 3 and isinstance(c[0], _torch.Tensor) and c[0].dim() == 2 and isinstance(c[2], int) and c[2] >= 0):
+        raise TypeError(name + " must be an Mx4")
+    rows, wide = c[0].shape[0], -(-c[2] // MX4_WIDE)
+    if device is None:
+        device = c[0].get_device()
+    return (_dense(c[0], name + ".codes", _torch.uint8, device, (rows, wide * (MX4_WIDE // 2))),
+            _dense(c[1], name + ".scales", _torch.uint8, device, (rows, wide * (MX4_WIDE // MX4_BLOCK))), rows, c[2])
+
+
+def mx4_pack(x):
+    """x [rows][cols] in microscaled 4-bit floating point (17/32 bytes a value), to be read by mx4_unpack and linear_mx4."""
+    torch = _torch or _load_torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a tensor")
+    device = x.get_device()
+    code = _dtype_code(x.dtype)
+    px, ldx, rows, cols = _rows(x, "x", x.dtype, device)
+    wide = -(-cols // MX4_WIDE)
+    c = Mx4(x.new_empty((rows, wide * (MX4_WIDE // 2)), dtype=torch.uint8), x.new_empty((rows, wide * (MX4_WIDE // MX4_BLOCK)), dtype=torch.uint8), cols)
+    _use_stream_on(device)
+    _check(lib().iolb_mx4_pack(px, ldx, rows, cols, code, c.codes.data_ptr(), c.scales.data_ptr()))
+    return c
+
+
+def mx4_unpack(c, dtype=None, y=None):
+    """The values of an Mx4 as a matrix of `dtype` (float32 unless y is given)."""
+    torch = _torch or _load_torch()
+    pc, ps, rows, cols = _mx4_of(c, "c")
+    device = c[0].get_device()
+    if dtype is None:
+        dtype = y.dtype if y is not None else torch.float32
+    code = _dtype_code(dtype)
+    if y is None:
+        y = c[0].new_empty((rows, cols), dtype=dtype)
+        py, ldy = y.data_ptr(), cols
+    else:
+        py, ldy = _rows(y, "y", dtype, device, (rows, cols))[:2]
+    _use_stream_on(device)
+    _check(lib().iolb_mx4_unpack(pc, ps, rows, cols, code, py, ldy))
+    return y
+
+
+def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False, dtype=None, y=None):
+    """linear() with both operands in microscaled 4-bit floating point: w is an Mx4 of [N][K], x an Mx4 of [M][K] or a tensor, which the call brings
+    into it.  y, bias and residual are of x's type, or where x is an Mx4 of `dtype` (bfloat16 unless y is given).  For answering: there are no gradients, and
+    a backward pass through y is an error."""
+    torch = _torch or _load_torch()
+    if isinstance(x, torch.Tensor):
+        if dtype is not None and dtype != x.dtype:
+            raise ValueError("dtype goes with an x in 4 bits")
+        dtype, device, like = x.dtype, x.get_device(), x
+        code = _dtype_code(dtype)
+        px, ldx, M, K = _rows(x, "x", dtype, device)
+        pxc = pxs = None
+    else:
+        pxc, pxs, M, K = _mx4_of(x, "x")
+        device, like = x[0].get_device(), x[0]
+        if dtype is None:
+            dtype = y.dtype if y is not None else torch.bfloat16
+        code = _dtype_code(dtype)
+        px, ldx = None, 0
+    pwc, pws, N, C = _mx4_of(w, "w", device)
+    if C != K:
+        raise ValueError("x and w have different numbers of columns")
+    pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else None
+    pr, ldr = _rows(residual, "residual", dtype, device, (M, N))[:2] if residual is not None else (None, 0)
+    inputs = (like, bias, residual)
+    wanted = _graph_wanted(inputs, (y,))
+    given = y is not None
+    if given:
+        py, ldy = _rows(y, "y", dtype, device, (M, N))[:2]
+    else:
+        y = like.new_empty((M, N), dtype=dtype)
+        py, ldy = y.data_ptr(), N
+    args = LinearMx4Args(M, N, K, code, _act_code(act), 1 if residual_first else 0, px, ldx, pxc, pxs, pwc, pws, pb, pr, py, ldr, ldy)
+    L = lib()
+    _use_stream_on(device)
+    _call_with_workspace(L.iolb_linear_mx4, L.iolb_linear_mx4_workspace_bytes, args, like)
+    if wanted:
+        y = _without_graph(y, given, inputs, "linear_mx4() has no gradients")
+    return y

@@ -1,0 +1,80 @@
+// What stands around the dense layers of a residual block: norms with gate and residual scale and their gradients, dropout, and
+// microscaled 4-bit floating point with its product.  What the kernels and the entry points share.
+#ifndef IOLB_BLOCK_H
+#define IOLB_BLOCK_H
+
+#include "dense.h"
+
+namespace iolb {
+
+// ---- norms -----------------------------------------------------------------------------------------
+// Rows are N values.  p = post(h);  x' = a x + g p, rounded to the type;  y = pre(x').
+struct BlockNorm {
+    const void *x, *h, *gate;               // h null: y = pre(x) alone
+    const void *post_weight, *post_bias, *pre_weight, *pre_bias;
+    void *out, *y;                          // x', y; either may be null
+    long long ldx, ldh, ldo, ldy;
+    int M, N;
+    int post, pre;                          // IOLB_NORM_...
+    int rows_per_group;                     // rows that share a row of the gate
+    float scale, eps;
+};
+hipError_t launch_block_norm(const BlockNorm& p, int dtype, hipStream_t st);
+
+// Gradients.  d = dout + (gradient of pre at x', of dy);  dx = a d;  dh = (gradient of post at h, of g d).
+// Column sums over the rows of a gate's group, S1 = sum of d hat(h), S0 = sum of d, and over all rows T1 = sum of dy hat(x'),
+// T0 = sum of dy, give what the weights and the gate get: dgate = wp S1 + bp S0, dwp = sum of g S1 over the groups,
+// dbp = sum of g S0, dw = T1, db = T0.
+struct BlockNormBackward {
+    const void *dy, *dout, *x, *h, *gate;   // dy, dout: either may be null
+    const void *post_weight, *post_bias, *pre_weight;
+    void *dx, *dh;                          // dense; null: not wanted
+    void *dgate, *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
+    long long lddy, lddout, ldx, ldh;
+    int M, N;
+    int post, pre;
+    int rows_per_group, groups;
+    float scale, eps;
+    float* rows;                            // [M][NORM_ROW_SUMS]: what the rows' pass leaves for the columns' pass
+    float* columns;                         // [pieces][NORM_COLUMN_SUMS][N rounded up to 8]
+};
+constexpr int NORM_ROW_SUMS = 8, NORM_COLUMN_SUMS = 4;
+// How the column sums are shared: `per` rows to a piece, no piece across two groups.
+struct NormPieces { int per, in_group; };
+struct NormBackwardPlan { NormPieces pieces; size_t row_bytes, column_bytes; bool launchable = true; };
+NormBackwardPlan block_norm_backward_plan(const BlockNormBackward& p, int dtype);
+hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBackwardPlan& plan, int dtype, hipStream_t st);
+
+// ---- dropout ---------------------------------------------------------------------------------------
+struct Dropout {
+    const void *x, *residual;               // residual may be null
+    void* y;
+    int8_t* zq;                             // checkpoint of y, or null
+    uint8_t* ze;
+    long long ldx, ldr, ldy;
+    int rows, cols;
+    unsigned least;                         // a value stays where its 16 random bits are at least this
+    float scale;
+    unsigned long long seed, offset;
+    const unsigned long long* counter;      // on the device: [0] is added to the seed, [1] to the offset; may be null
+};
+hipError_t launch_dropout(const Dropout& p, int dtype, hipStream_t st);
+
+// ---- microscaled 4-bit floating point ----------------------------------------------------------------
+constexpr int MX4_BLOCK = 32, MX4_WIDE = 128;       // values that share a scale; columns that rows are padded to
+inline long long mx4_pitch(long long cols) { return (cols + MX4_WIDE - 1) / MX4_WIDE * (MX4_WIDE / 2); }            // bytes of a row's codes
+inline long long mx4_scale_pitch(long long cols) { return (cols + MX4_WIDE - 1) / MX4_WIDE * (MX4_WIDE / MX4_BLOCK); }
+hipError_t launch_mx4_pack(const void* x, long long ldx, int rows, int cols, int dtype, uint8_t* codes, uint8_t* scales, hipStream_t st);
+hipError_t launch_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int rows, int cols, int dtype, void* y, long long ldy, hipStream_t st);
+
+// sums[m][n] = sum over k of a[m][k] b[n][k], both in 4 bits as mx4_pack lays them out, finished by p.f.
+struct Mx4Product {
+    const uint8_t *a, *a_scales, *b, *b_scales;
+    int M, N, K;
+    DenseFinish f;
+};
+hipError_t launch_mx4_product(const Mx4Product& p, int dtype, hipStream_t st);
+
+}  // namespace iolb
+
+#endif

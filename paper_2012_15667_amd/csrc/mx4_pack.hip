@@ -1,0 +1,105 @@
+// Tensors into microscaled 4-bit floating point and back.  Streaming kernels: bound by memory.
+#include "mx4_math.h"
+
+namespace iolb {
+
+namespace {
+
+// Four lanes share a block of 32, eight values each.  A workgroup covers `wide` threads of a row, up to its padded end, and 256 / wide rows.
+template <int DT>
+__global__ void __launch_bounds__(256)
+mx4_pack_kernel(const void* x, long long ldx, int rows, int cols, uint8_t* codes, uint8_t* scales, int wide_log)
+{
+    typedef typename DenseType<DT>::type T;
+    const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), ty = threadIdx.x >> wide_log;
+    const long long pitch = (cols + MX4_WIDE - 1LL) / MX4_WIDE * (MX4_WIDE / 2);
+    const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 8), have = cols - c;
+    for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r - ty < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (r < rows && have > 0) load_columns(static_cast<const T*>(x) + r * ldx + c, have, v);
+        unsigned most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned b = magnitude_bits(v[i]);
+            most = b > most ? b : most;
+        }
+#pragma unroll
+        for (int d = 1; d < 4; d *= 2) {
+            const unsigned b = (unsigned)__shfl_xor((int)most, d);
+            most = b > most ? b : most;
+        }
+        const int s = mx4_scale(most);
+        if (r >= rows || c / 2 >= pitch) continue;
+        *reinterpret_cast<unsigned*>(codes + r * pitch + c / 2) = s == MX4_NAN ? 0u : mx4_codes(v, mx4_unit(s));
+        if ((tx & 3) == 0) scales[r * (pitch / 16) + c / MX4_BLOCK] = (uint8_t)s;
+    }
+}
+
+template <int DT> __device__ __forceinline__ float largest()
+{
+    return DT == IOLB_F16 ? 65504.f : DT == IOLB_BF16 ? 0x1.fep127f : 0x1.fffffep127f;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(256)
+mx4_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int rows, int cols, void* y, long long ldy, int wide_log)
+{
+    typedef typename DenseType<DT>::type T;
+    const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), ty = threadIdx.x >> wide_log;
+    const long long pitch = (cols + MX4_WIDE - 1LL) / MX4_WIDE * (MX4_WIDE / 2);
+    const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 8), have = cols - c;
+    if (have <= 0) return;
+    for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
+        const int s = scales[r * (pitch / 16) + c / MX4_BLOCK];
+        const unsigned w = *reinterpret_cast<const unsigned*>(codes + r * pitch + c / 2);
+        const float unit = mx4_unit(s);
+        const f32x2 pair[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1),
+                               __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3)};
+        typename Piece<T, 8>::type t;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = fminf(fmaxf(pair[i / 2][i % 2], -largest<DT>()), largest<DT>());
+            t[i] = s == MX4_NAN ? (T)__builtin_nanf("") : (T)v;
+        }
+        T* const to = static_cast<T*>(y) + r * ldy + c;
+        if (have >= 8) {
+            *reinterpret_cast<typename Piece<T, 8>::type*>(to) = t;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) to[i] = t[i];
+        }
+    }
+}
+
+struct RowGrid { dim3 grid; int wide_log; };
+RowGrid row_grid(int rows, long long cols, long long each)
+{
+    int wide_log = 2;                               // whole blocks of 32
+    while (wide_log < 8 && (each << wide_log) < cols) ++wide_log;
+    const long long gx = (cols + (each << wide_log) - 1) / (each << wide_log), per = 256 >> wide_log;
+    const long long gy = (rows + per - 1) / per;
+    return {dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), wide_log};
+}
+
+}  // namespace
+
+hipError_t launch_mx4_pack(const void* x, long long ldx, int rows, int cols, int dtype, uint8_t* codes, uint8_t* scales, hipStream_t st)
+{
+    const RowGrid g = row_grid(rows, 2 * mx4_pitch(cols), 8);
+    if (dtype == IOLB_F32) mx4_pack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, codes, scales, g.wide_log);
+    else if (dtype == IOLB_F16) mx4_pack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, codes, scales, g.wide_log);
+    else mx4_pack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, codes, scales, g.wide_log);
+    return hipGetLastError();
+}
+
+hipError_t launch_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int rows, int cols, int dtype, void* y, long long ldy, hipStream_t st)
+{
+    const RowGrid g = row_grid(rows, cols, 8);
+    if (dtype == IOLB_F32) mx4_unpack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(codes, scales, rows, cols, y, ldy, g.wide_log);
+    else if (dtype == IOLB_F16) mx4_unpack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(codes, scales, rows, cols, y, ldy, g.wide_log);
+    else mx4_unpack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(codes, scales, rows, cols, y, ldy, g.wide_log);
+    return hipGetLastError();
+}
+
+}  // namespace iolb
