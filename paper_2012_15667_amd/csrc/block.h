@@ -71,9 +71,14 @@ hipError_t launch_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int ro
 struct Mx4Product {
     const uint8_t *a, *a_scales, *b, *b_scales;
     int M, N, K;
+    int splits;                             // workgroups that share a tile's K; their sums go to `partial` if > 1
+    float* partial;                         // [splits][M][N rounded up to 4]
     DenseFinish f;
 };
-hipError_t launch_mx4_product(const Mx4Product& p, int dtype, hipStream_t st);
+constexpr int MX4_FEW = 16;                 // rows of a of the kernel for the fewest
+hipError_t launch_mx4_few(const Mx4Product& p, int dtype, hipStream_t st);
+DenseTilePlan mx4_tile_plan(int M, int N, int K);
+hipError_t launch_mx4_tile(const Mx4Product& p, int tile, int dtype, hipStream_t st);
 
 }  // namespace iolb
 

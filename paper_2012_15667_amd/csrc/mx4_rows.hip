@@ -37,7 +37,7 @@ mx4_wave_kernel(Mx4Product p, int tiles_m)
 
 }  // namespace
 
-hipError_t launch_mx4_product(const Mx4Product& p, int dtype, hipStream_t st)
+hipError_t launch_mx4_few(const Mx4Product& p, int dtype, hipStream_t st)
 {
     const int tiles_m = (p.M + 15) / 16;
     const long long groups = ((long long)tiles_m * ((p.N + 15) / 16) + 3) / 4;
