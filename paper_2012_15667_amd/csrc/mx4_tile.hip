@@ -3,7 +3,8 @@
 // The shape of the dense layers' product kernel (dense_tile.hip) with stages of 256 k: a row of a stage is again 128 bytes, eight pieces of 16, and a piece is
 // a block of 32 codes, which is what a lane gives to a matrix instruction of 128 k.  A stage also takes the rows' eight scales, 8 bytes.  Lane group g
 // multiplies pieces 2 g and 2 g + 1 of a row, one in each half of the stage (both operands alike: the order of k does not matter), so its two scales
-// are neighbours, and one 16-bit read of LDS gives the instruction both, each by its byte number.
+// are neighbours, and one 16-bit read of LDS gives the instruction both, each by its byte
+// number.  (32 bits read at odd multiples of two bytes, of which the upper half is not looked at, take LDS 77 cycles an instruction.)
 #include "dense_math.h"
 #include "kernels.h"
 #include "lds_dma.h"
@@ -56,19 +57,29 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
     const int words = (p.K + MX4_WIDE - 1) / MX4_WIDE, steps_all = (words + 1) / 2;         // four scales to a word
     const int s0 = (int)((long long)steps_all * blockIdx.y / p.splits), s1 = (int)((long long)steps_all * (blockIdx.y + 1) / p.splits);
 
-    // Rows beyond the operand are read from its last row: their sums are never stored.
+    // A load takes eight rows.  Those beyond the operand are read from its last ones: their sums are never stored.  Registers are short, so a load's rows
+    // are in its base, and what a lane adds is one of two offsets, the second for the operand's last eight rows, which may be fewer.  (The empty
+    // assembly lines keep the compiler from working such things out before the loop: their registers would spill.)
     const unsigned pitch = (unsigned)words * 64u, scale_pitch = (unsigned)words * 4u;
-    unsigned a_off[LA], b_off[LB];
-    const int from_piece = place(lane >> 3, lane & 7);           // (a load's rows start at a multiple of 8)
+    const int rows_a = p.M - m0 < BM ? p.M - m0 : BM, rows_b = p.N - n0 < BN ? p.N - n0 : BN;
+    const int last_a = (rows_a - 1) & ~7, last_b = (rows_b - 1) & ~7;
+    // (a load's rows start at a multiple of 8; piece 2 g + kk lies where piece 4 kk + g would: what neighbouring lane groups read together are neighbours)
+    const int placed = place(lane >> 3, lane & 7), from_piece = 2 * (placed & 3) + (placed >> 2);
+    const auto offset_in = [&](int rows) {
+        const int r = lane >> 3;
+        unsigned at = __umul24(r < rows ? r : rows - 1, pitch) + 16u * from_piece;     // (a pitch is at most 2^21)
+        asm volatile("" : "+v"(at));
+        return at;
+    };
+    const unsigned inside = offset_in(8), end_a = offset_in(rows_a - last_a), end_b = offset_in(rows_b - last_b);
+    unsigned scale_off[(SCALE_LOADS + WAVES - 1) / WAVES];
 #pragma unroll
-    for (int i = 0; i < LA; ++i) {
-        const int r = (i * WAVES + wave) * 8 + (lane >> 3), have = p.M - 1 - m0;
-        a_off[i] = (unsigned)(r < have ? r : have) * pitch + 16u * from_piece;
-    }
-#pragma unroll
-    for (int i = 0; i < LB; ++i) {
-        const int r = (i * WAVES + wave) * 8 + (lane >> 3), have = p.N - 1 - n0;
-        b_off[i] = (unsigned)(r < have ? r : have) * pitch + 16u * from_piece;
+    for (int i = 0; i < (SCALE_LOADS + WAVES - 1) / WAVES; ++i) {
+        const int at = i * WAVES + wave;
+        const bool of_a = at < BM / 32;
+        const int r = (of_a ? at : at - BM / 32) * 32 + (lane >> 1), rows = of_a ? rows_a : rows_b;
+        scale_off[i] = __umul24(r < rows ? r : rows - 1, scale_pitch);
+        asm volatile("" : "+v"(scale_off[i]));
     }
     const uint8_t* const a0 = p.a + (long long)m0 * pitch;
     const uint8_t* const b0 = p.b + (long long)n0 * pitch;
@@ -82,30 +93,36 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
         // rows are whole words of scales: the last stage may have one of two
         if (2 * step + (from_piece >> 2) < words) {
 #pragma unroll
-            for (int i = 0; i < LA; ++i) dma16(a, a_off[i], to + (i * WAVES + wave) * 1024);
+            for (int i = 0; i < LA; ++i) {
+                const int r = (i * WAVES + wave) * 8;
+                int at = r < last_a ? r : last_a;
+                asm volatile("" : "+s"(at));
+                dma16(a + (size_t)((unsigned)at * pitch), at < last_a ? inside : end_a, to + (i * WAVES + wave) * 1024);
+            }
 #pragma unroll
-            for (int i = 0; i < LB; ++i) dma16(b, b_off[i], to + BM * ROW_BYTES + (i * WAVES + wave) * 1024);
+            for (int i = 0; i < LB; ++i) {
+                const int r = (i * WAVES + wave) * 8;
+                int at = r < last_b ? r : last_b;
+                asm volatile("" : "+s"(at));
+                dma16(b + (size_t)((unsigned)at * pitch), at < last_b ? inside : end_b, to + BM * ROW_BYTES + (i * WAVES + wave) * 1024);
+            }
         } else {
             // the end of the summed axis: pieces beyond it are zero on both sides
-            // (written where it is needed once: as part of the loop its addresses would be kept, in registers that the sums need)
-            unsigned at = buf * STAGE + wave * 1024 + lane * 16;
+            unsigned at = tid;
             asm volatile("" : "+v"(at));
+            at = buf * STAGE + at * 16;
 #pragma unroll
             for (int i = 0; i < LA; ++i) *reinterpret_cast<u32x4*>(lds + at + i * WAVES * 1024) = u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < LB; ++i) *reinterpret_cast<u32x4*>(lds + at + BM * ROW_BYTES + i * WAVES * 1024) = u32x4{0, 0, 0, 0};
         }
         // (a word beyond the end: the row's last one again, whose scales meet zeros, and NaN only in a row that has one)
-        const int word = 2 * step + (lane & 1) < words ? 2 * step + (lane & 1) : words - 1;
+        const unsigned word = 4u * (2 * step + (lane & 1) < words ? 2 * step + (lane & 1) : words - 1);
 #pragma unroll
         for (int i = 0; i < (SCALE_LOADS + WAVES - 1) / WAVES; ++i) {
             const int at = i * WAVES + wave;
-            if (at < SCALE_LOADS) {
-                const bool of_a = at < BM / 32;
-                const int r = (of_a ? at : at - BM / 32) * 32 + (lane >> 1), have = of_a ? p.M - 1 - m0 : p.N - 1 - n0;
-                lds_dma_load_4(reinterpret_cast<const float*>(of_a ? a0_scales : b0_scales), (unsigned)(r < have ? r : have) * scale_pitch + 4u * word,
-                               to + code_bytes(BM, BN) + at * 256);
-            }
+            if (at < SCALE_LOADS)
+                lds_dma_load_4(reinterpret_cast<const float*>(at < BM / 32 ? a0_scales : b0_scales), scale_off[i] + word, to + code_bytes(BM, BN) + at * 256);
         }
     };
 
@@ -116,20 +133,20 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
     // A stage is 2 MI groups of NI matrix instructions: half kk, sixteen rows i of A.  The order is written out and held: after each group the reads
-    // of the operands of a later one are issued, A into a ring of MI registers, AHEAD groups ahead, B a half ahead.  The one barrier of a stage
+    // of the operands of a later one are issued, A into a ring of RING fragments, AHEAD groups ahead, B a half ahead.  The one barrier of a stage
     // stands before its last groups, when all of it has been read: the next stage has arrived then, its first reads go out behind the last groups, and
     // the buffer is free for the stage after it.
-    constexpr int GROUPS = 2 * MI, AHEAD = MI > 2 ? MI - 2 : 1, LAST = MI == 8 ? 3 : MI == 4 ? 2 : 1;
-    static_assert(AHEAD < MI && LAST <= AHEAD && LAST < MI && NI <= GROUPS - LAST, "a stage is read before its barrier");
-    u32x4 fa[MI], fb[2][NI];
+    constexpr int GROUPS = 2 * MI, RING = MI < 4 ? MI : 4, AHEAD = MI == 8 ? 3 : MI == 4 ? 2 : 1, LAST = AHEAD;
+    static_assert(GROUPS % RING == 0 && AHEAD < RING && LAST < MI && NI <= GROUPS - LAST, "a stage is read before its barrier");
+    u32x4 fa[RING], fb[2][NI];
     unsigned sa[MI], sb[NI], next_sb[NI];
     // fragments: row l16 of sixteen, piece 2 grp + kk; the rest is the same for all lanes
-    const int frag_a = (wm * (BM / WM) + l16) * ROW_BYTES + 16 * place(l16, 2 * grp);
-    const int frag_b = (BM + wn * (BN / WN) + l16) * ROW_BYTES + 16 * place(l16, 2 * grp);
+    const int frag_a = (wm * (BM / WM) + l16) * ROW_BYTES + 16 * place(l16, grp);
+    const int frag_b = (BM + wn * (BN / WN) + l16) * ROW_BYTES + 16 * place(l16, grp);
     const int frag_sa = code_bytes(BM, BN) + (wm * (BM / WM) + l16) * ROW_SCALES + 2 * grp;
     const int frag_sb = code_bytes(BM, BN) + (BM + wn * (BN / WN) + l16) * ROW_SCALES + 2 * grp;
-    auto read_a = [&](const char* at, int g) { fa[g % MI] = *reinterpret_cast<const u32x4*>(at + (frag_a ^ 16 * (g / MI)) + g % MI * 16 * ROW_BYTES); };
-    auto read_b = [&](const char* at, int kk, int j) { fb[kk][j] = *reinterpret_cast<const u32x4*>(at + (frag_b ^ 16 * kk) + j * 16 * ROW_BYTES); };
+    auto read_a = [&](const char* at, int g) { fa[g % RING] = *reinterpret_cast<const u32x4*>(at + (frag_a ^ 64 * (g / MI)) + g % MI * 16 * ROW_BYTES); };
+    auto read_b = [&](const char* at, int kk, int j) { fb[kk][j] = *reinterpret_cast<const u32x4*>(at + (frag_b ^ 64 * kk) + j * 16 * ROW_BYTES); };
     auto read_sa = [&](const char* at, int i) { sa[i] = *reinterpret_cast<const unsigned short*>(at + frag_sa + i * 16 * ROW_SCALES); };
     auto scale_b = [&](const char* at, int j) -> unsigned { return *reinterpret_cast<const unsigned short*>(at + frag_sb + j * 16 * ROW_SCALES); };
     if (s1 > s0) {
@@ -159,7 +176,7 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < NI; ++j) acc[g % MI][j] = mx4_multiply<g / MI, g / MI>(fb[g / MI][j], sb[j], fa[g % MI], sa[g % MI], acc[g % MI][j]);
+            for (int j = 0; j < NI; ++j) acc[g % MI][j] = mx4_multiply<g / MI, g / MI>(fb[g / MI][j], sb[j], fa[g % RING], sa[g % MI], acc[g % MI][j]);
             __builtin_amdgcn_sched_barrier(0);
             // (the scales of the last rows of A: the others were read with the stage's first fragments)
             if constexpr (g == 0) {
