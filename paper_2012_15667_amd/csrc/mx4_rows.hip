@@ -27,7 +27,7 @@ mx4_wave_kernel(Mx4Product p, int tiles_m)
     for (int t = 0; t < steps; ++t) {
         const u32x4 u = *reinterpret_cast<const u32x4*>(a + t * 64LL), v = *reinterpret_cast<const u32x4*>(b + t * 64LL);
         const unsigned x = *reinterpret_cast<const unsigned*>(sa + t * 4LL) >> 8 * grp, y = *reinterpret_cast<const unsigned*>(sb + t * 4LL) >> 8 * grp;
-        sum = mx4_multiply<0, 0>(v, y, u, x, sum);
+        sum = mx4_multiply_16<0>(v, y, u, x, sum);
     }
     float bias[4];
     const int first = (int)n0 + 4 * grp;

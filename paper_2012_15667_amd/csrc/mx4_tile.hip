@@ -1,10 +1,9 @@
 // C = A B^T of operands in microscaled 4-bit floating point on the scaled matrix instructions, with bias, activation and residual in the epilogue.
 //
 // The shape of the dense layers' product kernel (dense_tile.hip) with stages of 256 k: a row of a stage is again 128 bytes, eight pieces of 16, and a piece is
-// a block of 32 codes, which is what a lane gives to a matrix instruction of 128 k.  A stage also takes the rows' eight scales, 8 bytes.  Lane group g
-// multiplies pieces 2 g and 2 g + 1 of a row, one in each half of the stage (both operands alike: the order of k does not matter), so its two scales
-// are neighbours, and one 16-bit read of LDS gives the instruction both, each by its byte
-// number.  (32 bits read at odd multiples of two bytes, of which the upper half is not looked at, take LDS 77 cycles an instruction.)
+// a block of 32 codes, which is what a lane gives to a matrix instruction of 64 k.  A stage also takes the rows' eight scales, 8 bytes.  The lanes of half h
+// multiply pieces 4 h + kk of a row, kk = 0 ... 3 (both operands alike: the order of k does not matter), so their four scales are one word of LDS, from
+// which the instruction takes byte kk.
 #include "dense_math.h"
 #include "kernels.h"
 #include "lds_dma.h"
@@ -22,6 +21,11 @@ constexpr int stage_bytes(int bm, int bn) { return code_bytes(bm, bn) + (bm + bn
 // How many times a block's sums go through LDS.
 constexpr int finish_passes(int bm, int bn) { return bm * bn * 4 > 2 * stage_bytes(bm, bn) ? 2 : 1; }
 
+// Where piece `piece` of a 128-byte row lies.  LDS serves a 16-byte read in turns of sixteen lanes, which are not neighbours: 0-3, 12-15 and 20-27 together,
+// then 4-11, 16-19 and 28-31 (found by counting conflicts).  Rows r and r + 1 lie in different halves of the banks; of either set the rows' upper
+// bits, 1 to 3, are eight different ones.
+__device__ __forceinline__ int mx4_place(int row, int piece) { return piece ^ (row >> 1 & 7); }
+
 __device__ __forceinline__ void dma16(const uint8_t* base, unsigned offset, unsigned lds)
 {
     lds_dma_load_16(reinterpret_cast<const float*>(base), offset, lds);
@@ -31,7 +35,7 @@ template <int DT, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, 2)
 mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
 {
-    constexpr int WAVES = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+    constexpr int WAVES = WM * WN, MI = BM / WM / 32, NI = BN / WN / 32;
     constexpr int LA = BM / 8 / WAVES, LB = BN / 8 / WAVES;           // loads of a wave and stage: 8 rows each
     constexpr int SCALE_LOADS = (BM + BN) / 32;                       // of a stage: 32 rows each
     constexpr unsigned STAGE = stage_bytes(BM, BN);
@@ -39,7 +43,7 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
     extern __shared__ u32x4 lds16[];
     char* const lds = reinterpret_cast<char*>(lds16);
     const unsigned lds0 = lds_byte_address(reinterpret_cast<const float*>(lds));
-    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
@@ -63,8 +67,9 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
     const unsigned pitch = (unsigned)words * 64u, scale_pitch = (unsigned)words * 4u;
     const int rows_a = p.M - m0 < BM ? p.M - m0 : BM, rows_b = p.N - n0 < BN ? p.N - n0 : BN;
     const int last_a = (rows_a - 1) & ~7, last_b = (rows_b - 1) & ~7;
-    // (a load's rows start at a multiple of 8; piece 2 g + kk lies where piece 4 kk + g would: what neighbouring lane groups read together are neighbours)
-    const int placed = place(lane >> 3, lane & 7), from_piece = 2 * (placed & 3) + (placed >> 2);
+    // (a load's rows start at a multiple of 8, and are alike in the bits that `place` looks at for all loads of a wave)
+    static_assert(WAVES % 4 == 0, "as said");
+    const int from_piece = mx4_place(wave * 8 + (lane >> 3), lane & 7);
     const auto offset_in = [&](int rows) {
         const int r = lane >> 3;
         unsigned at = __umul24(r < rows ? r : rows - 1, pitch) + 16u * from_piece;     // (a pitch is at most 2^21)
@@ -126,41 +131,43 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
         }
     };
 
-    f32x4 acc[MI][NI];
+    f32x16 acc[MI][NI];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int c = 0; c < 16; ++c) acc[i][j][c] = 0.f;
 
-    // A stage is 2 MI groups of NI matrix instructions: half kk, sixteen rows i of A.  The order is written out and held: after each group the reads
-    // of the operands of a later one are issued, A into a ring of RING fragments, AHEAD groups ahead, B a half ahead.  The one barrier of a stage
+    // A stage is 4 MI groups of NI matrix instructions: quarter kk, 32 rows i of A.  The order is written out and held: after each group the reads
+    // of the operands of a later one are issued, A into a ring of four fragments, AHEAD groups ahead, B a quarter ahead.  The one barrier of a stage
     // stands before its last groups, when all of it has been read: the next stage has arrived then, its first reads go out behind the last groups, and
     // the buffer is free for the stage after it.
-    constexpr int GROUPS = 2 * MI, RING = MI < 4 ? MI : 4, AHEAD = MI == 8 ? 3 : MI == 4 ? 2 : 1, LAST = AHEAD;
-    static_assert(GROUPS % RING == 0 && AHEAD < RING && LAST < MI && NI <= GROUPS - LAST, "a stage is read before its barrier");
+    constexpr int GROUPS = 4 * MI, RING = 4, AHEAD = MI == 1 ? 2 : 3, LAST = MI == 4 ? 3 : MI;
+    static_assert(LAST <= AHEAD && 2 * MI + NI <= GROUPS - LAST, "a stage is read before its barrier");
     u32x4 fa[RING], fb[2][NI];
-    unsigned sa[MI], sb[NI], next_sb[NI];
-    // fragments: row l16 of sixteen, piece 2 grp + kk; the rest is the same for all lanes
-    const int frag_a = (wm * (BM / WM) + l16) * ROW_BYTES + 16 * place(l16, grp);
-    const int frag_b = (BM + wn * (BN / WN) + l16) * ROW_BYTES + 16 * place(l16, grp);
-    const int frag_sa = code_bytes(BM, BN) + (wm * (BM / WM) + l16) * ROW_SCALES + 2 * grp;
-    const int frag_sb = code_bytes(BM, BN) + (BM + wn * (BN / WN) + l16) * ROW_SCALES + 2 * grp;
-    auto read_a = [&](const char* at, int g) { fa[g % RING] = *reinterpret_cast<const u32x4*>(at + (frag_a ^ 64 * (g / MI)) + g % MI * 16 * ROW_BYTES); };
-    auto read_b = [&](const char* at, int kk, int j) { fb[kk][j] = *reinterpret_cast<const u32x4*>(at + (frag_b ^ 64 * kk) + j * 16 * ROW_BYTES); };
-    auto read_sa = [&](const char* at, int i) { sa[i] = *reinterpret_cast<const unsigned short*>(at + frag_sa + i * 16 * ROW_SCALES); };
-    auto scale_b = [&](const char* at, int j) -> unsigned { return *reinterpret_cast<const unsigned short*>(at + frag_sb + j * 16 * ROW_SCALES); };
+    unsigned sa[MI], sb[NI], next_sa[MI], next_sb[NI];
+    // fragments: row l32 of 32, piece 4 hi + kk; the rest is the same for all lanes
+    const int frag_a = (wm * (BM / WM) + l32) * ROW_BYTES + 16 * mx4_place(l32, 4 * hi);
+    const int frag_b = (BM + wn * (BN / WN) + l32) * ROW_BYTES + 16 * mx4_place(l32, 4 * hi);
+    const int frag_sa = code_bytes(BM, BN) + (wm * (BM / WM) + l32) * ROW_SCALES + 4 * hi;
+    const int frag_sb = code_bytes(BM, BN) + (BM + wn * (BN / WN) + l32) * ROW_SCALES + 4 * hi;
+    auto read_a = [&](const char* at, int g) { fa[g % RING] = *reinterpret_cast<const u32x4*>(at + (frag_a ^ 16 * (g / MI)) + g % MI * 32 * ROW_BYTES); };
+    auto read_b = [&](const char* at, int kk, int j) { fb[kk % 2][j] = *reinterpret_cast<const u32x4*>(at + (frag_b ^ 16 * kk) + j * 32 * ROW_BYTES); };
+    auto read_scales = [&](const char* at, unsigned (&a)[MI], unsigned (&b)[NI]) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) a[i] = *reinterpret_cast<const unsigned*>(at + frag_sa + i * 32 * ROW_SCALES);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) b[j] = *reinterpret_cast<const unsigned*>(at + frag_sb + j * 32 * ROW_SCALES);
+    };
     if (s1 > s0) {
         load(s0, 0);
         lds_dma_wait_all();
         __syncthreads();
         if (s1 - s0 > 1) load(s0 + 1, 1);
+        read_scales(lds, sa, sb);
 #pragma unroll
-        for (int i = 0; i < MI - LAST; ++i) read_sa(lds, i);
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            sb[j] = scale_b(lds, j);
-            read_b(lds, 0, j);
-        }
+        for (int j = 0; j < NI; ++j) read_b(lds, 0, j);
 #pragma unroll
         for (int g = 0; g < AHEAD; ++g) read_a(lds, g);
     }
@@ -168,7 +175,7 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
         const char* const at = lds + (t - s0 & 1) * STAGE;
         const char* const next = lds + (~(t - s0) & 1) * STAGE;     // (after the last stage: read, not used)
         static_range<0, GROUPS>([&](auto group) {
-            constexpr int g = decltype(group)::value;
+            constexpr int g = decltype(group)::value, kk = g / MI, i = g % MI;
             if constexpr (g == GROUPS - LAST) {
                 lds_dma_wait_all();
                 __syncthreads();
@@ -176,51 +183,51 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < NI; ++j) acc[g % MI][j] = mx4_multiply<g / MI, g / MI>(fb[g / MI][j], sb[j], fa[g % RING], sa[g % MI], acc[g % MI][j]);
+            for (int j = 0; j < NI; ++j) acc[i][j] = mx4_multiply_32<kk>(fb[kk % 2][j], sb[j], fa[g % RING], sa[i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
-            // (the scales of the last rows of A: the others were read with the stage's first fragments)
-            if constexpr (g == 0) {
+            if constexpr (kk < 3 && i < NI) {
 #pragma unroll
-                for (int i = MI - LAST; i < MI; ++i) read_sa(at, i);
+                for (int j = i; j < NI; j += MI) read_b(at, kk + 1, j);
             }
-            if constexpr (g < NI) read_b(at, 1, g);
             if constexpr (g + AHEAD < GROUPS) read_a(at, g + AHEAD);
             if constexpr (g == GROUPS - LAST) {
+                read_scales(next, next_sa, next_sb);
 #pragma unroll
-                for (int i = 0; i < MI - LAST; ++i) read_sa(next, i);
-#pragma unroll
-                for (int j = 0; j < NI; ++j) {
-                    next_sb[j] = scale_b(next, j);
-                    read_b(next, 0, j);
-                }
+                for (int j = 0; j < NI; ++j) read_b(next, 0, j);
             }
             if constexpr (g >= GROUPS - LAST) {
                 constexpr int done = g - (GROUPS - LAST);                   // reads of A's next fragments: evenly over the last groups
 #pragma unroll
-                for (int i = AHEAD * done / LAST; i < AHEAD * (done + 1) / LAST; ++i) read_a(next, i);
+                for (int n = AHEAD * done / LAST; n < AHEAD * (done + 1) / LAST; ++n) read_a(next, n);
             }
         });
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sa[i] = next_sa[i];
 #pragma unroll
         for (int j = 0; j < NI; ++j) sb[j] = next_sb[j];
     }
 
+    // a lane's sums: row l32 of 32, columns 8 q + 4 hi + 0 ... 3 of 32 for q = 0 ... 3
+    const auto four = [&](int i, int j, int q) { return f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}; };
     if (p.splits > 1) {
-        const int mw = m0 + wm * (BM / WM) + l16, nw = n0 + wn * (BN / WN) + 4 * grp;
+        const int mw = m0 + wm * (BM / WM) + l32, nw = n0 + wn * (BN / WN) + 4 * hi;
         const long long ld = (p.N + 3) / 4 * 4;
         float* const out = p.partial + (long long)blockIdx.y * p.M * ld;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int m = mw + i * 16, n = nw + j * 16;
-                if (m < p.M && n < p.N) *reinterpret_cast<f32x4*>(out + m * ld + n) = acc[i][j];
-            }
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int m = mw + i * 32, n = nw + j * 32 + q * 8;
+                    if (m < p.M && n < p.N) *reinterpret_cast<f32x4*>(out + m * ld + n) = four(i, j, q);
+                }
         return;
     }
 
     // The sums go through LDS, as many rows at a time as fit, so that a thread finishes 16 bytes of a row and a wave's loads and stores are whole
     // rows.  16-byte piece c of row r lies at c ^ (r & 15).
-    constexpr int PASSES = finish_passes(BM, BN), PI = MI / PASSES, PASS_ROWS = WM * PI * 16;
+    constexpr int PASSES = finish_passes(BM, BN), PI = MI / PASSES, PASS_ROWS = WM * PI * 32;
     constexpr int W = FINISH_COLUMNS<DT>, LANES = BN / W, AT_ONCE = 64 * WAVES / LANES;   // threads of a row, rows of an iteration
     static_assert(PASS_ROWS * BN * 4 <= 2 * (int)STAGE && PASS_ROWS % AT_ONCE == 0, "a pass fits the stages' buffers");
     f32x4* const sums = reinterpret_cast<f32x4*>(lds);
@@ -233,10 +240,12 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
 #pragma unroll
         for (int i = 0; i < PI; ++i)
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int r = (wm * PI + i) * 16 + l16, c = wn * (BN / WN / 4) + j * 4 + grp;
-                sums[r * (BN / 4) + (c ^ l16)] = acc[pass * PI + i][j];
-            }
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = (wm * PI + i) * 32 + l32, c = wn * (BN / WN / 4) + j * 8 + 2 * q + hi;
+                    sums[r * (BN / 4) + (c ^ (r & 15))] = four(pass * PI + i, j, q);
+                }
         __syncthreads();
         by_activation(p.f.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll 1
@@ -244,11 +253,11 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
                 float z[W];
 #pragma unroll
                 for (int h = 0; h < W / 4; ++h) {
-                    const f32x4 four = sums[r * (BN / 4) + ((W / 4 * (tid % LANES) + h) ^ (r & 15))];
+                    const f32x4 part = sums[r * (BN / 4) + ((W / 4 * (tid % LANES) + h) ^ (r & 15))];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[4 * h + i] = four[i];
+                    for (int i = 0; i < 4; ++i) z[4 * h + i] = part[i];
                 }
-                const int m = m0 + r / (PI * 16) * (BM / WM) + pass * PI * 16 + r % (PI * 16);
+                const int m = m0 + r / (PI * 32) * (BM / WM) + pass * PI * 32 + r % (PI * 32);
                 finish_columns<DT, decltype(act)::value>(p.f, m, n, bias, z);
             }
         });
