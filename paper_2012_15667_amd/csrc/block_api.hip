@@ -97,7 +97,7 @@ int run_norm_backward(const iolb_block_norm_backward_args& a, void* ws, size_t* 
     *need = up256(plan.row_bytes) + up256(plan.column_bytes);
     if (!launch) return IOLB_OK;
     p.rows = static_cast<float*>(plan.row_bytes ? ws : nullptr);
-    p.columns = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(plan.row_bytes));
+    if (plan.column_bytes) p.columns = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(plan.row_bytes));
     BLOCK_HIP(launch_block_norm_backward(p, plan, a.dtype, call_stream()));
     return IOLB_OK;
 }

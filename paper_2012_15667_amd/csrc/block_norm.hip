@@ -6,23 +6,59 @@ namespace iolb {
 
 namespace {
 
-template <int WAVES>
-__device__ __forceinline__ float group_sum(float v, float (&part)[2][WAVES], int& turn)
+// v added over the lane's sixteen neighbours (DPP), then over the wave.  All lanes get the sum, in an order that does not depend on anything.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    if constexpr (WAVES > 1) {
-        // (two buffers in turn: who writes one again has passed the barrier behind all reads of it)
-        float* const at = part[turn];
-        turn ^= 1;
-        if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.f;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) v += at[i];
-    }
-    return v;
+    return v + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), CTRL, 0xf, 0xf, true));
 }
+
+__device__ __forceinline__ float sum_16(float v)
+{
+    v = dpp_add<0xb1>(v);                           // quad_perm [1,0,3,2]
+    v = dpp_add<0x4e>(v);                           // quad_perm [2,3,0,1]
+    v = dpp_add<0x141>(v);                          // row_half_mirror
+    return dpp_add<0x140>(v);                       // row_mirror
+}
+
+__device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+
+__device__ __forceinline__ float sum_64(float v)
+{
+    v = sum_16(v);
+    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
+
+// K values added over the TR threads of a row: sixteen lanes, a wave, or a workgroup of TR threads.
+template <int K, int TR>
+struct RowSum {
+    static constexpr int WAVES = TR / 64;
+    typedef float Part[2][K][WAVES > 1 ? WAVES : 1];
+    Part& part;
+    int turn = 0;
+    // (two buffers in turn: who writes one again has passed the barrier behind all reads of it)
+    template <int N>
+    __device__ __forceinline__ void operator()(float (&v)[N])
+    {
+        static_assert(N <= K, "room for as many");
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = TR == 16 ? sum_16(v[k]) : sum_64(v[k]);
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) part[turn][k][threadIdx.x >> 6] = v[k];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                v[k] = 0.f;
+#pragma unroll
+                for (int i = 0; i < WAVES; ++i) v[k] += part[turn][k][i];
+            }
+            turn ^= 1;
+        }
+    }
+};
 
 struct RowStats { float mean, r; };
 
@@ -68,11 +104,8 @@ __device__ __forceinline__ void load_or(const T* p, int c, int N, float or_else,
 }
 
 template <class T>
-__device__ __forceinline__ void store_columns_of(T* p, int have, const float (&v)[8])
+__device__ __forceinline__ void store_eight_of(T* p, int have, const typename Piece<T, 8>::type& t)
 {
-    typename Piece<T, 8>::type t;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = (T)v[i];
     if (have >= 8) {
         *reinterpret_cast<typename Piece<T, 8>::type*>(p) = t;
     } else {
@@ -82,15 +115,174 @@ __device__ __forceinline__ void store_columns_of(T* p, int have, const float (&v
     }
 }
 
+template <class T>
+__device__ __forceinline__ void store_columns_of(T* p, int have, const float (&v)[8])
+{
+    typename Piece<T, 8>::type t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = (T)v[i];
+    store_eight_of(p, have, t);
+}
+
+// ---- rows in registers ------------------------------------------------------------------------------------
+// Eight neighbouring values as they are in memory; zeros beyond the row's end.
+template <class T> using Eight = typename Piece<T, 8>::type;
+
+template <class T>
+__device__ __forceinline__ Eight<T> load_eight(const T* p, int have)
+{
+    if (have >= 8) return *reinterpret_cast<const Eight<T>*>(p);
+    Eight<T> t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = i < have ? p[i] : (T)0.f;
+    return t;
+}
+
+// A row's values, TR threads to a row, C times eight a thread: c-th piece at column 8 (c TR + thread).
+template <class T, int C> struct Row { Eight<T> of[C]; };
+
+template <int TR, int C, class T>
+__device__ __forceinline__ void load_row(const T* p, int N, int thread, Row<T, C>& row)
+{
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = 8 * (c * TR + thread);
+        row.of[c] = load_eight(p + at, N - at);
+    }
+}
+
+// A weight's, a bias's or a gate's values; `or_else` where there is none.
+template <int TR, int C, class T>
+__device__ __forceinline__ void load_row_or(const T* p, int N, int thread, float or_else, Row<T, C>& row)
+{
+    if (p) {
+        load_row<TR, C>(p, N, thread, row);
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) row.of[c][i] = (T)or_else;
+    }
+}
+
+// Keeps the compiler from holding the values in 32 bits across a step: they are taken from what is in memory's form again, for half the registers.
+template <class T, int C>
+__device__ __forceinline__ void hold(Row<T, C>& row)
+{
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            u32x4 w = __builtin_bit_cast(u32x4, row.of[c]);
+            asm volatile("" : "+v"(w));
+            row.of[c] = __builtin_bit_cast(Eight<T>, w);
+        }
+    }
+}
+
+// (v - mean) r is the row normalised; v [C][8] in 32 bits, zeros beyond the end.
+template <int TR, int C, class S>
+__device__ __forceinline__ RowStats stats_of_row(float (&v)[C][8], int N, int thread, int kind, float eps, S& sum)
+{
+    float one[1];
+    float mean = 0.f;
+    if (kind == IOLB_NORM_LAYER) {
+        one[0] = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) one[0] += v[c][i];
+        sum(one);
+        mean = one[0] / (float)N;
+    }
+    one[0] = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = 8 * (c * TR + thread) + i < N ? v[c][i] - mean : 0.f;
+            one[0] = __builtin_fmaf(d, d, one[0]);
+        }
+    sum(one);
+    return {mean, 1.f / sqrtf(one[0] / (float)N + eps)};
+}
+
+template <int DT, int TR, int C>
+__global__ void __launch_bounds__(TR > 256 ? TR : 256)
+block_norm_rows_kernel(BlockNorm p)
+{
+    typedef typename DenseType<DT>::type T;
+    constexpr int ROWS = TR > 256 ? 1 : 256 / TR;
+    __shared__ typename RowSum<1, TR>::Part part;
+    RowSum<1, TR> sum{part};
+    const int thread = threadIdx.x % TR;
+    // (more than a wave to a row: all threads of the workgroup alike)
+    for (long long m = (long long)blockIdx.x * ROWS + threadIdx.x / TR; m < p.M; m += (long long)gridDim.x * ROWS) {
+        Row<T, C> x, w, b;
+        load_row<TR, C>(static_cast<const T*>(p.x) + m * p.ldx, p.N, thread, x);
+        float v[C][8];
+        if (p.h) {
+            Row<T, C> h, g;
+            load_row<TR, C>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, h);
+            load_row_or<TR, C>(static_cast<const T*>(p.post_weight), p.N, thread, 1.f, w);
+            load_row_or<TR, C>(p.gate ? static_cast<const T*>(p.gate) + m / p.rows_per_group * p.N : nullptr, p.N, thread, 1.f, g);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] = (float)h.of[c][i];
+            RowStats s{0.f, 1.f};
+            if (p.post != IOLB_NORM_NONE) s = stats_of_row<TR, C>(v, p.N, thread, p.post, p.eps, sum);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] = (v[c][i] - s.mean) * s.r * (float)w.of[c][i];
+                const int at = 8 * (c * TR + thread);
+                if (p.post_bias) {
+                    const Eight<T> bias = load_eight(static_cast<const T*>(p.post_bias) + at, p.N - at);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[c][i] += (float)bias[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[c][i] = p.scale * (float)x.of[c][i] + (float)g.of[c][i] * v[c][i];
+                    x.of[c][i] = (T)v[c][i];
+                    v[c][i] = at + i < p.N ? (float)x.of[c][i] : 0.f;       // (as rounded: what a backward pass reads is what is normalised)
+                }
+                store_eight_of(static_cast<T*>(p.out) + m * p.ldo + at, p.N - at, x.of[c]);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] = (float)x.of[c][i];
+        }
+        if (!p.y) continue;
+        load_row_or<TR, C>(static_cast<const T*>(p.pre_weight), p.N, thread, 1.f, w);
+        load_row_or<TR, C>(static_cast<const T*>(p.pre_bias), p.N, thread, 0.f, b);
+        const RowStats s = stats_of_row<TR, C>(v, p.N, thread, p.pre, p.eps, sum);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = 8 * (c * TR + thread);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x.of[c][i] = (T)((v[c][i] - s.mean) * s.r * (float)w.of[c][i] + (float)b.of[c][i]);
+            store_eight_of(static_cast<T*>(p.y) + m * p.ldy + at, p.N - at, x.of[c]);
+        }
+    }
+}
+
+// ---- rows of any length ------------------------------------------------------------------------------------
 // A workgroup to a row, which it reads again from the caches for each step.
 template <int DT>
 __global__ void __launch_bounds__(256)
-block_norm_kernel(BlockNorm p)
+block_norm_long_kernel(BlockNorm p)
 {
     typedef typename DenseType<DT>::type T;
-    __shared__ float part[2][4];
-    int turn = 0;
-    const auto sum = [&](float v) { return group_sum<4>(v, part, turn); };
+    __shared__ RowSum<1, 256>::Part part;
+    RowSum<1, 256> sums{part};
+    const auto sum = [&](float v) {
+        float one[1] = {v};
+        sums(one);
+        return one[0];
+    };
     for (long long m = blockIdx.x; m < p.M; m += gridDim.x) {
         const T* from = static_cast<const T*>(p.x) + m * p.ldx;
         if (p.h) {
@@ -155,12 +347,16 @@ __device__ __forceinline__ void gradient_of_out(const BlockNormBackward& p, long
 
 template <int DT>
 __global__ void __launch_bounds__(256)
-norm_backward_rows_kernel(BlockNormBackward p)
+norm_backward_long_kernel(BlockNormBackward p)
 {
     typedef typename DenseType<DT>::type T;
-    __shared__ float part[2][4];
-    int turn = 0;
-    const auto sum = [&](float v) { return group_sum<4>(v, part, turn); };
+    __shared__ RowSum<1, 256>::Part part;
+    RowSum<1, 256> sums{part};
+    const auto sum = [&](float v) {
+        float one[1] = {v};
+        sums(one);
+        return one[0];
+    };
     const float per = 1.f / (float)p.N;
     for (long long m = blockIdx.x; m < p.M; m += gridDim.x) {
         RowSums s{0.f, 1.f, 0.f, 0.f, 0.f, 1.f, 0.f, 0.f};
@@ -289,14 +485,175 @@ norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces)
     }
 }
 
-// What weights, biases and gate get.  First the pieces of a group (its rows of the gate are done then, and all of it where there is one group); then
-// (`across`) the groups, whose sums lie in the place of their first piece.  A workgroup takes 16 columns, 16 threads to each.
-template <int DT>
-__global__ void __launch_bounds__(256)
-norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across)
+// The same for rows that are held in registers: a workgroup takes a piece's rows, TR threads to a row, reads everything once, and holds its columns' sums
+// meanwhile; the next row is on its way while one is worked on.  BIASES: whether S0 and T0 are wanted.
+template <int DT, int TR, int C, bool BIASES>
+__global__ void __launch_bounds__(TR > 256 ? TR : 256)
+norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wanted)
 {
     typedef typename DenseType<DT>::type T;
-    __shared__ float part[NORM_COLUMN_SUMS][16][16 + 1];
+    constexpr int ROWS = TR > 256 ? 1 : 256 / TR;
+    __shared__ typename RowSum<4, TR>::Part part;
+    RowSum<4, TR> sum{part};
+    const int thread = threadIdx.x % TR, slot = threadIdx.x / TR;
+    const int group = (int)(blockIdx.x / (unsigned)pieces.in_group), piece = (int)(blockIdx.x % (unsigned)pieces.in_group);
+    const long long first = (long long)group * p.rows_per_group, r0 = first + (long long)piece * pieces.per;
+    const long long r1 = r0 + pieces.per < first + p.rows_per_group ? r0 + pieces.per : first + p.rows_per_group;
+    const float per = 1.f / (float)p.N;
+
+    Row<T, C> w, wp, g;
+    load_row_or<TR, C>(static_cast<const T*>(p.pre_weight), p.N, thread, 1.f, w);
+    load_row_or<TR, C>(static_cast<const T*>(p.post_weight), p.N, thread, 1.f, wp);
+    load_row_or<TR, C>(p.gate ? static_cast<const T*>(p.gate) + (long long)group * p.N : nullptr, p.N, thread, 1.f, g);
+    float s1[C][8], t1[C][8], s0[BIASES ? C : 1][8], t0[BIASES ? C : 1][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s1[c][i] = t1[c][i] = 0.f;
+            if constexpr (BIASES) s0[c][i] = t0[c][i] = 0.f;
+        }
+    struct Rows { Row<T, C> x, h, dy, dout; };
+    const auto load = [&](long long m, Rows& r) {
+        if (m >= r1) return;
+        if (p.dy) {
+            load_row<TR, C>(static_cast<const T*>(p.x) + m * p.ldx, p.N, thread, r.x);
+            load_row<TR, C>(static_cast<const T*>(p.dy) + m * p.lddy, p.N, thread, r.dy);
+        }
+        if (p.dout) load_row<TR, C>(static_cast<const T*>(p.dout) + m * p.lddout, p.N, thread, r.dout);
+        if (p.h) load_row<TR, C>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, r.h);
+    };
+    Rows r{};
+    load(r0 + slot, r);
+    for (long long m = r0 + slot; m < r1; m += ROWS) {
+        Rows next{};
+        load(m + ROWS, next);
+        hold(w);
+        hold(wp);
+        hold(g);
+        float mean_x = 0.f, mean_h = 0.f;
+        if (p.pre == IOLB_NORM_LAYER || p.post == IOLB_NORM_LAYER) {
+            float v[2] = {0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[0] += (float)r.x.of[c][i];
+                    v[1] += (float)r.h.of[c][i];
+                }
+            sum(v);
+            if (p.pre == IOLB_NORM_LAYER) mean_x = v[0] * per;
+            if (p.post == IOLB_NORM_LAYER) mean_h = v[1] * per;
+        }
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool live = 8 * (c * TR + thread) + i < p.N;
+                const float x = live ? (float)r.x.of[c][i] - mean_x : 0.f, h = live ? (float)r.h.of[c][i] - mean_h : 0.f;
+                const float t = (float)r.dy.of[c][i] * (float)w.of[c][i];
+                v[0] = __builtin_fmaf(x, x, v[0]);
+                v[1] = __builtin_fmaf(t, x, v[1]);
+                v[2] += t;
+                v[3] = __builtin_fmaf(h, h, v[3]);
+            }
+        sum(v);
+        const float r_x = p.dy ? 1.f / sqrtf(v[0] * per + p.eps) : 0.f, along_x = v[1] * r_x * per, mean_d = p.pre == IOLB_NORM_LAYER ? v[2] * per : 0.f;
+        const float r_h = p.post != IOLB_NORM_NONE ? 1.f / sqrtf(v[3] * per + p.eps) : 1.f;
+        hold(r.x);
+        hold(r.h);
+        hold(r.dy);
+        float d[C][8], u[2] = {0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool live = 8 * (c * TR + thread) + i < p.N;
+                const float dy = (float)r.dy.of[c][i], hat_x = ((float)r.x.of[c][i] - mean_x) * r_x, hat_h = ((float)r.h.of[c][i] - mean_h) * r_h;
+                d[c][i] = live ? (float)r.dout.of[c][i] + r_x * (dy * (float)w.of[c][i] - hat_x * along_x - mean_d) : 0.f;
+                s1[c][i] = __builtin_fmaf(d[c][i], hat_h, s1[c][i]);
+                t1[c][i] = __builtin_fmaf(dy, hat_x, t1[c][i]);
+                if constexpr (BIASES) {
+                    s0[c][i] += d[c][i];
+                    t0[c][i] += dy;
+                }
+                const float t = d[c][i] * (float)g.of[c][i] * (float)wp.of[c][i];
+                u[0] = __builtin_fmaf(t, hat_h, u[0]);
+                u[1] += t;
+            }
+        if (p.post != IOLB_NORM_NONE) sum(u);
+        hold(r.h);
+        hold(g);
+        hold(wp);
+        const float along_h = p.post != IOLB_NORM_NONE ? u[0] * per : 0.f, mean_p = p.post == IOLB_NORM_LAYER ? u[1] * per : 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = 8 * (c * TR + thread);
+            Eight<T> to;
+            if (p.dh) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float hat_h = ((float)r.h.of[c][i] - mean_h) * r_h, t = d[c][i] * (float)g.of[c][i] * (float)wp.of[c][i];
+                    to[i] = (T)(r_h * (t - hat_h * along_h - mean_p));
+                }
+                store_eight_of(static_cast<T*>(p.dh) + m * p.N + at, p.N - at, to);
+            }
+            if (p.dx) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) to[i] = (T)(p.scale * d[c][i]);
+                store_eight_of(static_cast<T*>(p.dx) + m * p.N + at, p.N - at, to);
+            }
+        }
+        r = next;
+    }
+    if (!wanted) return;
+    // the rows' sums joined where several rows were taken at a time, and written
+    const long long ld = (p.N + 7) / 8 * 8;
+    float* const out = p.columns + (long long)blockIdx.x * NORM_COLUMN_SUMS * ld;
+    const auto put = [&](int k, const float (&v)[C][8]) {
+        if (!(wanted >> k & 1)) return;
+        if constexpr (ROWS == 1) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = 8 * (c * TR + thread);
+                if (at < p.N) {
+                    *reinterpret_cast<f32x4*>(out + k * ld + at) = f32x4{v[c][0], v[c][1], v[c][2], v[c][3]};
+                    *reinterpret_cast<f32x4*>(out + k * ld + at + 4) = f32x4{v[c][4], v[c][5], v[c][6], v[c][7]};
+                }
+            }
+        } else {
+            __shared__ float all[ROWS][8 * TR * C];
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) all[slot][8 * (c * TR + thread) + i] = v[c][i];
+            __syncthreads();
+            for (int n = threadIdx.x; n < 8 * TR * C && n < p.N; n += 256) {
+                float t = 0.f;
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) t += all[i][n];
+                out[k * ld + n] = t;
+            }
+        }
+    };
+    put(S1, s1);
+    put(T1, t1);
+    if constexpr (BIASES) {
+        put(S0, s0);
+        put(T0, t0);
+    }
+}
+
+// What weights, biases and gate get.  First the pieces of a group (its rows of the gate are done then, and all of it where there is one group); then
+// (`across`) the groups, whose sums lie in the place of their first piece.  A workgroup takes 16 columns, 64 threads to each.
+template <int DT>
+__global__ void __launch_bounds__(1024)
+norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across, unsigned wanted)
+{
+    typedef typename DenseType<DT>::type T;
+    __shared__ float part[NORM_COLUMN_SUMS][64][16 + 1];
     const unsigned blocks = (unsigned)(p.N + 15) / 16;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, n = (int)(blockIdx.x % blocks * 16) + tx;
     const long long ld = (p.N + 7) / 8 * 8;
@@ -304,30 +661,41 @@ norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across)
     const T* const gates = static_cast<const T*>(p.gate);
     float sums[NORM_COLUMN_SUMS] = {0.f, 0.f, 0.f, 0.f};
     float* const at = p.columns + (long long)group * in_group * NORM_COLUMN_SUMS * ld + n;
-    if (n < p.N)
-        for (int i = ty; i < count; i += 16) {
+    if (n < p.N) {
+#pragma unroll 4
+        for (int i = ty; i < count; i += 64) {
             const float* const from = at + (long long)(across ? i * (long long)in_group : i) * NORM_COLUMN_SUMS * ld;
             const float g = across && gates ? (float)gates[(long long)i * p.N + n] : 1.f;
-            sums[S1] += g * from[S1 * ld];
-            sums[S0] += g * from[S0 * ld];
-            sums[T1] += from[T1 * ld];
-            sums[T0] += from[T0 * ld];
+#pragma unroll
+            for (int k = 0; k < NORM_COLUMN_SUMS; ++k)
+                if (wanted >> k & 1) sums[k] += (k == S1 || k == S0 ? g : 1.f) * from[k * ld];
         }
+    }
 #pragma unroll
     for (int k = 0; k < NORM_COLUMN_SUMS; ++k) part[k][ty][tx] = sums[k];
     __syncthreads();
+    // a wave adds one of the four, four threads to a column
+    const int k = threadIdx.x >> 6;
+    if (k < NORM_COLUMN_SUMS) {
+        const int col = threadIdx.x & 15, row = threadIdx.x >> 4 & 3;
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t += part[k][4 * i + row][col];
+        t += __shfl_xor(t, 16);
+        t += __shfl_xor(t, 32);
+        __builtin_amdgcn_wave_barrier();
+        if (row == 0) part[k][0][col] = t;
+    }
+    __syncthreads();
     if (ty != 0 || n >= p.N) return;
 #pragma unroll
-    for (int k = 0; k < NORM_COLUMN_SUMS; ++k) {
-        sums[k] = 0.f;
-        for (int i = 0; i < 16; ++i) sums[k] += part[k][i][tx];
-    }
+    for (int j = 0; j < NORM_COLUMN_SUMS; ++j) sums[j] = part[j][0][tx];
     const T *const wp = static_cast<const T*>(p.post_weight), *const bp = static_cast<const T*>(p.post_bias);
     if (!across && p.dgate)
         static_cast<T*>(p.dgate)[(long long)group * p.N + n] = (T)((wp ? (float)wp[n] : 1.f) * sums[S1] + (bp ? (float)bp[n] * sums[S0] : 0.f));
     if (!across && p.groups > 1) {
 #pragma unroll
-        for (int k = 0; k < NORM_COLUMN_SUMS; ++k) at[k * ld] = sums[k];
+        for (int j = 0; j < NORM_COLUMN_SUMS; ++j) at[j * ld] = sums[j];
         return;
     }
     const float g = !across && gates ? (float)gates[n] : 1.f;
@@ -346,7 +714,32 @@ void by_type(int dtype, F f)
     else f(std::integral_constant<int, IOLB_BF16>{});
 }
 
-bool column_sums(const BlockNormBackward& p) { return p.dgate || p.dpost_weight || p.dpost_bias || p.dpre_weight || p.dpre_bias; }
+// Which of the column sums are wanted.
+unsigned column_sums(const BlockNormBackward& p)
+{
+    return (p.dgate || p.dpost_weight ? 1u << S1 : 0u) | (p.dpost_bias || (p.dgate && p.post_bias) ? 1u << S0 : 0u) | (p.dpre_weight ? 1u << T1 : 0u) |
+           (p.dpre_bias ? 1u << T0 : 0u);
+}
+
+constexpr int MOST_IN_REGISTERS = 512 * 8 * 4;          // values of a row, forward
+constexpr int MOST_BACKWARD = 512 * 8 * 2;              // backward
+
+// f called with the threads that take a row, and how many times eight values each; 0 where the row is not held in registers.
+template <class F>
+void by_row(int N, F f)
+{
+    const auto call = [&](auto tr, auto c) { f(tr, c); };
+#define IOLB_ROW(TR, C) if (N <= 8 * TR * C) return call(std::integral_constant<int, TR>{}, std::integral_constant<int, C>{})
+    IOLB_ROW(16, 1);
+    IOLB_ROW(64, 1);
+    IOLB_ROW(64, 2);
+    IOLB_ROW(256, 1);
+    IOLB_ROW(256, 2);
+    IOLB_ROW(512, 2);
+    if (N <= MOST_IN_REGISTERS) return call(std::integral_constant<int, 512>{}, std::integral_constant<int, 4>{});
+#undef IOLB_ROW
+    call(std::integral_constant<int, 256>{}, std::integral_constant<int, 0>{});
+}
 
 unsigned row_groups(int M) { return (unsigned)(M < 65536 ? M : 65536); }
 
@@ -354,40 +747,62 @@ unsigned row_groups(int M) { return (unsigned)(M < 65536 ? M : 65536); }
 
 hipError_t launch_block_norm(const BlockNorm& p, int dtype, hipStream_t st)
 {
-    by_type(dtype, [&](auto t) { block_norm_kernel<decltype(t)::value><<<row_groups(p.M), 256, 0, st>>>(p); });
+    by_type(dtype, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        by_row(p.N, [&](auto tr, auto c) {
+            constexpr int TR = decltype(tr)::value, C = decltype(c)::value;
+            if constexpr (C == 0) block_norm_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
+            else block_norm_rows_kernel<DT, TR, C><<<row_groups((p.M + (TR > 256 ? 0 : 256 / TR - 1)) / (TR > 256 ? 1 : 256 / TR)), TR > 256 ? TR : 256, 0, st>>>(p);
+        });
+    });
     return hipGetLastError();
 }
 
 NormBackwardPlan block_norm_backward_plan(const BlockNormBackward& p, int)
 {
     NormBackwardPlan plan{};
-    if (!column_sums(p)) return plan;
-    const int across = (p.N + 63) / 64, R = p.rows_per_group;
-    int wanted = 2048 / across / p.groups;
-    if (wanted > (R + 31) / 32) wanted = (R + 31) / 32;
+    const bool in_registers = p.N <= MOST_BACKWARD;
+    const long long across = in_registers ? 1 : (p.N + 63) / 64;
+    const int R = p.rows_per_group;
+    // Rows in registers: two workgroups of 256 threads to a compute unit, or one of 512, and no more: each writes a row of sums.  8192 x 4096 bf16: 768
+    // pieces 126 us, 512 111; 16384 x 1024 66 / 57; 4096 x 8192: 512 115, 256 106.
+    const int at_once = !in_registers ? 32 : p.N <= 128 ? 16 : p.N <= 1024 ? 4 : 1, all = !in_registers ? 2048 : p.N <= 4096 ? 512 : 256;
+    long long wanted = all / across / p.groups;
+    if (wanted > (R + at_once - 1) / at_once) wanted = (R + at_once - 1) / at_once;
     if (wanted < 1) wanted = 1;
     plan.pieces = {1, 1};                           // (no rows: sums of nothing)
     if (R > 0) {
-        plan.pieces.per = (R + wanted - 1) / wanted;
+        plan.pieces.per = (int)((R + wanted - 1) / wanted);
         plan.pieces.in_group = (R + plan.pieces.per - 1) / plan.pieces.per;
     }
     // (a launch counts its threads in 32 bits)
-    plan.launchable = (long long)(p.N + 15) / 16 * p.groups * 256 <= 0xffffffffLL && (long long)across * plan.pieces.in_group * p.groups * 256 <= 0xffffffffLL;
-    plan.row_bytes = (size_t)p.M * NORM_ROW_SUMS * 4;
-    plan.column_bytes = (size_t)plan.pieces.in_group * p.groups * NORM_COLUMN_SUMS * ((p.N + 7) / 8 * 8) * 4;
+    const long long pieces = (long long)plan.pieces.in_group * p.groups;
+    plan.launchable = (long long)(p.N + 15) / 16 * p.groups * 1024 <= 0xffffffffLL && across * pieces * 512 <= 0xffffffffLL;
+    if (!column_sums(p)) return plan;
+    plan.row_bytes = in_registers ? 0 : (size_t)p.M * NORM_ROW_SUMS * 4;
+    plan.column_bytes = (size_t)pieces * NORM_COLUMN_SUMS * ((p.N + 7) / 8 * 8) * 4;
     return plan;
 }
 
 hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBackwardPlan& plan, int dtype, hipStream_t st)
 {
+    const unsigned wanted = column_sums(p), pieces = (unsigned)(plan.pieces.in_group * p.groups);
     by_type(dtype, [&](auto t) {
         constexpr int DT = decltype(t)::value;
-        if (p.M) norm_backward_rows_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
-        if (!column_sums(p)) return;
-        norm_backward_columns_kernel<DT><<<(unsigned)((p.N + 63) / 64) * (unsigned)(plan.pieces.in_group * p.groups), 256, 0, st>>>(p, plan.pieces);
-        norm_backward_weights_kernel<DT><<<(unsigned)((p.N + 15) / 16) * (unsigned)p.groups, 256, 0, st>>>(p, plan.pieces.in_group, false);
+        by_row(p.N, [&](auto tr, auto c) {
+            constexpr int TR = decltype(tr)::value, C = decltype(c)::value;
+            if constexpr (C == 0 || 8 * TR * C > MOST_BACKWARD) {
+                if (p.M) norm_backward_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
+                if (wanted) norm_backward_columns_kernel<DT><<<(unsigned)((p.N + 63) / 64) * pieces, 256, 0, st>>>(p, plan.pieces);
+            } else {
+                const auto kernel = wanted >> S0 & 1 || wanted >> T0 & 1 ? norm_backward_rows_kernel<DT, TR, C, true> : norm_backward_rows_kernel<DT, TR, C, false>;
+                kernel<<<pieces, TR > 256 ? TR : 256, 0, st>>>(p, plan.pieces, wanted);
+            }
+        });
+        if (!wanted) return;
+        norm_backward_weights_kernel<DT><<<(unsigned)((p.N + 15) / 16) * (unsigned)p.groups, 1024, 0, st>>>(p, plan.pieces.in_group, false, wanted);
         if (p.groups > 1 && (p.dpost_weight || p.dpost_bias || p.dpre_weight || p.dpre_bias))
-            norm_backward_weights_kernel<DT><<<(unsigned)((p.N + 15) / 16), 256, 0, st>>>(p, plan.pieces.in_group, true);
+            norm_backward_weights_kernel<DT><<<(unsigned)((p.N + 15) / 16), 1024, 0, st>>>(p, plan.pieces.in_group, true, wanted);
     });
     return hipGetLastError();
 }
