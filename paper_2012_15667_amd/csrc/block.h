@@ -71,11 +71,17 @@ hipError_t launch_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int ro
 struct Mx4Product {
     const uint8_t *a, *a_scales, *b, *b_scales;
     int M, N, K;
+    const void* x;                          // few rows: a as a tensor of the type, rows ldx apart, in place of its codes; else null
+    long long ldx;
     int splits;                             // workgroups that share a tile's K; their sums go to `partial` if > 1
     float* partial;                         // [splits][M][N rounded up to 4]
     DenseFinish f;
 };
 constexpr int MX4_FEW = 16;                 // rows of a of the kernel for the fewest
+// Whether that kernel brings x into 4 bits itself.  Every sixteen columns do it again, some 0.13 us of a SIMD for 128 k, against a launch of 2 to 4 us
+// (calls, us, in the kernel / before it: 1 x 4096 -> 4096 bf16 8.1 / 12.4, 1 x 512 -> 1000 7.6 / 11.7, 1 x 4096 -> 16384 15.5 / 13.4, 1 x 16384 -> 4096 17.6 / 14.0).
+inline bool mx4_few_packs(long long N, long long K) { return K <= 8192 && N * K <= 1 << 25; }
+bool mx4_few_launchable(int N);
 hipError_t launch_mx4_few(const Mx4Product& p, int dtype, hipStream_t st);
 DenseTilePlan mx4_tile_plan(int M, int N, int K);
 hipError_t launch_mx4_tile(const Mx4Product& p, int tile, int dtype, hipStream_t st);

@@ -125,9 +125,9 @@ int run_linear(const iolb_linear_mx4_args& a, void* ws, size_t* need, bool launc
     p.a = a.x_codes; p.a_scales = a.x_scales;
     p.b = a.w_codes; p.b_scales = a.w_scales;
     p.f = DenseFinish{a.bias, a.residual, a.y, nullptr, nullptr, a.ldr, a.ldy, p.M, p.N, a.act, a.residual_first != 0};
-    const bool pack = a.x && a.K > 0, few = a.M <= MX4_FEW;
+    const bool few = a.M <= MX4_FEW, pack = a.x && a.K > 0 && !(few && mx4_few_packs(a.N, a.K));
     const DenseTilePlan plan = few ? DenseTilePlan{0, 1} : mx4_tile_plan(p.M, p.N, p.K);
-    if (few ? !launchable(((a.N + 15) / 16 + 3) / 4) : !dense_tile_launchable(plan, p.M, p.N)) return IOLB_EUNSUPPORTED;
+    if (few ? !mx4_few_launchable(p.N) : !dense_tile_launchable(plan, p.M, p.N)) return IOLB_EUNSUPPORTED;
     p.splits = plan.splits;
     const size_t codes = up256((size_t)a.M * mx4_pitch(a.K)), scales = up256((size_t)a.M * mx4_scale_pitch(a.K));
     const size_t partial = plan.splits > 1 ? up256(dense_partial_bytes(plan.splits, a.M, a.N)) : 0;
@@ -140,6 +140,7 @@ int run_linear(const iolb_linear_mx4_args& a, void* ws, size_t* need, bool launc
         p.a = to;
         p.a_scales = to + codes;
     }
+    if (few && !pack) { p.x = a.x; p.ldx = a.ldx; }
     if (partial) p.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + (pack ? codes + scales : 0));
     BLOCK_HIP(few ? launch_mx4_few(p, a.dtype, st) : launch_mx4_tile(p, plan.tile, a.dtype, st));
     return IOLB_OK;

@@ -38,6 +38,15 @@ __device__ __forceinline__ unsigned mx4_codes(const float (&v)[8], float unit)
 
 __device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// The largest of four neighbouring lanes'.
+__device__ __forceinline__ unsigned most_of_four(unsigned v)
+{
+    const unsigned a = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true);        // quad_perm [1,0,3,2]
+    v = a > v ? a : v;
+    const unsigned b = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true);        // quad_perm [2,3,0,1]
+    return b > v ? b : v;
+}
+
 // c += (rows of a) (rows of b)^T; a lane holds the 32 codes of one row in one block, and that block's scale in byte BYTE of its word.
 // 16 rows, 128 k: row lane % 16, block lane / 16; element i of c is a's row 4 (lane / 16) + i, b's row lane % 16.
 // 32 rows, 64 k: row lane % 32, block lane / 32; element i of c is a's row 8 (i / 4) + 4 (lane / 32) + i % 4, b's row lane % 32.

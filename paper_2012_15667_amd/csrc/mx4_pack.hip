@@ -5,29 +5,44 @@ namespace iolb {
 
 namespace {
 
-// Four lanes share a block of 32, eight values each.  A workgroup covers `wide` threads of a row, up to its padded end, and 256 / wide rows.
+// Four lanes share a block of 32, eight values each.  A workgroup covers `wide` threads of a row, up to its padded end, and 256 / wide rows, one after the
+// other, the next one on its way meanwhile.
 template <int DT>
 __global__ void __launch_bounds__(256)
 mx4_pack_kernel(const void* x, long long ldx, int rows, int cols, uint8_t* codes, uint8_t* scales, int wide_log)
 {
     typedef typename DenseType<DT>::type T;
+    typedef typename Piece<T, 8>::type Eight;
     const int wide = 1 << wide_log, tx = threadIdx.x & (wide - 1), ty = threadIdx.x >> wide_log;
-    const long long pitch = (cols + MX4_WIDE - 1LL) / MX4_WIDE * (MX4_WIDE / 2);
+    const long long pitch = (cols + MX4_WIDE - 1LL) / MX4_WIDE * (MX4_WIDE / 2), step = (long long)gridDim.y * (256 >> wide_log);
     const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 8), have = cols - c;
-    for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r - ty < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (r < rows && have > 0) load_columns(static_cast<const T*>(x) + r * ldx + c, have, v);
+    const T* const xs = static_cast<const T*>(x) + c;
+    Eight next{};
+    const auto load = [&](long long r) {
+        if (r >= rows || have <= 0) return;
+        const T* const from = xs + r * ldx;
+        if (have >= 8) {
+            next = *reinterpret_cast<const Eight*>(from);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) next[i] = from[i];
+        }
+    };
+    long long r = (long long)blockIdx.y * (256 >> wide_log) + ty;
+    load(r);
+    for (; r - ty < rows; r += step) {
+        const Eight now = next;
+        load(r + step);
+        float v[8];
         unsigned most = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+            v[i] = (float)now[i];
             const unsigned b = magnitude_bits(v[i]);
             most = b > most ? b : most;
         }
-#pragma unroll
-        for (int d = 1; d < 4; d *= 2) {
-            const unsigned b = (unsigned)__shfl_xor((int)most, d);
-            most = b > most ? b : most;
-        }
+        most = most_of_four(most);
         const int s = mx4_scale(most);
         if (r >= rows || c / 2 >= pitch) continue;
         *reinterpret_cast<unsigned*>(codes + r * pitch + c / 2) = s == MX4_NAN ? 0u : mx4_codes(v, mx4_unit(s));
@@ -49,9 +64,20 @@ mx4_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int rows, int col
     const long long pitch = (cols + MX4_WIDE - 1LL) / MX4_WIDE * (MX4_WIDE / 2);
     const int c = (int)((blockIdx.x * (unsigned)wide + tx) * 8), have = cols - c;
     if (have <= 0) return;
-    for (long long r = (long long)blockIdx.y * (256 >> wide_log) + ty; r < rows; r += (long long)gridDim.y * (256 >> wide_log)) {
-        const int s = scales[r * (pitch / 16) + c / MX4_BLOCK];
-        const unsigned w = *reinterpret_cast<const unsigned*>(codes + r * pitch + c / 2);
+    const long long step = (long long)gridDim.y * (256 >> wide_log);
+    int next_s = 0;
+    unsigned next_w = 0;
+    const auto load = [&](long long r) {
+        if (r >= rows) return;
+        next_s = scales[r * (pitch / 16) + c / MX4_BLOCK];
+        next_w = *reinterpret_cast<const unsigned*>(codes + r * pitch + c / 2);
+    };
+    long long r = (long long)blockIdx.y * (256 >> wide_log) + ty;
+    load(r);
+    for (; r < rows; r += step) {
+        const int s = next_s;
+        const unsigned w = next_w;
+        load(r + step);
         const float unit = mx4_unit(s);
         const f32x2 pair[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1),
                                __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3)};
@@ -72,14 +98,17 @@ mx4_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int rows, int col
     }
 }
 
+// Workgroups, more than fill the chip at once.
+constexpr int GROUPS = 16384;
+
 struct RowGrid { dim3 grid; int wide_log; };
 RowGrid row_grid(int rows, long long cols, long long each)
 {
     int wide_log = 2;                               // whole blocks of 32
     while (wide_log < 8 && (each << wide_log) < cols) ++wide_log;
     const long long gx = (cols + (each << wide_log) - 1) / (each << wide_log), per = 256 >> wide_log;
-    const long long gy = (rows + per - 1) / per;
-    return {dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), wide_log};
+    const long long gy = (rows + per - 1) / per, most = (GROUPS + gx - 1) / gx;
+    return {dim3((unsigned)gx, (unsigned)(gy < most ? gy : most)), wide_log};
 }
 
 }  // namespace
