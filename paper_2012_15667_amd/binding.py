@@ -31,6 +31,7 @@ ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 CHECKPOINT_BLOCK = 32                       # values of a row that share a scale
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 MX4_BLOCK, MX4_WIDE = 32, 128               # values of a row that share a scale; columns that rows in 4 bits are padded to
+MX4_FEW = 16                                # rows of a tensor that linear_mx4 may take without a workspace
 
 
 class LinearArgs(ctypes.Structure):
@@ -610,6 +611,14 @@ def _use_stream_on(device):
     _check(lib().iolb_set_stream(raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream))
 
 
+def _call_in_new_workspace(call, query, args, like):
+    """The same for a call that is known to need one."""
+    need = ctypes.c_size_t(0)
+    _check(query(args, need))
+    ws = like.new_empty(need.value, dtype=_torch.uint8)
+    _check(call(args, ws.data_ptr(), need.value))
+
+
 def _call_with_workspace(call, query, args, like):
     # A call that needs a workspace and has none launches nothing, so most small ones are made in one go.  The workspace comes from
     # torch's allocator, which hands memory out again in the order of the stream.
@@ -761,10 +770,15 @@ def _norm_code(kind, name):
 
 def _graph_wanted(inputs, given):
     """Whether a result of `inputs` has to stand in autograd's graph; `given`: tensors that the results are written to."""
-    wanted = any(t is not None and t.requires_grad for t in (*inputs, *given)) and _torch.is_grad_enabled()
-    if wanted and any(y is not None and y.requires_grad for y in given):
-        raise RuntimeError("a tensor that is written to must not require gradients")
-    return wanted
+    if not _torch.is_grad_enabled():
+        return False
+    for y in given:
+        if y is not None and y.requires_grad:
+            raise RuntimeError("a tensor that is written to must not require gradients")
+    for t in inputs:
+        if t is not None and t.requires_grad:
+            return True
+    return False
 
 
 def _gate_of(gate, dtype, device, M, N):
@@ -872,7 +886,8 @@ def block_norm_backward(dy, dx_out, x, h=None, post="none", post_weight=None, po
                                  lddy, lddo, ldx, ldh, *[t.data_ptr() if t is not None else None for t in g])
     L = lib()
     _use_stream_on(device)
-    _call_with_workspace(L.iolb_block_norm_backward, L.iolb_block_norm_backward_workspace_bytes, args, x)
+    run = _call_in_new_workspace if want_weights else _call_with_workspace
+    run(L.iolb_block_norm_backward, L.iolb_block_norm_backward_workspace_bytes, args, x)
     return g
 
 
@@ -999,7 +1014,8 @@ def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False,
     args = LinearMx4Args(M, N, K, code, _act_code(act), 1 if residual_first else 0, px, ldx, pxc, pxs, pwc, pws, pb, pr, py, ldr, ldy)
     L = lib()
     _use_stream_on(device)
-    _call_with_workspace(L.iolb_linear_mx4, L.iolb_linear_mx4_workspace_bytes, args, like)
+    run = _call_in_new_workspace if px is not None and M > MX4_FEW else _call_with_workspace
+    run(L.iolb_linear_mx4, L.iolb_linear_mx4_workspace_bytes, args, like)
     if wanted:
         y = _without_graph(y, given, inputs, "linear_mx4() has no gradients")
     return y

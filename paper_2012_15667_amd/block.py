@@ -1,0 +1,145 @@
+"""Residual dense blocks: the part of a transformer that is not attention, trained from 8-bit checkpoints and answering in 4 bits.
+
+A block adds to the residual stream x what a widening layer, gelu, dropout and a narrowing layer make of the stream's norm n:
+
+    h = down(dropout(gelu(up(n)))),   x' = scale x + gate post(h),   n' = pre(x')
+
+The last line is one call (block_norm): the end of this block and the start of the next.  What the forward pass keeps for the backward pass: the
+8-bit checkpoints of n, of the widening layer's pre-activation and of what dropout left, and h and x' themselves.  Dropout's mask is drawn again.
+
+    python -m paper_2012_15667_amd.block                                # a few steps of gradient descent
+    python -m paper_2012_15667_amd.block --width 1024 --blocks 4 --dtype float32
+    python -m paper_2012_15667_amd.block --one-token                    # latency of a token, weights in 16 and in 4 bits
+
+Synthetic data; one JSON line a step.
+"""
+import argparse
+import json
+import math
+import time
+from collections import namedtuple
+
+import torch
+
+from . import binding as B
+
+#: Weights of a block, as the calls take them; pre_weight is of the norm behind it.  Their gradients come in the same form.
+Weights = namedtuple("Weights", "up up_bias down down_bias post_weight gate pre_weight")
+
+
+class Blocks:
+    def __init__(self, width, hidden, blocks, dtype=torch.bfloat16, norm="rms", p=0.1, scale=1.0, seed=0):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+
+        def matrix(n, k):
+            return (torch.randn((n, k), generator=g, device="cuda") * math.sqrt(1.0 / k)).to(dtype)
+
+        def column(n, value):
+            return torch.full((n,), value, device="cuda", dtype=dtype)
+        self.norm, self.p, self.scale, self.seed = norm, p, scale, seed
+        self.first = column(width, 1.0)             # of the norm before the first block
+        self.blocks = [Weights(matrix(hidden, width), column(hidden, 0.0), matrix(width, hidden), column(width, 0.0), column(width, 1.0),
+                               column(width, 0.5), column(width, 1.0)) for _ in range(blocks)]
+        self.in_4_bits = None
+
+    def _end(self, w):
+        return dict(post=self.norm, post_weight=w.post_weight, gate=w.gate, scale=self.scale, pre=self.norm, pre_weight=w.pre_weight)
+
+    def forward(self, x, step=0):
+        """(the last norm, what the backward pass needs) of the rows x; `step` chooses dropout's masks."""
+        kept = []
+        n = B.block_norm(x, pre=self.norm, pre_weight=self.first).y
+        for i, w in enumerate(self.blocks):
+            n8 = B.checkpoint_pack(n)
+            a, z8 = B.linear(n, w.up, w.up_bias, act="gelu", checkpoint=True)
+            d, d8 = B.dropout(a, self.p, self.seed, step * len(self.blocks) + i, checkpoint=True)
+            h = B.linear(d, w.down, w.down_bias)
+            out, n = B.block_norm(x, h, **self._end(w))
+            kept.append((n8, z8, d8, h, out))
+            x = out
+        return n, kept
+
+    def backward(self, dn, x0, kept, step=0):
+        """(gradient of x0, gradient of `first`, [Weights of gradients]) from that of the last norm; x0 and step as the forward pass had them."""
+        grads = []
+        dx = None
+        for i in reversed(range(len(self.blocks))):
+            w = self.blocks[i]
+            n8, z8, d8, h, out = kept[i]
+            e = B.block_norm_backward(dn, dx, out, h, **self._end(w))
+            down = B.linear_backward(e.dh, w.down, d8)
+            da = B.dropout(down.dx, self.p, self.seed, step * len(self.blocks) + i)
+            up = B.linear_backward(da, w.up, n8, z8, act="gelu")
+            grads.append(Weights(up.dw, up.db, down.dw, down.db, e.dpost_weight, e.dgate, e.dpre_weight))
+            dx, dn = e.dx, up.dx
+        e = B.block_norm_backward(dn, dx, x0, pre=self.norm, pre_weight=self.first)
+        return e.dx, e.dpre_weight, grads[::-1]
+
+    def descend(self, dfirst, grads, rate):
+        self.first.add_(dfirst, alpha=-rate)
+        for w, g in zip(self.blocks, grads):
+            for t, d in zip(w, g):
+                t.add_(d, alpha=-rate)
+        self.in_4_bits = None
+
+    def answer(self, x, in_4_bits=False):
+        """The last norm, without dropout; in_4_bits: with weights and layers' inputs in microscaled 4-bit floating point."""
+        if in_4_bits and self.in_4_bits is None:
+            self.in_4_bits = [(B.mx4_pack(w.up), B.mx4_pack(w.down)) for w in self.blocks]
+        n = B.block_norm(x, pre=self.norm, pre_weight=self.first).y
+        for i, w in enumerate(self.blocks):
+            if in_4_bits:
+                up, down = self.in_4_bits[i]
+                h = B.linear_mx4(B.linear_mx4(n, up, w.up_bias, act="gelu"), down, w.down_bias)
+            else:
+                h = B.linear(B.linear(n, w.up, w.up_bias, act="gelu"), w.down, w.down_bias)
+            x, n = B.block_norm(x, h, **self._end(w))
+        return n
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--rows", type=int, default=2048)
+    ap.add_argument("--width", type=int, default=4096)
+    ap.add_argument("--hidden", type=int, default=0, help="four times the width if not given")
+    ap.add_argument("--blocks", type=int, default=2)
+    ap.add_argument("--norm", default="rms", choices=["rms", "layer"])
+    ap.add_argument("--dropout", type=float, default=0.1)
+    ap.add_argument("--steps", type=int, default=8)
+    ap.add_argument("--rate", type=float, default=0.05)
+    ap.add_argument("--dtype", default="bfloat16", choices=["float32", "float16", "bfloat16"])
+    ap.add_argument("--one-token", action="store_true")
+    a = ap.parse_args(argv)
+    dtype = getattr(torch, a.dtype)
+    model = Blocks(a.width, a.hidden or 4 * a.width, a.blocks, dtype, a.norm, a.dropout)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn((1 if a.one_token else a.rows, a.width), generator=g, device="cuda").to(dtype)
+    if a.one_token:
+        for in_4_bits in (False, True):
+            for _ in range(3):
+                model.answer(x, in_4_bits)
+            torch.cuda.synchronize()
+            began = time.perf_counter()
+            for _ in range(100):
+                model.answer(x, in_4_bits)
+            torch.cuda.synchronize()
+            print(json.dumps({"one_token_us": round((time.perf_counter() - began) * 1e4, 1), "bits": 4 if in_4_bits else 8 * x.element_size()}))
+        return
+    # rows towards others: the mean of squares
+    want = torch.randn((a.rows, a.width), generator=g, device="cuda").to(dtype)
+    for step in range(a.steps):
+        torch.cuda.synchronize()
+        began = time.perf_counter()
+        n, kept = model.forward(x, step)
+        off = n.float() - want.float()
+        _, dfirst, grads = model.backward((off * (2.0 / a.rows)).to(dtype), x, kept, step)
+        model.descend(dfirst, grads, a.rate / a.width)
+        torch.cuda.synchronize()
+        print(json.dumps({"step": step, "loss": round(float(off.square().mean()), 4), "ms": round((time.perf_counter() - began) * 1e3, 3),
+                          "dtype": a.dtype}), flush=True)
+
+
+if __name__ == "__main__":
+    main()

@@ -288,8 +288,34 @@ hipError_t launch_tile(const Mx4Product& p, int tile, hipStream_t st)
 
 }  // namespace
 
-// A stage has as many bytes and matrix cycles as one of 64 k of 16-bit operands.
-DenseTilePlan mx4_tile_plan(int M, int N, int K) { return dense_tile_plan(M, N, (K + STEP - 1) / STEP * 64, 1); }
+// Block and number of workgroups that share K: the least modelled time, ns.  A stage of 256 k takes a workgroup `alone` while it has a compute unit to itself, and
+// `each` of the unit's time among several; `end` is what a block's epilogue takes of it.  Sharing K costs a second launch and the partial sums' way through
+// memory.  Fitted to a sweep of 22 shapes, 17 <= M <= 4096, 64 <= N <= 16384, 512 <= K <= 25088.  Examples (us, 256 x 256 / 128 x 128 / 64 x 128 / 64 x 64, each
+// with its best share of K): 64 x 4096 x 4096 15.4 / 11.2 / 10.5 / 9.2, 64 x 25088 -> 4096 25.4 / 19.7 / 18.6 / 18.0, 2048 x 2048 x 2048 21.6 / 11.8 / 11.5 / 13.0,
+// 700 x 5000 -> 9000 40 / 29 / 42 / 43, 4096 x 4096 x 4096 43 / 50 / 62 / 75.
+DenseTilePlan mx4_tile_plan(int M, int N, int K)
+{
+    static const struct { int m, n, alone, each, end; } blocks[DENSE_TILES] = {{256, 256, 1390, 2050, 3300}, {128, 128, 600, 700, 1800}, {64, 128, 420, 430, 900}, {64, 64, 320, 265, 500}};
+    static const int shares[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    const long long steps = ((long long)K + STEP - 1) / STEP;
+    DenseTilePlan plan{DENSE_TILE_256, 1};
+    double least = -1;
+    for (int b = 0; b < DENSE_TILES; ++b) {
+        const auto& k = blocks[b];
+        const long long tiles = (((long long)M + k.m - 1) / k.m) * (((long long)N + k.n - 1) / k.n);
+        for (const int s : shares) {
+            if (s > 1 && s > steps) break;
+            // (the largest block has a unit to itself: its rounds are whole ones)
+            double load = (double)tiles * s / 256;
+            if (b == DENSE_TILE_256 && load > 1) load = (double)((tiles * s + 255) / 256);
+            const double stage = k.each * load > k.alone ? k.each * load : k.alone;
+            double ns = stage * ((steps + s - 1) / s) + k.end * (load > 1 ? load : 1);
+            if (s > 1) ns += 2500 + 0.48e-3 * s * M * N * 4;
+            if (least < 0 || ns < least) { least = ns; plan = {b, s}; }
+        }
+    }
+    return plan;
+}
 
 hipError_t launch_mx4_tile(const Mx4Product& p, int tile, int dtype, hipStream_t st)
 {

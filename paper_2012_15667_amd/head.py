@@ -3,11 +3,14 @@
 The last convolution layer of a VGG-shaped network (Winograd, as the library runs it), 2 x 2 pooling, and three dense layers on
 the dense-layer operators: features -> hidden -> hidden -> classes with ReLU between them.  What the forward pass keeps for the
 backward pass is the 8-bit checkpoint of the features and of the two hidden layers' pre-activations, a byte and a 32nd for each value;
-the hidden layers' outputs are recomputed from the checkpoints (x_act="relu") and not kept.
+the hidden layers' outputs are recomputed from the checkpoints (x_act="relu") and not kept.  With dropout behind the hidden layers, what it leaves is
+checkpointed too, and its mask is drawn again in the backward pass.
 
     python -m paper_2012_15667_amd.head                                # one batch, a few steps of gradient descent
     python -m paper_2012_15667_amd.head --batch 64 --hidden 4096 --dtype bfloat16
+    python -m paper_2012_15667_amd.head --dropout 0.5
     python -m paper_2012_15667_amd.head --one-image                    # latency of the head on a single image
+    python -m paper_2012_15667_amd.head --one-image --mx4              # with its weights in microscaled 4-bit floating point
 
 Synthetic images and labels; one JSON line a step.
 """
@@ -38,21 +41,42 @@ class Head:
         (w1, b1), (w2, b2), (w3, b3) = self.layers
         return B.linear(B.linear(B.linear(x, w1, b1, act="relu"), w2, b2, act="relu"), w3, b3)
 
-    def forward(self, x):
-        """(logits, what the backward pass needs: three checkpoints)."""
+    def in_4_bits(self):
+        """The layers' weights in microscaled 4-bit floating point, for infer_mx4."""
+        return [(B.mx4_pack(w), b) for w, b in self.layers]
+
+    @staticmethod
+    def infer_mx4(x, layers):
+        (w1, b1), (w2, b2), (w3, b3) = layers
+        return B.linear_mx4(B.linear_mx4(B.linear_mx4(x, w1, b1, act="relu"), w2, b2, act="relu"), w3, b3)
+
+    def forward(self, x, p=0.0, seed=0, step=0):
+        """(logits, what the backward pass needs: three checkpoints, and with dropout two more and how its masks are drawn)."""
         (w1, b1), (w2, b2), (w3, b3) = self.layers
         x8 = B.checkpoint_pack(x)
         y1, z1 = B.linear(x, w1, b1, act="relu", checkpoint=True)
+        if p:
+            y1, d1 = B.dropout(y1, p, seed, 2 * step, checkpoint=True)
         y2, z2 = B.linear(y1, w2, b2, act="relu", checkpoint=True)
-        return B.linear(y2, w3, b3), (x8, z1, z2)
+        if not p:
+            return B.linear(y2, w3, b3), (x8, z1, z2)
+        y2, d2 = B.dropout(y2, p, seed, 2 * step + 1, checkpoint=True)
+        return B.linear(y2, w3, b3), (x8, z1, z2, d1, d2, (p, seed, 2 * step))
 
     def backward(self, dlogits, kept):
         """[(dw, db)] of the three layers, and dx."""
-        x8, z1, z2 = kept
+        x8, z1, z2 = kept[:3]
         (w1, _), (w2, _), (w3, _) = self.layers
-        g3 = B.linear_backward(dlogits, w3, z2, x_act="relu")
-        g2 = B.linear_backward(g3.dx, w2, z1, z2, act="relu", x_act="relu")
-        g1 = B.linear_backward(g2.dx, w1, x8, z1, act="relu")
+        if len(kept) == 3:
+            g3 = B.linear_backward(dlogits, w3, z2, x_act="relu")
+            g2 = B.linear_backward(g3.dx, w2, z1, z2, act="relu", x_act="relu")
+            dy1 = g2.dx
+        else:
+            d1, d2, (p, seed, offset) = kept[3:]
+            g3 = B.linear_backward(dlogits, w3, d2)
+            g2 = B.linear_backward(B.dropout(g3.dx, p, seed, offset + 1), w2, d1, z2, act="relu")
+            dy1 = B.dropout(g2.dx, p, seed, offset)
+        g1 = B.linear_backward(dy1, w1, x8, z1, act="relu")
         return [(g.dw, g.db) for g in (g1, g2, g3)], g1.dx
 
     def descend(self, grads, rate):
@@ -81,7 +105,7 @@ def loss_and_slope(logits, labels):
 
 
 def bytes_of(kept):
-    return sum(t.numel() * t.element_size() for c in kept for t in c)
+    return sum(t.numel() * t.element_size() for c in kept for t in c if isinstance(t, torch.Tensor))
 
 
 def main(argv=None):
@@ -94,7 +118,9 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=8)
     ap.add_argument("--rate", type=float, default=0.002)
     ap.add_argument("--dtype", default="float32", choices=["float32", "float16", "bfloat16"])
+    ap.add_argument("--dropout", type=float, default=0.0, help="behind the hidden layers")
     ap.add_argument("--one-image", action="store_true")
+    ap.add_argument("--mx4", action="store_true", help="one image: weights in 4 bits")
     a = ap.parse_args(argv)
     dtype = getattr(torch, a.dtype)
     g = torch.Generator(device="cuda")
@@ -106,19 +132,23 @@ def main(argv=None):
     x = features_of(images, kernels, dtype)
     head = Head(x.shape[1], a.hidden, a.classes, dtype)
     if a.one_image:
+        layers = head.in_4_bits() if a.mx4 else None
+
+        def infer():
+            return head.infer_mx4(x, layers) if a.mx4 else head.infer(x)
         for _ in range(3):
-            head.infer(x)
+            infer()
         torch.cuda.synchronize()
         began = time.perf_counter()
         for _ in range(100):
-            head.infer(x)
+            infer()
         torch.cuda.synchronize()
-        print(json.dumps({"one_image_us": round((time.perf_counter() - began) * 1e4, 1), "dtype": a.dtype}))
+        print(json.dumps({"one_image_us": round((time.perf_counter() - began) * 1e4, 1), "dtype": a.dtype, "weights": "mx4" if a.mx4 else a.dtype}))
         return
     for step in range(a.steps):
         torch.cuda.synchronize()
         began = time.perf_counter()
-        logits, kept = head.forward(x)
+        logits, kept = head.forward(x, a.dropout, 1, step)
         loss, slope = loss_and_slope(logits, labels)
         grads, _ = head.backward(slope, kept)
         head.descend(grads, a.rate)
