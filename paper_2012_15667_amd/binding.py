@@ -5,6 +5,7 @@ memory and the current stream.  There is no CPU fallback: a missing library rais
 """
 import ctypes
 import os
+import struct
 from collections import namedtuple
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -130,6 +131,22 @@ class IolbError(RuntimeError):
 
 
 _lib = None
+#: Entry points that take the bytes of their arguments' structure, packed by `_packed`: a structure built field by field takes a small call a microsecond.
+_bytes_of = {}
+
+
+def _packed(structure):
+    """The `pack` that lays values out as the structure has them (addresses as numbers, 0 for none)."""
+    codes = {ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f", ctypes.c_double: "d", ctypes.c_uint64: "Q", ctypes.c_void_p: "P"}
+    # (the compiler's alignment, to whole words at the end)
+    s = struct.Struct("@" + "".join(codes[t] for _, t in structure._fields_) + "0q")
+    if s.size != ctypes.sizeof(structure):
+        raise RuntimeError("%s has another layout" % structure.__name__)
+    return s.pack
+
+
+_pack_block_norm, _pack_block_norm_backward, _pack_dropout, _pack_linear_mx4 = (
+    _packed(s) for s in (BlockNormArgs, BlockNormBackwardArgs, DropoutArgs, LinearMx4Args))
 
 
 def lib():
@@ -211,6 +228,12 @@ def lib():
         for name, args in (("iolb_block_norm", BlockNormArgs), ("iolb_dropout", DropoutArgs)):
             getattr(L, name).restype = i
             getattr(L, name).argtypes = [ctypes.POINTER(args)]
+        for name, more in (("iolb_block_norm", []), ("iolb_dropout", []), ("iolb_linear_mx4", [vp, sz]), ("iolb_block_norm_backward", [vp, sz]),
+                           ("iolb_linear_mx4_workspace_bytes", [ctypes.POINTER(sz)]), ("iolb_block_norm_backward_workspace_bytes", [ctypes.POINTER(sz)])):
+            f = L[name]                         # (a function object of its own)
+            f.restype = i
+            f.argtypes = [ctypes.c_char_p] + more
+            _bytes_of[name] = f
         L.iolb_mx4_pack.restype = i
         L.iolb_mx4_pack.argtypes = [vp] + [ctypes.c_int64] * 3 + [i, vp, vp]
         L.iolb_mx4_unpack.restype = i
@@ -603,12 +626,17 @@ def _new_checkpoint(like, rows, cols):
                       like.new_empty((rows, -(-cols // CHECKPOINT_BLOCK)), dtype=_torch.uint8))
 
 
+_raw_stream = None
+
+
 def _use_stream_on(device):
+    global _raw_stream
     torch = _torch
     if device != torch.cuda.current_device():
         raise ValueError("the tensors are not on the current GPU")
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    _check(lib().iolb_set_stream(raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream))
+    if _raw_stream is None:
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    _check((_lib or lib()).iolb_set_stream(_raw_stream(device)))
 
 
 def _call_in_new_workspace(call, query, args, like):
@@ -784,7 +812,7 @@ def _graph_wanted(inputs, given):
 def _gate_of(gate, dtype, device, M, N):
     """(address, groups)"""
     if gate is None:
-        return None, 1
+        return 0, 1
     if isinstance(gate, _torch.Tensor) and gate.dim() == 2:
         groups = gate.shape[0]
         if groups < 1 or M % groups:
@@ -818,30 +846,31 @@ def block_norm(x, h=None, post="none", post_weight=None, post_bias=None, gate=No
         raise ValueError("weight, bias and y go with a norm: pre is none")
     if h is None and not kind_pre:
         raise ValueError("there is nothing to do")
-    ph, ldh = _rows(h, "h", dtype, device, (M, N))[:2] if h is not None else (None, 0)
+    ph, ldh = _rows(h, "h", dtype, device, (M, N))[:2] if h is not None else (0, 0)
     pgate, groups = _gate_of(gate, dtype, device, M, N)
-    columns = [_dense(t, n, dtype, device, (N,)) if t is not None else None
-               for t, n in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"), (pre_bias, "pre_bias"))]
+    wp = _dense(post_weight, "post_weight", dtype, device, (N,)) if post_weight is not None else 0
+    bp = _dense(post_bias, "post_bias", dtype, device, (N,)) if post_bias is not None else 0
+    w = _dense(pre_weight, "pre_weight", dtype, device, (N,)) if pre_weight is not None else 0
+    b = _dense(pre_bias, "pre_bias", dtype, device, (N,)) if pre_bias is not None else 0
     inputs, given = (x, h, post_weight, post_bias, gate, pre_weight, pre_bias), (x_out, y)
     wanted = _graph_wanted(inputs, given)
     if h is None:
-        po, ldo = None, 0
+        po, ldo = 0, 0
     elif x_out is None:
         x_out = x.new_empty((M, N))
         po, ldo = x_out.data_ptr(), N
     else:
         po, ldo = _rows(x_out, "x_out", dtype, device, (M, N))[:2]
     if not kind_pre:
-        py, ldy = None, 0
+        py, ldy = 0, 0
     elif y is None:
         y = x.new_empty((M, N))
         py, ldy = y.data_ptr(), N
     else:
         py, ldy = _rows(y, "y", dtype, device, (M, N))[:2]
-    args = BlockNormArgs(M, N, groups, code, kind_post, kind_pre, scale, eps, px, ph, columns[0], columns[1], pgate, columns[2], columns[3],
-                         po, py, ldx, ldh, ldo, ldy)
+    args = _pack_block_norm(M, N, groups, code, kind_post, kind_pre, scale, eps, px, ph, wp, bp, pgate, w, b, po, py, ldx, ldh, ldo, ldy)
     _use_stream_on(device)
-    _check(lib().iolb_block_norm(args))
+    _check(_bytes_of["iolb_block_norm"](args))
     if wanted:
         why = "block_norm() records no gradients: they are block_norm_backward's"
         if x_out is not None:
@@ -871,23 +900,24 @@ def block_norm_backward(dy, dx_out, x, h=None, post="none", post_weight=None, po
         raise ValueError("weight, bias and dy go with a norm: pre is none")
     if dy is None and dx_out is None:
         raise ValueError("dy or dx_out is needed")
-    pdy, lddy = _rows(dy, "dy", dtype, device, (M, N))[:2] if dy is not None else (None, 0)
-    pdo, lddo = _rows(dx_out, "dx_out", dtype, device, (M, N))[:2] if dx_out is not None else (None, 0)
-    ph, ldh = _rows(h, "h", dtype, device, (M, N))[:2] if h is not None else (None, 0)
+    pdy, lddy = _rows(dy, "dy", dtype, device, (M, N))[:2] if dy is not None else (0, 0)
+    pdo, lddo = _rows(dx_out, "dx_out", dtype, device, (M, N))[:2] if dx_out is not None else (0, 0)
+    ph, ldh = _rows(h, "h", dtype, device, (M, N))[:2] if h is not None else (0, 0)
     pgate, groups = _gate_of(gate, dtype, device, M, N)
-    columns = [_dense(t, n, dtype, device, (N,)) if t is not None else None
-               for t, n in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"), (pre_bias, "pre_bias"))]
+    wp = _dense(post_weight, "post_weight", dtype, device, (N,)) if post_weight is not None else 0
+    bp = _dense(post_bias, "post_bias", dtype, device, (N,)) if post_bias is not None else 0
+    w = _dense(pre_weight, "pre_weight", dtype, device, (N,)) if pre_weight is not None else 0
+    b = _dense(pre_bias, "pre_bias", dtype, device, (N,)) if pre_bias is not None else 0
 
     def like(t, there=True):
         return x.new_empty(t.shape) if t is not None and want_weights and there else None
     g = BlockNormGrads(x.new_empty((M, N)) if want_dx else None, x.new_empty((M, N)) if want_dx and h is not None else None,
                        like(gate), like(post_weight), like(post_bias), like(pre_weight, dy is not None), like(pre_bias, dy is not None))
-    args = BlockNormBackwardArgs(M, N, groups, code, kind_post, kind_pre, scale, eps, pdy, pdo, px, ph, columns[0], columns[1], pgate, columns[2],
-                                 lddy, lddo, ldx, ldh, *[t.data_ptr() if t is not None else None for t in g])
-    L = lib()
+    args = _pack_block_norm_backward(M, N, groups, code, kind_post, kind_pre, scale, eps, pdy, pdo, px, ph, wp, bp, pgate, w,
+                                     lddy, lddo, ldx, ldh, *[t.data_ptr() if t is not None else 0 for t in g])
     _use_stream_on(device)
     run = _call_in_new_workspace if want_weights else _call_with_workspace
-    run(L.iolb_block_norm_backward, L.iolb_block_norm_backward_workspace_bytes, args, x)
+    run(_bytes_of["iolb_block_norm_backward"], _bytes_of["iolb_block_norm_backward_workspace_bytes"], args, x)
     return g
 
 
@@ -916,8 +946,8 @@ def dropout(x, p, seed, offset=0, counter=None, residual=None, checkpoint=False,
     if not 0.0 <= p <= 1.0:
         raise ValueError("p must be between 0 and 1")
     seed, offset = _word64(seed, "seed"), _word64(offset, "offset")
-    pc = _dense(counter, "counter", torch.int64, device, (2,)) if counter is not None else None
-    pr, ldr = _rows(residual, "residual", dtype, device, (rows, cols))[:2] if residual is not None else (None, 0)
+    pc = _dense(counter, "counter", torch.int64, device, (2,)) if counter is not None else 0
+    pr, ldr = _rows(residual, "residual", dtype, device, (rows, cols))[:2] if residual is not None else (0, 0)
     wanted = _graph_wanted((x, residual), (y,))
     given = y is not None
     if given:
@@ -926,10 +956,10 @@ def dropout(x, p, seed, offset=0, counter=None, residual=None, checkpoint=False,
         y = x.new_empty((rows, cols))
         py, ldy = y.data_ptr(), cols
     z = _new_checkpoint(x, rows, cols) if checkpoint else None
-    args = DropoutArgs(rows, cols, code, p, seed, offset, pc, px, pr, py, ldx, ldr, ldy,
-                       z.q.data_ptr() if checkpoint else None, z.e.data_ptr() if checkpoint else None)
+    args = _pack_dropout(rows, cols, code, p, seed, offset, pc, px, pr, py, ldx, ldr, ldy,
+                         z.q.data_ptr() if checkpoint else 0, z.e.data_ptr() if checkpoint else 0)
     _use_stream_on(device)
-    _check(lib().iolb_dropout(args))
+    _check(_bytes_of["iolb_dropout"](args))
     if wanted:
         y = _without_graph(y, given, (x, residual), "dropout() records no gradients: they are dropout()'s of the same seed and offset")
     return (y, z) if checkpoint else y
@@ -990,19 +1020,19 @@ def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False,
         dtype, device, like = x.dtype, x.get_device(), x
         code = _dtype_code(dtype)
         px, ldx, M, K = _rows(x, "x", dtype, device)
-        pxc = pxs = None
+        pxc = pxs = 0
     else:
         pxc, pxs, M, K = _mx4_of(x, "x")
         device, like = x[0].get_device(), x[0]
         if dtype is None:
             dtype = y.dtype if y is not None else torch.bfloat16
         code = _dtype_code(dtype)
-        px, ldx = None, 0
+        px, ldx = 0, 0
     pwc, pws, N, C = _mx4_of(w, "w", device)
     if C != K:
         raise ValueError("x and w have different numbers of columns")
-    pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else None
-    pr, ldr = _rows(residual, "residual", dtype, device, (M, N))[:2] if residual is not None else (None, 0)
+    pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else 0
+    pr, ldr = _rows(residual, "residual", dtype, device, (M, N))[:2] if residual is not None else (0, 0)
     inputs = (like, bias, residual)
     wanted = _graph_wanted(inputs, (y,))
     given = y is not None
@@ -1011,11 +1041,10 @@ def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False,
     else:
         y = like.new_empty((M, N), dtype=dtype)
         py, ldy = y.data_ptr(), N
-    args = LinearMx4Args(M, N, K, code, _act_code(act), 1 if residual_first else 0, px, ldx, pxc, pxs, pwc, pws, pb, pr, py, ldr, ldy)
-    L = lib()
+    args = _pack_linear_mx4(M, N, K, code, _act_code(act), 1 if residual_first else 0, px, ldx, pxc, pxs, pwc, pws, pb, pr, py, ldr, ldy)
     _use_stream_on(device)
-    run = _call_in_new_workspace if px is not None and M > MX4_FEW else _call_with_workspace
-    run(L.iolb_linear_mx4, L.iolb_linear_mx4_workspace_bytes, args, like)
+    run = _call_in_new_workspace if px and M > MX4_FEW else _call_with_workspace
+    run(_bytes_of["iolb_linear_mx4"], _bytes_of["iolb_linear_mx4_workspace_bytes"], args, like)
     if wanted:
         y = _without_graph(y, given, inputs, "linear_mx4() has no gradients")
     return y
