@@ -32,7 +32,6 @@ ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 CHECKPOINT_BLOCK = 32                       # values of a row that share a scale
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 MX4_BLOCK, MX4_WIDE = 32, 128               # values of a row that share a scale; columns that rows in 4 bits are padded to
-MX4_FEW = 16                                # rows of a tensor that linear_mx4 may take without a workspace
 
 
 class LinearArgs(ctypes.Structure):
@@ -1043,7 +1042,7 @@ def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False,
         py, ldy = y.data_ptr(), N
     args = _pack_linear_mx4(M, N, K, code, _act_code(act), 1 if residual_first else 0, px, ldx, pxc, pxs, pwc, pws, pb, pr, py, ldr, ldy)
     _use_stream_on(device)
-    run = _call_in_new_workspace if px and M > MX4_FEW else _call_with_workspace
+    run = _call_in_new_workspace if px and M > 64 else _call_with_workspace
     run(_bytes_of["iolb_linear_mx4"], _bytes_of["iolb_linear_mx4_workspace_bytes"], args, like)
     if wanted:
         y = _without_graph(y, given, inputs, "linear_mx4() has no gradients")

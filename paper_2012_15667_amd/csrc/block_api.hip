@@ -125,7 +125,7 @@ int run_linear(const iolb_linear_mx4_args& a, void* ws, size_t* need, bool launc
     p.a = a.x_codes; p.a_scales = a.x_scales;
     p.b = a.w_codes; p.b_scales = a.w_scales;
     p.f = DenseFinish{a.bias, a.residual, a.y, nullptr, nullptr, a.ldr, a.ldy, p.M, p.N, a.act, a.residual_first != 0};
-    const bool few = a.M <= MX4_FEW, pack = a.x && a.K > 0 && !(few && mx4_few_packs(a.N, a.K));
+    const bool few = mx4_few_wanted(a.M, a.N, a.K), pack = a.x && a.K > 0 && !mx4_short(a.M, a.N, a.K);
     const DenseTilePlan plan = few ? DenseTilePlan{0, 1} : mx4_tile_plan(p.M, p.N, p.K);
     if (few ? !mx4_few_launchable(p.N) : !dense_tile_launchable(plan, p.M, p.N)) return IOLB_EUNSUPPORTED;
     p.splits = plan.splits;

@@ -75,24 +75,33 @@ __device__ __forceinline__ unsigned block_codes(const T* x, int have, u32x4& cod
 }
 
 // A workgroup takes sixteen columns, its waves a share of the summed axis each, in turn steps of 128 k: the weights go from memory to the registers of
-// the wave that multiplies them, four steps ahead.  A lane holds a block of 32 of row lane % 16 of either operand.  PACKED: x is in 4 bits already; a
-// tensor's blocks are brought into them where they are multiplied, by every workgroup again, which a launch of its own would cost more than.
-// The columns' operand comes first, so that a lane holds four neighbouring columns of one row.
-template <int DT, bool PACKED>
+// the wave that multiplies them, four steps ahead, with MR times sixteen rows of x.  A lane holds a block of 32 of row lane % 16 of either operand.
+// PACKED: x is in 4 bits already; a tensor's blocks are brought into them where they are multiplied, by every workgroup again, which a launch of its own
+// would cost more than.  The columns' operand comes first, so that a lane holds four neighbouring columns of one row.
+// (x's next blocks on their way meanwhile: 64 x 4096 -> 4096 19.1 -> 20.4 us, and more registers.  What counts there is the lanes' 64 bytes each, far apart.)
+template <int DT, bool PACKED, int MR>
 __global__ void __launch_bounds__(64 * WAVES)
 mx4_few_kernel(Mx4Product p)
 {
     typedef typename DenseType<DT>::type T;
-    __shared__ f32x4 part[WAVES][64];
+    __shared__ f32x4 part[MR][WAVES][64];
     const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4, wave = threadIdx.x >> 6;
     // (rows beyond the operand are read from its last row: their sums are never stored)
     const long long n0 = (long long)blockIdx.x * 16, n = n0 + l16 < p.N ? n0 + l16 : p.N - 1;
-    const int m = l16 < p.M ? l16 : p.M - 1;
     const int steps = (p.K + MX4_WIDE - 1) / MX4_WIDE;
     const uint8_t *const b = p.b + n * (steps * 64LL) + grp * 16, *const sb = p.b_scales + n * (steps * 4LL) + grp;
-    const uint8_t *const a = p.a + m * (steps * 64LL) + grp * 16, *const sa = p.a_scales + m * (steps * 4LL) + grp;
-    const T* const x = static_cast<const T*>(p.x) + m * p.ldx + grp * MX4_BLOCK;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    const uint8_t *a[MR], *sa[MR];
+    const T* x[MR];
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+        const int m = 16 * r + l16 < p.M ? 16 * r + l16 : p.M - 1;
+        a[r] = p.a + m * (steps * 64LL) + grp * 16;
+        sa[r] = p.a_scales + m * (steps * 4LL) + grp;
+        x[r] = static_cast<const T*>(p.x) + m * p.ldx + grp * MX4_BLOCK;
+    }
+    f32x4 sum[MR];
+#pragma unroll
+    for (int r = 0; r < MR; ++r) sum[r] = f32x4{0.f, 0.f, 0.f, 0.f};
     constexpr int AHEAD = 4;
     u32x4 w[AHEAD];
     unsigned ws[AHEAD];
@@ -109,36 +118,50 @@ mx4_few_kernel(Mx4Product p)
         for (int i = 0; i < AHEAD; ++i) {
             const int t = t0 + i * WAVES;
             if (t < steps) {
-                u32x4 v;
-                unsigned s;
-                if constexpr (PACKED) {
-                    v = *reinterpret_cast<const u32x4*>(a + t * 64LL);
-                    s = sa[t * 4LL];
-                } else {
-                    s = block_codes(x + (long long)t * MX4_WIDE, p.K - t * MX4_WIDE - grp * MX4_BLOCK, v);
+#pragma unroll
+                for (int r = 0; r < MR; ++r) {
+                    u32x4 v;
+                    unsigned s;
+                    if constexpr (PACKED) {
+                        v = *reinterpret_cast<const u32x4*>(a[r] + t * 64LL);
+                        s = sa[r][t * 4LL];
+                    } else {
+                        s = block_codes(x[r] + (long long)t * MX4_WIDE, p.K - t * MX4_WIDE - grp * MX4_BLOCK, v);
+                    }
+                    sum[r] = mx4_multiply_16<0>(w[i], ws[i], v, s, sum[r]);
                 }
-                sum = mx4_multiply_16<0>(w[i], ws[i], v, s, sum);
             }
             load(t + AHEAD * WAVES, i);
         }
     }
-    part[wave][lane] = sum;
-    __syncthreads();
-    if (wave != 0) return;
 #pragma unroll
-    for (int i = 1; i < WAVES; ++i) sum += part[i][lane];
+    for (int r = 0; r < MR; ++r) part[r][wave][lane] = sum[r];
+    __syncthreads();
+    // a wave joins and finishes sixteen rows
+    if (wave >= MR) return;
+    f32x4 all = part[wave][0][lane];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) all += part[wave][i][lane];
     float bias[4];
     const int first = (int)n0 + 4 * grp;
     load_bias<DT>(p.f, first, bias);
-    finish_four<DT>(p.f, l16, first, bias, sum);
+    finish_four<DT>(p.f, 16 * wave + l16, first, bias, all);
 }
 
-template <int DT>
+template <int DT, int MR>
 void launch(const Mx4Product& p, hipStream_t st)
 {
     const unsigned groups = (unsigned)(((long long)p.N + 15) / 16);
-    if (p.x) mx4_few_kernel<DT, false><<<groups, 64 * WAVES, 0, st>>>(p);
-    else mx4_few_kernel<DT, true><<<groups, 64 * WAVES, 0, st>>>(p);
+    if (p.x) mx4_few_kernel<DT, false, MR><<<groups, 64 * WAVES, 0, st>>>(p);
+    else mx4_few_kernel<DT, true, MR><<<groups, 64 * WAVES, 0, st>>>(p);
+}
+
+template <int DT>
+void launch_rows(const Mx4Product& p, hipStream_t st)
+{
+    if (p.M <= 16) launch<DT, 1>(p, st);
+    else if (p.M <= 32) launch<DT, 2>(p, st);
+    else launch<DT, 4>(p, st);
 }
 
 }  // namespace
@@ -147,9 +170,9 @@ bool mx4_few_launchable(int N) { return ((long long)N + 15) / 16 * (64 * WAVES) 
 
 hipError_t launch_mx4_few(const Mx4Product& p, int dtype, hipStream_t st)
 {
-    if (dtype == IOLB_F32) launch<IOLB_F32>(p, st);
-    else if (dtype == IOLB_F16) launch<IOLB_F16>(p, st);
-    else launch<IOLB_BF16>(p, st);
+    if (dtype == IOLB_F32) launch_rows<IOLB_F32>(p, st);
+    else if (dtype == IOLB_F16) launch_rows<IOLB_F16>(p, st);
+    else launch_rows<IOLB_BF16>(p, st);
     return hipGetLastError();
 }
 

@@ -176,7 +176,7 @@ def check_linear(rng, M, N, K, dtype, act="none", bias=True, residual=None, gap=
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("packed", [False, True])
-@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 64, 64), (1, 1000, 512), (2, 7, 5), (3, 33, 40), (5, 100, 257), (16, 48, 96), (17, 130, 129), (33, 70, 500), (64, 128, 1000),
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 64, 64), (1, 1000, 512), (2, 7, 5), (3, 33, 40), (5, 100, 257), (16, 48, 96), (17, 130, 129), (33, 70, 500), (20, 200, 4000), (64, 100, 2100), (64, 128, 1000),
                                    (65, 129, 65), (100, 260, 200), (129, 257, 384), (200, 40, 1030), (300, 520, 136)])
 def test_linear_sizes(dtype, packed, M, N, K):
     check_linear(np.random.default_rng(M + 7 * N + K), M, N, K, dtype, packed=packed)
@@ -214,7 +214,7 @@ def test_linear_blocks_of_all_sizes_and_long_sums(dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M", [1, 5, 16, 17, 70, 400])
+@pytest.mark.parametrize("M", [1, 5, 16, 17, 31, 33, 64, 70, 400])
 def test_linear_gives_the_same_for_a_tensor_and_for_its_codes(M):
     torch = _torch()
     rng = np.random.default_rng(M)
@@ -327,7 +327,7 @@ P = 4096
     (dict(w_codes=None), -1), (dict(w_scales=None), -1), (dict(w_codes=P + 8), -1), (dict(w_scales=P + 1), -1), (dict(y=None), -1), (dict(ldx=63), -1), (dict(ldy=7), -1),
     (dict(residual=P, ldr=7), -1), (dict(x=P + 2), -1), (dict(y=P + 1), -1), (dict(M=1 << 30, N=1 << 30, ldy=1 << 30), -2), ({}, -4)])
 def test_c_linear_refuses_without_touching_the_gpu(change, code):
-    a = dict(M=40, N=8, K=64, dtype=0, act=0, residual_first=0, x=P, ldx=64, x_codes=None, x_scales=None, w_codes=P, w_scales=P, bias=None, residual=None, y=P, ldr=8, ldy=8)
+    a = dict(M=100, N=8, K=64, dtype=0, act=0, residual_first=0, x=P, ldx=64, x_codes=None, x_scales=None, w_codes=P, w_scales=P, bias=None, residual=None, y=P, ldr=8, ldy=8)
     a.update(change)
     args = B.LinearMx4Args(*[a[n] for n, _ in B.LinearMx4Args._fields_])
     assert B.lib().iolb_linear_mx4(ctypes.byref(args), None, 0) == code
