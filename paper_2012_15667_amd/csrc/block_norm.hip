@@ -647,10 +647,11 @@ norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wante
 }
 
 // What weights, biases and gate get.  First the pieces of a group (its rows of the gate are done then, and all of it where there is one group); then
-// (`across`) the groups, whose sums lie in the place of their first piece.  A workgroup takes 16 columns, 64 threads to each.
-template <int DT>
+// (`across`) the groups, whose sums lie in the place of their first piece.  A workgroup takes 16 columns, 64 threads to each.  BIASES: whether S0 and T0
+// are there; of a pair one may have been left out, and what stands in its place is then read but goes nowhere.
+template <int DT, bool BIASES>
 __global__ void __launch_bounds__(1024)
-norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across, unsigned wanted)
+norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across)
 {
     typedef typename DenseType<DT>::type T;
     __shared__ float part[NORM_COLUMN_SUMS][64][16 + 1];
@@ -668,7 +669,7 @@ norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across, uns
             const float g = across && gates ? (float)gates[(long long)i * p.N + n] : 1.f;
 #pragma unroll
             for (int k = 0; k < NORM_COLUMN_SUMS; ++k)
-                if (wanted >> k & 1) sums[k] += (k == S1 || k == S0 ? g : 1.f) * from[k * ld];
+                if (BIASES || k == S1 || k == T1) sums[k] += (k == S1 || k == S0 ? g : 1.f) * from[k * ld];
         }
     }
 #pragma unroll
@@ -703,6 +704,56 @@ norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across, uns
     if (p.dpost_bias) static_cast<T*>(p.dpost_bias)[n] = (T)(g * sums[S0]);
     if (p.dpre_weight) static_cast<T*>(p.dpre_weight)[n] = (T)sums[T1];
     if (p.dpre_bias) static_cast<T*>(p.dpre_bias)[n] = (T)sums[T0];
+}
+
+// The same in one launch for some groups: a wave takes a group after the other, four threads to a column, and what it has summed over them is joined.
+template <int DT, bool BIASES>
+__global__ void __launch_bounds__(1024)
+norm_backward_groups_kernel(BlockNormBackward p, int in_group)
+{
+    typedef typename DenseType<DT>::type T;
+    __shared__ float part[NORM_COLUMN_SUMS][16][16 + 1];
+    const int tx = threadIdx.x & 15, row = threadIdx.x >> 4 & 3, wave = threadIdx.x >> 6, n = (int)(blockIdx.x * 16) + tx;
+    const long long ld = (p.N + 7) / 8 * 8;
+    const bool live = n < p.N;
+    const T* const gates = static_cast<const T*>(p.gate);
+    const float wp = p.post_weight && live ? (float)static_cast<const T*>(p.post_weight)[n] : 1.f;
+    const float bp = p.post_bias && live ? (float)static_cast<const T*>(p.post_bias)[n] : 0.f;
+    float all[NORM_COLUMN_SUMS] = {0.f, 0.f, 0.f, 0.f};
+    for (int group = wave; group < p.groups; group += 16) {
+        float sums[NORM_COLUMN_SUMS] = {0.f, 0.f, 0.f, 0.f};
+        const float* from = p.columns + ((long long)group * in_group + row) * NORM_COLUMN_SUMS * ld + n;
+        const float g = live ? (float)gates[(long long)group * p.N + n] : 0.f;
+        if (live) {
+#pragma unroll 4
+            for (int i = row; i < in_group; i += 4, from += 4 * NORM_COLUMN_SUMS * ld)
+#pragma unroll
+                for (int k = 0; k < NORM_COLUMN_SUMS; ++k)
+                    if (BIASES || k == S1 || k == T1) sums[k] += from[k * ld];
+        }
+#pragma unroll
+        for (int k = 0; k < NORM_COLUMN_SUMS; ++k) {
+            sums[k] += __shfl_xor(sums[k], 16);
+            sums[k] += __shfl_xor(sums[k], 32);
+            all[k] += (k == S1 || k == S0 ? g : 1.f) * sums[k];
+        }
+        if (p.dgate && live && row == 0) static_cast<T*>(p.dgate)[(long long)group * p.N + n] = (T)(wp * sums[S1] + (p.post_bias ? bp * sums[S0] : 0.f));
+    }
+    if (row == 0) {
+#pragma unroll
+        for (int k = 0; k < NORM_COLUMN_SUMS; ++k) part[k][wave][tx] = all[k];
+    }
+    __syncthreads();
+    if (threadIdx.x >= 16 || !live) return;
+#pragma unroll
+    for (int k = 0; k < NORM_COLUMN_SUMS; ++k) {
+        all[k] = 0.f;
+        for (int i = 0; i < 16; ++i) all[k] += part[k][i][tx];
+    }
+    if (p.dpost_weight) static_cast<T*>(p.dpost_weight)[n] = (T)all[S1];
+    if (p.dpost_bias) static_cast<T*>(p.dpost_bias)[n] = (T)all[S0];
+    if (p.dpre_weight) static_cast<T*>(p.dpre_weight)[n] = (T)all[T1];
+    if (p.dpre_bias) static_cast<T*>(p.dpre_bias)[n] = (T)all[T0];
 }
 
 // f called with the type as an integral constant.
@@ -800,9 +851,19 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBack
             }
         });
         if (!wanted) return;
-        norm_backward_weights_kernel<DT><<<(unsigned)((p.N + 15) / 16) * (unsigned)p.groups, 1024, 0, st>>>(p, plan.pieces.in_group, false, wanted);
-        if (p.groups > 1 && (p.dpost_weight || p.dpost_bias || p.dpre_weight || p.dpre_bias))
-            norm_backward_weights_kernel<DT><<<(unsigned)((p.N + 15) / 16), 1024, 0, st>>>(p, plan.pieces.in_group, true, wanted);
+        const auto weights = [&](auto biases) {
+            constexpr bool BIASES = decltype(biases)::value;
+            const unsigned across = (unsigned)((p.N + 15) / 16);
+            if (p.groups >= 4 && p.groups <= 64) {
+                norm_backward_groups_kernel<DT, BIASES><<<across, 1024, 0, st>>>(p, plan.pieces.in_group);
+                return;
+            }
+            norm_backward_weights_kernel<DT, BIASES><<<across * (unsigned)p.groups, 1024, 0, st>>>(p, plan.pieces.in_group, false);
+            if (p.groups > 1 && (p.dpost_weight || p.dpost_bias || p.dpre_weight || p.dpre_bias))
+                norm_backward_weights_kernel<DT, BIASES><<<across, 1024, 0, st>>>(p, plan.pieces.in_group, true);
+        };
+        if (wanted >> S0 & 1 || wanted >> T0 & 1) weights(std::true_type{});
+        else weights(std::false_type{});
     });
     return hipGetLastError();
 }
