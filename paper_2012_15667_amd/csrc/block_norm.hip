@@ -103,11 +103,13 @@ __device__ __forceinline__ void load_or(const T* p, int c, int N, float or_else,
     }
 }
 
+// `past`: past the caches, where the tensors of a call are more than those hold.
 template <class T>
-__device__ __forceinline__ void store_eight_of(T* p, int have, const typename Piece<T, 8>::type& t)
+__device__ __forceinline__ void store_eight_of(T* p, int have, const typename Piece<T, 8>::type& t, int past = 0)
 {
     if (have >= 8) {
-        *reinterpret_cast<typename Piece<T, 8>::type*>(p) = t;
+        if (past) __builtin_nontemporal_store(t, reinterpret_cast<typename Piece<T, 8>::type*>(p));
+        else *reinterpret_cast<typename Piece<T, 8>::type*>(p) = t;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -247,7 +249,7 @@ block_norm_rows_kernel(BlockNorm p)
                     x.of[c][i] = (T)v[c][i];
                     v[c][i] = at + i < p.N ? (float)x.of[c][i] : 0.f;       // (as rounded: what a backward pass reads is what is normalised)
                 }
-                store_eight_of(static_cast<T*>(p.out) + m * p.ldo + at, p.N - at, x.of[c]);
+                store_eight_of(static_cast<T*>(p.out) + m * p.ldo + at, p.N - at, x.of[c], p.past);
             }
         } else {
 #pragma unroll
@@ -264,7 +266,7 @@ block_norm_rows_kernel(BlockNorm p)
             const int at = 8 * (c * TR + thread);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x.of[c][i] = (T)((v[c][i] - s.mean) * s.r * (float)w.of[c][i] + (float)b.of[c][i]);
-            store_eight_of(static_cast<T*>(p.y) + m * p.ldy + at, p.N - at, x.of[c]);
+            store_eight_of(static_cast<T*>(p.y) + m * p.ldy + at, p.N - at, x.of[c], p.past);
         }
     }
 }
@@ -486,7 +488,7 @@ norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces)
 }
 
 // The same for rows that are held in registers: a workgroup takes a piece's rows, TR threads to a row, reads everything once, and holds its columns' sums
-// meanwhile; the next row is on its way while one is worked on.  BIASES: whether S0 and T0 are wanted.
+// meanwhile; the next row's values are asked for where this row's have been used last.  BIASES: whether S0 and T0 are wanted.
 template <int DT, int TR, int C, bool BIASES>
 __global__ void __launch_bounds__(TR > 256 ? TR : 256)
 norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wanted)
@@ -514,20 +516,21 @@ norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wante
             if constexpr (BIASES) s0[c][i] = t0[c][i] = 0.f;
         }
     struct Rows { Row<T, C> x, h, dy, dout; };
-    const auto load = [&](long long m, Rows& r) {
+    Rows r{};
+    const auto load_x = [&](long long m) {
         if (m >= r1) return;
         if (p.dy) {
             load_row<TR, C>(static_cast<const T*>(p.x) + m * p.ldx, p.N, thread, r.x);
             load_row<TR, C>(static_cast<const T*>(p.dy) + m * p.lddy, p.N, thread, r.dy);
         }
         if (p.dout) load_row<TR, C>(static_cast<const T*>(p.dout) + m * p.lddout, p.N, thread, r.dout);
-        if (p.h) load_row<TR, C>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, r.h);
     };
-    Rows r{};
-    load(r0 + slot, r);
+    const auto load_h = [&](long long m) {
+        if (m < r1 && p.h) load_row<TR, C>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, r.h);
+    };
+    load_x(r0 + slot);
+    load_h(r0 + slot);
     for (long long m = r0 + slot; m < r1; m += ROWS) {
-        Rows next{};
-        load(m + ROWS, next);
         hold(w);
         hold(wp);
         hold(g);
@@ -582,6 +585,7 @@ norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wante
                 u[0] = __builtin_fmaf(t, hat_h, u[0]);
                 u[1] += t;
             }
+        load_x(m + ROWS);
         if (p.post != IOLB_NORM_NONE) sum(u);
         hold(r.h);
         hold(g);
@@ -597,15 +601,15 @@ norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wante
                     const float hat_h = ((float)r.h.of[c][i] - mean_h) * r_h, t = d[c][i] * (float)g.of[c][i] * (float)wp.of[c][i];
                     to[i] = (T)(r_h * (t - hat_h * along_h - mean_p));
                 }
-                store_eight_of(static_cast<T*>(p.dh) + m * p.N + at, p.N - at, to);
+                store_eight_of(static_cast<T*>(p.dh) + m * p.N + at, p.N - at, to, p.past);
             }
             if (p.dx) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) to[i] = (T)(p.scale * d[c][i]);
-                store_eight_of(static_cast<T*>(p.dx) + m * p.N + at, p.N - at, to);
+                store_eight_of(static_cast<T*>(p.dx) + m * p.N + at, p.N - at, to, p.past);
             }
         }
-        r = next;
+        load_h(m + ROWS);
     }
     if (!wanted) return;
     // the rows' sums joined where several rows were taken at a time, and written
@@ -796,8 +800,14 @@ unsigned row_groups(int M) { return (unsigned)(M < 65536 ? M : 65536); }
 
 }  // namespace
 
-hipError_t launch_block_norm(const BlockNorm& p, int dtype, hipStream_t st)
+// Whether outputs are stored past the caches: where the call's tensors together are more than half of the 256 MB before memory.  16384 x 1024 bf16 28.2 us,
+// so 23.1; 8192 x 4096 52.3 / 50.8, gradients 107 / 103; 4096 x 8192 101 / 97.
+static int past_caches(long long M, long long N, int dtype, int tensors) { return (double)M * N * (dtype == IOLB_F32 ? 4 : 2) * tensors > 128e6; }
+
+hipError_t launch_block_norm(const BlockNorm& given, int dtype, hipStream_t st)
 {
+    BlockNorm p = given;
+    p.past = past_caches(p.M, p.N, dtype, (p.h ? 3 : 1) + (p.y ? 1 : 0));
     by_type(dtype, [&](auto t) {
         constexpr int DT = decltype(t)::value;
         by_row(p.N, [&](auto tr, auto c) {
@@ -835,8 +845,10 @@ NormBackwardPlan block_norm_backward_plan(const BlockNormBackward& p, int)
     return plan;
 }
 
-hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBackwardPlan& plan, int dtype, hipStream_t st)
+hipError_t launch_block_norm_backward(const BlockNormBackward& given, const NormBackwardPlan& plan, int dtype, hipStream_t st)
 {
+    BlockNormBackward p = given;
+    p.past = past_caches(p.M, p.N, dtype, (p.dy ? 2 : 0) + (p.dout ? 1 : 0) + (p.h ? 1 : 0) + (p.dx ? 1 : 0) + (p.dh ? 1 : 0));
     const unsigned wanted = column_sums(p), pieces = (unsigned)(plan.pieces.in_group * p.groups);
     by_type(dtype, [&](auto t) {
         constexpr int DT = decltype(t)::value;
