@@ -17,7 +17,6 @@ struct BlockNorm {
     int M, N;
     int post, pre;                          // IOLB_NORM_...
     int rows_per_group;                     // rows that share a row of the gate
-    int past;                               // set by the launcher: outputs go past the caches
     float scale, eps;
 };
 hipError_t launch_block_norm(const BlockNorm& p, int dtype, hipStream_t st);
@@ -35,7 +34,6 @@ struct BlockNormBackward {
     int M, N;
     int post, pre;
     int rows_per_group, groups;
-    int past;                               // set by the launcher: outputs go past the caches
     float scale, eps;
     float* rows;                            // [M][NORM_ROW_SUMS]: what the rows' pass leaves for the columns' pass
     float* columns;                         // [pieces][NORM_COLUMN_SUMS][N rounded up to 8]

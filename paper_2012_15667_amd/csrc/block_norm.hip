@@ -103,12 +103,12 @@ __device__ __forceinline__ void load_or(const T* p, int c, int N, float or_else,
     }
 }
 
-// `past`: past the caches, where the tensors of a call are more than those hold.
-template <class T>
-__device__ __forceinline__ void store_eight_of(T* p, int have, const typename Piece<T, 8>::type& t, int past = 0)
+// PAST: past the caches, where the tensors of a call are more than those hold.
+template <bool PAST = false, class T>
+__device__ __forceinline__ void store_eight_of(T* p, int have, const typename Piece<T, 8>::type& t)
 {
     if (have >= 8) {
-        if (past) __builtin_nontemporal_store(t, reinterpret_cast<typename Piece<T, 8>::type*>(p));
+        if constexpr (PAST) __builtin_nontemporal_store(t, reinterpret_cast<typename Piece<T, 8>::type*>(p));
         else *reinterpret_cast<typename Piece<T, 8>::type*>(p) = t;
     } else {
 #pragma unroll
@@ -208,7 +208,7 @@ __device__ __forceinline__ RowStats stats_of_row(float (&v)[C][8], int N, int th
     return {mean, 1.f / sqrtf(one[0] / (float)N + eps)};
 }
 
-template <int DT, int TR, int C>
+template <int DT, int TR, int C, bool PAST>
 __global__ void __launch_bounds__(TR > 256 ? TR : 256)
 block_norm_rows_kernel(BlockNorm p)
 {
@@ -249,7 +249,7 @@ block_norm_rows_kernel(BlockNorm p)
                     x.of[c][i] = (T)v[c][i];
                     v[c][i] = at + i < p.N ? (float)x.of[c][i] : 0.f;       // (as rounded: what a backward pass reads is what is normalised)
                 }
-                store_eight_of(static_cast<T*>(p.out) + m * p.ldo + at, p.N - at, x.of[c], p.past);
+                store_eight_of<PAST>(static_cast<T*>(p.out) + m * p.ldo + at, p.N - at, x.of[c]);
             }
         } else {
 #pragma unroll
@@ -266,7 +266,7 @@ block_norm_rows_kernel(BlockNorm p)
             const int at = 8 * (c * TR + thread);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x.of[c][i] = (T)((v[c][i] - s.mean) * s.r * (float)w.of[c][i] + (float)b.of[c][i]);
-            store_eight_of(static_cast<T*>(p.y) + m * p.ldy + at, p.N - at, x.of[c], p.past);
+            store_eight_of<PAST>(static_cast<T*>(p.y) + m * p.ldy + at, p.N - at, x.of[c]);
         }
     }
 }
@@ -489,7 +489,7 @@ norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces)
 
 // The same for rows that are held in registers: a workgroup takes a piece's rows, TR threads to a row, reads everything once, and holds its columns' sums
 // meanwhile; the next row's values are asked for where this row's have been used last.  BIASES: whether S0 and T0 are wanted.
-template <int DT, int TR, int C, bool BIASES>
+template <int DT, int TR, int C, bool BIASES, bool PAST>
 __global__ void __launch_bounds__(TR > 256 ? TR : 256)
 norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wanted)
 {
@@ -601,12 +601,12 @@ norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wante
                     const float hat_h = ((float)r.h.of[c][i] - mean_h) * r_h, t = d[c][i] * (float)g.of[c][i] * (float)wp.of[c][i];
                     to[i] = (T)(r_h * (t - hat_h * along_h - mean_p));
                 }
-                store_eight_of(static_cast<T*>(p.dh) + m * p.N + at, p.N - at, to, p.past);
+                store_eight_of<PAST>(static_cast<T*>(p.dh) + m * p.N + at, p.N - at, to);
             }
             if (p.dx) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) to[i] = (T)(p.scale * d[c][i]);
-                store_eight_of(static_cast<T*>(p.dx) + m * p.N + at, p.N - at, to, p.past);
+                store_eight_of<PAST>(static_cast<T*>(p.dx) + m * p.N + at, p.N - at, to);
             }
         }
         load_h(m + ROWS);
@@ -802,18 +802,22 @@ unsigned row_groups(int M) { return (unsigned)(M < 65536 ? M : 65536); }
 
 // Whether outputs are stored past the caches: where the call's tensors together are more than half of the 256 MB before memory.  16384 x 1024 bf16 28.2 us,
 // so 23.1; 8192 x 4096 52.3 / 50.8, gradients 107 / 103; 4096 x 8192 101 / 97.
-static int past_caches(long long M, long long N, int dtype, int tensors) { return (double)M * N * (dtype == IOLB_F32 ? 4 : 2) * tensors > 128e6; }
+static bool past_caches(long long M, long long N, int dtype, int tensors) { return (double)M * N * (dtype == IOLB_F32 ? 4 : 2) * tensors > 128e6; }
 
-hipError_t launch_block_norm(const BlockNorm& given, int dtype, hipStream_t st)
+hipError_t launch_block_norm(const BlockNorm& p, int dtype, hipStream_t st)
 {
-    BlockNorm p = given;
-    p.past = past_caches(p.M, p.N, dtype, (p.h ? 3 : 1) + (p.y ? 1 : 0));
+    const bool past = past_caches(p.M, p.N, dtype, (p.h ? 3 : 1) + (p.y ? 1 : 0));
     by_type(dtype, [&](auto t) {
         constexpr int DT = decltype(t)::value;
         by_row(p.N, [&](auto tr, auto c) {
             constexpr int TR = decltype(tr)::value, C = decltype(c)::value;
-            if constexpr (C == 0) block_norm_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
-            else block_norm_rows_kernel<DT, TR, C><<<row_groups((p.M + (TR > 256 ? 0 : 256 / TR - 1)) / (TR > 256 ? 1 : 256 / TR)), TR > 256 ? TR : 256, 0, st>>>(p);
+            if constexpr (C == 0) {
+                block_norm_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
+            } else {
+                constexpr int ROWS = TR > 256 ? 1 : 256 / TR;
+                const auto kernel = past ? block_norm_rows_kernel<DT, TR, C, true> : block_norm_rows_kernel<DT, TR, C, false>;
+                kernel<<<row_groups((int)((p.M + (ROWS - 1LL)) / ROWS)), TR > 256 ? TR : 256, 0, st>>>(p);
+            }
         });
     });
     return hipGetLastError();
@@ -845,10 +849,9 @@ NormBackwardPlan block_norm_backward_plan(const BlockNormBackward& p, int)
     return plan;
 }
 
-hipError_t launch_block_norm_backward(const BlockNormBackward& given, const NormBackwardPlan& plan, int dtype, hipStream_t st)
+hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBackwardPlan& plan, int dtype, hipStream_t st)
 {
-    BlockNormBackward p = given;
-    p.past = past_caches(p.M, p.N, dtype, (p.dy ? 2 : 0) + (p.dout ? 1 : 0) + (p.h ? 1 : 0) + (p.dx ? 1 : 0) + (p.dh ? 1 : 0));
+    const bool past = past_caches(p.M, p.N, dtype, (p.dy ? 2 : 0) + (p.dout ? 1 : 0) + (p.h ? 1 : 0) + (p.dx ? 1 : 0) + (p.dh ? 1 : 0));
     const unsigned wanted = column_sums(p), pieces = (unsigned)(plan.pieces.in_group * p.groups);
     by_type(dtype, [&](auto t) {
         constexpr int DT = decltype(t)::value;
@@ -858,7 +861,9 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& given, const Norm
                 if (p.M) norm_backward_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
                 if (wanted) norm_backward_columns_kernel<DT><<<(unsigned)((p.N + 63) / 64) * pieces, 256, 0, st>>>(p, plan.pieces);
             } else {
-                const auto kernel = wanted >> S0 & 1 || wanted >> T0 & 1 ? norm_backward_rows_kernel<DT, TR, C, true> : norm_backward_rows_kernel<DT, TR, C, false>;
+                const bool biases = wanted >> S0 & 1 || wanted >> T0 & 1;
+                const auto kernel = biases ? (past ? norm_backward_rows_kernel<DT, TR, C, true, true> : norm_backward_rows_kernel<DT, TR, C, true, false>)
+                                           : (past ? norm_backward_rows_kernel<DT, TR, C, false, true> : norm_backward_rows_kernel<DT, TR, C, false, false>);
                 kernel<<<pieces, TR > 256 ? TR : 256, 0, st>>>(p, plan.pieces, wanted);
             }
         });
