@@ -7,6 +7,10 @@
 
 namespace iolb {
 
+// Whether a streaming call goes past the caches (non-temporal loads and stores): where its tensors together, `bytes`, are more than half of the 256 MB
+// before memory.  Smaller ones are faster through them, and so is whoever reads the result next.
+inline bool past_caches(double bytes) { return bytes > 128e6; }
+
 // ---- norms -----------------------------------------------------------------------------------------
 // Rows are N values.  p = post(h);  x' = a x + g p, rounded to the type;  y = pre(x').
 struct BlockNorm {

@@ -800,9 +800,8 @@ unsigned row_groups(int M) { return (unsigned)(M < 65536 ? M : 65536); }
 
 }  // namespace
 
-// Whether outputs are stored past the caches: where the call's tensors together are more than half of the 256 MB before memory.  16384 x 1024 bf16 28.2 us,
-// so 23.1; 8192 x 4096 52.3 / 50.8, gradients 107 / 103; 4096 x 8192 101 / 97.
-static bool past_caches(long long M, long long N, int dtype, int tensors) { return (double)M * N * (dtype == IOLB_F32 ? 4 : 2) * tensors > 128e6; }
+// Outputs past the caches: 16384 x 1024 bf16 28.2 us, so 23.1; 8192 x 4096 52.3 / 50.8, gradients 107 / 103; 4096 x 8192 101 / 97.
+static bool past_caches(long long M, long long N, int dtype, int tensors) { return past_caches((double)M * N * (dtype == IOLB_F32 ? 4 : 2) * tensors); }
 
 hipError_t launch_block_norm(const BlockNorm& p, int dtype, hipStream_t st)
 {

@@ -28,10 +28,13 @@ __device__ __forceinline__ u32x4 philox(unsigned long long low, unsigned long lo
 // Eight values as memory holds them; zeros beyond the row's end.
 template <class T> using Eight = typename Piece<T, 8>::type;
 
-template <class T>
+template <bool PAST, class T>
 __device__ __forceinline__ Eight<T> load_eight(const T* p, int have)
 {
-    if (have >= 8) return *reinterpret_cast<const Eight<T>*>(p);
+    if (have >= 8) {
+        if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const Eight<T>*>(p));
+        return *reinterpret_cast<const Eight<T>*>(p);
+    }
     Eight<T> t;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = i < have ? p[i] : (T)0.f;
@@ -39,9 +42,9 @@ __device__ __forceinline__ Eight<T> load_eight(const T* p, int have)
 }
 
 // A thread takes the eight columns of a counter in one row after the other, the next one on its way meanwhile; a workgroup `wide` threads of a row and
-// 256 / wide rows; four threads hold a checkpoint's block.  CHECKPOINT, RESIDUAL: whether there is one.
+// 256 / wide rows; four threads hold a checkpoint's block.  CHECKPOINT, RESIDUAL: whether there is one; PAST: past the caches.
 // Memory and the generator's 20 products a counter bind it alike: 16384 x 8192 bf16 without the generator 94 us.
-template <int DT, bool RESIDUAL, bool CHECKPOINT>
+template <int DT, bool RESIDUAL, bool CHECKPOINT, bool PAST>
 __global__ void __launch_bounds__(256)
 dropout_kernel(Dropout p, int wide_log)
 {
@@ -62,8 +65,8 @@ dropout_kernel(Dropout p, int wide_log)
     Eight<T> x{}, res{};
     const auto load = [&](long long at) {
         if (at >= p.rows || have <= 0) return;
-        x = load_eight(xs + at * p.ldx, have);
-        if constexpr (RESIDUAL) res = load_eight(rs + at * p.ldr, have);
+        x = load_eight<PAST>(xs + at * p.ldx, have);
+        if constexpr (RESIDUAL) res = load_eight<PAST>(rs + at * p.ldr, have);
     };
     load(r);
     for (; r - ty < p.rows; r += step) {
@@ -86,7 +89,8 @@ dropout_kernel(Dropout p, int wide_log)
         if (live) {
             T* const to = static_cast<T*>(p.y) + r * p.ldy + c;
             if (have >= 8) {
-                *reinterpret_cast<Eight<T>*>(to) = t;
+                if constexpr (PAST) __builtin_nontemporal_store(t, reinterpret_cast<Eight<T>*>(to));
+                else *reinterpret_cast<Eight<T>*>(to) = t;
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -118,13 +122,20 @@ dropout_kernel(Dropout p, int wide_log)
 // Workgroups, more than fill the chip at once (16384 x 8192 bf16: 2048 101 us, 4096 102, 8192 99, 16384 96, as many as rows take 120).
 constexpr int GROUPS = 16384;
 
+template <int DT, bool PAST>
+void launch(const Dropout& p, const dim3& grid, int wide_log, hipStream_t st)
+{
+    if (p.zq && p.residual) dropout_kernel<DT, true, true, PAST><<<grid, 256, 0, st>>>(p, wide_log);
+    else if (p.zq) dropout_kernel<DT, false, true, PAST><<<grid, 256, 0, st>>>(p, wide_log);
+    else if (p.residual) dropout_kernel<DT, true, false, PAST><<<grid, 256, 0, st>>>(p, wide_log);
+    else dropout_kernel<DT, false, false, PAST><<<grid, 256, 0, st>>>(p, wide_log);
+}
+
 template <int DT>
 void launch(const Dropout& p, const dim3& grid, int wide_log, hipStream_t st)
 {
-    if (p.zq && p.residual) dropout_kernel<DT, true, true><<<grid, 256, 0, st>>>(p, wide_log);
-    else if (p.zq) dropout_kernel<DT, false, true><<<grid, 256, 0, st>>>(p, wide_log);
-    else if (p.residual) dropout_kernel<DT, true, false><<<grid, 256, 0, st>>>(p, wide_log);
-    else dropout_kernel<DT, false, false><<<grid, 256, 0, st>>>(p, wide_log);
+    if (past_caches((double)p.rows * p.cols * (sizeof(typename DenseType<DT>::type) * (p.residual ? 3 : 2) + (p.zq ? 1 : 0)))) launch<DT, true>(p, grid, wide_log, st);
+    else launch<DT, false>(p, grid, wide_log, st);
 }
 
 }  // namespace

@@ -6,8 +6,8 @@ namespace iolb {
 namespace {
 
 // Four lanes share a block of 32, eight values each.  A workgroup covers `wide` threads of a row, up to its padded end, and 256 / wide rows, one after the
-// other, the next one on its way meanwhile.
-template <int DT>
+// other, the next one on its way meanwhile.  PAST: values past the caches.
+template <int DT, bool PAST>
 __global__ void __launch_bounds__(256)
 mx4_pack_kernel(const void* x, long long ldx, int rows, int cols, uint8_t* codes, uint8_t* scales, int wide_log)
 {
@@ -22,7 +22,8 @@ mx4_pack_kernel(const void* x, long long ldx, int rows, int cols, uint8_t* codes
         if (r >= rows || have <= 0) return;
         const T* const from = xs + r * ldx;
         if (have >= 8) {
-            next = *reinterpret_cast<const Eight*>(from);
+            if constexpr (PAST) next = __builtin_nontemporal_load(reinterpret_cast<const Eight*>(from));
+            else next = *reinterpret_cast<const Eight*>(from);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -55,7 +56,7 @@ template <int DT> __device__ __forceinline__ float largest()
     return DT == IOLB_F16 ? 65504.f : DT == IOLB_BF16 ? 0x1.fep127f : 0x1.fffffep127f;
 }
 
-template <int DT>
+template <int DT, bool PAST>
 __global__ void __launch_bounds__(256)
 mx4_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int rows, int cols, void* y, long long ldy, int wide_log)
 {
@@ -89,7 +90,8 @@ mx4_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int rows, int col
         }
         T* const to = static_cast<T*>(y) + r * ldy + c;
         if (have >= 8) {
-            *reinterpret_cast<typename Piece<T, 8>::type*>(to) = t;
+            if constexpr (PAST) __builtin_nontemporal_store(t, reinterpret_cast<typename Piece<T, 8>::type*>(to));
+            else *reinterpret_cast<typename Piece<T, 8>::type*>(to) = t;
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -113,22 +115,35 @@ RowGrid row_grid(int rows, long long cols, long long each)
 
 }  // namespace
 
+// f called with the type and with whether the values go past the caches, as integral constants.  Measured, 16384 x 8192 bf16: packed 61 us, past the
+// caches 58; unpacked 69 / 49, both in turn 143 / 109.  4096 x 4096 fp32 is faster through them: packed 12.3 / 14.4, unpacked 15.4 / 23.3.
+template <class F>
+static hipError_t by_type(int dtype, int rows, int cols, F f)
+{
+    const auto call = [&](auto type) {
+        if (past_caches((double)rows * cols * (sizeof(typename DenseType<decltype(type)::value>::type) + 0.53))) f(type, std::true_type{});
+        else f(type, std::false_type{});
+    };
+    if (dtype == IOLB_F32) call(std::integral_constant<int, IOLB_F32>{});
+    else if (dtype == IOLB_F16) call(std::integral_constant<int, IOLB_F16>{});
+    else call(std::integral_constant<int, IOLB_BF16>{});
+    return hipGetLastError();
+}
+
 hipError_t launch_mx4_pack(const void* x, long long ldx, int rows, int cols, int dtype, uint8_t* codes, uint8_t* scales, hipStream_t st)
 {
     const RowGrid g = row_grid(rows, 2 * mx4_pitch(cols), 8);
-    if (dtype == IOLB_F32) mx4_pack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, codes, scales, g.wide_log);
-    else if (dtype == IOLB_F16) mx4_pack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, codes, scales, g.wide_log);
-    else mx4_pack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, codes, scales, g.wide_log);
-    return hipGetLastError();
+    return by_type(dtype, rows, cols, [&](auto type, auto past) {
+        mx4_pack_kernel<decltype(type)::value, decltype(past)::value><<<g.grid, 256, 0, st>>>(x, ldx, rows, cols, codes, scales, g.wide_log);
+    });
 }
 
 hipError_t launch_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int rows, int cols, int dtype, void* y, long long ldy, hipStream_t st)
 {
     const RowGrid g = row_grid(rows, cols, 8);
-    if (dtype == IOLB_F32) mx4_unpack_kernel<IOLB_F32><<<g.grid, 256, 0, st>>>(codes, scales, rows, cols, y, ldy, g.wide_log);
-    else if (dtype == IOLB_F16) mx4_unpack_kernel<IOLB_F16><<<g.grid, 256, 0, st>>>(codes, scales, rows, cols, y, ldy, g.wide_log);
-    else mx4_unpack_kernel<IOLB_BF16><<<g.grid, 256, 0, st>>>(codes, scales, rows, cols, y, ldy, g.wide_log);
-    return hipGetLastError();
+    return by_type(dtype, rows, cols, [&](auto type, auto past) {
+        mx4_unpack_kernel<decltype(type)::value, decltype(past)::value><<<g.grid, 256, 0, st>>>(codes, scales, rows, cols, y, ldy, g.wide_log);
+    });
 }
 
 }  // namespace iolb
