@@ -31,7 +31,28 @@ __device__ __forceinline__ void dma16(const uint8_t* base, unsigned offset, unsi
     lds_dma_load_16(reinterpret_cast<const float*>(base), offset, lds);
 }
 
-template <int DT, int BM, int BN, int WM, int WN>
+// W columns of row m: bias, residual, activation, the one rounding to the type.  PAST: past the caches.
+template <int DT, int ACT, bool PAST, int W>
+__device__ __forceinline__ void finish_row(const DenseFinish& f, int m, int n, const float (&bias)[W], float (&z)[W])
+{
+    typedef typename DenseType<DT>::type T;
+    typedef typename Piece<T, W>::type TW;
+    const int have = f.N - n;
+    if (m >= f.M || have <= 0) return;
+#pragma unroll
+    for (int i = 0; i < W; ++i) z[i] += bias[i];
+    if (f.residual && f.first) add_residual<DT>(f, m, n, z);
+    if (!PAST || have < W) return store_columns<DT, ACT>(f, m, n, z);
+#pragma unroll
+    for (int i = 0; i < W; ++i) z[i] = activate<ACT>(z[i]);
+    if (f.residual && !f.first) add_residual<DT>(f, m, n, z);
+    TW t;
+#pragma unroll
+    for (int i = 0; i < W; ++i) t[i] = (T)z[i];
+    __builtin_nontemporal_store(t, reinterpret_cast<TW*>(static_cast<T*>(f.y) + m * f.ldy + n));
+}
+
+template <int DT, int BM, int BN, int WM, int WN, bool PAST>
 __global__ void __launch_bounds__(64 * WM * WN, 2)
 mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
 {
@@ -258,7 +279,7 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
                     for (int i = 0; i < 4; ++i) z[4 * h + i] = part[i];
                 }
                 const int m = m0 + r / (PI * 32) * (BM / WM) + pass * PI * 32 + r % (PI * 32);
-                finish_columns<DT, decltype(act)::value>(p.f, m, n, bias, z);
+                finish_row<DT, decltype(act)::value, PAST>(p.f, m, n, bias, z);
             }
         });
     }
@@ -267,7 +288,8 @@ mx4_tile_kernel(Mx4Product p, int tiles_m, int tiles_n)
 template <int DT, int BM, int BN, int WM, int WN>
 hipError_t launch(const Mx4Product& p, hipStream_t st)
 {
-    const auto kernel = mx4_tile_kernel<DT, BM, BN, WM, WN>;
+    const bool past = past_caches((double)p.M * p.N * sizeof(typename DenseType<DT>::type));
+    const auto kernel = past ? mx4_tile_kernel<DT, BM, BN, WM, WN, true> : mx4_tile_kernel<DT, BM, BN, WM, WN, false>;
     const hipError_t e = allow_large_lds(reinterpret_cast<const void*>(kernel));
     if (e != hipSuccess) return e;
     const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN;
