@@ -1042,7 +1042,7 @@ def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False,
         py, ldy = y.data_ptr(), N
     args = _pack_linear_mx4(M, N, K, code, _act_code(act), 1 if residual_first else 0, px, ldx, pxc, pxs, pwc, pws, pb, pr, py, ldr, ldy)
     _use_stream_on(device)
-    run = _call_in_new_workspace if px and M > 64 else _call_with_workspace
+    run = _call_in_new_workspace if px and M > 16 and M * N * K > 1 << 28 else _call_with_workspace
     run(_bytes_of["iolb_linear_mx4"], _bytes_of["iolb_linear_mx4_workspace_bytes"], args, like)
     if wanted:
         y = _without_graph(y, given, inputs, "linear_mx4() has no gradients")

@@ -81,16 +81,16 @@ struct Mx4Product {
     float* partial;                         // [splits][M][N rounded up to 4]
     DenseFinish f;
 };
-// The kernel for few rows reads weights once, for up to 64 rows of a, and can bring those into 4 bits itself.  It takes them all up to sixteen rows, and more
-// where the summed axis is short.  Every sixteen columns bring x into 4 bits again, some 0.13 us of a SIMD for sixteen rows and 128 k, against a launch of
-// 2 to 4 us.  Calls, us, x in the kernel / packed before it (beyond sixteen rows by the other kernel): 1 x 4096 -> 4096 bf16 8.1 / 12.4, 1 x 512 -> 1000
-// 7.6 / 11.7, 1 x 4096 -> 16384 15.5 / 13.4, 1 x 16384 -> 4096 17.6 / 14.0; 17 x 4096 -> 4096 10.3 / 14.0, 32 x 4096 -> 4096 11.6 / 14.5, 64 x 512 -> 1000
-// 8.5 / 10.8, 64 x 2048 -> 512 10.8 / 11.4, 64 x 4096 -> 1024 18.3 / 13.3.  Packed already, this kernel / the other: 32 x 4096 -> 4096 8.1 / 12.2,
-// 64 x 4096 -> 4096 11.4 / 9.6, 32 x 16384 -> 4096 24.7 / 15.2.
+// The kernel for few rows reads weights once for up to 64 rows of a, and can bring those into 4 bits itself.  It takes up to sixteen rows always, and more, in
+// groups of 64, where the summed axis is short and there is little to do.  Every sixteen columns bring x into 4 bits again, some 0.13 us of a SIMD for
+// sixteen rows and 128 k, against a launch of 2 to 4 us.  Calls, us, x in the kernel / packed before it (beyond sixteen rows by the other kernel): 1 x 4096 -> 4096
+// bf16 8.1 / 12.4, 1 x 512 -> 1000 7.6 / 11.7, 1 x 4096 -> 16384 15.5 / 13.4, 1 x 16384 -> 4096 17.6 / 14.0; 17 x 4096 -> 4096 10.3 / 14.0, 32 x 4096 -> 4096 11.6 / 14.5,
+// 64 x 512 -> 1000 8.5 / 10.8, 64 x 4096 -> 1024 18.3 / 13.3, 256 x 1000 -> 1000 7.9 / 11.1, 512 x 1000 -> 1000 9.8 / 11.1 (on the GPU alone 10.0 / 7.7),
+// 2048 x 512 -> 512 11.9 / 10.9.  Packed already, this kernel / the other: 32 x 4096 -> 4096 8.1 / 12.2, 64 x 4096 -> 4096 11.4 / 9.6, 32 x 16384 -> 4096 24.7 / 15.2.
 inline bool mx4_short(long long M, long long N, long long K)
 {
-    const long long sixteens = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    return M <= 64 && sixteens * K <= 8192 && sixteens * N * K <= 1 << 25;
+    const long long at_once = M <= 16 ? 1 : M <= 32 ? 2 : 4, blocks = ((M + 15) / 16) * ((N + 15) / 16);
+    return M <= 1 << 15 && at_once * K <= 8192 && blocks * K <= (M <= 32 ? 1 << 21 : 1 << 20);
 }
 inline bool mx4_few_wanted(long long M, long long N, long long K) { return M <= 16 || mx4_short(M, N, K); }
 bool mx4_few_launchable(int N);

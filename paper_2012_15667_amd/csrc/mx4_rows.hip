@@ -87,6 +87,7 @@ mx4_few_kernel(Mx4Product p)
     __shared__ f32x4 part[MR][WAVES][64];
     const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4, wave = threadIdx.x >> 6;
     // (rows beyond the operand are read from its last row: their sums are never stored)
+    const int m0 = (int)blockIdx.y * (16 * MR);
     const long long n0 = (long long)blockIdx.x * 16, n = n0 + l16 < p.N ? n0 + l16 : p.N - 1;
     const int steps = (p.K + MX4_WIDE - 1) / MX4_WIDE;
     const uint8_t *const b = p.b + n * (steps * 64LL) + grp * 16, *const sb = p.b_scales + n * (steps * 4LL) + grp;
@@ -94,7 +95,7 @@ mx4_few_kernel(Mx4Product p)
     const T* x[MR];
 #pragma unroll
     for (int r = 0; r < MR; ++r) {
-        const int m = 16 * r + l16 < p.M ? 16 * r + l16 : p.M - 1;
+        const int m = m0 + 16 * r + l16 < p.M ? m0 + 16 * r + l16 : p.M - 1;
         a[r] = p.a + m * (steps * 64LL) + grp * 16;
         sa[r] = p.a_scales + m * (steps * 4LL) + grp;
         x[r] = static_cast<const T*>(p.x) + m * p.ldx + grp * MX4_BLOCK;
@@ -145,13 +146,13 @@ mx4_few_kernel(Mx4Product p)
     float bias[4];
     const int first = (int)n0 + 4 * grp;
     load_bias<DT>(p.f, first, bias);
-    finish_four<DT>(p.f, 16 * wave + l16, first, bias, all);
+    finish_four<DT>(p.f, m0 + 16 * wave + l16, first, bias, all);
 }
 
 template <int DT, int MR>
 void launch(const Mx4Product& p, hipStream_t st)
 {
-    const unsigned groups = (unsigned)(((long long)p.N + 15) / 16);
+    const dim3 groups((unsigned)(((long long)p.N + 15) / 16), (unsigned)((p.M + 16 * MR - 1) / (16 * MR)));
     if (p.x) mx4_few_kernel<DT, false, MR><<<groups, 64 * WAVES, 0, st>>>(p);
     else mx4_few_kernel<DT, true, MR><<<groups, 64 * WAVES, 0, st>>>(p);
 }

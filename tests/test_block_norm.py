@@ -381,6 +381,27 @@ def test_other_streams_and_graphs(dtype, M, N):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,M,N", [("bfloat16", 9000, 4096), ("float32", 20000, 520), ("float16", 4100, 8200)])
+def test_tensors_larger_than_the_caches(dtype, M, N):
+    """Rows of a large call and of a small one are the same to the last bit."""
+    torch = _torch()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    T = getattr(torch, dtype)
+    x, h, dy, dout = (torch.randn((M, N), generator=g, device="cuda").to(T) for _ in range(4))
+    w = torch.randn((N,), generator=g, device="cuda").to(T)
+    k = dict(post="rms", post_weight=w, gate=w, scale=0.5, pre="layer", pre_weight=w, pre_bias=w)
+    n = B.block_norm(x, h, **k)
+    b = B.block_norm_backward(dy, dout, n.x, h, **k)
+    for at in (0, M // 2, M - 30):
+        s = slice(at, at + 30)
+        few = B.block_norm(x[s], h[s], **k)
+        assert torch.equal(n.x[s], few.x) and torch.equal(n.y[s], few.y)
+        back = B.block_norm_backward(dy[s], dout[s], few.x, h[s], **k)
+        assert torch.equal(b.dx[s], back.dx) and torch.equal(b.dh[s], back.dh)
+
+
+@pytest.mark.gpu
 def test_offsets_beyond_32_bits():
     torch = _torch()
     rng = np.random.default_rng(6)

@@ -203,6 +203,22 @@ def test_offsets_beyond_32_bits():
 
 
 @pytest.mark.gpu
+def test_tensors_larger_than_the_caches():
+    torch = _torch()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x, r = (torch.randn((9001, 8200), generator=g, device="cuda").bfloat16() for _ in range(2))
+    y, c = B.dropout(x, 0.5, 4, 5, residual=r, checkpoint=True)
+    plain = B.dropout(x, 0.5, 4, 5)
+    packed = B.checkpoint_pack(y)
+    assert torch.equal(c.q, packed.q) and torch.equal(c.e, packed.e)
+    for at in (0, 4500, 9000):
+        keep = torch.from_numpy(mask64(1, 8200, 0.5, 4, 5, at)[0]).cuda()
+        want = torch.where(keep, 2 * x[at:at + 1], torch.zeros_like(x[:1]))
+        assert torch.equal(plain[at:at + 1], want) and torch.equal(y[at:at + 1], want + r[at:at + 1])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,cols", [(0, 5), (5, 0), (0, 0)])
 def test_empty(rows, cols):
     y, c = B.dropout(_torch().empty((rows, cols), device="cuda"), 0.5, 1, checkpoint=True)

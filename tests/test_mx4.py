@@ -193,6 +193,58 @@ def test_linear_epilogue(dtype, act, residual, M):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act,residual", [("none", None), ("relu", "first"), ("silu", "after"), ("gelu", "first"), ("gelu_tanh", "after")])
+@pytest.mark.parametrize("M,N,K", [(1500, 1030, 200), (65, 129, 2500), (129, 257, 4103), (20, 70, 9000), (4100, 2050, 130)])
+def test_linear_epilogue_of_large_products_and_of_long_sums(dtype, act, residual, M, N, K):
+    """Beyond what the kernel for few rows takes: blocks of all sizes, K shared by workgroups, stages that end in the middle."""
+    check_linear(np.random.default_rng(M), M, N, K, dtype, act=act, residual=residual, bias=residual != "after", gap=3 if act == "silu" else 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,K", [(1500, 200), (129, 4103), (1500, 256), (1500, 384), (1500, 520)])
+def test_large_products_of_values_that_are_not_finite(M, K):
+    """A NaN in the last block of a row, and scales at both ends of their range, reach their own rows and columns alone, also where a stage has one word of two."""
+    torch = _torch()
+    rng = np.random.default_rng(M)
+    N = 1030
+    x, w = make(rng, (M, K), "bfloat16")[0], make(rng, (N, K), "bfloat16")[0]
+    clean = B.linear_mx4(x, B.mx4_pack(w), dtype=None)
+    x[7, K - 1] = float("nan")
+    w[1029, K - 1] = float("inf")
+    x[8] = 0
+    x[9] *= 2.0 ** -126
+    got = B.linear_mx4(x, B.mx4_pack(w))
+    assert bool(torch.isnan(got[7]).all()) and bool(torch.isnan(got[:, 1029]).all()) and bool((got[8, :1029] == 0).all())
+    rest = torch.ones((M, N), dtype=torch.bool, device="cuda")
+    rest[7:10], rest[:, 1029] = False, False
+    assert torch.equal(got[rest], clean[rest])
+    assert bool((got[9, :1029].float().abs() < 2.0 ** -110).all())
+
+
+@pytest.mark.gpu
+def test_tensors_larger_than_the_caches():
+    """Rows of a large call and of a small one are the same to the last bit: packed, read back, multiplied."""
+    torch = _torch()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn((9001, 8200), generator=g, device="cuda").bfloat16()
+    c = B.mx4_pack(x)
+    y = B.mx4_unpack(c, torch.bfloat16)
+    w = B.mx4_pack(torch.randn((9000, 200), generator=g, device="cuda"))
+    z = B.linear_mx4(x[:, :200], w, act="silu")
+    for at in (0, 4000, 8960):
+        part = x[at:at + 41]
+        few = B.mx4_pack(part)
+        assert torch.equal(c.codes[at:at + 41], few.codes) and torch.equal(c.scales[at:at + 41], few.scales)
+        assert torch.equal(y[at:at + 41], B.mx4_unpack(few, torch.bfloat16))
+        off = (z[at:at + 41].float() - B.linear_mx4(part[:, :200], w, act="silu", dtype=None).float()).abs()
+        # sums of 200 products in another order, each within 216 2^-24 of magnitudes that stay below 250 here, through a slope of at most 1.1: 7.1e-3; and a
+        # rounding of half a unit in the last place each
+        assert bool((off <= 2.0 ** -7 * z[at:at + 41].float().abs() + 2.0 ** -7).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("gap,lead", [(8, 0), (3, 0), (8, 8), (5, 1), (7, 9)])
 @pytest.mark.parametrize("M,N,K", [(2, 40, 64), (70, 140, 128), (33, 20, 61)])
 def test_linear_strides_and_alignment(dtype, gap, lead, M, N, K):
@@ -324,10 +376,10 @@ P = 4096
 @pytest.mark.parametrize("change,code", [
     (dict(M=-1), -1), (dict(N=-1), -1), (dict(K=-1), -1), (dict(M=1 << 31), -2), (dict(N=1 << 31), -2), (dict(K=1 << 23), -2), (dict(dtype=3), -2), (dict(act=5), -2),
     (dict(x=None), -1), (dict(x_codes=P, x_scales=P), -1), (dict(x=None, x_codes=P), -1), (dict(x=None, x_codes=P + 8, x_scales=P), -1), (dict(x=None, x_codes=P, x_scales=P + 2), -1),
-    (dict(w_codes=None), -1), (dict(w_scales=None), -1), (dict(w_codes=P + 8), -1), (dict(w_scales=P + 1), -1), (dict(y=None), -1), (dict(ldx=63), -1), (dict(ldy=7), -1),
+    (dict(w_codes=None), -1), (dict(w_scales=None), -1), (dict(w_codes=P + 8), -1), (dict(w_scales=P + 1), -1), (dict(y=None), -1), (dict(ldx=2999), -1), (dict(ldy=7), -1),
     (dict(residual=P, ldr=7), -1), (dict(x=P + 2), -1), (dict(y=P + 1), -1), (dict(M=1 << 30, N=1 << 30, ldy=1 << 30), -2), ({}, -4)])
 def test_c_linear_refuses_without_touching_the_gpu(change, code):
-    a = dict(M=100, N=8, K=64, dtype=0, act=0, residual_first=0, x=P, ldx=64, x_codes=None, x_scales=None, w_codes=P, w_scales=P, bias=None, residual=None, y=P, ldr=8, ldy=8)
+    a = dict(M=100, N=8, K=3000, dtype=0, act=0, residual_first=0, x=P, ldx=3000, x_codes=None, x_scales=None, w_codes=P, w_scales=P, bias=None, residual=None, y=P, ldr=8, ldy=8)
     a.update(change)
     args = B.LinearMx4Args(*[a[n] for n, _ in B.LinearMx4Args._fields_])
     assert B.lib().iolb_linear_mx4(ctypes.byref(args), None, 0) == code
