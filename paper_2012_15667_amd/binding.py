@@ -909,7 +909,7 @@ def block_norm_backward(dy, dx_out, x, h=None, post="none", post_weight=None, po
     b = _dense(pre_bias, "pre_bias", dtype, device, (N,)) if pre_bias is not None else 0
 
     def like(t, there=True):
-        return x.new_empty(t.shape) if t is not None and want_weights and there else None
+        return torch.empty_like(t) if t is not None and want_weights and there else None       # (they are contiguous)
     g = BlockNormGrads(x.new_empty((M, N)) if want_dx else None, x.new_empty((M, N)) if want_dx and h is not None else None,
                        like(gate), like(post_weight), like(post_bias), like(pre_weight, dy is not None), like(pre_bias, dy is not None))
     args = _pack_block_norm_backward(M, N, groups, code, kind_post, kind_pre, scale, eps, pdy, pdo, px, ph, wp, bp, pgate, w,
