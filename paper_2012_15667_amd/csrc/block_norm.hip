@@ -127,38 +127,82 @@ __device__ __forceinline__ void store_columns_of(T* p, int have, const float (&v
 }
 
 // ---- rows in registers ------------------------------------------------------------------------------------
-// Eight neighbouring values as they are in memory; zeros beyond the row's end.
+// How rows end: after a whole piece of eight values; within one; or within the first.
+enum RowEnd { WHOLE, CUT, SHORT };
+
+// Eight neighbouring values as they are in memory; zeros beyond the row's end.  A last piece that is cut is read in one access that ends with the row, and
+// settle_eight moves its values to their places, once other loads are on their way.  16-bit rows of 4094 values, 8192 of them: value by value 64 us, gradients
+// 116, so 54 / 99; of 157, 16356 of them, 16.3 / 35 and 14.6 / 29.  (With this in the kernel of whole rows those would hold twice the registers.)
 template <class T> using Eight = typename Piece<T, 8>::type;
 
-template <class T>
-__device__ __forceinline__ Eight<T> load_eight(const T* p, int have)
+template <int ENDS, class T>
+__device__ __forceinline__ Eight<T> load_eight(const T* row, int at, int N)
 {
-    if (have >= 8) return *reinterpret_cast<const Eight<T>*>(p);
-    Eight<T> t;
+    Eight<T> t = {};
+    if constexpr (ENDS == SHORT) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = i < have ? p[i] : (T)0.f;
+        for (int i = 0; i < 8; ++i) t[i] = at + i < N ? row[at + i] : (T)0.f;
+    } else if (at < N) {
+        t = *reinterpret_cast<const Eight<T>*>(row + (ENDS == WHOLE || at < N - 8 ? at : N - 8));
+    }
     return t;
+}
+
+// The values moved down by BY places, with zeros behind them.
+template <int BY, class T>
+__device__ __forceinline__ void move_down(Eight<T>& t)
+{
+    constexpr int W = 2 * sizeof(T), STEP = BY * (int)sizeof(T) / 4;    // words; words to move by, or half a word
+    typedef unsigned Words __attribute__((ext_vector_type(W)));
+    const Words w = __builtin_bit_cast(Words, t);
+    Words to;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if constexpr (STEP == 0) to[i] = __builtin_amdgcn_alignbyte(i + 1 < W ? w[i + 1 < W ? i + 1 : 0] : 0, w[i], 2);
+        else to[i] = i + STEP < W ? w[i + STEP < W ? i + STEP : 0] : 0;
+    }
+    t = __builtin_bit_cast(Eight<T>, to);
+}
+
+template <int ENDS, class T>
+__device__ __forceinline__ void settle_eight(Eight<T>& t, int at, int N)
+{
+    if constexpr (ENDS == CUT) {
+        if (at == N - (N & 7)) {
+            const int by = 8 - (N & 7);
+            if (by & 4) move_down<4, T>(t);
+            if (by & 2) move_down<2, T>(t);
+            if (by & 1) move_down<1, T>(t);
+        }
+    }
 }
 
 // A row's values, TR threads to a row, C times eight a thread: c-th piece at column 8 (c TR + thread).
 template <class T, int C> struct Row { Eight<T> of[C]; };
 
-template <int TR, int C, class T>
+template <int TR, int C, int ENDS, class T>
 __device__ __forceinline__ void load_row(const T* p, int N, int thread, Row<T, C>& row)
 {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int at = 8 * (c * TR + thread);
-        row.of[c] = load_eight(p + at, N - at);
+        row.of[c] = load_eight<ENDS>(p, at, N);
     }
 }
 
+template <int TR, int C, int ENDS, class T>
+__device__ __forceinline__ void settle(Row<T, C>& row, int N, int thread)
+{
+#pragma unroll
+    for (int c = 0; c < C; ++c) settle_eight<ENDS, T>(row.of[c], 8 * (c * TR + thread), N);
+}
+
 // A weight's, a bias's or a gate's values; `or_else` where there is none.
-template <int TR, int C, class T>
+template <int TR, int C, int ENDS, class T>
 __device__ __forceinline__ void load_row_or(const T* p, int N, int thread, float or_else, Row<T, C>& row)
 {
     if (p) {
-        load_row<TR, C>(p, N, thread, row);
+        load_row<TR, C, ENDS>(p, N, thread, row);
     } else {
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -208,7 +252,7 @@ __device__ __forceinline__ RowStats stats_of_row(float (&v)[C][8], int N, int th
     return {mean, 1.f / sqrtf(one[0] / (float)N + eps)};
 }
 
-template <int DT, int TR, int C, bool PAST>
+template <int DT, int TR, int C, int ENDS, bool PAST>
 __global__ void __launch_bounds__(TR > 256 ? TR : 256)
 block_norm_rows_kernel(BlockNorm p)
 {
@@ -220,13 +264,17 @@ block_norm_rows_kernel(BlockNorm p)
     // (more than a wave to a row: all threads of the workgroup alike)
     for (long long m = (long long)blockIdx.x * ROWS + threadIdx.x / TR; m < p.M; m += (long long)gridDim.x * ROWS) {
         Row<T, C> x, w, b;
-        load_row<TR, C>(static_cast<const T*>(p.x) + m * p.ldx, p.N, thread, x);
+        load_row<TR, C, ENDS>(static_cast<const T*>(p.x) + m * p.ldx, p.N, thread, x);
         float v[C][8];
         if (p.h) {
             Row<T, C> h, g;
-            load_row<TR, C>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, h);
-            load_row_or<TR, C>(static_cast<const T*>(p.post_weight), p.N, thread, 1.f, w);
-            load_row_or<TR, C>(p.gate ? static_cast<const T*>(p.gate) + m / p.rows_per_group * p.N : nullptr, p.N, thread, 1.f, g);
+            load_row<TR, C, ENDS>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, h);
+            load_row_or<TR, C, ENDS>(static_cast<const T*>(p.post_weight), p.N, thread, 1.f, w);
+            load_row_or<TR, C, ENDS>(p.gate ? static_cast<const T*>(p.gate) + m / p.rows_per_group * p.N : nullptr, p.N, thread, 1.f, g);
+            settle<TR, C, ENDS>(x, p.N, thread);
+            settle<TR, C, ENDS>(h, p.N, thread);
+            settle<TR, C, ENDS>(w, p.N, thread);
+            settle<TR, C, ENDS>(g, p.N, thread);
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -239,7 +287,8 @@ block_norm_rows_kernel(BlockNorm p)
                 for (int i = 0; i < 8; ++i) v[c][i] = (v[c][i] - s.mean) * s.r * (float)w.of[c][i];
                 const int at = 8 * (c * TR + thread);
                 if (p.post_bias) {
-                    const Eight<T> bias = load_eight(static_cast<const T*>(p.post_bias) + at, p.N - at);
+                    Eight<T> bias = load_eight<ENDS>(static_cast<const T*>(p.post_bias), at, p.N);
+                    settle_eight<ENDS, T>(bias, at, p.N);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[c][i] += (float)bias[i];
                 }
@@ -252,14 +301,17 @@ block_norm_rows_kernel(BlockNorm p)
                 store_eight_of<PAST>(static_cast<T*>(p.out) + m * p.ldo + at, p.N - at, x.of[c]);
             }
         } else {
+            settle<TR, C, ENDS>(x, p.N, thread);
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[c][i] = (float)x.of[c][i];
         }
         if (!p.y) continue;
-        load_row_or<TR, C>(static_cast<const T*>(p.pre_weight), p.N, thread, 1.f, w);
-        load_row_or<TR, C>(static_cast<const T*>(p.pre_bias), p.N, thread, 0.f, b);
+        load_row_or<TR, C, ENDS>(static_cast<const T*>(p.pre_weight), p.N, thread, 1.f, w);
+        load_row_or<TR, C, ENDS>(static_cast<const T*>(p.pre_bias), p.N, thread, 0.f, b);
+        settle<TR, C, ENDS>(w, p.N, thread);
+        settle<TR, C, ENDS>(b, p.N, thread);
         const RowStats s = stats_of_row<TR, C>(v, p.N, thread, p.pre, p.eps, sum);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -489,7 +541,7 @@ norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces)
 
 // The same for rows that are held in registers: a workgroup takes a piece's rows, TR threads to a row, reads everything once, and holds its columns' sums
 // meanwhile; the next row's values are asked for where this row's have been used last.  BIASES: whether S0 and T0 are wanted.
-template <int DT, int TR, int C, bool BIASES, bool PAST>
+template <int DT, int TR, int C, bool BIASES, int ENDS, bool PAST>
 __global__ void __launch_bounds__(TR > 256 ? TR : 256)
 norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wanted)
 {
@@ -504,9 +556,12 @@ norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wante
     const float per = 1.f / (float)p.N;
 
     Row<T, C> w, wp, g;
-    load_row_or<TR, C>(static_cast<const T*>(p.pre_weight), p.N, thread, 1.f, w);
-    load_row_or<TR, C>(static_cast<const T*>(p.post_weight), p.N, thread, 1.f, wp);
-    load_row_or<TR, C>(p.gate ? static_cast<const T*>(p.gate) + (long long)group * p.N : nullptr, p.N, thread, 1.f, g);
+    load_row_or<TR, C, ENDS>(static_cast<const T*>(p.pre_weight), p.N, thread, 1.f, w);
+    load_row_or<TR, C, ENDS>(static_cast<const T*>(p.post_weight), p.N, thread, 1.f, wp);
+    load_row_or<TR, C, ENDS>(p.gate ? static_cast<const T*>(p.gate) + (long long)group * p.N : nullptr, p.N, thread, 1.f, g);
+    settle<TR, C, ENDS>(w, p.N, thread);
+    settle<TR, C, ENDS>(wp, p.N, thread);
+    settle<TR, C, ENDS>(g, p.N, thread);
     float s1[C][8], t1[C][8], s0[BIASES ? C : 1][8], t0[BIASES ? C : 1][8];
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -520,17 +575,21 @@ norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wante
     const auto load_x = [&](long long m) {
         if (m >= r1) return;
         if (p.dy) {
-            load_row<TR, C>(static_cast<const T*>(p.x) + m * p.ldx, p.N, thread, r.x);
-            load_row<TR, C>(static_cast<const T*>(p.dy) + m * p.lddy, p.N, thread, r.dy);
+            load_row<TR, C, ENDS>(static_cast<const T*>(p.x) + m * p.ldx, p.N, thread, r.x);
+            load_row<TR, C, ENDS>(static_cast<const T*>(p.dy) + m * p.lddy, p.N, thread, r.dy);
         }
-        if (p.dout) load_row<TR, C>(static_cast<const T*>(p.dout) + m * p.lddout, p.N, thread, r.dout);
+        if (p.dout) load_row<TR, C, ENDS>(static_cast<const T*>(p.dout) + m * p.lddout, p.N, thread, r.dout);
     };
     const auto load_h = [&](long long m) {
-        if (m < r1 && p.h) load_row<TR, C>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, r.h);
+        if (m < r1 && p.h) load_row<TR, C, ENDS>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, r.h);
     };
     load_x(r0 + slot);
     load_h(r0 + slot);
     for (long long m = r0 + slot; m < r1; m += ROWS) {
+        settle<TR, C, ENDS>(r.x, p.N, thread);
+        settle<TR, C, ENDS>(r.h, p.N, thread);
+        settle<TR, C, ENDS>(r.dy, p.N, thread);
+        settle<TR, C, ENDS>(r.dout, p.N, thread);
         hold(w);
         hold(wp);
         hold(g);
@@ -796,6 +855,17 @@ void by_row(int N, F f)
     call(std::integral_constant<int, 256>{}, std::integral_constant<int, 0>{});
 }
 
+// f called with how the rows end.
+template <int TR, class F>
+void by_end(int N, F f)
+{
+    if (N % 8 == 0) return f(std::integral_constant<int, WHOLE>{});
+    if constexpr (TR == 16) {
+        if (N < 8) return f(std::integral_constant<int, SHORT>{});
+    }
+    f(std::integral_constant<int, CUT>{});
+}
+
 unsigned row_groups(int M) { return (unsigned)(M < 65536 ? M : 65536); }
 
 }  // namespace
@@ -814,8 +884,11 @@ hipError_t launch_block_norm(const BlockNorm& p, int dtype, hipStream_t st)
                 block_norm_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
             } else {
                 constexpr int ROWS = TR > 256 ? 1 : 256 / TR;
-                const auto kernel = past ? block_norm_rows_kernel<DT, TR, C, true> : block_norm_rows_kernel<DT, TR, C, false>;
-                kernel<<<row_groups((int)((p.M + (ROWS - 1LL)) / ROWS)), TR > 256 ? TR : 256, 0, st>>>(p);
+                by_end<TR>(p.N, [&](auto end) {
+                    constexpr int ENDS = decltype(end)::value;
+                    const auto kernel = past ? block_norm_rows_kernel<DT, TR, C, ENDS, true> : block_norm_rows_kernel<DT, TR, C, ENDS, false>;
+                    kernel<<<row_groups((int)((p.M + (ROWS - 1LL)) / ROWS)), TR > 256 ? TR : 256, 0, st>>>(p);
+                });
             }
         });
     });
@@ -861,9 +934,12 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBack
                 if (wanted) norm_backward_columns_kernel<DT><<<(unsigned)((p.N + 63) / 64) * pieces, 256, 0, st>>>(p, plan.pieces);
             } else {
                 const bool biases = wanted >> S0 & 1 || wanted >> T0 & 1;
-                const auto kernel = biases ? (past ? norm_backward_rows_kernel<DT, TR, C, true, true> : norm_backward_rows_kernel<DT, TR, C, true, false>)
-                                           : (past ? norm_backward_rows_kernel<DT, TR, C, false, true> : norm_backward_rows_kernel<DT, TR, C, false, false>);
-                kernel<<<pieces, TR > 256 ? TR : 256, 0, st>>>(p, plan.pieces, wanted);
+                by_end<TR>(p.N, [&](auto end) {
+                    constexpr int ENDS = decltype(end)::value;
+                    const auto kernel = biases ? (past ? norm_backward_rows_kernel<DT, TR, C, true, ENDS, true> : norm_backward_rows_kernel<DT, TR, C, true, ENDS, false>)
+                                               : (past ? norm_backward_rows_kernel<DT, TR, C, false, ENDS, true> : norm_backward_rows_kernel<DT, TR, C, false, ENDS, false>);
+                    kernel<<<pieces, TR > 256 ? TR : 256, 0, st>>>(p, plan.pieces, wanted);
+                });
             }
         });
         if (!wanted) return;
