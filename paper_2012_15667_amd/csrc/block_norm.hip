@@ -709,6 +709,149 @@ norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wante
     }
 }
 
+// Rows whose columns' sums do not fit beside them: a workgroup of 1024 to a row, which it reads once.  The sums are another pass, which reads all again.
+// 16-bit rows leave registers for the next row to be asked for meanwhile; 32-bit ones do not.  2048 x 16384 bf16 162 us (both passes; a row read again
+// for each step 240), 1640 x 14640 fp32 222 (317), 64 x 10000 bf16 22 (37).
+template <int DT, int C, int ENDS>
+__global__ void __launch_bounds__(1024)
+norm_backward_wide_kernel(BlockNormBackward p)
+{
+    typedef typename DenseType<DT>::type T;
+    constexpr int TR = 1024;
+    constexpr bool AHEAD = sizeof(T) == 2;
+    __shared__ typename RowSum<4, TR>::Part part;
+    RowSum<4, TR> sum{part};
+    const int thread = threadIdx.x;
+    const float per = 1.f / (float)p.N;
+    Row<T, C> x{}, h{}, dy{}, dout{}, w, g;
+    const auto load_x = [&](long long m) {
+        if (m >= p.M) return;
+        if (p.dy) {
+            load_row<TR, C, ENDS>(static_cast<const T*>(p.x) + m * p.ldx, p.N, thread, x);
+            load_row<TR, C, ENDS>(static_cast<const T*>(p.dy) + m * p.lddy, p.N, thread, dy);
+        }
+        if (p.dout) load_row<TR, C, ENDS>(static_cast<const T*>(p.dout) + m * p.lddout, p.N, thread, dout);
+    };
+    const auto load_h = [&](long long m) {
+        if (m < p.M && p.h) load_row<TR, C, ENDS>(static_cast<const T*>(p.h) + m * p.ldh, p.N, thread, h);
+    };
+    if (AHEAD) {
+        load_x(blockIdx.x);
+        load_h(blockIdx.x);
+    }
+    for (long long m = blockIdx.x; m < p.M; m += gridDim.x) {
+        if (!AHEAD) {
+            x = h = dy = dout = Row<T, C>{};
+            load_x(m);
+            load_h(m);
+        }
+        load_row_or<TR, C, ENDS>(static_cast<const T*>(p.pre_weight), p.N, thread, 1.f, w);
+        settle<TR, C, ENDS>(x, p.N, thread);
+        settle<TR, C, ENDS>(dy, p.N, thread);
+        settle<TR, C, ENDS>(h, p.N, thread);
+        settle<TR, C, ENDS>(w, p.N, thread);
+        settle<TR, C, ENDS>(dout, p.N, thread);
+        RowSums s{0.f, 1.f, 0.f, 0.f, 0.f, 1.f, 0.f, 0.f};
+        if (p.pre == IOLB_NORM_LAYER || p.post == IOLB_NORM_LAYER) {
+            float v[2] = {0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[0] += (float)x.of[c][i];
+                    v[1] += (float)h.of[c][i];
+                }
+            sum(v);
+            if (p.pre == IOLB_NORM_LAYER) s.mean_x = v[0] * per;
+            if (p.post == IOLB_NORM_LAYER) s.mean_h = v[1] * per;
+        }
+        hold(x);
+        hold(h);
+        hold(dy);
+        hold(w);
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool live = 8 * (c * TR + thread) + i < p.N;
+                const float vx = live ? (float)x.of[c][i] - s.mean_x : 0.f, vh = live ? (float)h.of[c][i] - s.mean_h : 0.f;
+                const float t = (float)dy.of[c][i] * (float)w.of[c][i];
+                v[0] = __builtin_fmaf(vx, vx, v[0]);
+                v[1] = __builtin_fmaf(t, vx, v[1]);
+                v[2] += t;
+                v[3] = __builtin_fmaf(vh, vh, v[3]);
+            }
+        sum(v);
+        if (p.dy) {
+            s.r_x = 1.f / sqrtf(v[0] * per + p.eps);
+            s.along_x = v[1] * s.r_x * per;
+            if (p.pre == IOLB_NORM_LAYER) s.mean_d = v[2] * per;
+        }
+        if (p.post != IOLB_NORM_NONE) s.r_h = 1.f / sqrtf(v[3] * per + p.eps);
+        hold(x);
+        hold(h);
+        hold(dy);
+        hold(w);
+        hold(dout);
+        float d[C][8];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool live = 8 * (c * TR + thread) + i < p.N;
+                const float along = ((float)x.of[c][i] - s.mean_x) * s.r_x * s.along_x;
+                d[c][i] = (float)dout.of[c][i];
+                if (p.dy) d[c][i] += s.r_x * ((float)dy.of[c][i] * (float)w.of[c][i] - along - s.mean_d);
+                if (!live) d[c][i] = 0.f;
+            }
+        if (AHEAD) load_x(m + gridDim.x);
+        if (p.dx) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = 8 * (c * TR + thread);
+                Eight<T> to;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) to[i] = (T)(p.scale * d[c][i]);
+                store_eight_of(static_cast<T*>(p.dx) + m * p.N + at, p.N - at, to);
+            }
+        }
+        if (p.h && (p.dh || p.rows)) {
+            load_row_or<TR, C, ENDS>(static_cast<const T*>(p.post_weight), p.N, thread, 1.f, w);
+            load_row_or<TR, C, ENDS>(p.gate ? static_cast<const T*>(p.gate) + m / p.rows_per_group * p.N : nullptr, p.N, thread, 1.f, g);
+            settle<TR, C, ENDS>(w, p.N, thread);
+            settle<TR, C, ENDS>(g, p.N, thread);
+            float u[2] = {0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    d[c][i] *= (float)g.of[c][i] * (float)w.of[c][i];
+                    u[0] = __builtin_fmaf(d[c][i], ((float)h.of[c][i] - s.mean_h) * s.r_h, u[0]);
+                    u[1] += d[c][i];
+                }
+            if (p.post != IOLB_NORM_NONE) {
+                sum(u);
+                s.along_h = u[0] * per;
+                if (p.post == IOLB_NORM_LAYER) s.mean_p = u[1] * per;
+            }
+            hold(h);
+            if (p.dh) {
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const int at = 8 * (c * TR + thread);
+                    Eight<T> to;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) to[i] = (T)(s.r_h * (d[c][i] - ((float)h.of[c][i] - s.mean_h) * s.r_h * s.along_h - s.mean_p));
+                    store_eight_of(static_cast<T*>(p.dh) + m * p.N + at, p.N - at, to);
+                }
+            }
+        }
+        if (AHEAD) load_h(m + gridDim.x);
+        if (p.rows && threadIdx.x == 0) reinterpret_cast<RowSums*>(p.rows)[m] = s;
+    }
+}
+
 // What weights, biases and gate get.  First the pieces of a group (its rows of the gate are done then, and all of it where there is one group); then
 // (`across`) the groups, whose sums lie in the place of their first piece.  A workgroup takes 16 columns, 64 threads to each.  BIASES: whether S0 and T0
 // are there; of a pair one may have been left out, and what stands in its place is then read but goes nowhere.
@@ -836,7 +979,7 @@ unsigned column_sums(const BlockNormBackward& p)
 }
 
 constexpr int MOST_IN_REGISTERS = 512 * 8 * 4;          // values of a row, forward
-constexpr int MOST_BACKWARD = 512 * 8 * 2;              // backward
+constexpr int MOST_BACKWARD = 512 * 8 * 2;              // backward, with the columns' sums
 
 // f called with the threads that take a row, and how many times eight values each; 0 where the row is not held in registers.
 template <class F>
@@ -930,7 +1073,11 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBack
         by_row(p.N, [&](auto tr, auto c) {
             constexpr int TR = decltype(tr)::value, C = decltype(c)::value;
             if constexpr (C == 0 || 8 * TR * C > MOST_BACKWARD) {
-                if (p.M) norm_backward_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
+                if constexpr (C == 0) {
+                    if (p.M) norm_backward_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
+                } else if (p.M) {
+                    by_end<1024>(p.N, [&](auto end) { norm_backward_wide_kernel<DT, TR * C / 1024, decltype(end)::value><<<(unsigned)(p.M < 256 ? p.M : 256), 1024, 0, st>>>(p); });
+                }
                 if (wanted) norm_backward_columns_kernel<DT><<<(unsigned)((p.N + 63) / 64) * pieces, 256, 0, st>>>(p, plan.pieces);
             } else {
                 const bool biases = wanted >> S0 & 1 || wanted >> T0 & 1;

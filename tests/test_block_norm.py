@@ -292,6 +292,29 @@ def test_backward_many_rows(dtype, M, N, gate):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,M,N,gate,bias", [("bfloat16", 600, 9001, 40, False), ("float16", 520, 8201, None, True), ("float32", 300, 16383, "columns", True)])
+def test_backward_many_wide_rows(dtype, M, N, gate, bias):
+    check_backward(np.random.default_rng(N), M, N, dtype, "rms", "layer", gate, bias)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dout,dy,post,pre", [(False, True, "rms", "rms"), (True, False, "layer", "layer"), (True, True, "none", "layer"), (True, True, "rms", "none")])
+def test_backward_wide_rows_of_each_kind(dtype, dout, dy, post, pre):
+    check_backward(np.random.default_rng(4), 6, 8195, dtype, post, pre, 3, True, dout=dout, dy=dy and pre != "none")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("last", range(1, 8))
+@pytest.mark.parametrize("whole", [0, 8, 128, 520, 1032, 2056, 4104, 8200])
+def test_rows_that_end_within_a_piece(dtype, last, whole):
+    rng = np.random.default_rng(whole + last)
+    check_forward(rng, 5, whole + last, dtype, "layer", "rms", "columns", True)
+    check_backward(rng, 5, whole + last, dtype, "layer", "rms", "columns", True)
+
+
+@pytest.mark.gpu
 def test_backward_without_a_block_and_of_what_is_wanted_only():
     torch = _torch()
     rng = np.random.default_rng(8)
