@@ -315,6 +315,14 @@ def test_rows_that_end_within_a_piece(dtype, last, whole):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,gate", [(1, 129, "columns"), (700, 200, 7), (2100, 256, None), (16500, 136, 50)])
+def test_rows_of_two_pieces_to_a_lane(dtype, M, N, gate):
+    check_forward(np.random.default_rng(M), M, N, dtype, "rms", "layer", gate, True)
+    check_backward(np.random.default_rng(M), M, N, dtype, "rms", "layer", gate, True)
+
+
+@pytest.mark.gpu
 def test_backward_without_a_block_and_of_what_is_wanted_only():
     torch = _torch()
     rng = np.random.default_rng(8)
