@@ -43,7 +43,7 @@ __device__ __forceinline__ Eight<T> load_eight(const T* p, int have)
 
 // A thread takes the eight columns of a counter in one row after the other, the next one on its way meanwhile; a workgroup `wide` threads of a row and
 // 256 / wide rows; four threads hold a checkpoint's block.  CHECKPOINT, RESIDUAL: whether there is one; PAST: past the caches.
-// Memory and the generator's 20 products a counter bind it alike: 16384 x 8192 bf16 without the generator 94 us.
+// Memory and the generator's 20 products a counter bind it alike: 16384 x 8192 bf16 87 us (6.1 TB/s); through the caches 96, and 94 without the generator.
 template <int DT, bool RESIDUAL, bool CHECKPOINT, bool PAST>
 __global__ void __launch_bounds__(256)
 dropout_kernel(Dropout p, int wide_log)

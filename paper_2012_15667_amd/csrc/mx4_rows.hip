@@ -78,6 +78,7 @@ __device__ __forceinline__ unsigned block_codes(const T* x, int have, u32x4& cod
 // the wave that multiplies them, four steps ahead, with MR times sixteen rows of x.  A lane holds a block of 32 of row lane % 16 of either operand.
 // PACKED: x is in 4 bits already; a tensor's blocks are brought into them where they are multiplied, by every workgroup again, which a launch of its own
 // would cost more than.  The columns' operand comes first, so that a lane holds four neighbouring columns of one row.
+// A row's time is a trip to memory, x into 4 bits and the waves' exchange: 1 x 4096 -> 4096 bf16 6.9 us on the GPU, of which 1.6 for W's bytes.
 // (x's next blocks on their way meanwhile: 64 x 4096 -> 4096 19.1 -> 20.4 us, and more registers.  What counts there is the lanes' 64 bytes each, far apart.)
 template <int DT, bool PACKED, int MR>
 __global__ void __launch_bounds__(64 * WAVES)

@@ -4,6 +4,10 @@
 // a block of 32 codes, which is what a lane gives to a matrix instruction of 64 k.  A stage also takes the rows' eight scales, 8 bytes.  The lanes of half h
 // multiply pieces 4 h + kk of a row, kk = 0 ... 3 (both operands alike: the order of k does not matter), so their four scales are one word of LDS, from
 // which the instruction takes byte kk.
+//
+// Bound by the stage: 2.0 us for 256 x 256 x 256 on a compute unit, where the matrix instructions alone need 1.3 at the rate that the card's power leaves them.
+// 8192^3 276 us (4.0 PFLOP/s), 8192 x 4096 -> 16384 bf16 with gelu 368 to 393 with packing x (18) and a third of a block's time in prologue, gelu and stores.
+// Workgroups that stay and take block after block were slower (394 -> 418).
 #include "dense_math.h"
 #include "kernels.h"
 #include "lds_dma.h"
