@@ -63,6 +63,7 @@ int check_norm_backward(const iolb_block_norm_backward_args& a)
     if (a.M < 0 || a.N < 0) return IOLB_EINVAL;
     if (!known_type(a.dtype) || !known_norm(a.post) || !known_norm(a.pre) || a.M > MOST_K || a.N > MOST_K) return IOLB_EUNSUPPORTED;
     if (a.gate && (a.groups < 1 || a.M % a.groups)) return IOLB_EINVAL;
+    if (a.gate && a.groups > MOST_K) return IOLB_EUNSUPPORTED;      // (without rows any number divides them)
     if (!(a.eps >= 0.f)) return IOLB_EINVAL;
     if (a.M == 0 || a.N == 0) return IOLB_OK;               // (tensors without values may have no address)
     if (!a.h && (a.gate || a.dh || a.dgate || a.post != IOLB_NORM_NONE || a.scale != 1.f)) return IOLB_EINVAL;

@@ -518,6 +518,14 @@ def test_backward_workspace():
         assert code == (-2 if groups > 1 else 0)
 
 
+@pytest.mark.parametrize("groups", [(1 << 22) + 1, 1 << 31, 1 << 32, 1 << 62])
+def test_backward_of_no_rows_refuses_more_groups_than_it_counts(groups):
+    need = ctypes.c_size_t(0)
+    args = _backward_args(M=0, groups=groups)
+    assert B.lib().iolb_block_norm_backward_workspace_bytes(ctypes.byref(args), ctypes.byref(need)) == -2
+    assert B.lib().iolb_block_norm_backward(ctypes.byref(args), P, 1 << 40) == -2
+
+
 def test_python_refuses_cpu_tensors_and_unknown_names():
     torch = _torch()
     x = torch.zeros((4, 8))

@@ -277,6 +277,17 @@ def test_linear_gives_the_same_for_a_tensor_and_for_its_codes(M):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("packed", [False, True])
+def test_nothing_to_sum_for_many_rows(packed):
+    torch = _torch()
+    M, N = 33000, 70
+    x, w = torch.empty((M, 0), dtype=torch.float32, device="cuda"), B.mx4_pack(torch.empty((N, 0), dtype=torch.float32, device="cuda"))
+    b, b64 = make(np.random.default_rng(1), (N,), "float32")
+    y = B.linear_mx4(B.mx4_pack(x) if packed else x, w, b, act="relu", dtype=torch.float32 if packed else None)
+    assert_within(y, np.broadcast_to(np.maximum(b64, 0), (M, N)), np.zeros((M, N)))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("M,N,K", [(0, 5, 8), (5, 0, 8), (5, 40, 0), (0, 0, 0), (1, 3, 0), (600, 30, 0)])
 def test_empty(dtype, M, N, K):
