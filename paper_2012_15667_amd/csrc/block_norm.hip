@@ -1004,12 +1004,12 @@ void by_row(int N, F f)
     call(std::integral_constant<int, 256>{}, std::integral_constant<int, 0>{});
 }
 
-// f called with how the rows end.
-template <int TR, class F>
+// f called with how the rows end, of a kernel that takes up to PIECES times eight values.
+template <int PIECES, class F>
 void by_end(int N, F f)
 {
     if (N % 8 == 0) return f(std::integral_constant<int, WHOLE>{});
-    if constexpr (TR == 16) {
+    if constexpr (PIECES == 16) {
         if (N < 8) return f(std::integral_constant<int, SHORT>{});
     }
     f(std::integral_constant<int, CUT>{});
@@ -1033,7 +1033,7 @@ hipError_t launch_block_norm(const BlockNorm& p, int dtype, hipStream_t st)
                 block_norm_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
             } else {
                 constexpr int ROWS = TR > 256 ? 1 : 256 / TR;
-                by_end<TR>(p.N, [&](auto end) {
+                by_end<TR * C>(p.N, [&](auto end) {
                     constexpr int ENDS = decltype(end)::value;
                     const auto kernel = past ? block_norm_rows_kernel<DT, TR, C, ENDS, true> : block_norm_rows_kernel<DT, TR, C, ENDS, false>;
                     kernel<<<row_groups((int)((p.M + (ROWS - 1LL)) / ROWS)), TR > 256 ? TR : 256, 0, st>>>(p);
@@ -1082,12 +1082,12 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBack
                 if constexpr (C == 0) {
                     if (p.M) norm_backward_long_kernel<DT><<<row_groups(p.M), 256, 0, st>>>(p);
                 } else if (p.M) {
-                    by_end<1024>(p.N, [&](auto end) { norm_backward_wide_kernel<DT, TR * C / 1024, decltype(end)::value><<<(unsigned)(p.M < 256 ? p.M : 256), 1024, 0, st>>>(p); });
+                    by_end<TR * C>(p.N, [&](auto end) { norm_backward_wide_kernel<DT, TR * C / 1024, decltype(end)::value><<<(unsigned)(p.M < 256 ? p.M : 256), 1024, 0, st>>>(p); });
                 }
                 if (wanted) norm_backward_columns_kernel<DT><<<(unsigned)((p.N + 63) / 64) * pieces, 256, 0, st>>>(p, plan.pieces);
             } else {
                 const bool biases = wanted >> S0 & 1 || wanted >> T0 & 1;
-                by_end<TR>(p.N, [&](auto end) {
+                by_end<TR * C>(p.N, [&](auto end) {
                     constexpr int ENDS = decltype(end)::value;
                     const auto kernel = biases ? (past ? norm_backward_rows_kernel<DT, TR, C, true, ENDS, true> : norm_backward_rows_kernel<DT, TR, C, true, ENDS, false>)
                                                : (past ? norm_backward_rows_kernel<DT, TR, C, false, ENDS, true> : norm_backward_rows_kernel<DT, TR, C, false, ENDS, false>);
