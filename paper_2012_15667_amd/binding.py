@@ -339,10 +339,23 @@ def _dev_f32(t, name):
     return t.data_ptr()                        # (an address: the functions' argtypes make pointers of it)
 
 
+_increment_version = None
+
+
+def _written(t):
+    """Tells autograd that a caller's tensor was written to: who has kept what stood there must not take the new values for it."""
+    global _increment_version
+    if _increment_version is None:
+        _increment_version = _torch.autograd.graph.increment_version
+    if not t.is_inference():
+        _increment_version(t)
+
+
 def conv_direct(x, w, stride=1, pad=0, y=None, cfg=None):
     """y = direct convolution of x [N][C][H][W] with w [K][C][R][S] on the current stream.  pad: zeros per
     side, or (pad_h, pad_w) for a padding of its own per axis (tuned tile only)."""
     torch = _torch or _load_torch()
+    given = y is not None
     N, C, H, W = x.shape
     K, C2, R, S = w.shape
     if C2 != C:
@@ -361,6 +374,8 @@ def conv_direct(x, w, stride=1, pad=0, y=None, cfg=None):
         _use_current_stream()
         _check(lib().conv_direct_pad2(_dev_f32(x, "x"), _dev_f32(w, "w"), _dev_f32(y, "y"), N, C, H, W, K, R, S,
                                       stride, ph, pw))
+        if given:
+            _written(y)
         return y
     valid = stride >= 1 and pad >= 0 and H + 2 * pad >= R and W + 2 * pad >= S
     if valid:
@@ -378,6 +393,8 @@ def conv_direct(x, w, stride=1, pad=0, y=None, cfg=None):
     else:
         c = cfg if isinstance(cfg, TileConfig) else TileConfig.from_dict(cfg)
         _check(lib().conv_direct_cfg(*args, ctypes.byref(c)))
+    if given:
+        _written(y)
     return y
 
 
@@ -386,6 +403,7 @@ def conv_direct_layout(x, w, stride=1, pad=0, layout=LAYOUT_HWC, y=None, cfg=Non
     x [N][H][W][C] and returns y [N][P][Q][K]; LAYOUT_CWH takes x [N][C][W][H] and returns y [N][K][Q][P].
     w is [K][C][R][S] for all."""
     torch = _torch or _load_torch()
+    given = y is not None
     if layout == LAYOUT_HWC:
         N, H, W, C = x.shape
     elif layout == LAYOUT_CWH:
@@ -411,6 +429,8 @@ def conv_direct_layout(x, w, stride=1, pad=0, layout=LAYOUT_HWC, y=None, cfg=Non
         c = ctypes.byref(cfg if isinstance(cfg, TileConfig) else TileConfig.from_dict(cfg))
     _check(lib().conv_direct_layout(_dev_f32(x, "x"), _dev_f32(w, "w"), _dev_f32(y, "y"), N, C, H, W, K, R, S,
                                     stride, pad, int(layout), c))
+    if given:
+        _written(y)
     return y
 
 
@@ -423,6 +443,7 @@ def conv_direct_noalloc(x, w, stride, pad, y):
         raise ValueError("channel mismatch")
     _use_current_stream()
     _check(lib().conv_direct_noalloc(_dev_f32(x, "x"), _dev_f32(w, "w"), _dev_f32(y, "y"), N, C, H, W, K, R, S, stride, pad))
+    _written(y)
     return y
 
 
@@ -430,6 +451,7 @@ def conv_winograd(x, w, m, y=None, cfg=None, workspace=None, pad=1):
     """y = Winograd F(m x m, 3 x 3) convolution (stride 1, pad 1 unless `pad` says otherwise) on the current
     stream.  Another padding runs with the tuned tile and the library's workspace only."""
     torch = _torch or _load_torch()
+    given = y is not None
     N, C, H, W = x.shape
     K, C2, R, S = w.shape
     if C2 != C or R != 3 or S != 3:
@@ -446,6 +468,8 @@ def conv_winograd(x, w, m, y=None, cfg=None, workspace=None, pad=1):
             raise ValueError("y has the wrong shape")
         _use_current_stream()
         _check(lib().conv_winograd_pad(_dev_f32(x, "x"), _dev_f32(w, "w"), _dev_f32(y, "y"), N, C, H, W, K, m, pad))
+        if given:
+            _written(y)
         return y
     if y is None:
         y = torch.empty((N, K, H, W), dtype=torch.float32, device=x.device)
@@ -455,6 +479,8 @@ def conv_winograd(x, w, m, y=None, cfg=None, workspace=None, pad=1):
     L = lib()
     if cfg is None and workspace is None:
         _check(L.conv_winograd(_dev_f32(x, "x"), _dev_f32(w, "w"), _dev_f32(y, "y"), N, C, H, W, K, m))
+        if given:
+            _written(y)
         return y
     need = L.conv_winograd_workspace_bytes(N, C, H, W, K, m)
     if need == 0:
@@ -466,6 +492,8 @@ def conv_winograd(x, w, m, y=None, cfg=None, workspace=None, pad=1):
         c = ctypes.byref(cfg if isinstance(cfg, TileConfig) else TileConfig.from_dict(cfg))
     _check(L.conv_winograd_ws(_dev_f32(x, "x"), _dev_f32(w, "w"), _dev_f32(y, "y"), N, C, H, W, K, m,
                               ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size(), c))
+    if given:
+        _written(y)
     return y
 
 
@@ -488,6 +516,7 @@ def winograd_transform_kernels(w, m):
 def conv_winograd_pre(x, U, K, m, y=None, cfg=None, workspace=None):
     """conv_winograd with kernels transformed beforehand by winograd_transform_kernels."""
     torch = _torch or _load_torch()
+    given = y is not None
     N, C, H, W = x.shape
     if y is None:
         y = torch.empty((N, K, H, W), dtype=torch.float32, device=x.device)
@@ -505,6 +534,8 @@ def conv_winograd_pre(x, U, K, m, y=None, cfg=None, workspace=None):
     _use_current_stream()
     _check(L.conv_winograd_pre(_dev_f32(x, "x"), _dev_f32(U, "U"), _dev_f32(y, "y"), N, C, H, W, K, m,
                                ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size(), c))
+    if given:
+        _written(y)
     return y
 
 
@@ -716,6 +747,8 @@ def linear(x, w, bias=None, act="none", residual=None, residual_first=False, che
     L = lib()
     _use_stream_on(device)
     _call_with_workspace(L.iolb_linear, L.iolb_linear_workspace_bytes, args, x)
+    if given:
+        _written(y)
     if wanted:
         y = _without_graph(y, given, (x, w, bias, residual))
     return (y, z) if checkpoint else y
@@ -746,6 +779,7 @@ def checkpoint_unpack(c, dtype=None, act="none", y=None):
         dtype = y.dtype if y is not None else torch.float32
     code = _dtype_code(dtype)
     pq, pe = _checkpoint_of(c, "c", device, rows, cols)
+    given = y is not None
     if y is None:
         y = c[0].new_empty((rows, cols), dtype=dtype)
         py, ldy = y.data_ptr(), cols
@@ -753,6 +787,8 @@ def checkpoint_unpack(c, dtype=None, act="none", y=None):
         py, ldy = _rows(y, "y", dtype, device, (rows, cols))[:2]
     _use_stream_on(device)
     _check(lib().iolb_checkpoint_unpack(pq, pe, rows, cols, _act_code(act), code, py, ldy))
+    if given:
+        _written(y)
     return y
 
 
@@ -870,6 +906,9 @@ def block_norm(x, h=None, post="none", post_weight=None, post_bias=None, gate=No
     args = _pack_block_norm(M, N, groups, code, kind_post, kind_pre, scale, eps, px, ph, wp, bp, pgate, w, b, po, py, ldx, ldh, ldo, ldy)
     _use_stream_on(device)
     _check(_bytes_of["iolb_block_norm"](args))
+    for t in given:
+        if t is not None:
+            _written(t)
     if wanted:
         why = "block_norm() records no gradients: they are block_norm_backward's"
         if x_out is not None:
@@ -959,6 +998,8 @@ def dropout(x, p, seed, offset=0, counter=None, residual=None, checkpoint=False,
                          z.q.data_ptr() if checkpoint else 0, z.e.data_ptr() if checkpoint else 0)
     _use_stream_on(device)
     _check(_bytes_of["iolb_dropout"](args))
+    if given:
+        _written(y)
     if wanted:
         y = _without_graph(y, given, (x, residual), "dropout() records no gradients: they are dropout()'s of the same seed and offset")
     return (y, z) if checkpoint else y
@@ -998,6 +1039,7 @@ def mx4_unpack(c, dtype=None, y=None):
     if dtype is None:
         dtype = y.dtype if y is not None else torch.float32
     code = _dtype_code(dtype)
+    given = y is not None
     if y is None:
         y = c[0].new_empty((rows, cols), dtype=dtype)
         py, ldy = y.data_ptr(), cols
@@ -1005,6 +1047,8 @@ def mx4_unpack(c, dtype=None, y=None):
         py, ldy = _rows(y, "y", dtype, device, (rows, cols))[:2]
     _use_stream_on(device)
     _check(lib().iolb_mx4_unpack(pc, ps, rows, cols, code, py, ldy))
+    if given:
+        _written(y)
     return y
 
 
@@ -1044,6 +1088,8 @@ def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False,
     _use_stream_on(device)
     run = _call_in_new_workspace if px and M > 16 and M * N * K > 1 << 28 else _call_with_workspace
     run(_bytes_of["iolb_linear_mx4"], _bytes_of["iolb_linear_mx4_workspace_bytes"], args, like)
+    if given:
+        _written(y)
     if wanted:
         y = _without_graph(y, given, inputs, "linear_mx4() has no gradients")
     return y
