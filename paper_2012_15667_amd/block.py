@@ -41,7 +41,7 @@ class Blocks:
         self.first = column(width, 1.0)             # of the norm before the first block
         self.blocks = [Weights(matrix(hidden, width), column(hidden, 0.0), matrix(width, hidden), column(width, 0.0), column(width, 1.0),
                                column(width, 0.5), column(width, 1.0)) for _ in range(blocks)]
-        self.in_4_bits = None
+        self.in_4_bits = None                       # weights that answer(in_4_bits=True) has packed, for whoever looks; no call reads them
 
     def _end(self, w):
         return dict(post=self.norm, post_weight=w.post_weight, gate=w.gate, scale=self.scale, pre=self.norm, pre_weight=w.pre_weight)
@@ -83,14 +83,25 @@ class Blocks:
                 t.add_(d, alpha=-rate)
         self.in_4_bits = None
 
+    def packed(self):
+        """The layers' weights in microscaled 4-bit floating point, as they are now, for answer()."""
+        return [(B.mx4_pack(w.up), B.mx4_pack(w.down)) for w in self.blocks]
+
     def answer(self, x, in_4_bits=False):
-        """The last norm, without dropout; in_4_bits: with weights and layers' inputs in microscaled 4-bit floating point."""
-        if in_4_bits and self.in_4_bits is None:
-            self.in_4_bits = [(B.mx4_pack(w.up), B.mx4_pack(w.down)) for w in self.blocks]
+        """The last norm, without dropout; in_4_bits: with weights and layers' inputs in microscaled 4-bit floating point.  in_4_bits=True packs the
+        weights as they are in this call, and leaves them in self.in_4_bits; who answers often gives what packed() returned, and packs again
+        when the weights have changed: what happens to public tensors is not followed."""
+        four = None
+        if isinstance(in_4_bits, (list, tuple)):
+            four = in_4_bits
+            if len(four) != len(self.blocks):
+                raise ValueError("in_4_bits must have the weights of every block")
+        elif in_4_bits:
+            four = self.in_4_bits = self.packed()
         n = B.block_norm(x, pre=self.norm, pre_weight=self.first).y
         for i, w in enumerate(self.blocks):
-            if in_4_bits:
-                up, down = self.in_4_bits[i]
+            if four is not None:
+                up, down = four[i]
                 h = B.linear_mx4(B.linear_mx4(n, up, w.up_bias, act="gelu"), down, w.down_bias)
             else:
                 h = B.linear(B.linear(n, w.up, w.up_bias, act="gelu"), w.down, w.down_bias)
@@ -117,7 +128,7 @@ def main(argv=None):
     g.manual_seed(1)
     x = torch.randn((1 if a.one_token else a.rows, a.width), generator=g, device="cuda").to(dtype)
     if a.one_token:
-        for in_4_bits in (False, True):
+        for in_4_bits in (False, model.packed()):
             for _ in range(3):
                 model.answer(x, in_4_bits)
             torch.cuda.synchronize()
