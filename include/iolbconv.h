@@ -322,7 +322,8 @@ int iolb_block_norm(const iolb_block_norm_args* args);
  *   d = dx_out + (gradient of pre at x', of dy);  dx = scale d;  dh = (gradient of post at h, of gate d)
  * and of weights, biases and gate the sums of their factors over the rows that share them.  Outputs are dense, dx, dh [M][N], dgate [groups][N], the
  * others [N]; each may be NULL.  dh needs h, dgate the gate (and post_bias, where p had one), dpost_... a norm of h, dpre_... dy.
- * Sums are added in a fixed order: equal calls give equal bits.  M, N and groups up to 2^22.  Outputs overlap nothing. */
+ * Sums are added in a fixed order: equal calls give equal bits.  M, N and groups up to 2^22, and with
+ * gradients of weights, biases or gate groups x ceil(N / 16) below 2^32 (the workspace, 16 bytes a column and group and more, would be 2^40).  Outputs overlap nothing. */
 typedef struct iolb_block_norm_backward_args {
     int64_t M, N, groups;
     int32_t dtype, post, pre;

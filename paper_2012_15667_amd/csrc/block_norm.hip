@@ -485,14 +485,14 @@ norm_backward_long_kernel(BlockNormBackward p)
 
 enum { S1, S0, T1, T0 };
 
-// A workgroup takes 64 columns of a piece's rows: eight threads across, 32 along.
+// A workgroup takes 64 columns of a piece's rows: eight threads across, 32 along.  skip: workgroups of the launches before this one.
 template <int DT>
 __global__ void __launch_bounds__(256)
-norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces)
+norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces, unsigned skip)
 {
     typedef typename DenseType<DT>::type T;
     __shared__ float part[32][64 + 1];
-    const unsigned across = (unsigned)(p.N + 63) / 64, row = blockIdx.x / across, c0 = blockIdx.x % across * 64;
+    const unsigned across = (unsigned)(p.N + 63) / 64, at = skip + blockIdx.x, row = at / across, c0 = at % across * 64;
     const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, c = (int)c0 + tx * 8;
     const long long ld = (p.N + 7) / 8 * 8;
     const int group = (int)(row / pieces.in_group), piece = (int)(row % pieces.in_group);
@@ -857,17 +857,17 @@ norm_backward_wide_kernel(BlockNormBackward p)
 
 // What weights, biases and gate get.  First the pieces of a group (its rows of the gate are done then, and all of it where there is one group); then
 // (`across`) the groups, whose sums lie in the place of their first piece.  A workgroup takes 16 columns, 64 threads to each.  BIASES: whether S0 and T0
-// are there; of a pair one may have been left out, and what stands in its place is then read but goes nowhere.
+// are there; of a pair one may have been left out, and what stands in its place is then read but goes nowhere.  skip: workgroups of the launches before.
 template <int DT, bool BIASES>
 __global__ void __launch_bounds__(1024)
-norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across)
+norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across, unsigned skip)
 {
     typedef typename DenseType<DT>::type T;
     __shared__ float part[NORM_COLUMN_SUMS][64][16 + 1];
-    const unsigned blocks = (unsigned)(p.N + 15) / 16;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, n = (int)(blockIdx.x % blocks * 16) + tx;
+    const unsigned blocks = (unsigned)(p.N + 15) / 16, block = skip + blockIdx.x;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, n = (int)(block % blocks * 16) + tx;
     const long long ld = (p.N + 7) / 8 * 8;
-    const int group = (int)(blockIdx.x / blocks), count = across ? p.groups : in_group;
+    const int group = (int)(block / blocks), count = across ? p.groups : in_group;
     const T* const gates = static_cast<const T*>(p.gate);
     float sums[NORM_COLUMN_SUMS] = {0.f, 0.f, 0.f, 0.f};
     float* const at = p.columns + (long long)group * in_group * NORM_COLUMN_SUMS * ld + n;
@@ -1015,6 +1015,15 @@ void by_end(int N, F f)
     f(std::integral_constant<int, CUT>{});
 }
 
+// launch(workgroups, of them before) for `all` workgroups, a million at a time: a launch counts its threads in 32 bits, and one of a million takes
+// so long that another one behind it does not show.
+template <class F>
+void in_turns(long long all, F launch)
+{
+    constexpr long long MOST = 1 << 20;
+    for (long long at = 0; at < all; at += MOST) launch((unsigned)(all - at < MOST ? all - at : MOST), (unsigned)at);
+}
+
 unsigned row_groups(int M) { return (unsigned)(M < 65536 ? M : 65536); }
 
 }  // namespace
@@ -1061,10 +1070,11 @@ NormBackwardPlan block_norm_backward_plan(const BlockNormBackward& p, int)
         plan.pieces.per = (int)((R + wanted - 1) / wanted);
         plan.pieces.in_group = (R + plan.pieces.per - 1) / plan.pieces.per;
     }
-    // (a launch counts its threads in 32 bits)
-    const long long pieces = (long long)plan.pieces.in_group * p.groups;
-    plan.launchable = (long long)(p.N + 15) / 16 * p.groups * 1024 <= 0xffffffffLL && across * pieces * 512 <= 0xffffffffLL;
     if (!column_sums(p)) return plan;
+    // (the kernels count blocks of columns, 16 to a group and 64 to a piece, in 32 bits: beyond that the sums are 2^40 bytes and more.  The rows' kernels
+    // have a workgroup to a piece, of which there are no more than 512 or than groups.)
+    const long long pieces = (long long)plan.pieces.in_group * p.groups;
+    plan.launchable = (p.N + 15LL) / 16 * p.groups <= 0xffffffffLL && across * pieces <= 0xffffffffLL;
     plan.row_bytes = in_registers ? 0 : (size_t)p.M * NORM_ROW_SUMS * 4;
     plan.column_bytes = (size_t)pieces * NORM_COLUMN_SUMS * ((p.N + 7) / 8 * 8) * 4;
     return plan;
@@ -1084,7 +1094,8 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBack
                 } else if (p.M) {
                     by_end<TR * C>(p.N, [&](auto end) { norm_backward_wide_kernel<DT, TR * C / 1024, decltype(end)::value><<<(unsigned)(p.M < 256 ? p.M : 256), 1024, 0, st>>>(p); });
                 }
-                if (wanted) norm_backward_columns_kernel<DT><<<(unsigned)((p.N + 63) / 64) * pieces, 256, 0, st>>>(p, plan.pieces);
+                if (wanted)
+                    in_turns((p.N + 63LL) / 64 * pieces, [&](unsigned n, unsigned skip) { norm_backward_columns_kernel<DT><<<n, 256, 0, st>>>(p, plan.pieces, skip); });
             } else {
                 const bool biases = wanted >> S0 & 1 || wanted >> T0 & 1;
                 by_end<TR * C>(p.N, [&](auto end) {
@@ -1103,9 +1114,11 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBack
                 norm_backward_groups_kernel<DT, BIASES><<<across, 1024, 0, st>>>(p, plan.pieces.in_group);
                 return;
             }
-            norm_backward_weights_kernel<DT, BIASES><<<across * (unsigned)p.groups, 1024, 0, st>>>(p, plan.pieces.in_group, false);
+            in_turns((long long)across * p.groups, [&](unsigned n, unsigned skip) {
+                norm_backward_weights_kernel<DT, BIASES><<<n, 1024, 0, st>>>(p, plan.pieces.in_group, false, skip);
+            });
             if (p.groups > 1 && (p.dpost_weight || p.dpost_bias || p.dpre_weight || p.dpre_bias))
-                norm_backward_weights_kernel<DT, BIASES><<<across, 1024, 0, st>>>(p, plan.pieces.in_group, true);
+                norm_backward_weights_kernel<DT, BIASES><<<across, 1024, 0, st>>>(p, plan.pieces.in_group, true, 0);
         };
         if (wanted >> S0 & 1 || wanted >> T0 & 1) weights(std::true_type{});
         else weights(std::false_type{});
