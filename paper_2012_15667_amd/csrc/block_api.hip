@@ -22,7 +22,6 @@ bool all_aligned_to(std::initializer_list<const void*> all, size_t bytes)
         if (!aligned_to(p, bytes)) return false;
     return true;
 }
-bool launchable(int64_t workgroups) { return workgroups * 256 <= 0xffffffffLL; }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 #define BLOCK_HIP(call)                                          \
@@ -65,12 +64,12 @@ int check_norm_backward(const iolb_block_norm_backward_args& a)
     if (a.gate && (a.groups < 1 || a.M % a.groups)) return IOLB_EINVAL;
     if (a.gate && a.groups > MOST_K) return IOLB_EUNSUPPORTED;      // (without rows any number divides them)
     if (!(a.eps >= 0.f)) return IOLB_EINVAL;
+    if (a.N && !a.gate && a.dgate) return IOLB_EINVAL;
     if (a.M == 0 || a.N == 0) return IOLB_OK;               // (tensors without values may have no address)
     if (!a.h && (a.gate || a.dh || a.dgate || a.post != IOLB_NORM_NONE || a.scale != 1.f)) return IOLB_EINVAL;
     if (a.post == IOLB_NORM_NONE && (a.post_weight || a.post_bias || a.dpost_weight || a.dpost_bias)) return IOLB_EINVAL;
     if (a.pre == IOLB_NORM_NONE && (a.pre_weight || a.dy)) return IOLB_EINVAL;
     if (!a.dy && (a.dpre_weight || a.dpre_bias)) return IOLB_EINVAL;
-    if (!a.gate && a.dgate) return IOLB_EINVAL;
     if (!all_aligned_to({a.dy, a.dx_out, a.x, a.h, a.post_weight, a.post_bias, a.gate, a.pre_weight, a.dx, a.dh, a.dgate, a.dpost_weight, a.dpost_bias,
                          a.dpre_weight, a.dpre_bias}, size_of(a.dtype))) return IOLB_EINVAL;
     if ((!a.dy && !a.dx_out) || (a.dy && !a.x)) return IOLB_EINVAL;
@@ -93,6 +92,7 @@ int run_norm_backward(const iolb_block_norm_backward_args& a, void* ws, size_t* 
     p.groups = a.gate ? (int)a.groups : 1;
     p.rows_per_group = p.M / p.groups;
     p.scale = a.scale; p.eps = a.eps;
+    if (p.M == 0) p.gate = p.post_weight = p.post_bias = nullptr;   // (sums of nothing are 0: no factor of theirs, an infinite one, makes them NaN)
     const NormBackwardPlan plan = block_norm_backward_plan(p, a.dtype);
     if (!plan.launchable) return IOLB_EUNSUPPORTED;
     *need = up256(plan.row_bytes) + up256(plan.column_bytes);

@@ -932,7 +932,7 @@ norm_backward_groups_kernel(BlockNormBackward p, int in_group)
     for (int group = wave; group < p.groups; group += 16) {
         float sums[NORM_COLUMN_SUMS] = {0.f, 0.f, 0.f, 0.f};
         const float* from = p.columns + ((long long)group * in_group + row) * NORM_COLUMN_SUMS * ld + n;
-        const float g = live ? (float)gates[(long long)group * p.N + n] : 0.f;
+        const float g = live && gates ? (float)gates[(long long)group * p.N + n] : 1.f;
         if (live) {
 #pragma unroll 4
             for (int i = row; i < in_group; i += 4, from += 4 * NORM_COLUMN_SUMS * ld)
