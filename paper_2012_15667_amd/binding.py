@@ -712,11 +712,22 @@ def _without_graph(y, given, inputs, why="linear() records no gradients: they ar
     return _NoGraph.apply(why, y, given, *inputs)
 
 
+def _refuse_tangents(name, *tensors):
+    """A result of tensors that carry tangents would lose them without a word, and a tensor that is written to would keep an old one."""
+    forward_ad = _torch.autograd.forward_ad
+    # (the level is not part of torch's public interface; a torch without it looks at every tensor)
+    if getattr(forward_ad, "_current_level", 0) < 0:
+        return
+    for t in tensors:
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise RuntimeError(name + "() has no forward-mode derivatives")
+
+
 def linear(x, w, bias=None, act="none", residual=None, residual_first=False, checkpoint=False, y=None):
     """y = act(x w^T + bias) + residual, or act(x w^T + bias + residual) with residual_first, for x [M][K], w [N][K],
     bias [N], residual [M][N]; all float32, all float16 or all bfloat16, rows contiguous.  checkpoint=True returns (y,
     Checkpoint of what the activation was applied to).  y may be given, and may be the residual.  Gradients come from
-    linear_backward(): a backward pass through y is an error."""
+    linear_backward(): a backward pass through y is an error, and so are tangents of the arguments."""
     torch = _torch or _load_torch()
     if not isinstance(x, torch.Tensor):
         raise TypeError("x must be a tensor")
@@ -728,6 +739,7 @@ def linear(x, w, bias=None, act="none", residual=None, residual_first=False, che
         raise ValueError("x and w have different numbers of columns")
     pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else None
     pr, ldr = _rows(residual, "residual", dtype, device, (M, N))[:2] if residual is not None else (None, 0)
+    _refuse_tangents("linear", x, w, bias, residual, y)
     if y is None:
         y = x.new_empty((M, N))
         py, ldy = y.data_ptr(), N
@@ -810,6 +822,7 @@ def linear_backward(dy, w, x=None, z=None, act="none", x_act="none", want_dx=Tru
         raise ValueError("the activation's slope needs z")
     if want_dw and x is None:
         raise ValueError("dw needs x")
+    _refuse_tangents("linear_backward", dy, w)
     xq, xe = _checkpoint_of(x, "x", device, M, K) if x is not None else (None, None)
     zq, ze = _checkpoint_of(z, "z", device, M, N) if z is not None else (None, None)
     g = LinearGrads(dy.new_empty((M, K)) if want_dx else None, dy.new_empty((N, K)) if want_dw else None,
@@ -865,7 +878,7 @@ def block_norm(x, h=None, post="none", post_weight=None, post_bias=None, gate=No
     for the residual stream x [M][N] and the block's result h [M][N] (None: x' is None, and y = pre(x)).  post, pre: "rms", "layer" or "none" (post: h
     itself; pre: y is None), with weights and biases [N] of their own, or none; gate [N], or [groups][N] where M / groups neighbouring rows share each of
     its rows.  All float32, all float16 or all bfloat16, rows contiguous.  y is of x' as rounded to the type.  x_out, y may be given, and x_out may
-    be x.  Gradients come from block_norm_backward(): a backward pass through the results is an error."""
+    be x.  Gradients come from block_norm_backward(): a backward pass through the results is an error, and so are tangents of the arguments."""
     torch = _torch or _load_torch()
     if not isinstance(x, torch.Tensor):
         raise TypeError("x must be a tensor")
@@ -888,6 +901,7 @@ def block_norm(x, h=None, post="none", post_weight=None, post_bias=None, gate=No
     w = _dense(pre_weight, "pre_weight", dtype, device, (N,)) if pre_weight is not None else 0
     b = _dense(pre_bias, "pre_bias", dtype, device, (N,)) if pre_bias is not None else 0
     inputs, given = (x, h, post_weight, post_bias, gate, pre_weight, pre_bias), (x_out, y)
+    _refuse_tangents("block_norm", *inputs, *given)
     wanted = _graph_wanted(inputs, given)
     if h is None:
         po, ldo = 0, 0
@@ -946,6 +960,7 @@ def block_norm_backward(dy, dx_out, x, h=None, post="none", post_weight=None, po
     bp = _dense(post_bias, "post_bias", dtype, device, (N,)) if post_bias is not None else 0
     w = _dense(pre_weight, "pre_weight", dtype, device, (N,)) if pre_weight is not None else 0
     b = _dense(pre_bias, "pre_bias", dtype, device, (N,)) if pre_bias is not None else 0
+    _refuse_tangents("block_norm_backward", dy, dx_out, x, h, post_weight, post_bias, gate, pre_weight, pre_bias)
 
     def like(t, there=True):
         return torch.empty_like(t) if t is not None and want_weights and there else None       # (they are contiguous)
@@ -973,7 +988,7 @@ def dropout(x, p, seed, offset=0, counter=None, residual=None, checkpoint=False,
     seed, offset and the value's place, and is not stored: dropout(dy, p, seed, offset) is the backward pass.  Take another offset for every call and
     step.  counter: int64 [2] on the GPU, added to seed and offset when the kernel runs (a captured graph draws new masks by it).  p is taken to
     16 bits, and the scale fits it.  checkpoint=True returns (y, Checkpoint of y), as linear_backward reads it.  y may be given, and may be x or the residual.  A
-    backward pass through y is an error."""
+    backward pass through y is an error, and so are tangents of the arguments."""
     torch = _torch or _load_torch()
     if not isinstance(x, torch.Tensor):
         raise TypeError("x must be a tensor")
@@ -986,6 +1001,7 @@ def dropout(x, p, seed, offset=0, counter=None, residual=None, checkpoint=False,
     seed, offset = _word64(seed, "seed"), _word64(offset, "offset")
     pc = _dense(counter, "counter", torch.int64, device, (2,)) if counter is not None else 0
     pr, ldr = _rows(residual, "residual", dtype, device, (rows, cols))[:2] if residual is not None else (0, 0)
+    _refuse_tangents("dropout", x, residual, y)
     wanted = _graph_wanted((x, residual), (y,))
     given = y is not None
     if given:
@@ -1055,7 +1071,7 @@ def mx4_unpack(c, dtype=None, y=None):
 def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False, dtype=None, y=None):
     """linear() with both operands in microscaled 4-bit floating point: w is an Mx4 of [N][K], x an Mx4 of [M][K] or a tensor, which the call brings
     into it.  y, bias and residual are of x's type, or where x is an Mx4 of `dtype` (bfloat16 unless y is given).  For answering: there are no gradients, and
-    a backward pass through y is an error."""
+    a backward pass through y is an error, and so are tangents of the arguments."""
     torch = _torch or _load_torch()
     if isinstance(x, torch.Tensor):
         if dtype is not None and dtype != x.dtype:
@@ -1077,6 +1093,7 @@ def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False,
     pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else 0
     pr, ldr = _rows(residual, "residual", dtype, device, (M, N))[:2] if residual is not None else (0, 0)
     inputs = (like, bias, residual)
+    _refuse_tangents("linear_mx4", *inputs, y)
     wanted = _graph_wanted(inputs, (y,))
     given = y is not None
     if given:
