@@ -306,7 +306,9 @@ enum { IOLB_NORM_NONE = 0, IOLB_NORM_RMS = 1, IOLB_NORM_LAYER = 2 };
  * and bias (pre: there is no y).  x, h [M][N]; weights and biases [N], each may be NULL; gate [groups][N] or NULL: groups divides M, and
  * row m takes the gate's row m / (M / groups).  x' is rounded to the type, and y is of x' as rounded: what a backward pass reads is what was normalised.
  * x_out [M][N] may be x itself, and y and x_out overlap nothing else.  h NULL: y = pre(x) alone; post, gate, x_out are none then, and scale is 1.
- * Sums in fp32, of squares too: fp32 rows with values beyond 2^63 may overflow, to 0 or NaN.  A row with a NaN becomes NaN. */
+ * Sums in fp32, of squares too, before they are divided by N: rows of fp32 and bf16 (what h, x' hold) are normalised as said while their values stay below
+ * 2^63 / sqrt(N) (N = 4096: 2^57), and become 0 where the sum of squares reaches 2^128.  With eps 0 a row needs a value, with the mean taken off, of 2^-60
+ * or more; one of equal values is NaN then.  A row with a NaN becomes NaN. */
 typedef struct iolb_block_norm_args {
     int64_t M, N, groups;
     int32_t dtype, post, pre;
@@ -322,6 +324,8 @@ int iolb_block_norm(const iolb_block_norm_args* args);
  *   d = dx_out + (gradient of pre at x', of dy);  dx = scale d;  dh = (gradient of post at h, of gate d)
  * and of weights, biases and gate the sums of their factors over the rows that share them.  Outputs are dense, dx, dh [M][N], dgate [groups][N], the
  * others [N]; each may be NULL.  dh needs h, dgate the gate (and post_bias, where p had one), dpost_... a norm of h, dpre_... dy.
+ * For rows within the limits above.  Their sums are fp32's too: with T, D, X the largest |dy pre_weight|, |d gate post_weight| and |x'| of a row, N T X, N^1.5 T
+ * and N^1.5 D must stay below 2^126.
  * Sums are added in a fixed order: equal calls give equal bits.  M, N and groups up to 2^22, and with
  * gradients of weights, biases or gate groups x ceil(N / 16) below 2^32 (the workspace, 16 bytes a column and group and more, would be 2^40).  Outputs overlap nothing. */
 typedef struct iolb_block_norm_backward_args {
