@@ -485,14 +485,14 @@ norm_backward_long_kernel(BlockNormBackward p)
 
 enum { S1, S0, T1, T0 };
 
-// A workgroup takes 64 columns of a piece's rows: eight threads across, 32 along.  skip: workgroups of the launches before this one.
+// A workgroup takes 64 columns of a piece's rows: eight threads across, 32 along.
 template <int DT>
 __global__ void __launch_bounds__(256)
-norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces, unsigned skip)
+norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces)
 {
     typedef typename DenseType<DT>::type T;
     __shared__ float part[32][64 + 1];
-    const unsigned across = (unsigned)(p.N + 63) / 64, at = skip + blockIdx.x, row = at / across, c0 = at % across * 64;
+    const unsigned across = (unsigned)(p.N + 63) / 64, row = blockIdx.x / across, c0 = blockIdx.x % across * 64;
     const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, c = (int)c0 + tx * 8;
     const long long ld = (p.N + 7) / 8 * 8;
     const int group = (int)(row / pieces.in_group), piece = (int)(row % pieces.in_group);
@@ -857,17 +857,17 @@ norm_backward_wide_kernel(BlockNormBackward p)
 
 // What weights, biases and gate get.  First the pieces of a group (its rows of the gate are done then, and all of it where there is one group); then
 // (`across`) the groups, whose sums lie in the place of their first piece.  A workgroup takes 16 columns, 64 threads to each.  BIASES: whether S0 and T0
-// are there; of a pair one may have been left out, and what stands in its place is then read but goes nowhere.  skip: workgroups of the launches before.
+// are there; of a pair one may have been left out, and what stands in its place is then read but goes nowhere.
 template <int DT, bool BIASES>
 __global__ void __launch_bounds__(1024)
-norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across, unsigned skip)
+norm_backward_weights_kernel(BlockNormBackward p, int in_group, bool across)
 {
     typedef typename DenseType<DT>::type T;
     __shared__ float part[NORM_COLUMN_SUMS][64][16 + 1];
-    const unsigned blocks = (unsigned)(p.N + 15) / 16, block = skip + blockIdx.x;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, n = (int)(block % blocks * 16) + tx;
+    const unsigned blocks = (unsigned)(p.N + 15) / 16;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, n = (int)(blockIdx.x % blocks * 16) + tx;
     const long long ld = (p.N + 7) / 8 * 8;
-    const int group = (int)(block / blocks), count = across ? p.groups : in_group;
+    const int group = (int)(blockIdx.x / blocks), count = across ? p.groups : in_group;
     const T* const gates = static_cast<const T*>(p.gate);
     float sums[NORM_COLUMN_SUMS] = {0.f, 0.f, 0.f, 0.f};
     float* const at = p.columns + (long long)group * in_group * NORM_COLUMN_SUMS * ld + n;
@@ -1015,13 +1015,32 @@ void by_end(int N, F f)
     f(std::integral_constant<int, CUT>{});
 }
 
-// launch(workgroups, of them before) for `all` workgroups, a million at a time: a launch counts its threads in 32 bits, and one of a million takes
-// so long that another one behind it does not show.
-template <class F>
-void in_turns(long long all, F launch)
+// The call as a launch sees it that starts with this group.
+template <int DT>
+BlockNormBackward from_group(BlockNormBackward p, const NormPieces& pieces, long long group)
 {
-    constexpr long long MOST = 1 << 20;
-    for (long long at = 0; at < all; at += MOST) launch((unsigned)(all - at < MOST ? all - at : MOST), (unsigned)at);
+    typedef typename DenseType<DT>::type T;
+    const long long row = group * p.rows_per_group;
+    const auto move = [](const void*& t, long long by) { if (t) t = static_cast<const T*>(t) + by; };
+    move(p.dy, row * p.lddy);
+    move(p.dout, row * p.lddout);
+    move(p.x, row * p.ldx);
+    move(p.h, row * p.ldh);
+    move(p.gate, group * p.N);
+    if (p.dgate) p.dgate = static_cast<T*>(p.dgate) + group * p.N;
+    if (p.rows) p.rows += row * NORM_ROW_SUMS;
+    p.columns += group * pieces.in_group * NORM_COLUMN_SUMS * ((p.N + 7) / 8 * 8);
+    return p;
+}
+
+// launch(call, workgroups) for all groups, `each` workgroups to a group, about a million at a time: a launch counts its threads in 32 bits, and one of a
+// million workgroups takes so long that another one behind it does not show.
+template <int DT, class F>
+void in_turns(const BlockNormBackward& p, const NormPieces& pieces, long long each, F launch)
+{
+    const long long most = each < 1 << 20 ? (1 << 20) / each : 1;
+    for (long long group = 0; group < p.groups; group += most)
+        launch(from_group<DT>(p, pieces, group), (unsigned)(each * (p.groups - group < most ? p.groups - group : most)));
 }
 
 unsigned row_groups(int M) { return (unsigned)(M < 65536 ? M : 65536); }
@@ -1071,10 +1090,9 @@ NormBackwardPlan block_norm_backward_plan(const BlockNormBackward& p, int)
         plan.pieces.in_group = (R + plan.pieces.per - 1) / plan.pieces.per;
     }
     if (!column_sums(p)) return plan;
-    // (the kernels count blocks of columns, 16 to a group and 64 to a piece, in 32 bits: beyond that the sums are 2^40 bytes and more.  The rows' kernels
-    // have a workgroup to a piece, of which there are no more than 512 or than groups.)
+    // (blocks of 16 columns and a group: more of them than 2^32 have sums of 2^40 bytes and more)
     const long long pieces = (long long)plan.pieces.in_group * p.groups;
-    plan.launchable = (p.N + 15LL) / 16 * p.groups <= 0xffffffffLL && across * pieces <= 0xffffffffLL;
+    plan.launchable = (p.N + 15LL) / 16 * p.groups <= 0xffffffffLL;
     plan.row_bytes = in_registers ? 0 : (size_t)p.M * NORM_ROW_SUMS * 4;
     plan.column_bytes = (size_t)pieces * NORM_COLUMN_SUMS * ((p.N + 7) / 8 * 8) * 4;
     return plan;
@@ -1095,7 +1113,9 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBack
                     by_end<TR * C>(p.N, [&](auto end) { norm_backward_wide_kernel<DT, TR * C / 1024, decltype(end)::value><<<(unsigned)(p.M < 256 ? p.M : 256), 1024, 0, st>>>(p); });
                 }
                 if (wanted)
-                    in_turns((p.N + 63LL) / 64 * pieces, [&](unsigned n, unsigned skip) { norm_backward_columns_kernel<DT><<<n, 256, 0, st>>>(p, plan.pieces, skip); });
+                    in_turns<DT>(p, plan.pieces, (p.N + 63LL) / 64 * plan.pieces.in_group, [&](const BlockNormBackward& turn, unsigned n) {
+                        norm_backward_columns_kernel<DT><<<n, 256, 0, st>>>(turn, plan.pieces);
+                    });
             } else {
                 const bool biases = wanted >> S0 & 1 || wanted >> T0 & 1;
                 by_end<TR * C>(p.N, [&](auto end) {
@@ -1114,11 +1134,11 @@ hipError_t launch_block_norm_backward(const BlockNormBackward& p, const NormBack
                 norm_backward_groups_kernel<DT, BIASES><<<across, 1024, 0, st>>>(p, plan.pieces.in_group);
                 return;
             }
-            in_turns((long long)across * p.groups, [&](unsigned n, unsigned skip) {
-                norm_backward_weights_kernel<DT, BIASES><<<n, 1024, 0, st>>>(p, plan.pieces.in_group, false, skip);
+            in_turns<DT>(p, plan.pieces, across, [&](const BlockNormBackward& turn, unsigned n) {
+                norm_backward_weights_kernel<DT, BIASES><<<n, 1024, 0, st>>>(turn, plan.pieces.in_group, false);
             });
             if (p.groups > 1 && (p.dpost_weight || p.dpost_bias || p.dpre_weight || p.dpre_bias))
-                norm_backward_weights_kernel<DT, BIASES><<<across, 1024, 0, st>>>(p, plan.pieces.in_group, true, 0);
+                norm_backward_weights_kernel<DT, BIASES><<<across, 1024, 0, st>>>(p, plan.pieces.in_group, true);
         };
         if (wanted >> S0 & 1 || wanted >> T0 & 1) weights(std::true_type{});
         else weights(std::false_type{});
