@@ -315,9 +315,12 @@ _torch = None
 
 def _load_torch():
     # once: an import statement in every function of a call is a look-up under the import lock each
-    global _torch
+    global _torch, _dual
     import torch
+    from torch.autograd import forward_ad
     _torch = torch
+    if hasattr(forward_ad, "_current_level"):
+        _dual = forward_ad
     return torch
 
 
@@ -339,6 +342,12 @@ def _dev_f32(t, name):
     return t.data_ptr()                        # (an address: the functions' argtypes make pointers of it)
 
 
+class _dual:
+    """The level of forward-mode derivatives, below 0 outside all: torch.autograd.forward_ad, once it is loaded.  The level is not part of torch's public
+    interface; with a torch without it every tensor is looked at."""
+    _current_level = 0
+
+
 _increment_version = None
 
 
@@ -347,8 +356,7 @@ def _written(t):
     global _increment_version
     if _increment_version is None:
         _increment_version = _torch.autograd.graph.increment_version
-    if not t.is_inference():
-        _increment_version(t)
+    _increment_version(t)
 
 
 def conv_direct(x, w, stride=1, pad=0, y=None, cfg=None):
@@ -714,12 +722,8 @@ def _without_graph(y, given, inputs, why="linear() records no gradients: they ar
 
 def _refuse_tangents(name, *tensors):
     """A result of tensors that carry tangents would lose them without a word, and a tensor that is written to would keep an old one."""
-    forward_ad = _torch.autograd.forward_ad
-    # (the level is not part of torch's public interface; a torch without it looks at every tensor)
-    if getattr(forward_ad, "_current_level", 0) < 0:
-        return
     for t in tensors:
-        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+        if t is not None and _torch.autograd.forward_ad.unpack_dual(t).tangent is not None:
             raise RuntimeError(name + "() has no forward-mode derivatives")
 
 
@@ -739,7 +743,8 @@ def linear(x, w, bias=None, act="none", residual=None, residual_first=False, che
         raise ValueError("x and w have different numbers of columns")
     pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else None
     pr, ldr = _rows(residual, "residual", dtype, device, (M, N))[:2] if residual is not None else (None, 0)
-    _refuse_tangents("linear", x, w, bias, residual, y)
+    if _dual._current_level >= 0:
+        _refuse_tangents("linear", x, w, bias, residual, y)
     if y is None:
         y = x.new_empty((M, N))
         py, ldy = y.data_ptr(), N
@@ -822,7 +827,8 @@ def linear_backward(dy, w, x=None, z=None, act="none", x_act="none", want_dx=Tru
         raise ValueError("the activation's slope needs z")
     if want_dw and x is None:
         raise ValueError("dw needs x")
-    _refuse_tangents("linear_backward", dy, w)
+    if _dual._current_level >= 0:
+        _refuse_tangents("linear_backward", dy, w)
     xq, xe = _checkpoint_of(x, "x", device, M, K) if x is not None else (None, None)
     zq, ze = _checkpoint_of(z, "z", device, M, N) if z is not None else (None, None)
     g = LinearGrads(dy.new_empty((M, K)) if want_dx else None, dy.new_empty((N, K)) if want_dw else None,
@@ -901,7 +907,8 @@ def block_norm(x, h=None, post="none", post_weight=None, post_bias=None, gate=No
     w = _dense(pre_weight, "pre_weight", dtype, device, (N,)) if pre_weight is not None else 0
     b = _dense(pre_bias, "pre_bias", dtype, device, (N,)) if pre_bias is not None else 0
     inputs, given = (x, h, post_weight, post_bias, gate, pre_weight, pre_bias), (x_out, y)
-    _refuse_tangents("block_norm", *inputs, *given)
+    if _dual._current_level >= 0:
+        _refuse_tangents("block_norm", *inputs, *given)
     wanted = _graph_wanted(inputs, given)
     if h is None:
         po, ldo = 0, 0
@@ -960,7 +967,8 @@ def block_norm_backward(dy, dx_out, x, h=None, post="none", post_weight=None, po
     bp = _dense(post_bias, "post_bias", dtype, device, (N,)) if post_bias is not None else 0
     w = _dense(pre_weight, "pre_weight", dtype, device, (N,)) if pre_weight is not None else 0
     b = _dense(pre_bias, "pre_bias", dtype, device, (N,)) if pre_bias is not None else 0
-    _refuse_tangents("block_norm_backward", dy, dx_out, x, h, post_weight, post_bias, gate, pre_weight, pre_bias)
+    if _dual._current_level >= 0:
+        _refuse_tangents("block_norm_backward", dy, dx_out, x, h, post_weight, post_bias, gate, pre_weight, pre_bias)
 
     def like(t, there=True):
         return torch.empty_like(t) if t is not None and want_weights and there else None       # (they are contiguous)
@@ -1001,7 +1009,8 @@ def dropout(x, p, seed, offset=0, counter=None, residual=None, checkpoint=False,
     seed, offset = _word64(seed, "seed"), _word64(offset, "offset")
     pc = _dense(counter, "counter", torch.int64, device, (2,)) if counter is not None else 0
     pr, ldr = _rows(residual, "residual", dtype, device, (rows, cols))[:2] if residual is not None else (0, 0)
-    _refuse_tangents("dropout", x, residual, y)
+    if _dual._current_level >= 0:
+        _refuse_tangents("dropout", x, residual, y)
     wanted = _graph_wanted((x, residual), (y,))
     given = y is not None
     if given:
@@ -1093,7 +1102,8 @@ def linear_mx4(x, w, bias=None, act="none", residual=None, residual_first=False,
     pb = _dense(bias, "bias", dtype, device, (N,)) if bias is not None else 0
     pr, ldr = _rows(residual, "residual", dtype, device, (M, N))[:2] if residual is not None else (0, 0)
     inputs = (like, bias, residual)
-    _refuse_tangents("linear_mx4", *inputs, y)
+    if _dual._current_level >= 0:
+        _refuse_tangents("linear_mx4", *inputs, y)
     wanted = _graph_wanted(inputs, (y,))
     given = y is not None
     if given:
