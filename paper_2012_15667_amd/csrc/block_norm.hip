@@ -326,7 +326,7 @@ block_norm_rows_kernel(BlockNorm p)
 }
 
 // ---- rows of any length ------------------------------------------------------------------------------------
-// A workgroup to a row, which it reads again from the caches for each step.
+// A workgroup to a row, which it reads again from the caches for each step: 2048 x 20000 bf16 114 us (2.9 TB/s), gradients with the columns' pass 320.
 template <int DT>
 __global__ void __launch_bounds__(256)
 block_norm_long_kernel(BlockNorm p)
@@ -543,7 +543,8 @@ norm_backward_columns_kernel(BlockNormBackward p, NormPieces pieces)
 
 // The same for rows that are held in registers: a workgroup takes a piece's rows, TR threads to a row, reads everything once, and holds its columns' sums
 // meanwhile; the next row's values are asked for where this row's have been used last.  BIASES: whether S0 and T0 are wanted.
-// Memory and a row's two exchanges bind it: 8192 x 4096 bf16 86 to 95 us (4.2 to 4.7 TB/s), and 8 to join the pieces' sums.
+// Memory and a row's two exchanges bind it: 8192 x 4096 bf16 86 to 95 us (4.2 to 4.7 TB/s), and 8 to join the pieces' sums.  fp32 (a call): 8192 x 4096 176 us,
+// with means off and biases 191; of 4097 to 8192 values some of a row's do not fit the registers, 38 to 41 of a lane's, with biases 116 to 129: 4096 x 8192 189 / 257.
 template <int DT, int TR, int C, bool BIASES, int ENDS, bool PAST>
 __global__ void __launch_bounds__(TR > 256 ? TR : 256)
 norm_backward_rows_kernel(BlockNormBackward p, NormPieces pieces, unsigned wanted)
@@ -1079,7 +1080,8 @@ NormBackwardPlan block_norm_backward_plan(const BlockNormBackward& p, int)
     const long long across = in_registers ? 1 : (p.N + 63) / 64;
     const int R = p.rows_per_group;
     // Rows in registers: two workgroups of 256 threads to a compute unit, or one of 512, and no more: each writes a row of sums.  8192 x 4096 bf16: 768
-    // pieces 126 us, 512 111; 16384 x 1024 66 / 57; 4096 x 8192: 512 115, 256 106.
+    // pieces 126 us, 512 111; 16384 x 1024 66 / 57; 4096 x 8192: 512 115, 256 106.  fp32 takes the same numbers, unmeasured against others: of 2049 to 4096
+    // values a workgroup's registers fill a unit, so that two follow one another.
     const int at_once = !in_registers ? 32 : p.N <= 256 ? 16 : p.N <= 1024 ? 4 : 1, all = !in_registers ? 2048 : p.N <= 4096 ? 512 : 256;
     long long wanted = all / across / p.groups;
     if (wanted > (R + at_once - 1) / at_once) wanted = (R + at_once - 1) / at_once;

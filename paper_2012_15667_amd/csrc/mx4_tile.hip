@@ -6,7 +6,7 @@
 // which the instruction takes byte kk.
 //
 // Bound by the stage: 2.0 us for 256 x 256 x 256 on a compute unit, where the matrix instructions alone need 1.3 at the rate that the card's power leaves them.
-// 8192^3 276 us (4.0 PFLOP/s), 8192 x 4096 -> 16384 bf16 with gelu 368 to 393 with packing x (18) and a third of a block's time in prologue, gelu and stores.
+// 8192^3 276 us (4.0 PFLOP/s), 8192 x 4096 -> 16384 bf16 with gelu 368 to 393 with packing x (18) and a quarter of a block's time (12 of 44 us) in prologue, gelu and stores.
 // Workgroups that stay and take block after block were slower (394 -> 418).
 #include "dense_math.h"
 #include "kernels.h"
